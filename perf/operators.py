@@ -12,7 +12,8 @@ A case says which operator runs (``op``) and on what:
   w4       rows times a matrix of 4-bit codes with group scales
 
 The cache is a pool of blocks of 64 slots.  Keys are held as [block, kv head,
-slot, dim], values as [block, kv head, dim, place(slot)]; one power-of-two scale
+slot, dim], values as [block, kv head, 4, dim, 16]: slot t of a block stands in
+group (t / 4) % 4, there at place (t / 16) * 4 + t % 4.  One power-of-two scale
 for a block and head; code times scale is the value.  A sequence is a row of the
 block table (blocks in any order) and a length.
 """
@@ -30,7 +31,7 @@ TOP = {"e4m3": 448.0, "int8": 127.0}      # largest code
 LEAST = -100                              # least exponent of a scale
 CODE = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}
 TYPE = {"bf16": torch.bfloat16, "f16": torch.float16}
-# where a value's slot stands inside its block
+# where a value's slot stands inside its block: group * 16 + place
 PLACE = [((t >> 2) & 3) * 16 + (t >> 4) * 4 + (t & 3) for t in range(BLOCK)]
 
 
@@ -178,6 +179,18 @@ def work(case):
 
 # -- inputs -------------------------------------------------------------------
 
+def _by_slot(x):
+    """Values held as [.., 4, dim, 16], slot by slot: [.., 64, dim]."""
+    at = torch.tensor(PLACE, device=x.device)
+    return x.transpose(-1, -2).flatten(-3, -2)[..., at, :]
+
+
+def _as_held(x):
+    """Values slot by slot, as they are held."""
+    at = torch.argsort(torch.tensor(PLACE, device=x.device))
+    return x[..., at, :].unflatten(-2, (4, 16)).transpose(-1, -2)
+
+
 def _codes(x, fmt):
     """Block scales and codes of values [block, head, 64, dim]."""
     a = x.abs().amax(dim=(2, 3))
@@ -221,17 +234,15 @@ def prepare(case, seed):
     n_blocks = total + 1
     channel = torch.exp(0.7 * rnd(kv, 1, d))
     k_codes = torch.empty((n_blocks, kv, BLOCK, d), dtype=CODE[fmt], device=dev)
-    v_codes = torch.empty((n_blocks, kv, d, BLOCK), dtype=CODE[fmt], device=dev)
+    v_codes = torch.empty((n_blocks, kv, 4, d, 16), dtype=CODE[fmt], device=dev)
     k_scale = torch.empty((n_blocks, kv), device=dev)
     v_scale = torch.empty((n_blocks, kv), device=dev)
-    place = torch.tensor(PLACE, device=dev)
-    slot_at = torch.argsort(place)
     step = max(1, (1 << 28) // (kv * BLOCK * d))
     for b in range(0, n_blocks, step):
         e = min(n_blocks, b + step)
         k_scale[b:e], k_codes[b:e] = _codes(rnd(e - b, kv, BLOCK, d) * channel, fmt)
         v_scale[b:e], q = _codes(rnd(e - b, kv, BLOCK, d), fmt)
-        v_codes.view(torch.uint8)[b:e] = q.view(torch.uint8)[:, :, slot_at].transpose(2, 3)
+        v_codes.view(torch.uint8)[b:e] = _as_held(q.view(torch.uint8))
     lengths = torch.tensor([x for x, _ in both], dtype=torch.int32, device=dev)
     start = np.concatenate([[0], np.cumsum([n for _, n in both])]).astype(np.int32)
     table = torch.tensor(table, dtype=torch.int32, device=dev)
@@ -248,7 +259,9 @@ def prepare(case, seed):
             if length % BLOCK:
                 last, used = int(table[b, length // BLOCK]), length % BLOCK
                 k_codes.view(torch.uint8)[last, :, used:] = 0x7f
-                v_codes.view(torch.uint8)[last][:, :, place[used:]] = 0x7f
+                held = _by_slot(v_codes.view(torch.uint8)[last])
+                held[:, used:] = 0x7f
+                v_codes.view(torch.uint8)[last] = _as_held(held)
     s = {"case": c, "k_codes": k_codes, "v_codes": v_codes, "k_scale": k_scale,
          "v_scale": v_scale, "position": position, "weight": weight, "table": table,
          "lengths": lengths, "n_rows": int(start[-1]), "max_new": max(n for _, n in both),
@@ -332,9 +345,8 @@ def _encode(y, fmt):
     return torch.where(y.isnan(), 0.0, y).round().to(torch.int8).view(torch.uint8)
 
 
-def _write(x, codes, scale, fmt, blk, off, first_blk, held, rows_dim):
-    """New values x [row, head, dim] into `codes` [block, head, ..]; rows_dim is
-    the slots' dimension behind the head's (0 keys, 1 values)."""
+def _write(x, codes, scale, fmt, blk, off, first_blk, held):
+    """New values x [row, head, dim] into the keys' or the values' codes."""
     xf = x.float()
     a = torch.where(xf.isfinite(), xf.abs(), 0.0).amax(-1)
     need = torch.zeros_like(scale).scatter_reduce(0, blk[:, None].expand_as(a), a, "amax")
@@ -347,16 +359,17 @@ def _write(x, codes, scale, fmt, blk, off, first_blk, held, rows_dim):
     # the codes held by a block whose scale grows (only a sequence's first block holds any)
     ratio = torch.where(held[:, None], scale[first_blk] / grown[first_blk], 1.0)
     raw = codes.view(torch.uint8)
-    raw[first_blk] = _encode(codes[first_blk].float() * ratio[:, :, None, None], fmt)
+    held = codes[first_blk].float()
+    raw[first_blk] = _encode(held * ratio.view(ratio.shape + (1,) * (held.ndim - 2)), fmt)
     scale.copy_(grown)
     y = _encode(xf / scale[blk][:, :, None], fmt)
     heads = torch.arange(scale.shape[1], device=x.device)
-    if rows_dim == 0:
+    if raw.ndim == 4:
         raw[blk[:, None], heads, off[:, None]] = y
     else:
-        dims = torch.arange(x.shape[2], device=x.device)
         at = torch.tensor(PLACE, device=x.device)[off]
-        raw[blk[:, None, None], heads[:, None], dims, at[:, None, None]] = y
+        raw.view(*raw.shape[:2], 4, -1, 16)[blk[:, None], heads, at[:, None] // 16, :,
+                                            at[:, None] % 16] = y
 
 
 def _rows(s):
@@ -379,8 +392,8 @@ def _plain_append(s):
     first = start.clamp(min=0) // BLOCK
     held = (n > 0) & (start > 0) & (start % BLOCK != 0)
     first_blk = table.gather(1, first.clamp(max=table.shape[1] - 1)[:, None])[:, 0]
-    _write(s["k"][keep], s["k_codes"], s["k_scale"], fmt, blk, off, first_blk, held, 0)
-    _write(s["v"][keep], s["v_codes"], s["v_scale"], fmt, blk, off, first_blk, held, 1)
+    _write(s["k"][keep], s["k_codes"], s["k_scale"], fmt, blk, off, first_blk, held)
+    _write(s["v"][keep], s["v_codes"], s["v_scale"], fmt, blk, off, first_blk, held)
     heads = torch.arange(s["position"].shape[1], device=blk.device)
     pos = (s["first"][seq] + i).int()
     s["position"][blk[:, None], heads, off[:, None]] = pos[:, None]
@@ -390,9 +403,10 @@ def _plain_append(s):
 
 def _values(s, table, name):
     """Cached values of every sequence's slots in single precision [seq, head, slot, dim]."""
-    x = s[name + "_codes"][table].float() * s[name + "_scale"][table][..., None, None]
+    x = s[name + "_codes"][table].float()
     if name == "v":
-        x = x.transpose(3, 4)[:, :, :, torch.tensor(PLACE, device=x.device)]
+        x = _by_slot(x)
+    x = x * s[name + "_scale"][table][..., None, None]
     b, nb, h, _, d = x.shape
     return x.transpose(1, 2).reshape(b, h, nb * BLOCK, d)
 
@@ -442,7 +456,8 @@ def _refill(s, name, table, src, hole, fmt):
     if name == "k":
         got = raw[blk, heads, src % BLOCK]
     else:
-        got = raw[blk, heads, :, torch.tensor(PLACE, device=src.device)[src % BLOCK]]
+        at = torch.tensor(PLACE, device=src.device)[src % BLOCK]
+        got = raw[blk, heads, at // 16, :, at % 16]
     x = got.view(codes.dtype).float() * scale[blk, heads][..., None]
     x = torch.where(hole[..., None], x, 0.0)
     a = torch.where(x.isfinite(), x.abs(), 0.0).amax(-1).view(seqs, kv, nb, BLOCK).amax(-1)
@@ -451,14 +466,13 @@ def _refill(s, name, table, src, hole, fmt):
     grown = torch.where(any_hole, torch.maximum(old, _power(a, fmt)), old)
     held = codes[table].float()
     if name == "v":
-        held = held.transpose(3, 4)[:, :, :, torch.tensor(PLACE, device=src.device)]
+        held = _by_slot(held)
     held = held.transpose(1, 2) * (old / grown)[..., None, None]            # [seq, head, nb, 64, d]
     y = torch.where(hole.view(seqs, kv, nb, BLOCK, 1),
                     x.view(seqs, kv, nb, BLOCK, -1) / grown[..., None, None], held)
     y = _encode(y, fmt).transpose(1, 2)
     if name == "v":
-        back = torch.argsort(torch.tensor(PLACE, device=src.device))
-        y = y[:, :, :, back].transpose(3, 4)
+        y = _as_held(y)
     raw[table] = y
     scale[table] = grown.transpose(1, 2)
 
@@ -542,10 +556,11 @@ class _Host:
 
     def __init__(self, s):
         self.fmt = s["case"]["format"]
-        slot_at = PLACE
         f64 = lambda x: x.float().cpu().numpy().astype(np.float64)  # noqa: E731
         self.k = f64(s["k_codes"])
-        self.v = f64(s["v_codes"]).transpose(0, 1, 3, 2)[:, :, slot_at]
+        v = f64(s["v_codes"])
+        v = v.transpose(0, 1, 2, 4, 3).reshape(v.shape[0], v.shape[1], BLOCK, -1)
+        self.v = v[:, :, PLACE]
         self.ks, self.vs = f64(s["k_scale"]), f64(s["v_scale"])
         self.pos, self.weight = s["position"].cpu().numpy().copy(), f64(s["weight"])
         self.table = s["table"].cpu().numpy()
@@ -563,8 +578,8 @@ class _Host:
         scale[blk, h] = new
 
     def out(self):
-        back = np.argsort(PLACE)
-        v = self.v[:, :, back].transpose(0, 1, 3, 2)
+        v = self.v[:, :, np.argsort(PLACE)]
+        v = v.reshape(v.shape[0], v.shape[1], 4, 16, -1).transpose(0, 1, 2, 4, 3)
         return {"k_codes": self.k, "v_codes": v, "k_scale": self.ks, "v_scale": self.vs,
                 "position": self.pos, "weight": self.weight}
 
@@ -611,9 +626,9 @@ def _exact_attend(c, s):
         ids = s["table"][b, :-(-length // BLOCK)].long()
         for h in range(kv):
             key = s["k_codes"][ids, h].double() * s["k_scale"][ids, h].double()[:, None, None]
-            val = s["v_codes"][ids, h].double() * s["v_scale"][ids, h].double()[:, None, None]
+            val = s["v_codes"][ids, h].double() * s["v_scale"][ids, h].double()[:, None, None, None]
             key = key.reshape(-1, d)[:length]
-            val = val[:, :, at].transpose(1, 2).reshape(-1, d)[:length]
+            val = val.transpose(2, 3).reshape(-1, BLOCK, d)[:, at].reshape(-1, d)[:length]
             q = s["q"][start[b]:start[b + 1], h * g:(h + 1) * g].double().reshape(n * g, d)
             sc = (q @ key.t().contiguous()) / math.sqrt(d)
             last = length - n + torch.arange(n, device="cuda").repeat_interleave(g)
