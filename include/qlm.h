@@ -490,6 +490,185 @@ int qlm_apply_profile(const qlm_problem *problem, const qlm_profile *profile,
                       const float *req_slo, int64_t n_requests, float *req_slo_out,
                       qlm_stream stream);
 
+/*
+ * Operators of a serving instance's decode step.  The profile above says what
+ * an instance needs for a token (d), for a prompt (P) and how many tokens its
+ * memory holds; these calls are what an MI355X instance spends that time and
+ * memory on, so that a class of such instances can be measured instead of
+ * described: a token cache held in 8 bits (written, attended to, cut to a
+ * budget) and products with 4-bit weights.
+ *
+ * The cache is a pool of blocks of QLM_KV_BLOCK slots.  For every block and kv
+ * head it holds a code of 8 bits for each slot and dim of keys and values, one
+ * scale for the keys and one for the values, and each slot's position and
+ * accumulated attention weight.  value = code * scale.
+ *   keys    [n_blocks][n_kv_heads][64][head_dim]
+ *   values  [n_blocks][n_kv_heads][4][head_dim][16]: slot t of the block stands
+ *           in group (t / 4) % 4, there at place (t / 16) * 4 + t % 4
+ * which is the order in which the matrix instructions take them.  The pools are
+ * 16-byte aligned.  Scales are finite and > 0 wherever a sequence has slots;
+ * qlm_kv_append writes powers of two.
+ */
+#define QLM_KV_BLOCK 64
+
+enum { QLM_F16 = 0, QLM_BF16 = 1 };           /* types of rows                 */
+enum { QLM_KV_E4M3 = 0, QLM_KV_INT8 = 1 };    /* codes: e4m3 (largest 448),
+                                                 two's complement (127)        */
+
+typedef struct qlm_kv_cache {
+    int32_t n_blocks;            /* >= 1                                         */
+    int32_t n_kv_heads;          /* 1..1024                                      */
+    int32_t head_dim;            /* a multiple of 16, 16..256                    */
+    int32_t format;              /* QLM_KV_E4M3 or QLM_KV_INT8                   */
+    void *k_codes, *v_codes;     /* one byte a code, laid out as above           */
+    float *k_scale, *v_scale;    /* [n_blocks][n_kv_heads]                       */
+    int32_t *position;           /* [n_blocks][n_kv_heads][64]: the token's place
+                                    in its sequence; NULL = not kept             */
+    float *weight;               /* [n_blocks][n_kv_heads][64]: accumulated
+                                    attention weight; NULL = not kept            */
+} qlm_kv_cache;
+
+/*
+ * The sequences of one call.  Sequence s holds slots 0 .. lengths[s] - 1, slot j
+ * in block block_table[s][j / 64] at j % 64, and has row_start[s + 1] -
+ * row_start[s] new tokens (rows of the call's row arrays), which take its last
+ * slots; a length shorter than its new tokens leaves the first of them without a
+ * slot.  A block belongs to one sequence.  The device arrays are not checked by
+ * the calls, but nothing is read or written out of bounds for any content:
+ * lengths are clamped to [0, max_length], rows to [0, n_rows) and max_new, and
+ * block numbers outside [0, n_blocks) name no slots.
+ */
+typedef struct qlm_kv_batch {
+    int32_t n_seqs;              /* >= 0                                         */
+    int32_t n_rows;              /* rows in all, >= 0                            */
+    int32_t max_new;             /* the most rows of a sequence, >= 1            */
+    int32_t max_length;          /* the most slots of a sequence, >= 0           */
+    int64_t table_stride;        /* elements between the table's rows,
+                                    >= ceil(max_length / 64)                     */
+    const int32_t *block_table;  /* [n_seqs][table_stride]                       */
+    const int32_t *lengths;      /* [n_seqs], the new tokens included            */
+    const int32_t *row_start;    /* [n_seqs + 1], ascending; NULL = one row for
+                                    each sequence (n_rows = n_seqs)              */
+} qlm_kv_batch;
+
+/* Rows of heads, [n_rows][heads][head_dim], each head's dims contiguous.       */
+typedef struct qlm_rows {
+    void *data;
+    int64_t row_stride, head_stride;  /* elements                                */
+    int32_t dtype;                    /* QLM_F16 or QLM_BF16                     */
+} qlm_rows;
+
+/*
+ * Writes the new tokens' keys and values [n_rows][n_kv_heads][head_dim] into
+ * their slots.  For each block and head that takes new slots, with a the
+ * largest finite magnitude among its new values and top the largest code:
+ *   need   = 2^e, the least e >= -100 with a <= top 2^e
+ *   scale' = need where the block's slot 0 is new, else max(scale, need)
+ *   every code held becomes the nearest code to code * scale / scale' when the
+ *   scale grows, and a new value x the nearest code to x / scale' (ties to
+ *   even, clamped to the largest code; a NaN stays one in e4m3 and is 0 in int8)
+ * The slots' positions (where kept) become first_position[s] and on (the slot's
+ * number where first_position is NULL), their weights (where kept) 0.
+ * An infinite value is held as the largest code.
+ *   k, v            dtype QLM_F16 or QLM_BF16, each its own
+ *   first_position  [n_seqs] device or NULL
+ */
+int qlm_kv_append(const qlm_kv_cache *cache, const qlm_kv_batch *batch, const qlm_rows *k,
+                  const qlm_rows *v, const int32_t *first_position, qlm_stream stream);
+
+/*
+ * Attention of each sequence's new tokens over its slots, the new ones
+ * included (after qlm_kv_append).  Row t of the n rows of a sequence of length L
+ * sees the slots j <= L - n + t; head h reads kv head h / (n_heads /
+ * n_kv_heads):
+ *   p = softmax over the seen slots of  scale * q . key_j
+ *   out = sum of p_j value_j;  a row that sees no slot gives 0
+ * With `accumulate`, for every slot j < L of every sequence and kv head
+ *   weight_j = weight_decay * weight_j + (sum of p_j over the rows and the heads
+ *              that read the kv head)
+ * (the old weight is not read when weight_decay is 0).  Slots that a row does
+ * not see have no part in its result, whatever they hold.  Scores, their
+ * maxima and sums, weights and outputs are formed in single precision from
+ * exact products; p is rounded to half precision (relative to the running
+ * maximum) for the sum over values.  Bit-for-bit reproducible for the same
+ * inputs and sizes.
+ *   q, out  [n_rows][n_heads][head_dim], the same dtype; out may not alias q
+ *   ws      device workspace of at least qlm_kv_attention_workspace_bytes for
+ *           this batch's sizes or larger ones, 256-byte aligned, scratch
+ */
+typedef struct qlm_kv_query {
+    qlm_rows q, out;
+    int32_t n_heads;             /* a multiple of n_kv_heads                     */
+    float scale;                 /* finite                                       */
+    int32_t accumulate;          /* nonzero: add to the cache's weights          */
+    float weight_decay;          /* finite, >= 0                                 */
+} qlm_kv_query;
+
+size_t qlm_kv_attention_workspace_bytes(const qlm_kv_cache *cache, const qlm_kv_batch *batch,
+                                        int32_t n_heads, int32_t accumulate);
+int qlm_kv_attention(const qlm_kv_cache *cache, const qlm_kv_batch *batch,
+                     const qlm_kv_query *query, void *ws, size_t ws_bytes, qlm_stream stream);
+
+/*
+ * Cuts every sequence to `budget` slots, for each kv head by itself.  Protected
+ * are the slots whose position is greater than the sequence's (and head's)
+ * greatest position less `recent`.  Of a sequence of length L > budget the budget slots
+ * that are kept come first by protection, then by greater weight (a NaN is the
+ * least), then by lower slot.  Kept slots at or past the budget move into the
+ * slots that fall free below it, the first of the one into the first of the
+ * other, with their position and weight; a block that takes them has its scale
+ * renewed as in qlm_kv_append.  The blocks past the budget are then free.
+ * Sequences of at most budget slots, and sequences whose table names a block
+ * outside the pool, stay as they are.
+ *   budget       slots kept, a multiple of 64, >= 64
+ *   recent       0 <= recent <= budget
+ *   lengths_out  [n_seqs] device out: min(length, budget) (the length where the
+ *                sequence stays); may be the batch's own lengths
+ *   ws           device workspace of at least qlm_kv_evict_workspace_bytes,
+ *                256-byte aligned, scratch
+ * The cache keeps positions and weights; the batch's rows are not used.
+ */
+size_t qlm_kv_evict_workspace_bytes(const qlm_kv_cache *cache, const qlm_kv_batch *batch,
+                                    int32_t budget);
+int qlm_kv_evict(const qlm_kv_cache *cache, const qlm_kv_batch *batch, int32_t budget,
+                 int32_t recent, int32_t *lengths_out, void *ws, size_t ws_bytes,
+                 qlm_stream stream);
+
+/*
+ * Products with 4-bit weights.  A matrix of n_out outputs and n_in inputs holds
+ * a code c in 0..15 for each weight, and for each output and group of `group`
+ * inputs (the last one may be short) a half-precision scale s and a zero point
+ * z in 0..15; weight = (c - z) * s.
+ * qlm_w4_pack lays the codes out once, in the order in which the kernel reads
+ * them (qlm_w4_packed_bytes bytes, 256-byte aligned).
+ *   codes  [n_out][n_in] one code a byte (its low four bits)
+ *   scale  [n_out][ceil(n_in / group)] half precision
+ *   zero   [n_out][ceil(n_in / group)] or NULL (8 everywhere)
+ */
+typedef struct qlm_w4 {
+    int32_t n_out, n_in;         /* 1 .. 2^24 each                               */
+    int32_t group;               /* 32, 64 or 128                                */
+    void *packed;
+} qlm_w4;
+
+size_t qlm_w4_packed_bytes(int32_t n_out, int32_t n_in, int32_t group);
+int qlm_w4_pack(const qlm_w4 *weight, const uint8_t *codes, const void *scale,
+                const uint8_t *zero, qlm_stream stream);
+
+/*
+ * out[m][n] = sum over k of x[m][k] * weight[n][k], the sums in single
+ * precision from exact products within a group, rounded once.
+ *   x    [n_rows][n_in], x_stride elements between rows (>= n_in)
+ *   out  [n_rows][n_out], out_stride elements between rows; of x's dtype, may
+ *        not alias x
+ *   ws   device workspace of at least qlm_w4_workspace_bytes, 256-byte aligned,
+ *        scratch; may be NULL when that is 0
+ */
+size_t qlm_w4_workspace_bytes(const qlm_w4 *weight, int32_t n_rows);
+int qlm_w4_matmul(const qlm_w4 *weight, const void *x, int64_t x_stride, void *out,
+                  int64_t out_stride, int32_t n_rows, int32_t dtype, void *ws, size_t ws_bytes,
+                  qlm_stream stream);
+
 /* Largest G the scoring kernels accept for these M, C, I (on-chip budget). */
 int32_t qlm_max_groups(int32_t n_models, int32_t n_classes, int32_t n_instances,
                        int32_t with_eviction);

@@ -14,7 +14,8 @@ ROOT = os.path.dirname(HERE)
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 LIB = os.path.join(HERE, "libqlm.so")
 ARCH = "gfx950"
-SOURCES = ["qlm.hip", "search.hip", "fcfs.hip", "profile.hip"]
+SOURCES = ["qlm.hip", "search.hip", "fcfs.hip", "profile.hip", "kv.hip", "kv_attention.hip",
+           "w4.hip"]
 
 HIP_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=" + ARCH, "-fPIC", "-shared",

@@ -8,7 +8,8 @@ Function names follow the C interface: ``rwt_score``, ``rwt_score_exact``,
 ``best_plan`` (with ``best_plan_workspace_bytes``), ``validate_plans``,
 ``validate_problem``, ``search_n_moves``, ``search_workspace_bytes``,
 ``search_moves``, ``search_screen``, ``local_search``, ``seed_plans``,
-``place_group``.
+``place_group``; and of a serving instance's decode step ``kv_append``,
+``kv_attention``, ``kv_evict``, ``w4_pack``, ``w4_matmul``.
 """
 from __future__ import annotations
 
@@ -63,6 +64,37 @@ class Profile(ctypes.Structure):
     _fields_ = [("prefill", ctypes.c_void_p), ("decode_time", ctypes.c_void_p),
                 ("ineff", ctypes.c_void_p), ("max_tokens", ctypes.c_void_p),
                 ("kv_tokens", ctypes.c_void_p), ("mean_tokens", ctypes.c_void_p)]
+
+
+class KvCacheStruct(ctypes.Structure):
+    _fields_ = [("n_blocks", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("format", ctypes.c_int32),
+                ("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("position", ctypes.c_void_p), ("weight", ctypes.c_void_p)]
+
+
+class KvBatchStruct(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_rows", ctypes.c_int32),
+                ("max_new", ctypes.c_int32), ("max_length", ctypes.c_int32),
+                ("table_stride", ctypes.c_int64), ("block_table", ctypes.c_void_p),
+                ("lengths", ctypes.c_void_p), ("row_start", ctypes.c_void_p)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+class KvQuery(ctypes.Structure):
+    _fields_ = [("q", Rows), ("out", Rows), ("n_heads", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("accumulate", ctypes.c_int32),
+                ("weight_decay", ctypes.c_float)]
+
+
+class W4Struct(ctypes.Structure):
+    _fields_ = [("n_out", ctypes.c_int32), ("n_in", ctypes.c_int32), ("group", ctypes.c_int32),
+                ("packed", ctypes.c_void_p)]
 
 
 PROFILE_FIELDS = ("prefill", "decode_time", "ineff", "max_tokens", "kv_tokens", "mean_tokens")
@@ -122,6 +154,24 @@ def library():
             lib.qlm_place_begin.argtypes = [P, PL, vp, sz, vp]
             lib.qlm_place_step.argtypes = [P, i64, i32, vp, sz, vp, vp, vp]
             lib.qlm_place_end.argtypes = [P, i64, ctypes.POINTER(PlansOut), vp, sz, vp, vp]
+            C, B = ctypes.POINTER(KvCacheStruct), ctypes.POINTER(KvBatchStruct)
+            R, Q, W = ctypes.POINTER(Rows), ctypes.POINTER(KvQuery), ctypes.POINTER(W4Struct)
+            lib.qlm_kv_append.argtypes = [C, B, R, R, vp, vp]
+            lib.qlm_kv_attention_workspace_bytes.argtypes = [C, B, i32, i32]
+            lib.qlm_kv_attention_workspace_bytes.restype = ctypes.c_size_t
+            lib.qlm_kv_attention.argtypes = [C, B, Q, vp, sz, vp]
+            lib.qlm_kv_evict_workspace_bytes.argtypes = [C, B, i32]
+            lib.qlm_kv_evict_workspace_bytes.restype = ctypes.c_size_t
+            lib.qlm_kv_evict.argtypes = [C, B, i32, i32, vp, vp, sz, vp]
+            lib.qlm_w4_packed_bytes.argtypes = [i32, i32, i32]
+            lib.qlm_w4_packed_bytes.restype = ctypes.c_size_t
+            lib.qlm_w4_pack.argtypes = [W, vp, vp, vp, vp]
+            lib.qlm_w4_workspace_bytes.argtypes = [W, i32]
+            lib.qlm_w4_workspace_bytes.restype = ctypes.c_size_t
+            lib.qlm_w4_matmul.argtypes = [W, vp, i64, vp, i64, i32, i32, vp, sz, vp]
+            for name in ("qlm_kv_append", "qlm_kv_attention", "qlm_kv_evict", "qlm_w4_pack",
+                         "qlm_w4_matmul"):
+                getattr(lib, name).restype = ctypes.c_int
             for name in ("qlm_rwt_score", "qlm_rwt_score_exact", "qlm_best_plan", "qlm_best_plan_static",
                          "qlm_score_form",
                          "qlm_validate_plans", "qlm_validate_problem", "qlm_timing_enable",
@@ -629,3 +679,275 @@ class PlaceSession:
                                        ctypes.byref(o), _ptr(self.ws), self.ws.numel(),
                                        _ptr(score), _stream(self.stream)))
         return out, score[:self.n_plans]
+
+
+# -- a serving instance's decode step ------------------------------------------
+
+KV_BLOCK = 64
+_KV_FORMATS = ("float8_e4m3fn", "int8")
+
+
+def _row_type(t, what):
+    import torch
+    if t.dtype == torch.float16:
+        return 0
+    if t.dtype == torch.bfloat16:
+        return 1
+    raise ValueError("%s must be float16 or bfloat16" % what)
+
+
+def _rows(t, heads, dim, what):
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+        raise ValueError("%s must be [rows, %d, %d]" % (what, heads, dim))
+    if t.stride(2) != 1 and dim > 1:
+        raise ValueError("%s: a head's dims must be contiguous" % what)
+    return Rows(t.data_ptr(), t.stride(0), t.stride(1), _row_type(t, what))
+
+
+class DeviceKvCache:
+    """An 8-bit token cache in device memory plus the C struct (qlm_kv_cache).
+
+    k_codes   [n_blocks, n_kv_heads, 64, head_dim], float8_e4m3fn or int8
+    v_codes   [n_blocks, n_kv_heads, 4, head_dim, 16], the same type: slot t of a
+              block stands in group (t // 4) % 4, there at place (t // 16) * 4 + t % 4
+    k_scale, v_scale   [n_blocks, n_kv_heads] float32
+    position  [n_blocks, n_kv_heads, 64] int32 or None
+    weight    [n_blocks, n_kv_heads, 64] float32 or None
+
+    Every tensor is contiguous.  ``DeviceKvCache.empty`` allocates one."""
+
+    def __init__(self, k_codes, v_codes, k_scale, v_scale, position=None, weight=None):
+        import torch
+        if k_codes.dim() != 4 or k_codes.shape[2] != KV_BLOCK:
+            raise ValueError("k_codes must be [n_blocks, n_kv_heads, 64, head_dim]")
+        nb, h, _, d = k_codes.shape
+        kinds = [getattr(torch, n) for n in _KV_FORMATS]
+        if k_codes.dtype not in kinds or v_codes.dtype != k_codes.dtype:
+            raise ValueError("codes must be float8_e4m3fn or int8, keys and values alike")
+        want = {"v_codes": (v_codes, (nb, h, 4, d, 16), v_codes.dtype),
+                "k_scale": (k_scale, (nb, h), torch.float32),
+                "v_scale": (v_scale, (nb, h), torch.float32),
+                "position": (position, (nb, h, KV_BLOCK), torch.int32),
+                "weight": (weight, (nb, h, KV_BLOCK), torch.float32),
+                "k_codes": (k_codes, (nb, h, KV_BLOCK, d), k_codes.dtype)}
+        for name, (x, shape, dtype) in want.items():
+            if x is None and name in ("position", "weight"):
+                continue
+            if tuple(x.shape) != shape or x.dtype != dtype or not x.is_contiguous():
+                raise ValueError("%s must be contiguous %s of %s" % (name, shape, dtype))
+        self.n_blocks, self.n_kv_heads, self.head_dim = int(nb), int(h), int(d)
+        self.k_codes, self.v_codes = k_codes, v_codes
+        self.k_scale, self.v_scale = k_scale, v_scale
+        self.position, self.weight = position, weight
+        self.struct = KvCacheStruct(self.n_blocks, self.n_kv_heads, self.head_dim,
+                                    kinds.index(k_codes.dtype), _ptr(k_codes), _ptr(v_codes),
+                                    _ptr(k_scale), _ptr(v_scale), _ptr(position), _ptr(weight))
+        self._ref = ctypes.byref(self.struct)
+
+    @classmethod
+    def empty(cls, n_blocks, n_kv_heads, head_dim, dtype=None, keep_weights=True, device="cuda"):
+        """An unwritten cache; positions and weights are kept unless
+        keep_weights is False."""
+        import torch
+        dtype = torch.float8_e4m3fn if dtype is None else dtype
+        codes = lambda *s: torch.empty(s, dtype=torch.uint8, device=device).view(dtype)  # noqa: E731
+        slots = (n_blocks, n_kv_heads, KV_BLOCK)
+        return cls(codes(*slots, head_dim), codes(n_blocks, n_kv_heads, 4, head_dim, 16),
+                   torch.empty((n_blocks, n_kv_heads), dtype=torch.float32, device=device),
+                   torch.empty((n_blocks, n_kv_heads), dtype=torch.float32, device=device),
+                   torch.empty(slots, dtype=torch.int32, device=device) if keep_weights else None,
+                   torch.empty(slots, dtype=torch.float32, device=device) if keep_weights else None)
+
+
+class KvBatch:
+    """The sequences of a call (qlm_kv_batch): ``block_table`` [n_seqs, blocks]
+    int32, ``lengths`` [n_seqs] int32 (new tokens included), ``row_start``
+    [n_seqs + 1] int32 or None (one row each), ``n_rows`` rows in all, at most
+    ``max_new`` of a sequence, which holds at most ``max_length`` slots (default:
+    what the table's rows can hold)."""
+
+    def __init__(self, block_table, lengths, row_start=None, n_rows=None, max_new=1,
+                 max_length=None):
+        import torch
+        for name, x in (("block_table", block_table), ("lengths", lengths),
+                        ("row_start", row_start)):
+            if x is not None and x.dtype != torch.int32:
+                raise ValueError(name + " must be int32")
+        n = int(lengths.numel())
+        if block_table.dim() != 2 or block_table.shape[0] != n or not lengths.is_contiguous():
+            raise ValueError("block_table must be [n_seqs, blocks] and lengths [n_seqs]")
+        if block_table.shape[1] > 1 and block_table.stride(1) != 1:
+            raise ValueError("a row of block_table must be contiguous")
+        if row_start is not None and (row_start.numel() != n + 1 or not row_start.is_contiguous()):
+            raise ValueError("row_start must be [n_seqs + 1]")
+        if row_start is not None and n_rows is None:
+            raise ValueError("n_rows is required with row_start")
+        width = int(block_table.shape[1])
+        if max_length is None:
+            max_length = width * KV_BLOCK
+        if max_length > width * KV_BLOCK:
+            raise ValueError("max_length exceeds the blocks of block_table's rows")
+        self.block_table, self.lengths, self.row_start = block_table, lengths, row_start
+        self.n_seqs, self.max_new, self.max_length = n, int(max_new), int(max_length)
+        self.n_rows = n if row_start is None else int(n_rows)
+        # (the stride of a table of one row says nothing)
+        stride = int(block_table.stride(0)) if n > 1 else width
+        self.struct = KvBatchStruct(n, self.n_rows, self.max_new, self.max_length, stride,
+                                    _ptr(block_table), _ptr(lengths), _ptr(row_start))
+        self._ref = ctypes.byref(self.struct)
+
+
+def _check_n_rows(batch, t, what):
+    if t.shape[0] != batch.n_rows:
+        raise ValueError("%s must have the batch's %d rows" % (what, batch.n_rows))
+
+
+def kv_append(cache: DeviceKvCache, batch: KvBatch, k, v, first_position=None, stream=None):
+    """Writes the new tokens' keys and values [n_rows, n_kv_heads, head_dim]
+    (float16 or bfloat16) into the last slots of their sequences.
+    first_position [n_seqs] int32: the position of each sequence's first new
+    token (the slot's number when None)."""
+    import torch
+    _check_n_rows(batch, k, "k")
+    _check_n_rows(batch, v, "v")
+    if first_position is not None and (first_position.dtype != torch.int32 or
+                                       first_position.numel() != batch.n_seqs or
+                                       not first_position.is_contiguous()):
+        raise ValueError("first_position must be [n_seqs] int32")
+    rk = _rows(k, cache.n_kv_heads, cache.head_dim, "k")
+    rv = _rows(v, cache.n_kv_heads, cache.head_dim, "v")
+    _check(library().qlm_kv_append(cache._ref, batch._ref, ctypes.byref(rk), ctypes.byref(rv),
+                                   _ptr(first_position), _stream(stream)))
+
+
+def kv_attention_workspace_bytes(cache: DeviceKvCache, batch: KvBatch, n_heads: int,
+                                 accumulate: bool = False) -> int:
+    return int(library().qlm_kv_attention_workspace_bytes(cache._ref, batch._ref, int(n_heads),
+                                                          int(bool(accumulate))))
+
+
+def kv_attention_workspace(cache: DeviceKvCache, batch: KvBatch, n_heads: int,
+                           accumulate: bool = False):
+    import torch
+    nbytes = kv_attention_workspace_bytes(cache, batch, n_heads, accumulate)
+    return torch.empty(max(nbytes, 1), dtype=torch.uint8, device=cache.k_codes.device)
+
+
+def kv_attention(cache: DeviceKvCache, batch: KvBatch, q, scale=None, weight_decay=None,
+                 out=None, ws=None, stream=None):
+    """Attention of the batch's rows q [n_rows, n_heads, head_dim] over their
+    sequences' slots; the outputs, of q's shape and type.  scale: of the
+    scores, head_dim ** -0.5 when None.  weight_decay: when given, the cache's
+    weights become weight_decay * weight plus the step's attention weights."""
+    import torch
+    _check_n_rows(batch, q, "q")
+    heads = int(q.shape[1])
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out must have q's shape and type")
+    if ws is None:
+        ws = kv_attention_workspace(cache, batch, heads, weight_decay is not None)
+    query = KvQuery(_rows(q, heads, cache.head_dim, "q"), _rows(out, heads, cache.head_dim, "out"),
+                    heads, cache.head_dim ** -0.5 if scale is None else scale,
+                    weight_decay is not None, weight_decay or 0.0)
+    _check(library().qlm_kv_attention(cache._ref, batch._ref, ctypes.byref(query), ws.data_ptr(),
+                                      ws.numel(), _stream(stream)))
+    return out
+
+
+def kv_evict_workspace_bytes(cache: DeviceKvCache, batch: KvBatch, budget: int) -> int:
+    return int(library().qlm_kv_evict_workspace_bytes(cache._ref, batch._ref, int(budget)))
+
+
+def kv_evict_workspace(cache: DeviceKvCache, batch: KvBatch, budget: int):
+    import torch
+    return torch.empty(max(kv_evict_workspace_bytes(cache, batch, budget), 1), dtype=torch.uint8,
+                       device=cache.k_codes.device)
+
+
+def kv_evict(cache: DeviceKvCache, batch: KvBatch, budget: int, recent: int = 0, out=None,
+             ws=None, stream=None):
+    """Cuts the sequences to `budget` slots (a multiple of 64) for each kv head:
+    the slots of the `recent` newest positions and those of the greatest weight
+    stay.  Returns the new lengths [n_seqs] int32 (`out`, which may be the
+    batch's own lengths)."""
+    import torch
+    if out is None:
+        out = torch.empty_like(batch.lengths)
+    elif out.dtype != torch.int32 or out.numel() != batch.n_seqs or not out.is_contiguous():
+        raise ValueError("out must be [n_seqs] int32")
+    if ws is None:
+        ws = kv_evict_workspace(cache, batch, budget)
+    _check(library().qlm_kv_evict(cache._ref, batch._ref, int(budget), int(recent),
+                                  out.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)))
+    return out
+
+
+class W4:
+    """A matrix of 4-bit weights as the kernels read it (qlm_w4): made by
+    ``w4_pack``."""
+
+    def __init__(self, packed, n_out, n_in, group):
+        self.packed, self.n_out, self.n_in, self.group = packed, n_out, n_in, group
+        self.struct = W4Struct(n_out, n_in, group, _ptr(packed))
+        self._ref = ctypes.byref(self.struct)
+
+
+def w4_pack(codes, scale, zero=None, group=None, stream=None):
+    """Lays out 4-bit weights (code - zero) * scale once: ``codes`` [n_out, n_in]
+    uint8 (0..15), ``scale`` [n_out, groups] float16, ``zero`` [n_out, groups]
+    uint8 (8 everywhere when None), a group for each 32, 64 or 128 inputs
+    (found from the shapes when None)."""
+    import torch
+    if codes.dim() != 2 or codes.dtype != torch.uint8 or not codes.is_contiguous():
+        raise ValueError("codes must be contiguous [n_out, n_in] uint8")
+    n, k = (int(x) for x in codes.shape)
+    fits = [g for g in (128, 64, 32) if scale.dim() == 2 and -(-k // g) == scale.shape[1]]
+    if group is None:
+        if not fits:
+            raise ValueError("scale's groups fit no group of 32, 64 or 128 inputs")
+        group = fits[0]
+    if group not in fits or scale.shape[0] != n or scale.dtype != torch.float16 or \
+            not scale.is_contiguous():
+        raise ValueError("scale must be contiguous [n_out, ceil(n_in / group)] float16")
+    if zero is not None and (zero.shape != scale.shape or zero.dtype != torch.uint8 or
+                             not zero.is_contiguous()):
+        raise ValueError("zero must be contiguous uint8 of scale's shape")
+    packed = torch.empty(int(library().qlm_w4_packed_bytes(n, k, group)), dtype=torch.uint8,
+                         device=codes.device)
+    w = W4(packed, n, k, group)
+    _check(library().qlm_w4_pack(w._ref, _ptr(codes), _ptr(scale), _ptr(zero), _stream(stream)))
+    return w
+
+
+def w4_workspace_bytes(weight: W4, n_rows: int) -> int:
+    return int(library().qlm_w4_workspace_bytes(weight._ref, int(n_rows)))
+
+
+def w4_workspace(weight: W4, n_rows: int):
+    import torch
+    return torch.empty(max(w4_workspace_bytes(weight, n_rows), 1), dtype=torch.uint8,
+                       device=weight.packed.device)
+
+
+def w4_matmul(x, weight: W4, out=None, ws=None, stream=None):
+    """x [n_rows, n_in] (float16 or bfloat16) times the matrix: [n_rows, n_out]
+    of x's type."""
+    import torch
+    if x.dim() != 2 or x.shape[1] != weight.n_in or (x.stride(1) != 1 and weight.n_in > 1):
+        raise ValueError("x must be [rows, %d] with contiguous rows" % weight.n_in)
+    kind = _row_type(x, "x")
+    n = int(x.shape[0])
+    if out is None:
+        out = torch.empty((n, weight.n_out), dtype=x.dtype, device=x.device)
+    elif tuple(out.shape) != (n, weight.n_out) or out.dtype != x.dtype or \
+            (out.stride(1) != 1 and weight.n_out > 1):
+        raise ValueError("out must be [rows, %d] of x's type with contiguous rows" % weight.n_out)
+    if ws is None:
+        ws = w4_workspace(weight, n)
+    # (the stride of a matrix of one row says nothing)
+    xs, os_ = (x.stride(0), out.stride(0)) if n > 1 else (weight.n_in, weight.n_out)
+    _check(library().qlm_w4_matmul(weight._ref, x.data_ptr(), xs, out.data_ptr(), os_, n, kind,
+                                   ws.data_ptr(), ws.numel(), _stream(stream)))
+    return out
