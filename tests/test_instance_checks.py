@@ -1,0 +1,211 @@
+"""The instance operators without a GPU: host-side argument checks of the C
+interface and of the binding, before anything reaches the device."""
+import ctypes
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def qlm():
+    from paper_2407_00047_amd import qlm
+    return qlm
+
+
+@pytest.fixture(scope="module")
+def lib(qlm):
+    return qlm.library()
+
+
+A = 0x100000          # a pointer that the checks never follow
+P = ctypes.byref
+
+
+def cache(qlm, **more):
+    f = dict(n_blocks=8, n_kv_heads=2, head_dim=64, format=0, k_codes=A, v_codes=A, k_scale=A,
+             v_scale=A, position=A, weight=A)
+    f.update(more)
+    return qlm.KvCacheStruct(*f.values())
+
+
+def batch(qlm, **more):
+    f = dict(n_seqs=2, n_rows=2, max_new=1, max_length=100, table_stride=2, block_table=A,
+             lengths=A, row_start=None)
+    f.update(more)
+    return qlm.KvBatchStruct(*f.values())
+
+
+def rows(qlm, **more):
+    f = dict(data=A, row_stride=128, head_stride=64, dtype=0)
+    f.update(more)
+    return qlm.Rows(*f.values())
+
+
+BAD_CACHE = [dict(n_blocks=0), dict(n_kv_heads=0), dict(n_kv_heads=1025), dict(head_dim=0),
+             dict(head_dim=8), dict(head_dim=72), dict(head_dim=272), dict(format=2),
+             dict(format=-1), dict(k_codes=None), dict(v_codes=None), dict(k_scale=None),
+             dict(v_scale=None), dict(k_codes=A + 8), dict(v_codes=A + 4)]
+BAD_BATCH = [dict(n_seqs=-1), dict(n_rows=-1), dict(max_new=0), dict(max_length=-1),
+             dict(max_length=(1 << 28) + 1, table_stride=1 << 23), dict(table_stride=1),
+             dict(block_table=None), dict(lengths=None), dict(n_rows=3), dict(max_new=2),
+             dict(n_seqs=(1 << 20) + 1, n_rows=(1 << 20) + 1)]
+
+
+def calls(qlm, lib, c, b):
+    """The three calls with otherwise good arguments."""
+    r = rows(qlm)
+    out = rows(qlm, data=A + 4096)
+    q = qlm.KvQuery(r, out, 4, 0.125, 0, 0.0)
+    big = 1 << 40
+    return [lib.qlm_kv_append(c, b, P(r), P(r), None, None),
+            lib.qlm_kv_attention(c, b, P(q), A, big, None),
+            lib.qlm_kv_evict(c, b, 64, 0, A, A, big, None)]
+
+
+@pytest.mark.parametrize("bad", BAD_CACHE, ids=str)
+def test_bad_caches(qlm, lib, bad):
+    assert calls(qlm, lib, P(cache(qlm, **bad)), P(batch(qlm))) == [qlm.QLM_ERR_ARG] * 3
+
+
+@pytest.mark.parametrize("bad", BAD_BATCH, ids=str)
+def test_bad_batches(qlm, lib, bad):
+    assert calls(qlm, lib, P(cache(qlm)), P(batch(qlm, **bad))) == [qlm.QLM_ERR_ARG] * 3
+
+
+def test_null_structs(qlm, lib):
+    assert calls(qlm, lib, None, P(batch(qlm))) == [qlm.QLM_ERR_ARG] * 3
+    assert calls(qlm, lib, P(cache(qlm)), None) == [qlm.QLM_ERR_ARG] * 3
+    assert b"batch" in lib.qlm_last_error()
+
+
+def test_append_checks(qlm, lib):
+    c, b = cache(qlm), batch(qlm)
+    good = rows(qlm)
+    for bad in (None, rows(qlm, data=None), rows(qlm, dtype=2), rows(qlm, data=A + 1)):
+        p = None if bad is None else P(bad)
+        assert lib.qlm_kv_append(P(c), P(b), p, P(good), None, None) == qlm.QLM_ERR_ARG
+        assert lib.qlm_kv_append(P(c), P(b), P(good), p, None, None) == qlm.QLM_ERR_ARG
+    # nothing to write: no device work
+    none = batch(qlm, n_seqs=0, n_rows=0)
+    assert lib.qlm_kv_append(P(c), P(none), None, None, None, None) == qlm.QLM_OK
+
+
+def test_attention_checks(qlm, lib):
+    c, b = cache(qlm), batch(qlm)
+    good = dict(q=rows(qlm), out=rows(qlm, data=A + 4096), n_heads=4, scale=0.1, accumulate=0,
+                weight_decay=0.0)
+    need = lib.qlm_kv_attention_workspace_bytes(P(c), P(b), 4, 0)
+    assert need > 0
+    assert lib.qlm_kv_attention_workspace_bytes(P(c), P(b), 4, 1) > need
+    assert lib.qlm_kv_attention_workspace_bytes(None, P(b), 4, 0) == 0
+    assert lib.qlm_kv_attention_workspace_bytes(P(c), P(b), 0, 0) == 0
+
+    def call(ws=A, size=need, cc=c, **more):
+        f = dict(good)
+        f.update(more)
+        return lib.qlm_kv_attention(P(cc), P(b), P(qlm.KvQuery(*f.values())), ws, size, None)
+
+    assert lib.qlm_kv_attention(P(c), P(b), None, A, need, None) == qlm.QLM_ERR_ARG
+    nan, inf = float("nan"), float("inf")
+    for bad in (dict(n_heads=0), dict(n_heads=3), dict(n_heads=1 << 17), dict(scale=nan),
+                dict(scale=inf), dict(q=rows(qlm, data=None)), dict(out=rows(qlm, dtype=1)),
+                dict(out=rows(qlm)), dict(accumulate=1, weight_decay=nan),
+                dict(accumulate=1, weight_decay=-1.0), dict(accumulate=1, weight_decay=inf),
+                dict(accumulate=1, cc=cache(qlm, weight=None))):
+        assert call(**bad) == qlm.QLM_ERR_ARG, bad
+    for bad in (dict(ws=None), dict(ws=A + 16), dict(size=need - 1)):
+        assert call(**bad) == qlm.QLM_ERR_WORKSPACE, bad
+
+
+def test_evict_checks(qlm, lib):
+    c, b = cache(qlm), batch(qlm)
+    need = lib.qlm_kv_evict_workspace_bytes(P(c), P(b), 64)
+    assert need > 0 and lib.qlm_kv_evict_workspace_bytes(P(c), P(b), 128) > need
+    assert lib.qlm_kv_evict_workspace_bytes(P(c), P(b), 0) == 0
+
+    def call(cc=c, budget=64, recent=0, out=A, ws=A, size=need):
+        return lib.qlm_kv_evict(P(cc), P(b), budget, recent, out, ws, size, None)
+
+    for bad in (dict(budget=0), dict(budget=-64), dict(budget=63), dict(budget=100),
+                dict(recent=-1), dict(recent=65), dict(out=None), dict(cc=cache(qlm, weight=None)),
+                dict(cc=cache(qlm, position=None))):
+        assert call(**bad) == qlm.QLM_ERR_ARG, bad
+    for bad in (dict(ws=None), dict(ws=A + 64), dict(size=need - 1)):
+        assert call(**bad) == qlm.QLM_ERR_WORKSPACE, bad
+
+
+def test_w4_checks(qlm, lib):
+    good = dict(n_out=100, n_in=4096, group=64, packed=A)
+    for bad in (dict(n_out=0), dict(n_in=0), dict(group=16), dict(group=0), dict(group=256),
+                dict(packed=None), dict(packed=A + 128), dict(n_in=(1 << 24) + 1)):
+        w = qlm.W4Struct(*{**good, **bad}.values())
+        assert lib.qlm_w4_pack(P(w), A, A, None, None) == qlm.QLM_ERR_ARG, bad
+        assert lib.qlm_w4_matmul(P(w), A, 4096, 2 * A, 100, 1, 0, A, 1 << 40, None) == \
+            qlm.QLM_ERR_ARG, bad
+    w = qlm.W4Struct(*good.values())
+    assert lib.qlm_w4_pack(P(w), None, A, None, None) == qlm.QLM_ERR_ARG
+    assert lib.qlm_w4_pack(P(w), A, None, None, None) == qlm.QLM_ERR_ARG
+    assert lib.qlm_w4_pack(None, A, A, None, None) == qlm.QLM_ERR_ARG
+    mm = lib.qlm_w4_matmul
+    big = 1 << 40
+    assert mm(P(w), None, 4096, 2 * A, 100, 1, 0, A, big, None) == qlm.QLM_ERR_ARG
+    assert mm(P(w), A, 4096, None, 100, 1, 0, A, big, None) == qlm.QLM_ERR_ARG
+    assert mm(P(w), A, 4096, A, 100, 1, 0, A, big, None) == qlm.QLM_ERR_ARG
+    assert mm(P(w), A, 4095, 2 * A, 100, 1, 0, A, big, None) == qlm.QLM_ERR_ARG
+    assert mm(P(w), A, 4096, 2 * A, 99, 1, 0, A, big, None) == qlm.QLM_ERR_ARG
+    assert mm(P(w), A, 4096, 2 * A, 100, -1, 0, A, big, None) == qlm.QLM_ERR_ARG
+    assert mm(P(w), A, 4096, 2 * A, 100, 1, 2, A, big, None) == qlm.QLM_ERR_ARG
+    assert mm(P(w), A, 4096, 2 * A, 100, 0, 0, None, 0, None) == qlm.QLM_OK
+    need = lib.qlm_w4_workspace_bytes(P(w), 64)
+    if need:
+        assert mm(P(w), A, 4096, 2 * A, 100, 64, 0, None, need, None) == qlm.QLM_ERR_WORKSPACE
+        assert mm(P(w), A, 4096, 2 * A, 100, 64, 0, A, need - 1, None) == qlm.QLM_ERR_WORKSPACE
+    assert lib.qlm_w4_packed_bytes(16, 128, 128) == 1024 + 64
+    assert lib.qlm_w4_packed_bytes(17, 129, 32) == 4 * (1024 + 256)
+    assert lib.qlm_w4_packed_bytes(17, 129, 48) == 0
+
+
+def test_binding_refusals(qlm):
+    """Shapes and types that the binding turns down (host tensors: nothing is launched)."""
+    import torch
+    i32 = torch.int32
+    c = qlm.DeviceKvCache.empty(4, 2, 32, device="cpu")
+    with pytest.raises(ValueError):
+        qlm.DeviceKvCache(c.k_codes, c.v_codes.view(torch.int8), c.k_scale, c.v_scale)
+    with pytest.raises(ValueError):
+        qlm.DeviceKvCache(c.k_codes, c.k_codes, c.k_scale, c.v_scale)
+    with pytest.raises(ValueError):
+        qlm.DeviceKvCache(c.k_codes, c.v_codes, c.k_scale.double(), c.v_scale)
+    with pytest.raises(ValueError):
+        qlm.DeviceKvCache(c.k_codes, c.v_codes, c.k_scale, c.v_scale, position=c.weight)
+    t, n = torch.zeros((2, 3), dtype=i32), torch.zeros(2, dtype=i32)
+    for bad in (dict(block_table=t.long(), lengths=n), dict(block_table=t[0], lengths=n),
+                dict(block_table=t, lengths=n.long()), dict(block_table=t.t(), lengths=n),
+                dict(block_table=t, lengths=n, max_length=193),
+                dict(block_table=t, lengths=n, row_start=n, n_rows=2),
+                dict(block_table=t, lengths=n, row_start=torch.zeros(3, dtype=i32))):
+        with pytest.raises(ValueError):
+            qlm.KvBatch(**bad)
+    b = qlm.KvBatch(t, n)
+    half = lambda *s: torch.zeros(s, dtype=torch.float16)  # noqa: E731
+    for k in (half(3, 2, 32), half(2, 1, 32), half(2, 2, 16), half(2, 2, 32).float(),
+              half(2, 32, 2).transpose(1, 2)):
+        with pytest.raises(ValueError):
+            qlm.kv_append(c, b, k, half(2, 2, 32))
+    with pytest.raises(ValueError):
+        qlm.kv_append(c, b, half(2, 2, 32), half(2, 2, 32), first_position=n.long())
+    with pytest.raises(ValueError):
+        qlm.kv_attention(c, b, half(2, 4, 32), out=half(2, 4, 16), ws=n)
+    with pytest.raises(ValueError):
+        qlm.kv_evict(c, b, 64, out=n.long())
+    u8 = torch.zeros((4, 64), dtype=torch.uint8)
+    for codes, scale, zero in ((u8.int(), half(4, 2), None), (u8, half(4, 3), None),
+                               (u8, half(3, 2), None), (u8, half(4, 2).float(), None),
+                               (u8, half(4, 2), half(4, 2)), (u8.t(), half(4, 2), None)):
+        with pytest.raises(ValueError):
+            qlm.w4_pack(codes, scale, zero)
+    w = qlm.W4(torch.zeros(1024 + 128, dtype=torch.uint8), 16, 64, 32)
+    for x in (half(2, 63), half(64), half(2, 64).float(), half(64, 2).t()[:, :1]):
+        with pytest.raises(ValueError):
+            qlm.w4_matmul(x, w)
+    with pytest.raises(ValueError):
+        qlm.w4_matmul(half(2, 64), w, out=half(2, 15))
