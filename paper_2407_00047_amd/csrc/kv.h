@@ -48,6 +48,15 @@ __device__ inline int seq_rows(const Seqs &q, int s, int *row0)
     return min(r1 - r0, q.max_new);
 }
 
+// Reads through the scalar cache what every lane reads alike and no kernel
+// writes while it runs (the loads of a table entry then stand in no queue
+// behind the wide loads of codes).
+template <typename T> __device__ inline T uniform(const T *p)
+{
+    typedef const T __attribute__((address_space(4))) *scalar_ptr;
+    return *(scalar_ptr)(uintptr_t)p;
+}
+
 // -- codes ----------------------------------------------------------------
 
 template <int FMT> __host__ __device__ constexpr float top_code()

@@ -29,23 +29,43 @@ struct AttnArgs {
     int64_t q_row, q_head, o_row, o_head;
     int32_t dtype, wide;                 // wide: q may be read 16 bytes at a time
     float scale;                         // times log2(e)
-    int32_t nsplit, per_split, tiles;    // key splits, blocks of one, column tiles
+    int32_t tile;                        // columns of a tile
+    int32_t workers;                     // waves that share the units (k_attend_rows)
     int32_t cols, blocks;                // max_new * G, ceil(max_length / 64)
-    float *part_o, *part_lse;            // [seq][head][split][cols]([D])
+    float *part_o, *part_lse;            // [2 worker + which][tile]([D])
     float *lse;                          // [row][heads], log2 units; +inf: nothing seen
     float *s;                            // [seq][block][head][cols][64] scores, or NULL
     float decay;
 };
 
+// Maximum and sum over the four lanes of a column (16 lanes apart).
+__device__ inline void swap16(float x, float *a, float *b)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    *a = __builtin_bit_cast(float, (uint32_t)r[0]);
+    *b = __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+__device__ inline void swap32(float x, float *a, float *b)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    *a = __builtin_bit_cast(float, (uint32_t)r[0]);
+    *b = __builtin_bit_cast(float, (uint32_t)r[1]);
+}
 __device__ inline float group_max(float x)
 {
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
+    float a, b;
+    swap16(x, &a, &b);
+    swap32(fmaxf(a, b), &a, &b);
+    return fmaxf(a, b);
 }
 __device__ inline float group_sum(float x)
 {
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
+    float a, b;
+    swap16(x, &a, &b);
+    swap32(a + b, &a, &b);
+    return a + b;
 }
 
 // The codes of a dword that stand for NaN (e4m3), as a mask of their bytes.
@@ -103,78 +123,211 @@ __device__ inline void load_query(const AttnArgs &a, int64_t row, int head, bool
                     __builtin_bit_cast(float, (uint32_t)u[c][m * 8 + e] << 16) * by);
 }
 
-// Few query rows (decode): the columns of a tile are the query rows and heads
-// of one (sequence, kv head); the workgroup's four waves take blocks of 64 slots in
-// turn, each with its own running maximum, sum and output, joined at the end.
+// -- few query rows ---------------------------------------------------------
+//
+// The work is a list of units: one block of 64 slots for one tile of columns
+// (query rows and heads) of one kv head, in the order sequence, kv head, tile,
+// block.  Each worker (a wave) takes an equal run of units, whatever sequences they
+// belong to, so ragged lengths leave no worker behind; what it has for a tile
+// goes out as the result if it held every unit of the tile, else as a part that
+// k_attend_join adds up.
+
+struct Units {
+    int nb, tiles;       // blocks of the sequence, tiles of a kv head
+};
+
+__device__ inline Units units_of(const AttnArgs &a, int s)
+{
+    int row0;
+    const int n = seq_rows(a.q, s, &row0);
+    return {(seq_length(a.q, s) + kBlock - 1) / kBlock, (n * a.G + a.tile - 1) / a.tile};
+}
+
+// Units of each chunk of ceil(n_seqs / kThreads) sequences before it, and of all.
+__device__ inline int unit_prefix(const AttnArgs &a, int *pre, int *wave_sum)
+{
+    const int t = threadIdx.x, lane = t & 63, wv = t >> 6;
+    const int chunk = (a.q.n_seqs + kThreads - 1) / kThreads;
+    int sum = 0;
+    for (int s = t * chunk; s < min(a.q.n_seqs, (t + 1) * chunk); ++s) {
+        const Units u = units_of(a, s);
+        sum += u.nb * u.tiles * a.H;
+    }
+    int run = sum;
+    for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(run, o);
+        run += lane >= o ? v : 0;
+    }
+    if (lane == 63) wave_sum[wv] = run;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int k = 0; k < kWaves; ++k) {
+        before += k < wv ? wave_sum[k] : 0;
+        all += wave_sum[k];
+    }
+    pre[t] = before + run - sum;
+    __syncthreads();
+    return all;
+}
+
+__device__ inline int units_each(const AttnArgs &a, int all)
+{
+    return max(1, (all + a.workers - 1) / a.workers);
+}
+
+// Where a worker stands: unit `block` of item (kv head, tile) of a sequence.
+struct Cursor {
+    int s, h, tile, block, nb, tiles;
+
+    __device__ void enter(const AttnArgs &a, int seq)   // the first sequence from seq on with units
+    {
+        s = seq;
+        h = tile = block = 0;
+        nb = tiles = 0;
+        for (; s < a.q.n_seqs; ++s) {
+            const int len = max(0, min(uniform(a.q.lengths + s), a.q.max_length));
+            int n = 1;
+            if (a.q.row_start) {
+                const int r0 = max(0, min(uniform(a.q.row_start + s), a.q.n_rows));
+                n = min(max(r0, min(uniform(a.q.row_start + s + 1), a.q.n_rows)) - r0, a.q.max_new);
+            } else if (s >= a.q.n_rows) {
+                n = 0;
+            }
+            nb = (len + kBlock - 1) / kBlock;
+            tiles = (n * a.G + a.tile - 1) / a.tile;
+            if (nb * tiles > 0) break;
+        }
+    }
+    __device__ void next(const AttnArgs &a)
+    {
+        if (++block < nb) return;
+        block = 0;
+        if (++tile < tiles) return;
+        tile = 0;
+        if (++h < a.H) return;
+        enter(a, s + 1);
+    }
+    __device__ int block_id(const AttnArgs &a) const
+    {
+        return s < a.q.n_seqs ? uniform(a.q.table + s * a.q.table_stride + block) : -1;
+    }
+    // (an unmapped block: any memory of the pool)
+    __device__ int64_t row(const AttnArgs &a, int id) const
+    {
+        return (int64_t)((unsigned)id < (unsigned)a.n_blocks ? id : 0) * a.H + h;
+    }
+};
+
 // Scores S^T[slot][column] = K Q^T and outputs O^T[dim][column] = V^T P^T are
 // 16x16x32 matrix instructions; the score's layout (a lane holds 4 slots of a
 // column) is the layout in which P^T is taken, because the values are held in
-// that order of slots, so nothing passes through shared memory.
+// that order of slots, so nothing passes through shared memory.  A block's keys
+// and values stay in registers; the next unit's keys are loaded as soon as this
+// one's scores are formed, its values as soon as this one's are added, so that
+// loads are always under way.
 template <int FMT, int ND, int NT>
-__global__ __launch_bounds__(kThreads) void k_attend_rows(AttnArgs a)
+__global__ __launch_bounds__(kThreads, ND * NT <= 2 ? 2 : 1) void k_attend_rows(AttnArgs a)
 {
     constexpr int DT = ND * 4;                   // tiles of 16 dims
-    __shared__ float lo[kWaves][16][DT * 16 + 4];
-    __shared__ float llse[kWaves][NT][16];
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    __shared__ int pre[kThreads], wave_sum[kWaves];
+    const int lane = threadIdx.x & 63;
     const int g = lane >> 4, c16 = lane & 15;
-    int64_t at = blockIdx.x;
-    const int sp = (int)(at % a.nsplit);
-    at /= a.nsplit;
-    const int ct = (int)(at % a.tiles);
-    at /= a.tiles;
-    const int h = (int)(at % a.H), s = (int)(at / a.H);
-    int row0;
-    const int n = seq_rows(a.q, s, &row0);
-    const int len = seq_length(a.q, s);
-    const int cols = n * a.G, col0 = ct * NT * 16;
-    if (col0 >= cols) return;
-    const int before = len - n;                  // slots that row 0 sees, less one
-    const int hi_lim = before + min(cols - 1, col0 + NT * 16 - 1) / a.G + 1;
-    const int lo_lim = before + col0 / a.G + 1;
-    const int nb = (max(hi_lim, 0) + kBlock - 1) / kBlock;
-    const int b0 = sp * a.per_split, b1 = min(nb, b0 + a.per_split);
-    if (sp > 0 && b0 >= nb) return;
-    const int live = max(1, (nb + a.per_split - 1) / a.per_split);
+    const int all = __builtin_amdgcn_readfirstlane(unit_prefix(a, pre, wave_sum));
+    const int each = units_each(a, all);
+    const int worker = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + (threadIdx.x >> 6));
+    if ((int64_t)worker * each >= all) return;
+    const int u0 = worker * each, u1 = min(all, u0 + each);
+
+    // the chunk of sequences that holds unit u0, then the sequence, then the item
+    int chunk = 0;
+    for (int k = 0; k < kWaves; ++k) chunk += __popcll(__ballot(pre[k * 64 + lane] <= u0));
+    chunk = __builtin_amdgcn_readfirstlane(chunk) - 1;
+    Cursor cur;
+    cur.enter(a, chunk * ((a.q.n_seqs + kThreads - 1) / kThreads));
+    int left = u0 - __builtin_amdgcn_readfirstlane(pre[chunk]);
+    while (left >= cur.nb * cur.tiles * a.H) {
+        left -= cur.nb * cur.tiles * a.H;
+        cur.enter(a, cur.s + 1);
+    }
+    cur.h = left / (cur.nb * cur.tiles);
+    cur.tile = left / cur.nb % cur.tiles;
+    cur.block = left % cur.nb;
+
+    const int D = a.D;
+    // Dims past the last are read from the last ones: their query is 0, their
+    // output unused.  (32 bits beside a uniform base)
+    uint32_t koff[ND], voff[DT];
+    for (int c = 0; c < ND; ++c) koff[c] = c16 * D + min(c * 64 + g * 16, D - 16);
+    for (int d = 0; d < DT; ++d) voff[d] = (g * D + min(d * 16, D - 16) + c16) * 16;
+    uint4 kk[4][ND], vv[DT];
+    auto load_keys = [&](int64_t bh) {
+        const uint8_t *kp = a.kc + bh * kBlock * D;
+        for (int t = 0; t < 4; ++t)
+            for (int c = 0; c < ND; ++c) kk[t][c] = *(const uint4 *)(kp + t * 16 * D + koff[c]);
+    };
+    auto load_values = [&](int64_t bh) {
+        const uint8_t *vp = a.vc + bh * kBlock * D;
+        for (int d = 0; d < DT; ++d) vv[d] = *(const uint4 *)(vp + voff[d]);
+    };
+    int id = cur.block_id(a);
+    int64_t bh = cur.row(a, id);
+    load_keys(bh);
+    load_values(bh);
+    float ksc = uniform(a.ks + bh), vsc = uniform(a.vs + bh);
+    Cursor nxt = cur;
+    nxt.next(a);
+    int id1 = nxt.block_id(a);
 
     half8v qf[NT][ND][2];
-    float fac[NT];
+    float fac[NT], m[NT], l[NT], vscale = 0.f;
     int lim[NT];
-    for (int k = 0; k < NT; ++k) {
-        const int c = col0 + k * 16 + c16;
-        const bool valid = c < cols;
-        load_query<ND>(a, row0 + (valid ? c / a.G : 0), h * a.G + (valid ? c % a.G : 0), valid, g,
-                       qf[k], &fac[k]);
-        fac[k] *= a.scale;
-        lim[k] = valid ? before + c / a.G + 1 : 0;
-    }
     float4v acc[NT][DT];
-    float m[NT], l[NT];
+    int seg0 = u0;                               // first unit of the item at hand
+    int row0 = 0, cols = 0, col0 = 0, before = 0, hi_lim = 0, lo_lim = 0;
     for (int k = 0; k < NT; ++k) {
-        m[k] = -__builtin_inff();
-        l[k] = 0.f;
+        fac[k] = m[k] = l[k] = 0.f;
+        lim[k] = 0;
         for (int d = 0; d < DT; ++d) acc[k][d] = float4v{0.f, 0.f, 0.f, 0.f};
+        for (int c = 0; c < ND; ++c)
+            for (int x = 0; x < 2; ++x) qf[k][c][x] = half8v{0, 0, 0, 0, 0, 0, 0, 0};
     }
-    float vscale = 0.f;                          // the values' common scale so far
-    const int32_t *table = a.q.table + s * a.q.table_stride;
-    const int D = a.D;
 
-    for (int j = b0 + wv; j < b1; j += kWaves) {
-        const int id = __builtin_amdgcn_readfirstlane(table[j]);
-        if ((unsigned)id >= (unsigned)a.n_blocks) continue;   // no slots there
-        const int64_t bh = (int64_t)id * a.H + h;
-        const uint8_t *kp = a.kc + bh * kBlock * D, *vp = a.vc + bh * kBlock * D;
-        uint4 kk[4][ND], vv[DT];
-        for (int t = 0; t < 4; ++t)
-            for (int c = 0; c < ND; ++c) {
-                const int d = c * 64 + g * 16;
-                kk[t][c] = d < D ? *(const uint4 *)(kp + (t * 16 + c16) * D + d)
-                                 : uint4{0, 0, 0, 0};
+    for (int u = u0; u < u1; ++u) {
+        const int s = cur.s, h = cur.h, j = cur.block;
+        if (u == u0 || j == 0) {                 // a new item
+            seg0 = u;
+            int n = 1;
+            row0 = s;
+            if (a.q.row_start) {
+                row0 = max(0, min(uniform(a.q.row_start + s), a.q.n_rows));
+                n = min(max(row0, min(uniform(a.q.row_start + s + 1), a.q.n_rows)) - row0,
+                        a.q.max_new);
             }
-        for (int d = 0; d < DT; ++d)
-            vv[d] = d * 16 < D ? *(const uint4 *)(vp + (g * D + d * 16 + c16) * 16)
-                               : uint4{0, 0, 0, 0};
-        const float ksc = a.ks[bh], vsc = a.vs[bh];
+            before = max(0, min(uniform(a.q.lengths + s), a.q.max_length)) - n;
+            cols = n * a.G;
+            col0 = cur.tile * NT * 16;
+            hi_lim = before + min(cols - 1, col0 + NT * 16 - 1) / a.G + 1;
+            lo_lim = before + col0 / a.G + 1;
+            vscale = 1e-38f;                     // the values' common scale so far
+            for (int k = 0; k < NT; ++k) {
+                const int c = col0 + k * 16 + c16;
+                const bool valid = c < cols;
+                load_query<ND>(a, row0 + (valid ? c / a.G : 0), h * a.G + (valid ? c % a.G : 0),
+                               valid, g, qf[k], &fac[k]);
+                fac[k] *= a.scale;
+                lim[k] = valid ? before + c / a.G + 1 : 0;
+                m[k] = -__builtin_inff();
+                l[k] = 0.f;
+                for (int d = 0; d < DT; ++d) acc[k][d] = float4v{0.f, 0.f, 0.f, 0.f};
+            }
+        }
+        const bool mapped = (unsigned)id < (unsigned)a.n_blocks, more = u + 1 < u1;
+        const int64_t bh1 = nxt.row(a, id1);
+        const float ksc1 = uniform(a.ks + bh1), vsc1 = uniform(a.vs + bh1);
+        Cursor nxt2 = nxt;
+        if (u + 2 < u1) nxt2.next(a);
+        const int id2 = nxt2.block_id(a);
+        if (!mapped) vsc = 0.f;
 
         float4v sc[NT][4];
         for (int t = 0; t < 4; ++t) {
@@ -190,7 +343,8 @@ __global__ __launch_bounds__(kThreads) void k_attend_rows(AttnArgs a)
                 }
             }
         }
-        const bool masked = (j + 1) * kBlock > lo_lim;
+        if (more) load_keys(bh1);
+        const bool masked = (j + 1) * kBlock > lo_lim || !mapped;
         const int slot0 = j * kBlock + 4 * g;    // of tile 0, element 0
         float top[NT];
         bool grow = false;
@@ -200,7 +354,7 @@ __global__ __launch_bounds__(kThreads) void k_attend_rows(AttnArgs a)
             for (int t = 0; t < 4; ++t)
                 for (int i = 0; i < 4; ++i) {
                     float x = sc[k][t][i] * f;
-                    if (masked && slot0 + t * 16 + i >= lim[k]) x = -__builtin_inff();
+                    if (masked && (slot0 + t * 16 + i >= lim[k] || !mapped)) x = -__builtin_inff();
                     sc[k][t][i] = x;
                     top[k] = fmaxf(top[k], x);
                 }
@@ -248,7 +402,7 @@ __global__ __launch_bounds__(kThreads) void k_attend_rows(AttnArgs a)
             for (int d = 0; d < DT; ++d)
                 for (int t = 0; t < 4; ++t) {
                     uint32_t &w = (&vv[d].x)[t];
-                    const int left = hi_lim - (slot0 + t * 16);
+                    const int left = mapped ? hi_lim - (slot0 + t * 16) : 0;
                     w = left <= 0 ? 0u : left < 4 ? w & (0xffffffffu >> (8 * (4 - left))) : w;
                     if (FMT == QLM_KV_E4M3) nans |= nan_bytes(w);
                 }
@@ -288,96 +442,135 @@ __global__ __launch_bounds__(kThreads) void k_attend_rows(AttnArgs a)
                 acc[k][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x1, pb[k][1], acc[k][d], 0, 0, 0);
             }
         }
-    }
+        if (more) load_values(bh1);
 
-    // the four waves' results, a tile of columns at a time: normalised outputs
-    // weighted by exp2(lse)
-    for (int k = 0; k < NT; ++k) {
-        const float sum = group_sum(l[k]);
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        if (g == 0)
-            llse[wv][k][c16] = sum == 0.f ? -__builtin_inff() : m[k] - kRaise + __builtin_amdgcn_logf(sum);
-        __syncthreads();
-        for (int d = 0; d < DT; ++d) {
-            const float4v o = acc[k][d] * inv;
-            for (int i = 0; i < 4; ++i) lo[wv][c16][d * 16 + 4 * g + i] = o[i] * vscale;
-        }
-        __syncthreads();
-        // 16 threads to a column
-        const int cc = threadIdx.x >> 4, c = col0 + k * 16 + cc;
-        float f[kWaves], M = -__builtin_inff(), L = 0.f;
-        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, llse[w][k][cc]);
-        for (int w = 0; w < kWaves; ++w) {
-            f[w] = M == -__builtin_inff() && !(llse[w][k][cc] != llse[w][k][cc])
-                       ? 0.f : __builtin_amdgcn_exp2f(llse[w][k][cc] - M);
-            L += f[w];
-        }
-        const float li = L == 0.f ? 0.f : 1.f / L;
-        if (c < cols) {
-            const int64_t pi = (((int64_t)s * a.H + h) * a.nsplit + sp) * a.cols + c;
-            const int row = row0 + c / a.G, head = h * a.G + c % a.G;
-            for (int d = threadIdx.x & 15; d < D; d += 16) {
-                float o = 0.f;
-                for (int w = 0; w < kWaves; ++w) o += f[w] == 0.f ? 0.f : f[w] * lo[w][cc][d];
-                o *= li;
-                if (live > 1)
-                    a.part_o[pi * D + d] = o;
-                else
-                    ((uint16_t *)a.od)[row * a.o_row + head * a.o_head + d] =
-                        row_bits(o, a.dtype);
-            }
-            if ((threadIdx.x & 15) == 0) {
-                const float z = M + __builtin_amdgcn_logf(L);
-                if (live > 1)
-                    a.part_lse[pi] = L == 0.f ? -__builtin_inff() : z;
-                else
-                    a.lse[(int64_t)row * a.H * a.G + head] = L == 0.f ? __builtin_inff() : z;
+        if (!more || j + 1 == cur.nb) {          // the item ends here
+            const bool whole = j + 1 == cur.nb && j == u - seg0;
+            const int64_t part = 2 * (int64_t)worker + (seg0 == u0 ? 0 : 1);
+            for (int k = 0; k < NT; ++k) {
+                const float sum = group_sum(l[k]);
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                const int c = col0 + k * 16 + c16;
+                if (c >= cols) continue;
+                const int64_t row = row0 + c / a.G;
+                const int head = h * a.G + c % a.G;
+                const float lse = m[k] - kRaise + __builtin_amdgcn_logf(sum);
+                if (g == 0) {
+                    if (whole)
+                        a.lse[row * a.H * a.G + head] = sum == 0.f ? __builtin_inff() : lse;
+                    else
+                        a.part_lse[part * a.tile + k * 16 + c16] =
+                            sum == 0.f ? -__builtin_inff() : lse;
+                }
+                for (int d = 0; d < DT; ++d) {
+                    if (d * 16 >= D) break;
+                    const float4v o = acc[k][d] * inv * vscale;
+                    if (!whole) {
+                        *(float4v *)(a.part_o + (part * a.tile + k * 16 + c16) * D + d * 16 +
+                                     4 * g) = o;
+                    } else {
+                        uint16_t *p = (uint16_t *)a.od + row * a.o_row + head * a.o_head +
+                                      d * 16 + 4 * g;
+                        for (int i = 0; i < 4; ++i) p[i] = row_bits(o[i], a.dtype);
+                    }
+                }
             }
         }
+        cur = nxt;
+        nxt = nxt2;
+        id = id1;
+        id1 = id2;
+        bh = bh1;
+        ksc = ksc1;
+        vsc = vsc1;
     }
 }
 
-// Joins the key splits of a column: one wave to a (sequence, kv head, column).
-__global__ __launch_bounds__(kThreads) void k_attend_join(AttnArgs a, int tile_cols)
+// Adds up the parts of the columns whose units several workers held, and gives
+// the columns that see nothing their zeros: WPC waves to a column, the parts in
+// turn.
+template <int WPC> __global__ __launch_bounds__(kThreads) void k_attend_join(AttnArgs a)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-    const int64_t sh = w / a.cols;
-    const int c = (int)(w % a.cols);
-    if (sh >= (int64_t)a.q.n_seqs * a.H) return;
+    __shared__ float part[kWaves][256], sum[kWaves];
+    __shared__ int below[kWaves], total[kWaves];
+    constexpr int CPG = kWaves / WPC;            // columns of a workgroup
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    const int groups = (a.cols + CPG - 1) / CPG;
+    const int64_t sh = blockIdx.x / groups;
+    const int c = (int)(blockIdx.x % groups) * CPG + wv / WPC;
     const int s = (int)(sh / a.H), h = (int)(sh % a.H);
+    // units of the sequences before, and of all
+    int lo = 0, all = 0;
+    for (int k = threadIdx.x; k < a.q.n_seqs; k += kThreads) {
+        const Units u = units_of(a, k);
+        const int v = u.nb * u.tiles * a.H;
+        all += v;
+        lo += k < s ? v : 0;
+    }
+    for (int o = 32; o; o >>= 1) {
+        all += __shfl_xor(all, o);
+        lo += __shfl_xor(lo, o);
+    }
+    if (lane == 0) {
+        below[wv] = lo;
+        total[wv] = all;
+    }
+    __syncthreads();
+    lo = below[0] + below[1] + below[2] + below[3];
+    all = total[0] + total[1] + total[2] + total[3];
     int row0;
     const int n = seq_rows(a.q, s, &row0);
-    const int cols = n * a.G;
-    if (c >= cols) return;
-    // the splits of its tile, as the workgroups of the tile counted them
-    const int col0 = c / tile_cols * tile_cols;
-    const int hi = seq_length(a.q, s) - n + min(cols - 1, col0 + tile_cols - 1) / a.G + 1;
-    const int nb = (max(hi, 0) + kBlock - 1) / kBlock;
-    const int live = max(1, (nb + a.per_split - 1) / a.per_split);
-    if (live <= 1) return;
-    const int64_t p0 = sh * a.nsplit * a.cols + c;
-    float M = -__builtin_inff();
-    for (int k = lane; k < live; k += 64) M = fmaxf(M, a.part_lse[p0 + (int64_t)k * a.cols]);
-    for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
-    float L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < live; ++k) {
-        const float z = a.part_lse[p0 + (int64_t)k * a.cols];
-        const float f = z == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(z - M);
-        L += f;
-        if (f == 0.f) continue;
-        const float *po = a.part_o + (p0 + (int64_t)k * a.cols) * a.D;
-        for (int e = 0; e < 4; ++e)
-            if (e * 64 + lane < a.D) acc[e] += f * po[e * 64 + lane];
+    const Units u = units_of(a, s);
+    const int each = units_each(a, all);
+    const int u0 = lo + (h * u.tiles + c / a.tile) * u.nb, u1 = u0 + u.nb;
+    const int w0 = u0 / each, w1 = u.nb ? (u1 - 1) / each : w0 - 1;
+    // (whole at one worker: written there)
+    const bool mine = c < n * a.G && w0 != w1;
+    float M = -__builtin_inff(), L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+    auto place = [&](int w) {                    // of the part that worker w left
+        return (2 * (int64_t)w + (w == w0 && u0 % each ? 1 : 0)) * a.tile + c % a.tile;
+    };
+    if (mine) {
+        for (int w = w0 + lane; w <= w1; w += 64) M = fmaxf(M, a.part_lse[place(w)]);
+        for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+        for (int b = w0 + wv % WPC; b <= w1; b += 4 * WPC) {
+            float f[4], x[4][4];
+            for (int k = 0; k < 4; ++k) {
+                const int64_t at = place(min(b + k * WPC, w1));
+                f[k] = a.part_lse[at];
+                for (int e = 0; e < 4; ++e)
+                    x[k][e] = a.part_o[at * a.D + min(e * 64 + lane, a.D - 1)];
+            }
+            for (int k = 0; k < 4; ++k) {
+                const float z = b + k * WPC > w1 || f[k] == -__builtin_inff()
+                                    ? 0.f : __builtin_amdgcn_exp2f(f[k] - M);
+                L += z;
+                for (int e = 0; e < 4; ++e) acc[e] += z == 0.f ? 0.f : z * x[k][e];
+            }
+        }
     }
-    const int row = row0 + c / a.G, head = h * a.G + c % a.G;
-    const float li = L == 0.f ? 0.f : 1.f / L;
+    if (WPC > 1) {
+        for (int e = 0; e < 4; ++e) part[wv][e * 64 + lane] = acc[e];
+        if (lane == 0) sum[wv] = L;
+        __syncthreads();
+        if (wv % WPC) return;
+        L = 0.f;
+        for (int e = 0; e < 4; ++e) acc[e] = 0.f;
+        for (int k = wv; k < wv + WPC; ++k) {
+            L += sum[k];
+            for (int e = 0; e < 4; ++e) acc[e] += part[k][e * 64 + lane];
+        }
+    }
+    if (!mine) return;
+    const int64_t row = row0 + c / a.G;
+    const int head = h * a.G + c % a.G;
     for (int e = 0; e < 4; ++e)
         if (e * 64 + lane < a.D)
             ((uint16_t *)a.od)[row * a.o_row + head * a.o_head + e * 64 + lane] =
-                row_bits(acc[e] * li, a.dtype);
+                row_bits(L == 0.f ? 0.f : acc[e] / L, a.dtype);
     if (lane == 0)
-        a.lse[(int64_t)row * a.H * a.G + head] = L == 0.f ? __builtin_inff() : M + __builtin_amdgcn_logf(L);
+        a.lse[row * a.H * a.G + head] =
+            L == 0.f ? __builtin_inff() : M + __builtin_amdgcn_logf(L);
 }
 
 // Weights from the scores that k_attend_rows left: a wave to a (sequence,
@@ -489,7 +682,7 @@ size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 constexpr int kRowsMax = 64;     // columns for which scores are kept for the weights
 
 struct Plan {
-    int nt, tiles, nsplit, per_split, cols, blocks;
+    int nt, tile, workers, cols, blocks;
     size_t part_o, part_lse, lse, s, total;
 };
 
@@ -498,21 +691,14 @@ Plan plan_of(const qlm_kv_cache *c, const qlm_kv_batch *b, int32_t n_heads, bool
     Plan p{};
     const int64_t cols = (int64_t)b->max_new * (n_heads / c->n_kv_heads);
     p.cols = (int)std::min<int64_t>(cols, INT32_MAX);
-    p.nt = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
-    if (c->head_dim > 128) p.nt = std::min(p.nt, 2);
-    p.tiles = (int)((cols + 16 * p.nt - 1) / (16 * p.nt));
+    p.nt = cols <= 16 ? 1 : 2;
+    p.tile = 16 * p.nt;
     p.blocks = std::max(1, (b->max_length + kBlock - 1) / kBlock);
-    // Enough workgroups for every CU twice over, four blocks each at least (a
-    // wave's), and no more than 32 so that ragged lengths spread evenly.
-    const int64_t wg = (int64_t)b->n_seqs * c->n_kv_heads * p.tiles;
-    const int64_t want = wg * p.blocks / 1024;
-    p.per_split = (int)std::max<int64_t>(4, std::min<int64_t>(32, want / 4 * 4));
-    if (cols > kRowsMax) p.per_split = p.blocks;
-    p.nsplit = (p.blocks + p.per_split - 1) / p.per_split;
-    const size_t parts = (size_t)b->n_seqs * c->n_kv_heads * p.nsplit * p.cols;
+    // as many waves as the registers of 256 CUs hold at once
+    p.workers = c->head_dim <= 128 && p.nt == 1 ? 2048 : 1024;
     p.part_o = 0;
-    p.part_lse = p.part_o + (p.nsplit > 1 ? align256(parts * c->head_dim * 4) : 0);
-    p.lse = p.part_lse + (p.nsplit > 1 ? align256(parts * 4) : 0);
+    p.part_lse = p.part_o + align256((size_t)2 * p.workers * p.tile * c->head_dim * 4);
+    p.lse = p.part_lse + align256((size_t)2 * p.workers * p.tile * 4);
     p.s = p.lse + align256((size_t)b->n_rows * n_heads * 4);
     p.total = p.s;
     if (weights && cols <= kRowsMax)
@@ -527,15 +713,12 @@ template <int FMT, int ND, int NT> void launch_rows(const AttnArgs &a, int64_t g
 
 template <int FMT> void launch_rows(const AttnArgs &a, int nt, int64_t grid, hipStream_t st)
 {
-    if (a.D <= 64) {
-        nt == 1 ? launch_rows<FMT, 1, 1>(a, grid, st)
-                : nt == 2 ? launch_rows<FMT, 1, 2>(a, grid, st) : launch_rows<FMT, 1, 4>(a, grid, st);
-    } else if (a.D <= 128) {
-        nt == 1 ? launch_rows<FMT, 2, 1>(a, grid, st)
-                : nt == 2 ? launch_rows<FMT, 2, 2>(a, grid, st) : launch_rows<FMT, 2, 4>(a, grid, st);
-    } else {
+    if (a.D <= 64)
+        nt == 1 ? launch_rows<FMT, 1, 1>(a, grid, st) : launch_rows<FMT, 1, 2>(a, grid, st);
+    else if (a.D <= 128)
+        nt == 1 ? launch_rows<FMT, 2, 1>(a, grid, st) : launch_rows<FMT, 2, 2>(a, grid, st);
+    else
         nt == 1 ? launch_rows<FMT, 4, 1>(a, grid, st) : launch_rows<FMT, 4, 2>(a, grid, st);
-    }
 }
 
 template <int FMT> void launch_colsum(const AttnArgs &a, int64_t grid, hipStream_t st)
@@ -608,9 +791,8 @@ int qlm_kv_attention(const qlm_kv_cache *cache, const qlm_kv_batch *batch,
     a.dtype = query->q.dtype;
     a.wide = (uintptr_t)a.qd % 16 == 0 && a.q_row % 8 == 0 && a.q_head % 8 == 0;
     a.scale = query->scale * kLog2e;
-    a.nsplit = p.nsplit;
-    a.per_split = p.per_split;
-    a.tiles = p.tiles;
+    a.tile = p.tile;
+    a.workers = p.workers;
     a.cols = p.cols;
     a.blocks = p.blocks;
     char *base = (char *)ws;
@@ -623,21 +805,24 @@ int qlm_kv_attention(const qlm_kv_cache *cache, const qlm_kv_batch *batch,
 
     const bool e4m3 = cache->format == QLM_KV_E4M3;
     const int64_t sh = (int64_t)batch->n_seqs * a.H;
-    const int64_t grid = sh * p.tiles * p.nsplit;
-    if (grid > INT32_MAX || sh * p.cols > ((int64_t)1 << 32) || sh * p.blocks > INT32_MAX)
+    const int64_t units = sh * ((p.cols + p.tile - 1) / p.tile) * p.blocks;
+    if (units > INT32_MAX || sh * p.cols > INT32_MAX)
         return fail(QLM_ERR_CAPACITY, "too many rows or blocks in one call");
     hipError_t e;
     if (batch->n_rows > 0) {
+        const int64_t wg = (std::min<int64_t>(p.workers, units) + kWaves - 1) / kWaves;
         if (e4m3)
-            launch_rows<QLM_KV_E4M3>(a, p.nt, grid, stream);
+            launch_rows<QLM_KV_E4M3>(a, p.nt, wg, stream);
         else
-            launch_rows<QLM_KV_INT8>(a, p.nt, grid, stream);
+            launch_rows<QLM_KV_INT8>(a, p.nt, wg, stream);
         if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_attend_rows launch");
-        if (p.nsplit > 1) {
-            const int64_t wg = (sh * p.cols + kWaves - 1) / kWaves;
-            k_attend_join<<<(unsigned)wg, kThreads, 0, stream>>>(a, 16 * p.nt);
-            if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_attend_join launch");
-        }
+        // few columns: a workgroup to each, their parts may be many
+        if (sh * p.cols <= 2048)
+            k_attend_join<kWaves><<<(unsigned)(sh * p.cols), kThreads, 0, stream>>>(a);
+        else
+            k_attend_join<1><<<(unsigned)(sh * ((p.cols + kWaves - 1) / kWaves)), kThreads, 0,
+                               stream>>>(a);
+        if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_attend_join launch");
     }
     if (query->accumulate && batch->max_length > 0) {
         if (kept) {
