@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 import threading
 
 import numpy as np
@@ -155,11 +156,11 @@ def library():
             lib.qlm_place_step.argtypes = [P, i64, i32, vp, sz, vp, vp, vp]
             lib.qlm_place_end.argtypes = [P, i64, ctypes.POINTER(PlansOut), vp, sz, vp, vp]
             C, B = ctypes.POINTER(KvCacheStruct), ctypes.POINTER(KvBatchStruct)
-            R, Q, W = ctypes.POINTER(Rows), ctypes.POINTER(KvQuery), ctypes.POINTER(W4Struct)
-            lib.qlm_kv_append.argtypes = [C, B, R, R, vp, vp]
+            W = ctypes.POINTER(W4Struct)
+            lib.qlm_kv_append.argtypes = [C, B, vp, vp, vp, vp]  # (rows packed as bytes)
             lib.qlm_kv_attention_workspace_bytes.argtypes = [C, B, i32, i32]
             lib.qlm_kv_attention_workspace_bytes.restype = ctypes.c_size_t
-            lib.qlm_kv_attention.argtypes = [C, B, Q, vp, sz, vp]
+            lib.qlm_kv_attention.argtypes = [C, B, vp, vp, sz, vp]
             lib.qlm_kv_evict_workspace_bytes.argtypes = [C, B, i32]
             lib.qlm_kv_evict_workspace_bytes.restype = ctypes.c_size_t
             lib.qlm_kv_evict.argtypes = [C, B, i32, i32, vp, vp, sz, vp]
@@ -687,21 +688,39 @@ KV_BLOCK = 64
 _KV_FORMATS = ("float8_e4m3fn", "int8")
 
 
+# A decode step makes these calls once a layer, each of a few microseconds on
+# the GPU: their structs are packed as bytes and the stream is taken as a number
+# (a few microseconds less a call than ctypes objects and torch.cuda.Stream).
+_ROWS = struct.Struct("@Pqqi0P")
+_KV_QUERY = struct.Struct("@Pqqi0PPqqi0Pifif0P")
+_row_types = {}
+
+
 def _row_type(t, what):
-    import torch
-    if t.dtype == torch.float16:
-        return 0
-    if t.dtype == torch.bfloat16:
-        return 1
-    raise ValueError("%s must be float16 or bfloat16" % what)
+    if not _row_types:
+        import torch
+        _row_types.update({torch.float16: 0, torch.bfloat16: 1})
+    kind = _row_types.get(t.dtype)
+    if kind is None:
+        raise ValueError("%s must be float16 or bfloat16" % what)
+    return kind
 
 
-def _rows(t, heads, dim, what):
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
-        raise ValueError("%s must be [rows, %d, %d]" % (what, heads, dim))
-    if t.stride(2) != 1 and dim > 1:
+def _rows(t, n_rows, heads, dim, what):
+    """(pointer, row stride, head stride, type) of rows [n_rows, heads, dim]."""
+    if t.shape != (n_rows, heads, dim):
+        raise ValueError("%s must be [%d rows, %d, %d]" % (what, n_rows, heads, dim))
+    row, head, one = t.stride()
+    if one != 1:
         raise ValueError("%s: a head's dims must be contiguous" % what)
-    return Rows(t.data_ptr(), t.stride(0), t.stride(1), _row_type(t, what))
+    return t.data_ptr(), row, head, _row_type(t, what)
+
+
+def _raw_stream(stream):
+    if stream is not None:
+        return stream.cuda_stream
+    import torch
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 class DeviceKvCache:
@@ -797,27 +816,22 @@ class KvBatch:
         self._ref = ctypes.byref(self.struct)
 
 
-def _check_n_rows(batch, t, what):
-    if t.shape[0] != batch.n_rows:
-        raise ValueError("%s must have the batch's %d rows" % (what, batch.n_rows))
-
-
 def kv_append(cache: DeviceKvCache, batch: KvBatch, k, v, first_position=None, stream=None):
     """Writes the new tokens' keys and values [n_rows, n_kv_heads, head_dim]
     (float16 or bfloat16) into the last slots of their sequences.
     first_position [n_seqs] int32: the position of each sequence's first new
     token (the slot's number when None)."""
-    import torch
-    _check_n_rows(batch, k, "k")
-    _check_n_rows(batch, v, "v")
-    if first_position is not None and (first_position.dtype != torch.int32 or
+    if first_position is not None and (first_position.dtype != batch.lengths.dtype or
                                        first_position.numel() != batch.n_seqs or
                                        not first_position.is_contiguous()):
         raise ValueError("first_position must be [n_seqs] int32")
-    rk = _rows(k, cache.n_kv_heads, cache.head_dim, "k")
-    rv = _rows(v, cache.n_kv_heads, cache.head_dim, "v")
-    _check(library().qlm_kv_append(cache._ref, batch._ref, ctypes.byref(rk), ctypes.byref(rv),
-                                   _ptr(first_position), _stream(stream)))
+    rk = _rows(k, batch.n_rows, cache.n_kv_heads, cache.head_dim, "k")
+    rv = _rows(v, batch.n_rows, cache.n_kv_heads, cache.head_dim, "v")
+    rc = (_lib or library()).qlm_kv_append(
+        cache._ref, batch._ref, _ROWS.pack(*rk), _ROWS.pack(*rv),
+        None if first_position is None else first_position.data_ptr(), _raw_stream(stream))
+    if rc:
+        _check(rc)
 
 
 def kv_attention_workspace_bytes(cache: DeviceKvCache, batch: KvBatch, n_heads: int,
@@ -840,19 +854,23 @@ def kv_attention(cache: DeviceKvCache, batch: KvBatch, q, scale=None, weight_dec
     scores, head_dim ** -0.5 when None.  weight_decay: when given, the cache's
     weights become weight_decay * weight plus the step's attention weights."""
     import torch
-    _check_n_rows(batch, q, "q")
-    heads = int(q.shape[1])
+    if q.dim() != 3:
+        raise ValueError("q must be [rows, n_heads, head_dim]")
+    heads, dim = q.shape[1], cache.head_dim
+    rq = _rows(q, batch.n_rows, heads, dim, "q")
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     elif out.shape != q.shape or out.dtype != q.dtype:
         raise ValueError("out must have q's shape and type")
     if ws is None:
         ws = kv_attention_workspace(cache, batch, heads, weight_decay is not None)
-    query = KvQuery(_rows(q, heads, cache.head_dim, "q"), _rows(out, heads, cache.head_dim, "out"),
-                    heads, cache.head_dim ** -0.5 if scale is None else scale,
-                    weight_decay is not None, weight_decay or 0.0)
-    _check(library().qlm_kv_attention(cache._ref, batch._ref, ctypes.byref(query), ws.data_ptr(),
-                                      ws.numel(), _stream(stream)))
+    query = _KV_QUERY.pack(*rq, *_rows(out, batch.n_rows, heads, dim, "out"), heads,
+                           dim ** -0.5 if scale is None else scale, weight_decay is not None,
+                           weight_decay or 0.0)
+    rc = (_lib or library()).qlm_kv_attention(cache._ref, batch._ref, query, ws.data_ptr(),
+                                              ws.numel(), _raw_stream(stream))
+    if rc:
+        _check(rc)
     return out
 
 
@@ -872,15 +890,17 @@ def kv_evict(cache: DeviceKvCache, batch: KvBatch, budget: int, recent: int = 0,
     the slots of the `recent` newest positions and those of the greatest weight
     stay.  Returns the new lengths [n_seqs] int32 (`out`, which may be the
     batch's own lengths)."""
-    import torch
     if out is None:
+        import torch
         out = torch.empty_like(batch.lengths)
-    elif out.dtype != torch.int32 or out.numel() != batch.n_seqs or not out.is_contiguous():
+    elif out.dtype != batch.lengths.dtype or out.numel() != batch.n_seqs or not out.is_contiguous():
         raise ValueError("out must be [n_seqs] int32")
     if ws is None:
         ws = kv_evict_workspace(cache, batch, budget)
-    _check(library().qlm_kv_evict(cache._ref, batch._ref, int(budget), int(recent),
-                                  out.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)))
+    rc = (_lib or library()).qlm_kv_evict(cache._ref, batch._ref, budget, recent, out.data_ptr(),
+                                          ws.data_ptr(), ws.numel(), _raw_stream(stream))
+    if rc:
+        _check(rc)
     return out
 
 
@@ -938,7 +958,7 @@ def w4_matmul(x, weight: W4, out=None, ws=None, stream=None):
     if x.dim() != 2 or x.shape[1] != weight.n_in or (x.stride(1) != 1 and weight.n_in > 1):
         raise ValueError("x must be [rows, %d] with contiguous rows" % weight.n_in)
     kind = _row_type(x, "x")
-    n = int(x.shape[0])
+    n = x.shape[0]
     if out is None:
         out = torch.empty((n, weight.n_out), dtype=x.dtype, device=x.device)
     elif tuple(out.shape) != (n, weight.n_out) or out.dtype != x.dtype or \
@@ -948,6 +968,8 @@ def w4_matmul(x, weight: W4, out=None, ws=None, stream=None):
         ws = w4_workspace(weight, n)
     # (the stride of a matrix of one row says nothing)
     xs, os_ = (x.stride(0), out.stride(0)) if n > 1 else (weight.n_in, weight.n_out)
-    _check(library().qlm_w4_matmul(weight._ref, x.data_ptr(), xs, out.data_ptr(), os_, n, kind,
-                                   ws.data_ptr(), ws.numel(), _stream(stream)))
+    rc = (_lib or library()).qlm_w4_matmul(weight._ref, x.data_ptr(), xs, out.data_ptr(), os_, n,
+                                           kind, ws.data_ptr(), ws.numel(), _raw_stream(stream))
+    if rc:
+        _check(rc)
     return out
