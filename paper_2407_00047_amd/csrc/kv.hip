@@ -124,6 +124,27 @@ template <int FMT> __device__ inline uint32_t requant4(uint32_t w, float ratio)
     return o;
 }
 
+// The code of a code's magnitude (its low byte counts); 0 for a NaN.
+template <int FMT> __device__ inline uint32_t magnitude(uint32_t c)
+{
+    if (FMT == QLM_KV_E4M3) return (c & 0x7f) == 0x7f ? 0u : c & 0x7f;
+    return (uint32_t)abs((int)(int8_t)c);       // (128 is its own negative, read as -128)
+}
+
+// Four codes of scale `was` as codes of scale `now`.
+template <int FMT> __device__ inline uint32_t rescale4(uint32_t w, float was, float now)
+{
+    // between powers of two the quotient is exact, and a product gives the same
+    const bool exact = ((__builtin_bit_cast(uint32_t, was) | __builtin_bit_cast(uint32_t, now)) &
+                        0x7fffffu) == 0;
+    const float ratio = was / now;
+    uint32_t o = 0;
+    for (int b = 0; b < 4; ++b)
+        o |= code_of<FMT>(exact ? code_value<FMT>((w >> (8 * b)) & 0xff) * ratio
+                                : code_value<FMT>((w >> (8 * b)) & 0xff) * was / now) << (8 * b);
+    return o;
+}
+
 struct AppendArgs {
     CacheArgs c;
     Seqs q;
@@ -139,11 +160,8 @@ template <int FMT> __global__ __launch_bounds__(kThreads) void k_append(AppendAr
 {
     __shared__ float red[2 * kThreads / 64];
     const int t = threadIdx.x, nt = blockDim.x;
-    int64_t at = blockIdx.x;
-    const int h = (int)(at % a.c.H);
-    at /= a.c.H;
-    const int tb = (int)(at % a.touched);
-    const int s = (int)(at / a.touched);
+    const uint32_t bt = blockIdx.x / (uint32_t)a.c.H, h = blockIdx.x % (uint32_t)a.c.H;
+    const int tb = (int)(bt % (uint32_t)a.touched), s = (int)(bt / (uint32_t)a.touched);
     int row0;
     const int n = seq_rows(a.q, s, &row0);
     const int len = seq_length(a.q, s);
@@ -230,13 +248,10 @@ struct EvictArgs {
     CacheArgs c;
     Seqs q;
     int32_t budget, recent, slots;      // slots: max_length in whole blocks
-    uint32_t *key;                      // [seq][head][slots]
+    uint32_t *key;                      // [seq][head][slots] (k_evict_select, R = 0)
     int32_t *src, *hole, *moved;        // [seq][head][budget]
     int32_t *newlen, *out;              // [seq]
 };
-
-constexpr int kSelThreads = 1024;
-constexpr int kBins = 256;
 
 // A slot's key: greater is kept first.  Protected slots above all, then the
 // weights in their order, NaN last.
@@ -248,228 +263,403 @@ __device__ inline uint32_t weight_key(float w, bool safe)
     return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
 
-// Sum of one flag over the lower threads of the workgroup, and over all.
-__device__ inline int scan_flag(bool f, int *wave_sum, int *total)
-{
-    const uint64_t m = __ballot(f);
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int below = __popcll(m & ((1ull << lane) - 1));
-    if (lane == 0) wave_sum[w] = __popcll(m);
-    __syncthreads();
-    int before = 0, all = 0;
-    for (int k = 0; k < kSelThreads / 64; ++k) {
-        const int c = wave_sum[k];
-        before += k < w ? c : 0;
-        all += c;
-    }
-    __syncthreads();
-    *total = all;
-    return before + below;
-}
+// Which slots a (sequence, kv head) keeps, and what moves where.  One workgroup
+// of T threads; wave w of them takes blocks w, w + T/64, ..., a lane to a slot,
+// up to R blocks, whose keys stay in registers (R = 0: any number, keys in
+// memory).  The budget-th greatest key is found in three digits from the top (11,
+// 11 and 10 bits: the first covers sign, exponent and two bits of a weight, so
+// that the counters of one wave's lanes seldom meet), then holes and moved slots
+// are numbered in slot order from one table of counts a block.
+constexpr int kBins = 2048;
 
-// Which slots a (sequence, kv head) keeps, and what moves where: the budget
-// greatest keys by four rounds of a radix selection (8 bits each, from the
-// top), then one ordered walk that numbers holes and moved slots.
-__global__ __launch_bounds__(kSelThreads) void k_evict_select(EvictArgs a)
+template <int T, int R> __global__ __launch_bounds__(T) void k_evict_select(EvictArgs a)
 {
-    __shared__ uint32_t hist[kSelThreads / 64][kBins];
-    __shared__ int wave_sum[kSelThreads / 64];
-    __shared__ int red[kSelThreads / 64];
-    __shared__ uint32_t s_prefix;
-    __shared__ int s_left;
-    const int t = threadIdx.x, lane = t & 63, wv = t >> 6;
-    const int h = (int)(blockIdx.x % a.c.H), s = (int)(blockIdx.x / a.c.H);
+    constexpr int W = T / 64, REG = R ? R : 1;
+    __shared__ int hist[kBins], red[W], s_digit, s_left;
+    __shared__ int table_eq[W * REG], table_hm[W * REG];
+    __shared__ uint16_t moved[R ? W * REG * 32 : 1];   // (at most half of the slots)
+    const int t = threadIdx.x, lane = t & 63;
+    const int wv = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int h = (int)(blockIdx.x % (uint32_t)a.c.H), s = (int)(blockIdx.x / (uint32_t)a.c.H);
     const int len = seq_length(a.q, s);
     const int64_t sh = (int64_t)s * a.c.H + h;
     const int32_t *table = a.q.table + s * a.q.table_stride;
     int32_t *src = a.src + sh * a.budget;
     const int nb = (len + kBlock - 1) / kBlock;
-    bool bad = false;
-    if (len > a.budget)
-        for (int j = t; j < nb; j += kSelThreads)
-            bad = bad || (unsigned)table[j] >= (unsigned)a.c.n_blocks;
-    const bool stays = len <= a.budget || __syncthreads_or(bad);
-    if (h == 0 && t == 0) a.newlen[s] = stays ? len : a.budget;
-    if (stays) {
-        for (int o = t; o < a.budget; o += kSelThreads) src[o] = -1;
-        return;
-    }
-    // the newest position
+    bool bad = false;                            // a block outside the pool
+    auto leave = [&]() {                         // the sequence stays as it is
+        if (h == 0 && t == 0) a.newlen[s] = len;
+        for (int o = t; o < a.budget; o += T) src[o] = -1;
+    };
+    if (len <= a.budget) return leave();
+    uint32_t *kmem = a.key + sh * a.slots;
+    auto slot_data = [&](int j) {                // (j is uniform over the wave)
+        const int id = uniform(table + j);
+        const bool in = (unsigned)id < (unsigned)a.c.n_blocks;
+        bad = bad || !in;
+        return ((int64_t)(in ? id : 0) * a.c.H + h) * kBlock + lane;
+    };
+    auto largest = [&](int v) {
+        for (int o = 32; o; o >>= 1) v = max(v, __shfl_xor(v, o));
+        if (lane == 0) red[wv] = v;
+        __syncthreads();
+        for (int k = 0; k < W; ++k) v = max(v, red[k]);
+        return v;
+    };
+    // the newest position, then the keys
+    uint32_t key[REG];
     int newest = INT32_MIN;
-    for (int o = t; o < len; o += kSelThreads)
-        newest = max(newest, a.c.pos[((int64_t)table[o >> 6] * a.c.H + h) * kBlock + (o & 63)]);
-    for (int o = 32; o; o >>= 1) newest = max(newest, __shfl_xor(newest, o));
-    if (lane == 0) red[wv] = newest;
-    __syncthreads();
-    for (int k = 0; k < kSelThreads / 64; ++k) newest = max(newest, red[k]);
-    const int64_t safe_over = (int64_t)newest - a.recent;
-
-    uint32_t *key = a.key + sh * a.slots;
-    for (int o = t; o < len; o += kSelThreads) {
-        const int64_t at = ((int64_t)table[o >> 6] * a.c.H + h) * kBlock + (o & 63);
-        key[o] = weight_key(a.c.weight[at], (int64_t)a.c.pos[at] > safe_over);
-    }
-    // the budget-th greatest key: its digits from the top
-    uint32_t prefix = 0;
-    int left = a.budget;                    // of the keys that share the prefix, kept
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int b = lane; b < kBins; b += 64) hist[wv][b] = 0;
-        __syncthreads();
-        for (int o = t; o < len; o += kSelThreads) {
-            const uint32_t x = key[o];
-            if (shift == 24 || (x >> (shift + 8)) == (prefix >> (shift + 8)))
-                atomicAdd(&hist[wv][(x >> shift) & 255], 1u);
-        }
-        __syncthreads();
-        if (t < kBins) {
-            uint32_t c = 0;
-            for (int k = 0; k < kSelThreads / 64; ++k) c += hist[k][t];
-            hist[0][t] = c;
-        }
-        __syncthreads();
-        if (wv == 0) {
-            // lane l owns bins 4l .. 4l + 3; counts of the bins above them
-            int c[4], sum = 0;
-            for (int k = 0; k < 4; ++k) sum += c[k] = (int)hist[0][4 * lane + k];
-            int above = sum;
-            for (int o = 1; o < 64; o <<= 1) {
-                const int v = __shfl_down(above, o);
-                above += lane + o < 64 ? v : 0;
+    if (R) {
+        // eight blocks at a time; past the last one it is read again (unused)
+        constexpr int U = REG < 8 ? REG : 8;
+        int pos[U];
+        float w[U];
+        for (int r0 = 0; r0 < REG; r0 += U) {
+            if (r0 * W >= nb) break;
+            for (int u = 0; u < U; ++u) {
+                const int64_t at = slot_data(min((r0 + u) * W + wv, nb - 1));
+                pos[u] = a.c.pos[at];
+                if (REG == U) w[u] = a.c.weight[at];
             }
-            above -= sum;
-            for (int k = 3; k >= 0; --k) {
-                if (above < left && above + c[k] >= left) {
-                    s_prefix = prefix | (uint32_t)(4 * lane + k) << shift;
-                    s_left = left - above;
+            for (int u = 0; u < U; ++u)
+                newest = max(newest, ((r0 + u) * W + wv) * kBlock + lane < len ? pos[u] : INT32_MIN);
+        }
+        newest = largest(newest);
+        const int64_t over = (int64_t)newest - a.recent;
+        for (int r0 = 0; r0 < REG; r0 += U) {
+            for (int u = 0; u < U; ++u) key[r0 + u] = 0;
+            if (r0 * W >= nb) continue;
+            for (int u = 0; u < U && REG > U; ++u) {
+                const int64_t at = slot_data(min((r0 + u) * W + wv, nb - 1));
+                w[u] = a.c.weight[at];
+                pos[u] = a.c.pos[at];
+            }
+            for (int u = 0; u < U; ++u)
+                if (((r0 + u) * W + wv) * kBlock + lane < len)
+                    key[r0 + u] = weight_key(w[u], (int64_t)pos[u] > over);
+        }
+    } else {
+        for (int j = wv; j < nb; j += W)
+            if (j * kBlock + lane < len) newest = max(newest, a.c.pos[slot_data(j)]);
+        newest = largest(newest);
+        const int64_t over = (int64_t)newest - a.recent;
+        for (int j = wv; j < nb; j += W)
+            if (j * kBlock + lane < len) {
+                const int64_t at = slot_data(j);
+                kmem[j * kBlock + lane] =
+                    weight_key(a.c.weight[at], (int64_t)a.c.pos[at] > over);
+            }
+    }
+    if (__syncthreads_or(bad)) return leave();
+    if (h == 0 && t == 0) a.newlen[s] = a.budget;
+    // f(key, slot, block) for each of the wave's blocks, in order
+    auto each = [&](auto &&f) {
+        if (R) {
+            for (int r = 0; r < REG; ++r) {
+                if (r * W >= nb) break;
+                f(key[r], (r * W + wv) * kBlock + lane, r * W + wv);
+            }
+        } else {
+            for (int j = wv; j < nb; j += W)
+                f(j * kBlock + lane < len ? kmem[j * kBlock + lane] : 0u, j * kBlock + lane, j);
+        }
+    };
+    // p: the greatest key that at least `budget` keys reach; spare: of the keys
+    // equal to it, those that stay (the first in slot order)
+    uint32_t p = 0;
+    int spare = a.budget;
+    constexpr int B = kBins / T;                 // bins of a thread, from the top
+    for (int b = 0; b < B; ++b) hist[b * T + t] = 0;
+    __syncthreads();
+    for (int round = 0; round < 3; ++round) {
+        const int shift = round == 0 ? 21 : round == 1 ? 10 : 0;
+        const int bins = round == 2 ? kBins / 2 : kBins;
+        each([&](uint32_t x, int o, int) {
+            const uint32_t digit = x >> shift & (bins - 1);
+            const uint64_t in = __ballot(
+                o < len && (round == 0 || (x ^ p) >> (round == 1 ? 21 : 10) == 0));
+            if (!in) return;
+            // (equal weights, protected slots: one count for all)
+            const uint32_t one = __builtin_amdgcn_readlane(digit, __ffsll((long long)in) - 1);
+            if ((__ballot(digit == one) & in) == in) {
+                if (lane == 0) atomicAdd(&hist[one], (int)__popcll(in));
+            } else if (in >> lane & 1) {
+                atomicAdd(&hist[digit], 1);
+            }
+        });
+        __syncthreads();
+        int c[B], sum = 0;
+        for (int b = 0; b < B; ++b) {
+            const int bin = kBins - 1 - (t * B + b);
+            sum += c[b] = hist[bin];
+            hist[bin] = 0;
+        }
+        int run = sum;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(run, o);
+            run += lane >= o ? v : 0;
+        }
+        if (lane == 63) red[wv] = run;
+        __syncthreads();
+        int over = run - sum;                    // keys in the bins above this thread's
+        for (int k = 0; k < W; ++k) over += k < wv ? red[k] : 0;
+        if (over < spare && over + sum >= spare) {
+            int b = 0;
+            for (; over + c[b] < spare; ++b) over += c[b];
+            s_digit = kBins - 1 - (t * B + b);
+            s_left = spare - over;
+        }
+        __syncthreads();
+        p |= (uint32_t)s_digit << shift;
+        spare = s_left;
+    }
+    const uint64_t under = (1ull << lane) - 1;
+    if (R) {
+        // counts a block, their running sums by the first wave, then the ranks
+        auto running = [&](int *table_) {
+            constexpr int PER = (W * REG + 63) / 64;
+            __syncthreads();
+            if (wv == 0) {
+                int v[PER], sum = 0;
+                for (int k = 0; k < PER; ++k) {
+                    const int i = lane * PER + k;
+                    v[k] = i < W * REG ? table_[i] : 0;
+                    sum += v[k];
                 }
-                above += c[k];
+                int run = sum;
+                for (int o = 1; o < 64; o <<= 1) {
+                    const int x = __shfl_up(run, o);
+                    run += lane >= o ? x : 0;
+                }
+                run -= sum;
+                for (int k = 0; k < PER; ++k) {
+                    if (lane * PER + k < W * REG) table_[lane * PER + k] = run;
+                    run += v[k];
+                }
             }
+            __syncthreads();
+        };
+        each([&](uint32_t x, int o, int j) {
+            const int c = __popcll(__ballot(o < len && x == p));
+            if (lane == 0) table_eq[j] = c;
+        });
+        running(table_eq);
+        uint32_t keeps = 0;                      // (a bit for each r; R <= 32)
+        int r = 0;
+        each([&](uint32_t x, int o, int j) {
+            const uint64_t eq = __ballot(o < len && x == p);
+            const int rank = table_eq[j] + __popcll(eq & under);
+            const bool keep = o < len && (x > p || (x == p && rank < spare));
+            keeps |= (uint32_t)keep << r++;
+            // holes below the budget, moved slots past it (a block is one or the other)
+            const uint64_t m = __ballot(o < a.budget ? !keep : keep);
+            if (lane == 0) table_hm[j] = __popcll(m);
+        });
+        // the two kinds are numbered by themselves: blocks below the budget hold holes
+        running(table_hm);
+        const int first = a.budget / kBlock;     // (there is such a block: len > budget)
+        const int holes = table_hm[first];
+        r = 0;
+        each([&](uint32_t, int o, int j) {
+            const bool keep = keeps >> r++ & 1;
+            const bool it = o < a.budget ? !keep : keep;
+            const uint64_t m = __ballot(it);
+            const int rank = table_hm[j] + __popcll(m & under);
+            if (it && o >= a.budget) moved[rank - holes] = (uint16_t)o;
+        });
+        __syncthreads();
+        r = 0;
+        each([&](uint32_t, int o, int j) {
+            const bool keep = keeps >> r++ & 1;
+            const uint64_t m = __ballot(!keep);
+            if (o < a.budget) src[o] = keep ? -1 : moved[table_hm[j] + __popcll(m & under)];
+        });
+    } else {
+        int32_t *hole = a.hole + sh * a.budget, *shift = a.moved + sh * a.budget;
+        // (many blocks: wave by wave in slot order would be one wave's walk, so T
+        // slots at a time)
+        int n_eq = 0, n_hole = 0, n_moved = 0;
+        auto rank_of = [&](bool f, int *base) {
+            const uint64_t m = __ballot(f);
+            __syncthreads();
+            if (lane == 0) red[wv] = __popcll(m);
+            __syncthreads();
+            int before = *base, total = 0;
+            for (int k = 0; k < W; ++k) {
+                before += k < wv ? red[k] : 0;
+                total += red[k];
+            }
+            *base += total;
+            return before + __popcll(m & under);
+        };
+        for (int b = 0; b < len; b += T) {
+            const int o = b + t;
+            const uint32_t x = o < len ? kmem[o] : 0;
+            const bool eq = o < len && x == p;
+            const int rank = rank_of(eq, &n_eq);
+            const bool keep = o < len && (x > p || (eq && rank < spare));
+            const bool is_hole = o < a.budget && !keep, is_moved = o >= a.budget && keep;
+            const int rh = rank_of(is_hole, &n_hole), rm = rank_of(is_moved, &n_moved);
+            if (o < a.budget) src[o] = -1;
+            if (is_hole) hole[rh] = o;
+            if (is_moved) shift[rm] = o;
         }
         __syncthreads();
-        prefix = s_prefix;
-        left = s_left;
+        for (int i = t; i < min(n_hole, n_moved); i += T) src[hole[i]] = shift[i];
     }
-    // in slot order: of the keys equal to the last one kept the first `left` stay
-    int n_eq = 0, n_hole = 0, n_moved = 0;
-    int32_t *hole = a.hole + sh * a.budget, *moved = a.moved + sh * a.budget;
-    for (int base = 0; base < len; base += kSelThreads) {
-        const int o = base + t;
-        const uint32_t x = o < len ? key[o] : 0;
-        const bool eq = o < len && x == prefix;
-        int all;
-        const int rank = n_eq + scan_flag(eq, wave_sum, &all);
-        n_eq += all;
-        const bool keep = o < len && (x > prefix || (eq && rank < left));
-        const bool is_hole = o < a.budget && !keep, is_moved = o >= a.budget && keep;
-        const int rh = n_hole + scan_flag(is_hole, wave_sum, &all);
-        n_hole += all;
-        const int rm = n_moved + scan_flag(is_moved, wave_sum, &all);
-        n_moved += all;
-        if (o < a.budget) src[o] = -1;
-        if (is_hole) hole[rh] = o;
-        if (is_moved) moved[rm] = o;
-    }
-    __syncthreads();
-    for (int i = t; i < min(n_hole, n_moved); i += kSelThreads) src[hole[i]] = moved[i];
 }
 
-// One workgroup for each (sequence, block below the budget, kv head): fetches
-// what moves into the block's holes, renews the scales, writes.
-template <int FMT> __global__ __launch_bounds__(kThreads) void k_evict_move(EvictArgs a)
+// One workgroup for each (sequence, block below the budget, kv head): WPB waves,
+// each with 4 / WPB groups of 16 slots (qlm.h's order of the values).  A wave fetches
+// what moves into its groups' holes, four tokens at a time and one token's address
+// for a load, into shared memory (fetching it again for the second pass instead
+// took half as long again); the waves agree on the block's scales and write.
+// A lane holds ND neighbouring dims of a key and dims lane, lane + 64, ... of a
+// value, whose bytes stand 16 apart: a group that takes a token is read and
+// written whole (2 KiB at 128 dims; writing single bytes took as long).
+template <int ND> struct DimsOf;                // ND codes of a key
+template <> struct DimsOf<1> { typedef uint8_t type; };
+template <> struct DimsOf<2> { typedef uint16_t type; };
+template <> struct DimsOf<4> { typedef uint32_t type; };
+
+template <int FMT, int ND, int WPB> __global__ __launch_bounds__(64 * WPB) void k_evict_move(EvictArgs a)
 {
-    __shared__ int32_t from[kBlock];
-    __shared__ int64_t fbh[kBlock];             // block and head of the source
-    __shared__ float fks[kBlock], fvs[kBlock];
-    __shared__ float red[2 * kThreads / 64];
-    __shared__ uint8_t kx[kBlock * 256], vx[kBlock * 256];   // incoming codes [slot][dim]
-    const int t = threadIdx.x;
-    const int nb = a.budget / kBlock;
-    int64_t at = blockIdx.x;
-    const int j = (int)(at % nb);
-    at /= nb;
-    const int h = (int)(at % a.c.H), s = (int)(at / a.c.H);
+    typedef typename DimsOf<ND>::type dims;
+    __shared__ float red[2 * WPB];
+    extern __shared__ uint4 moving[];           // incoming codes, laid out as a block's
+    const int lane = threadIdx.x & 63;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t nb = a.budget / kBlock;
+    const uint32_t sh = blockIdx.x / nb, j = blockIdx.x % nb;
+    const uint32_t s = sh / (uint32_t)a.c.H, h = sh % (uint32_t)a.c.H;
     const int D = a.c.D;
-    if (h == 0 && j == 0 && t == 0) a.out[s] = a.newlen[s];
+    if (h == 0 && j == 0 && threadIdx.x == 0) a.out[s] = a.newlen[s];
     const int32_t *table = a.q.table + s * a.q.table_stride;
-    bool any = false;
-    if (t < kBlock) {
-        const int o = a.src[((int64_t)s * a.c.H + h) * a.budget + j * kBlock + t];
-        from[t] = o;
-        any = o >= 0;
-        if (any) {
-            const int64_t b = (int64_t)table[o >> 6] * a.c.H + h;
-            fbh[t] = b;
-            fks[t] = a.c.ks[b];
-            fvs[t] = a.c.vs[b];
-        }
-    }
-    if (!__syncthreads_or(any)) return;
-    const int64_t bh = (int64_t)table[j] * a.c.H + h;
-    float ak = 0.f, av = 0.f;
-    for (int e = t; e < kBlock * (D / 4); e += kThreads) {
-        const int i = e / (D / 4), d = 4 * (e % (D / 4));
-        const int o = from[i];
-        if (o < 0) continue;
-        const uint8_t *kp = a.c.kc + (fbh[i] * kBlock + (o & 63)) * D + d;
-        const uint8_t *vp = a.c.vc + fbh[i] * kBlock * D +
-                            (value_group(o & 63) * D + d) * 16 + value_place(o & 63);
-        const uint32_t kw = *(const uint32_t *)kp;
-        uint32_t vw = 0;
-        for (int b = 0; b < 4; ++b) vw |= (uint32_t)vp[16 * b] << (8 * b);
-        *(uint32_t *)(kx + i * D + d) = kw;
-        *(uint32_t *)(vx + i * D + d) = vw;
-        for (int b = 0; b < 4; ++b) {
-            ak = fmaxf(ak, finite_abs(code_value<FMT>((kw >> (8 * b)) & 0xff) * fks[i]));
-            av = fmaxf(av, finite_abs(code_value<FMT>((vw >> (8 * b)) & 0xff) * fvs[i]));
-        }
-    }
+    // lane l: where slot l's new token comes from (blocks past the budget: not
+    // written here)
+    const int mine = a.src[(int64_t)sh * a.budget + j * kBlock + lane];
+    const uint64_t holes = __ballot(mine >= 0); // (both waves read the same 64)
+    if (!holes) return;
+    const int id = mine >= 0 ? table[mine >> 6] : 0;
+    const float sk = a.c.ks[(int64_t)id * a.c.H + h], sv = a.c.vs[(int64_t)id * a.c.H + h];
+    const int64_t bh = (int64_t)uniform(table + j) * a.c.H + h;
     const float oldk = a.c.ks[bh], oldv = a.c.vs[bh];
-    max2(ak, av, red);                          // (its barrier: every thread has the old scales)
+    auto lane_of = [](float x, int l) {
+        return __builtin_bit_cast(float,
+                                  __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), l));
+    };
+    uint8_t *kl = (uint8_t *)moving, *vl = kl + kBlock * D;
+    const uint64_t slots_of = (WPB == 2 ? 0x00ff00ff00ff00ffull : 0x000f000f000f000full)
+                              << (16 / WPB * wv);
+    const bool in_k = lane * ND < D;            // (D is a multiple of 16)
+    float ak = 0.f, av = 0.f;
+    for (uint64_t left = holes & slots_of; left;) {
+        // (the first again where there are fewer than four: a branch would hold each
+        // load back until the one before)
+        int slot[4];
+        uint32_t kx[4], vx[4][ND];
+        for (int u = 0; u < 4; ++u) {
+            slot[u] = left ? __ffsll((long long)left) - 1 : slot[0];
+            left &= left - 1;
+            const int o = __builtin_amdgcn_readlane(mine, slot[u]) & 63;
+            const int64_t b = (int64_t)__builtin_amdgcn_readlane(id, slot[u]) * a.c.H + h;
+            const uint8_t *kp = a.c.kc + (b * kBlock + o) * D;
+            const uint8_t *vp = a.c.vc + b * kBlock * D + value_group(o) * D * 16 + value_place(o);
+            // (past the last dim the last is read again: neither counts nor is written)
+            kx[u] = *(const dims *)(kp + (uint32_t)min(lane * ND, D - ND));
+            for (int k = 0; k < ND; ++k) vx[u][k] = vp[(uint32_t)min(lane + 64 * k, D - 1) * 16];
+        }
+        for (int u = 0; u < 4; ++u) {
+            uint32_t tk = 0, tv = 0;
+            uint8_t *to = vl + value_group(slot[u]) * D * 16 + value_place(slot[u]);
+            for (int k = 0; k < ND; ++k) {
+                tk = max(tk, magnitude<FMT>(kx[u] >> (8 * k)));
+                tv = max(tv, magnitude<FMT>(vx[u][k]));
+                if (lane + 64 * k < D) to[(lane + 64 * k) * 16] = (uint8_t)vx[u][k];
+            }
+            if (in_k) *(dims *)(kl + slot[u] * D + lane * ND) = (dims)kx[u];
+            ak = fmaxf(ak, finite_abs(code_value<FMT>(tk) * lane_of(sk, slot[u])));
+            av = fmaxf(av, finite_abs(code_value<FMT>(tv) * lane_of(sv, slot[u])));
+        }
+    }
+    max2(ak, av, red);                          // (its barrier: every wave has the old scales)
     const float newk = fmaxf(oldk, scale_for<FMT>(ak)), newv = fmaxf(oldv, scale_for<FMT>(av));
-    if (t == 0) {
+    if (threadIdx.x == 0) {
         a.c.ks[bh] = newk;
         a.c.vs[bh] = newv;
     }
-    uint8_t *kc = a.c.kc + bh * kBlock * D;
-    const bool growk = newk > oldk;
-    const float ratiok = oldk / newk;
-    for (int e = t; e < kBlock * (D / 4); e += kThreads) {
-        const int i = e / (D / 4), d = 4 * (e % (D / 4));
-        uint32_t *p = (uint32_t *)(kc + i * D + d);
-        if (from[i] >= 0) {
-            const uint32_t x = *(const uint32_t *)(kx + i * D + d);
-            uint32_t w = 0;
-            for (int b = 0; b < 4; ++b)
-                w |= code_of<FMT>(code_value<FMT>((x >> (8 * b)) & 0xff) * fks[i] / newk)
-                     << (8 * b);
-            *p = w;
-        } else if (growk) {
-            *p = requant4<FMT>(*p, ratiok);
+    uint8_t *kc = a.c.kc + bh * kBlock * D, *vc = a.c.vc + bh * kBlock * D;
+    const bool growv = newv > oldv;
+    for (uint64_t left = holes & slots_of; left; left &= left - 1) {
+        const int slot = __ffsll((long long)left) - 1;
+        const float fk = lane_of(sk, slot), fv = lane_of(sv, slot);
+        if (in_k) {
+            uint32_t x = *(dims *)(kl + slot * D + lane * ND);
+            if (fk != newk) x = rescale4<FMT>(x, fk, newk);
+            *(dims *)(kc + slot * D + lane * ND) = (dims)x;
+        }
+        if (fv != newv)
+            for (int d = lane; d < D; d += 64) {
+                uint8_t *x = vl + (value_group(slot) * D + d) * 16 + value_place(slot);
+                *x = (uint8_t)rescale4<FMT>(*x, fv, newv);
+            }
+    }
+    if (newk > oldk && in_k)
+        for (uint64_t left = ~holes & slots_of; left; left &= left - 1) {
+            dims *x = (dims *)(kc + (__ffsll((long long)left) - 1) * D + lane * ND);
+            *x = (dims)requant4<FMT>(*x, oldk / newk);
+        }
+    const float ratio = oldv / newv;
+    for (int g = wv * (4 / WPB); g < (wv + 1) * (4 / WPB); ++g) {
+        const uint64_t in_g = holes & 0x000f000f000f000full << (4 * g);
+        if (!in_g && !growv) continue;
+        uint32_t take[4];                        // the bytes of the holes, place after place
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t n = (uint32_t)(in_g >> (16 * q + 4 * g)) & 15u;
+            take[q] = ((n & 1) | (n & 2) << 7 | (n & 4) << 14 | (n & 8) << 21) * 0xffu;
+        }
+        for (int d = lane; d < D; d += 64) {     // (the lane that wrote these bytes)
+            uint4 *to = (uint4 *)(vc + (g * D + d) * 16);
+            const uint4 w = *to, x = *(const uint4 *)(vl + (g * D + d) * 16);
+            uint32_t o[4] = {w.x, w.y, w.z, w.w};
+            const uint32_t n[4] = {x.x, x.y, x.z, x.w};
+            for (int q = 0; q < 4; ++q) {
+                if (growv) o[q] = requant4<FMT>(o[q], ratio);
+                o[q] = (o[q] & ~take[q]) | (n[q] & take[q]);
+            }
+            *to = uint4{o[0], o[1], o[2], o[3]};
         }
     }
-    uint8_t *vc = a.c.vc + bh * kBlock * D;
-    const bool growv = newv > oldv;
-    const float ratiov = oldv / newv;
-    for (int e = t; e < 16 * D; e += kThreads) {
-        const int p = 4 * (e & 3), d = (e >> 2) % D, g = (e >> 2) / D;
-        const int o = value_slot(g, p);
-        const bool some = from[o] >= 0 || from[o + 1] >= 0 || from[o + 2] >= 0 || from[o + 3] >= 0;
-        if (!growv && !some) continue;
-        uint32_t *at4 = (uint32_t *)(vc + (g * D + d) * 16 + p);
-        uint32_t w = *at4;
-        if (growv) w = requant4<FMT>(w, ratiov);
-        for (int b = 0; b < 4; ++b)
-            if (from[o + b] >= 0)
-                w = (w & ~(0xffu << (8 * b))) |
-                    code_of<FMT>(code_value<FMT>(vx[(o + b) * D + d]) * fvs[o + b] / newv)
-                        << (8 * b);
-        *at4 = w;
-    }
-    if (t < kBlock && from[t] >= 0) {
-        const int64_t to = bh * kBlock + t, fr = fbh[t] * kBlock + (from[t] & 63);
+    if (wv == 0 && mine >= 0) {
+        const int64_t to = bh * kBlock + lane;
+        const int64_t fr = ((int64_t)id * a.c.H + h) * kBlock + (mine & 63);
         a.c.pos[to] = a.c.pos[fr];
         a.c.weight[to] = a.c.weight[fr];
     }
+}
+
+template <int FMT, int ND> void launch_move(const EvictArgs &a, int waves, unsigned grid,
+                                            hipStream_t st)
+{
+    const int bytes = 2 * kBlock * a.c.D;
+    if (waves == 2)
+        k_evict_move<FMT, ND, 2><<<grid, 128, bytes, st>>>(a);
+    else
+        k_evict_move<FMT, ND, 4><<<grid, 256, bytes, st>>>(a);
+}
+
+template <int FMT> void launch_move(const EvictArgs &a, int max_length, unsigned grid, hipStream_t st)
+{
+    // two waves to a block where at most a quarter of its slots can fall free (4 of
+    // 64, 8192 blocks: 31 us, four waves 36), four where more can (48 of 64, 3072
+    // blocks: 48 us, two waves 62)
+    const int waves = max_length - a.budget <= a.budget / 4 ? 2 : 4;
+    if (a.c.D <= 64)
+        launch_move<FMT, 1>(a, waves, grid, st);
+    else if (a.c.D <= 128)
+        launch_move<FMT, 2>(a, waves, grid, st);
+    else
+        launch_move<FMT, 4>(a, waves, grid, st);
 }
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
@@ -484,7 +674,7 @@ EvictLayout evict_layout(const qlm_kv_cache *c, const qlm_kv_batch *b, int32_t b
     const size_t slots = ((size_t)b->max_length + kBlock - 1) / kBlock * kBlock;
     EvictLayout l{};
     l.key = 0;
-    l.src = l.key + align256(sh * slots * 4);
+    l.src = l.key + (slots > kBlock * 16 * 32 ? align256(sh * slots * 4) : 0);
     l.hole = l.src + align256(sh * budget * 4);
     l.moved = l.hole + align256(sh * budget * 4);
     l.newlen = l.moved + align256(sh * budget * 4);
@@ -573,12 +763,24 @@ int qlm_kv_evict(const qlm_kv_cache *cache, const qlm_kv_batch *batch, int32_t b
     const int64_t sh = (int64_t)batch->n_seqs * a.c.H;
     const int64_t grid = sh * (budget / kBlock);
     if (grid > INT32_MAX) return fail(QLM_ERR_CAPACITY, "too many blocks in one eviction");
-    k_evict_select<<<(unsigned)sh, kSelThreads, 0, stream>>>(a);
+    const int blocks = a.slots / kBlock;        // of the longest sequence
+    const unsigned n = (unsigned)sh;
+    if (blocks <= 4 * 8)
+        k_evict_select<256, 8><<<n, 256, 0, stream>>>(a);
+    else if (blocks <= 16 * 8)
+        k_evict_select<1024, 8><<<n, 1024, 0, stream>>>(a);
+    else if (blocks <= 16 * 16)
+        k_evict_select<1024, 16><<<n, 1024, 0, stream>>>(a);
+    else if (blocks <= 16 * 32)
+        k_evict_select<1024, 32><<<n, 1024, 0, stream>>>(a);
+    else
+        k_evict_select<1024, 0><<<n, 1024, 0, stream>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return hip_fail(e, "k_evict_select launch");
-    auto kern = cache->format == QLM_KV_E4M3 ? k_evict_move<QLM_KV_E4M3>
-                                             : k_evict_move<QLM_KV_INT8>;
-    kern<<<(unsigned)grid, kThreads, 0, stream>>>(a);
+    if (cache->format == QLM_KV_E4M3)
+        launch_move<QLM_KV_E4M3>(a, batch->max_length, (unsigned)grid, stream);
+    else
+        launch_move<QLM_KV_INT8>(a, batch->max_length, (unsigned)grid, stream);
     e = hipGetLastError();
     return e == hipSuccess ? QLM_OK : hip_fail(e, "k_evict_move launch");
 }
