@@ -29,14 +29,26 @@ struct AttnArgs {
     int64_t q_row, q_head, o_row, o_head;
     int32_t dtype, wide;                 // wide: q may be read 16 bytes at a time
     float scale;                         // times log2(e)
-    int32_t tile;                        // columns of a tile
+    int32_t few;                         // columns up to which a sequence has few rows
+    int32_t tile;                        // columns of a tile (k_attend_rows)
     int32_t workers;                     // waves that share the units (k_attend_rows)
     int32_t cols, blocks;                // max_new * G, ceil(max_length / 64)
     float *part_o, *part_lse;            // [2 worker + which][tile]([D])
-    float *lse;                          // [row][heads], log2 units; +inf: nothing seen
-    float *s;                            // [seq][block][head][cols][64] scores, or NULL
+    float *lse;                          // [kv head][row][G], log2 units; +inf: nothing seen
+    float *s;                            // [seq][block][head][few][64] scores, or NULL
     float decay;
+    // sequences of many rows
+    uint16_t *qh;                        // [kv head][8 ND][row][G][8] queries as halves
+    float *qfac;                         // [kv head][row][G] what takes their scaling out
+    int32_t splits;                      // of the keys
+    float *split_o, *split_lse;          // [split][kv head][row][G]([D])
 };
+
+// Column of head e of a row among all rows of kv head h.
+__device__ inline int64_t column(const AttnArgs &a, int h, int64_t row, int e)
+{
+    return ((int64_t)h * a.q.n_rows + row) * a.G + e;
+}
 
 // Maximum and sum over the four lanes of a column (16 lanes apart).
 __device__ inline void swap16(float x, float *a, float *b)
@@ -140,6 +152,7 @@ __device__ inline Units units_of(const AttnArgs &a, int s)
 {
     int row0;
     const int n = seq_rows(a.q, s, &row0);
+    if (n * a.G > a.few) return {0, 0};          // (k_attend_prompt)
     return {(seq_length(a.q, s) + kBlock - 1) / kBlock, (n * a.G + a.tile - 1) / a.tile};
 }
 
@@ -194,7 +207,7 @@ struct Cursor {
                 n = 0;
             }
             nb = (len + kBlock - 1) / kBlock;
-            tiles = (n * a.G + a.tile - 1) / a.tile;
+            tiles = n * a.G > a.few ? 0 : (n * a.G + a.tile - 1) / a.tile;
             if (nb * tiles > 0) break;
         }
     }
@@ -365,7 +378,7 @@ __global__ __launch_bounds__(kThreads, ND * NT <= 2 ? 2 : 1) void k_attend_rows(
             for (int k = 0; k < NT; ++k) {
                 const int c = col0 + k * 16 + c16;
                 if (c < cols) {
-                    float *p = a.s + ((((int64_t)s * a.blocks + j) * a.H + h) * a.cols + c) * kBlock;
+                    float *p = a.s + ((((int64_t)s * a.blocks + j) * a.H + h) * min(a.cols, a.few) + c) * kBlock;
                     for (int t = 0; t < 4; ++t) *(float4v *)(p + t * 16 + 4 * g) = sc[k][t];
                 }
             }
@@ -457,7 +470,7 @@ __global__ __launch_bounds__(kThreads, ND * NT <= 2 ? 2 : 1) void k_attend_rows(
                 const float lse = m[k] - kRaise + __builtin_amdgcn_logf(sum);
                 if (g == 0) {
                     if (whole)
-                        a.lse[row * a.H * a.G + head] = sum == 0.f ? __builtin_inff() : lse;
+                        a.lse[column(a, h, row, c % a.G)] = sum == 0.f ? __builtin_inff() : lse;
                     else
                         a.part_lse[part * a.tile + k * 16 + c16] =
                             sum == 0.f ? -__builtin_inff() : lse;
@@ -495,7 +508,7 @@ template <int WPC> __global__ __launch_bounds__(kThreads) void k_attend_join(Att
     __shared__ int below[kWaves], total[kWaves];
     constexpr int CPG = kWaves / WPC;            // columns of a workgroup
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    const int groups = (a.cols + CPG - 1) / CPG;
+    const int groups = (min(a.cols, a.few) + CPG - 1) / CPG;
     const int64_t sh = blockIdx.x / groups;
     const int c = (int)(blockIdx.x % groups) * CPG + wv / WPC;
     const int s = (int)(sh / a.H), h = (int)(sh % a.H);
@@ -525,7 +538,7 @@ template <int WPC> __global__ __launch_bounds__(kThreads) void k_attend_join(Att
     const int u0 = lo + (h * u.tiles + c / a.tile) * u.nb, u1 = u0 + u.nb;
     const int w0 = u0 / each, w1 = u.nb ? (u1 - 1) / each : w0 - 1;
     // (whole at one worker: written there)
-    const bool mine = c < n * a.G && w0 != w1;
+    const bool mine = c < n * a.G && n * a.G <= a.few && w0 != w1;
     float M = -__builtin_inff(), L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
     auto place = [&](int w) {                    // of the part that worker w left
         return (2 * (int64_t)w + (w == w0 && u0 % each ? 1 : 0)) * a.tile + c % a.tile;
@@ -569,7 +582,7 @@ template <int WPC> __global__ __launch_bounds__(kThreads) void k_attend_join(Att
             ((uint16_t *)a.od)[row * a.o_row + head * a.o_head + e * 64 + lane] =
                 row_bits(L == 0.f ? 0.f : acc[e] / L, a.dtype);
     if (lane == 0)
-        a.lse[row * a.H * a.G + head] =
+        a.lse[column(a, h, row, c % a.G)] =
             L == 0.f ? __builtin_inff() : M + __builtin_amdgcn_logf(L);
 }
 
@@ -589,101 +602,455 @@ __global__ __launch_bounds__(kThreads) void k_attend_weights(AttnArgs a)
     if ((unsigned)id >= (unsigned)a.n_blocks) return;
     int row0;
     const int n = seq_rows(a.q, s, &row0);
-    const float *sc = a.s + w * a.cols * kBlock + lane;
-    const float *lse = a.lse + ((int64_t)row0 * a.H + h) * a.G;
+    if (n * a.G > a.few) return;                 // (k_attend_colsum)
+    const float *sc = a.s + w * min(a.cols, a.few) * kBlock + lane;
+    const float *lse = a.lse + column(a, h, row0, 0);
     float sum = 0.f;
     const int before = len - n;
     for (int t = 0; t < n; ++t) {
         if (before + t < j * kBlock) continue;    // (the row's scores were not formed)
         for (int e = 0; e < a.G; ++e)
-            sum += __builtin_amdgcn_exp2f(sc[(t * a.G + e) * kBlock] - lse[(int64_t)t * a.H * a.G + e]);
+            sum += __builtin_amdgcn_exp2f(sc[(t * a.G + e) * kBlock] - lse[t * a.G + e]);
     }
     if (j * kBlock + lane >= len) return;
     float *at = a.weight + ((int64_t)id * a.H + h) * kBlock + lane;
     *at = a.decay == 0.f ? sum : a.decay * *at + sum;
 }
 
-// Weights where the query rows are many: a workgroup to a (sequence, block, kv
-// head) forms the block's scores again, tile of columns by tile, and adds up
-// their probabilities.
+// -- many query rows --------------------------------------------------------
+
+typedef float float16v __attribute__((ext_vector_type(16)));
+
+// Queries in half precision, dims padded with zeros to whole 64s, in the order of
+// the matrix operands (8 dims of a column after the next column's): scaled by a
+// power of two where they come in bfloat16 (load_query), negated where the scale
+// of the scores is negative.  A wave to a (row, head).
+template <int ND> __global__ __launch_bounds__(kThreads) void k_query_half(AttnArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const uint32_t rh = blockIdx.x * kWaves + (threadIdx.x >> 6), heads = a.H * a.G;
+    const uint32_t row = rh / heads, head = rh % heads, h = head / (uint32_t)a.G;
+    if (row >= (uint32_t)a.q.n_rows) return;
+    const uint16_t *p = (const uint16_t *)a.qd + row * a.q_row + head * a.q_head;
+    const int64_t all = (int64_t)a.q.n_rows * a.G, col = (int64_t)row * a.G + head % (uint32_t)a.G;
+    uint16_t u[ND];
+    uint32_t top = 0;
+    for (int k = 0; k < ND; ++k) {
+        u[k] = lane + 64 * k < a.D ? p[lane + 64 * k] : 0;
+        const uint32_t x = (u[k] >> 7) & 0xff;
+        top = x < 255 ? max(top, x) : top;
+    }
+    float unscale = 1.f, by = a.scale < 0.f ? -1.f : 1.f;
+    if (a.dtype == QLM_BF16) {
+        for (int o = 32; o; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+        const int up = min(15 - ((int)top - 126), 126);
+        by *= ldexpf(1.f, up);
+        unscale = ldexpf(1.f, -up);
+    }
+    for (int k = 0; k < ND; ++k) {
+        const float x = a.dtype == QLM_BF16 ? __builtin_bit_cast(float, (uint32_t)u[k] << 16)
+                                            : (float)__builtin_bit_cast(_Float16, u[k]);
+        a.qh[((h * ND * 8 + k * 8 + (lane >> 3)) * all + col) * 8 + (lane & 7)] =
+            __builtin_bit_cast(uint16_t, (_Float16)(x * by));
+    }
+    // (a scale of 0: small enough, and no 0 times infinity)
+    if (lane == 0) a.qfac[h * all + col] = fmaxf(unscale * fabsf(a.scale), 1e-37f);
+}
+
+// The sequences of many rows: one workgroup to 128 columns (query rows and heads
+// of a kv head, 32 a wave) and a split of the keys.  Every block's codes are
+// turned into halves once, in shared memory and in the order of the matrix
+// operands (two buffers, the next block's codes on their way meanwhile), and
+// serve the four waves.  S^T = K Q^T and O^T = V^T P^T are 32x32x16 matrix
+// instructions; a lane's scores are again the operand of the second product, so
+// only keys and values pass through shared memory.
+template <int FMT, int ND, bool FULL>
+__global__ __launch_bounds__(kThreads, ND <= 2 ? 2 : 1) void k_attend_prompt(AttnArgs a)
+{
+    constexpr int DP = ND * 64, KS = DP / 16, DT = DP / 32;
+    constexpr int KP = kBlock * 8 + 8;               // halves between chunks of 8 dims
+    __shared__ uint4 ldsk[2][KS * 2 * KP / 8], ldsv[2][kBlock * DP / 8];
+    __shared__ int some_nan[3];                      // of blocks j, j + 1, j + 2 in turn
+    const int t = threadIdx.x, lane = t & 63;
+    const int wv = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int hi = lane >> 5, c32 = lane & 31;
+    const uint32_t most = (uint32_t)(a.cols + 127) / 128;
+    uint32_t at = blockIdx.x;
+    // (the last rows see most: they come first)
+    const int ct = (int)(most - 1 - at % most);
+    at /= most;
+    const int h = (int)(at % (uint32_t)a.H), s = (int)(at / (uint32_t)a.H), sp = blockIdx.y;
+    int row0;
+    const int n = seq_rows(a.q, s, &row0);
+    const int cols = n * a.G, col0 = ct * 128;
+    if (cols <= a.few || col0 >= cols) return;
+    const int before = seq_length(a.q, s) - n;
+    const int hi_lim = before + min(cols - 1, col0 + 127) / a.G + 1;
+    const int lo_lim = before + col0 / a.G + 1;
+    const int nb = (max(hi_lim, 0) + kBlock - 1) / kBlock;
+    const int b0 = (int)((int64_t)nb * sp / a.splits), b1 = (int)((int64_t)nb * (sp + 1) / a.splits);
+    const int wcol0 = col0 + wv * 32, c = wcol0 + c32;
+    const int w_hi = before + min(cols - 1, wcol0 + 31) / a.G + 1;   // the wave's limits
+    const int w_lo = before + min(cols - 1, wcol0) / a.G + 1;
+    const bool valid = c < cols;
+    const int64_t all = (int64_t)a.q.n_rows * a.G, rh = column(a, h, row0, valid ? c : 0);
+    const int lim = valid ? before + c / a.G + 1 : 0;
+    const int D = a.D;
+
+    half8v qf[KS];
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+        qf[k] = *(const half8v *)(a.qh + (((int64_t)h * (DP / 8 - 1) + 2 * k + hi) * all + rh) * 8);
+    const float fac = a.qfac[rh];
+    float16v acc[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
+    float m = -__builtin_inff(), l = 0.f, vscale = 1e-38f;
+
+    const int32_t *table = a.q.table + s * a.q.table_stride;
+    uint4 kr[ND], vr[ND];
+    float ksc = 0.f, vsc = 0.f;
+    auto fetch = [&](int j) {
+        const int id = uniform(table + j);
+        const bool mapped = (unsigned)id < (unsigned)a.n_blocks;
+        const int64_t bh = (int64_t)(mapped ? id : 0) * a.H + h;
+        const uint8_t *kp = a.kc + bh * kBlock * D, *vp = a.vc + bh * kBlock * D;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+            const int e = t + kThreads * i, tok = e / (DP / 16), ch = e % (DP / 16);
+            const int g = e / DP, d = e % DP;
+            kr[i] = *(const uint4 *)(kp + (uint32_t)(tok * D + (FULL ? ch * 16
+                                                                     : min(ch * 16, D - 16))));
+            vr[i] = *(const uint4 *)(vp + (uint32_t)((g * D + (FULL ? d : min(d, D - 1))) * 16));
+        }
+        ksc = uniform(a.ks + bh);
+        vsc = mapped ? uniform(a.vs + bh) : 0.f;
+        return mapped;
+    };
+    auto stage = [&](int buf, int j, bool mapped) {
+        _Float16 *ks = (_Float16 *)ldsk[buf], *vs = (_Float16 *)ldsv[buf];
+        const bool masked = (j + 1) * kBlock > lo_lim || !mapped;
+        uint32_t nans = 0;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+            const int e = t + kThreads * i, tok = e / (DP / 16), ch = e % (DP / 16);
+            *(half8v *)(ks + (2 * ch) * KP + tok * 8) = halves8<FMT>(kr[i].x, kr[i].y);
+            *(half8v *)(ks + (2 * ch + 1) * KP + tok * 8) = halves8<FMT>(kr[i].z, kr[i].w);
+            const int g = e / DP, d = e % DP;
+            uint32_t x[4] = {vr[i].x, vr[i].y, vr[i].z, vr[i].w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (masked) {                    // slots that no column here sees are zeroed
+                    const int left = mapped ? hi_lim - (j * kBlock + q * 16 + 4 * g) : 0;
+                    x[q] = left <= 0 ? 0u : left < 4 ? x[q] & (0xffffffffu >> (8 * (4 - left)))
+                                                     : x[q];
+                    if (FMT == QLM_KV_E4M3) nans |= nan_bytes(x[q]);
+                }
+                half2v lo, up;
+                halves4<FMT>(x[q], &lo, &up);
+                typedef _Float16 half4v __attribute__((ext_vector_type(4)));
+                *(half4v *)(vs + ((q * 2 + (g & 1)) * DP + d) * 8 + (g >> 1) * 4) =
+                    half4v{lo[0], lo[1], up[0], up[1]};
+            }
+        }
+        if (FMT == QLM_KV_E4M3 && masked && nans) some_nan[j % 3] = 1;
+    };
+    if (t < 3) some_nan[t] = 0;
+    __syncthreads();
+    bool mapped = false;
+    if (b0 < b1) {
+        mapped = fetch(b0);
+        stage(0, b0, mapped);
+    }
+    __syncthreads();
+    for (int j = b0; j < b1; ++j) {
+        const int buf = (j - b0) & 1;
+        const bool here = mapped;
+        const float ks1 = ksc, vs1 = vsc;
+        if (j + 1 < b1) mapped = fetch(j + 1);
+        if (j * kBlock < w_hi && wcol0 < cols && here) {
+            const _Float16 *ks = (const _Float16 *)ldsk[buf], *vs = (const _Float16 *)ldsv[buf];
+            float16v sc[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[u][i] = 0.f;
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    if (!FULL && k * 16 >= D) break;
+                    const half8v x = *(const half8v *)(ks + (2 * k + hi) * KP +
+                                                       (u * 32 + c32) * 8);
+                    sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, qf[k], sc[u], 0, 0, 0);
+                }
+            }
+            const bool masked = (j + 1) * kBlock > w_lo;
+            const int slot0 = j * kBlock + 4 * hi;
+            if (masked)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (slot0 + u * 32 + (i & 3) + 8 * (i >> 2) >= lim)
+                            sc[u][i] = -__builtin_inff();
+            float tops[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                tops[q] = sc[0][q];
+#pragma unroll
+                for (int i = q + 4; i < 32; i += 4) tops[q] = fmaxf(tops[q], sc[i >> 4][i & 15]);
+            }
+            float top, other;
+            swap32(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), &top, &other);
+            const float f = fac * ks1;
+            top = fmaxf(top, other) * f;
+            if (__any(top > m + kSlack)) {
+                const float mn = fmaxf(m, top);
+                const float al = mn == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+                m = mn;
+                l *= al;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) acc[d] *= al;
+            }
+            if (vs1 > vscale) {                      // (uniform over the wave)
+                const float al = vscale / vs1;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) acc[d] *= al;
+                vscale = vs1;
+            }
+            // p times the block's part of the common scale; the sum takes it out again
+            const float vrel = fmaxf(vs1 / vscale, 1e-30f);
+            const float base = (m == -__builtin_inff() ? 0.f : m - kRaise) -
+                               __builtin_amdgcn_logf(vrel);
+            half8v pb[4];
+            float sums[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float p = __builtin_amdgcn_exp2f(fmaf(sc[u][i], f, -base));
+                    sums[i & 3] += p;
+                    pb[2 * u + (i >> 3)][i & 7] = (_Float16)p;
+                }
+            l += ((sums[0] + sums[1]) + (sums[2] + sums[3])) / vrel;
+            if (FMT == QLM_KV_E4M3 && masked && some_nan[j % 3]) {
+                // not-a-numbers that some columns see: taken out, and given to those
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    float16v cnt;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) cnt[i] = 0.f;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        half8v x = *(const half8v *)(vs + ((q * 2 + hi) * DP + d * 32 + c32) * 8);
+                        half8v z, seen;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const bool bad = x[e] != x[e];
+                            z[e] = bad ? (_Float16)1.f : (_Float16)0.f;
+                            x[e] = bad ? (_Float16)0.f : x[e];
+                            seen[e] = slot0 + q * 16 + (e & 3) + 8 * (e >> 2) < lim
+                                          ? (_Float16)1.f : (_Float16)0.f;
+                        }
+                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, pb[q], acc[d], 0, 0, 0);
+                        cnt = __builtin_amdgcn_mfma_f32_32x32x16_f16(z, seen, cnt, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        acc[d][i] += cnt[i] > 0.f ? __builtin_nanf("") : 0.f;
+                }
+            } else {
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    if (!FULL && d * 32 >= D) break;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const half8v x =
+                            *(const half8v *)(vs + ((q * 2 + hi) * DP + d * 32 + c32) * 8);
+                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, pb[q], acc[d], 0, 0, 0);
+                    }
+                }
+            }
+        }
+        if (j + 1 < b1) stage(buf ^ 1, j + 1, mapped);
+        // (read in the last round, set in the next one: a barrier lies on either side)
+        if (t == 0) some_nan[(j + 2) % 3] = 0;
+        __syncthreads();
+    }
+
+    float l0, l1;
+    swap32(l, &l0, &l1);
+    const float sum = l0 + l1, inv = sum == 0.f ? 0.f : 1.f / sum;
+    if (!valid) return;
+    const float lse = m - kRaise + __builtin_amdgcn_logf(sum);
+    const int64_t sr = (int64_t)sp * a.q.n_rows * a.H * a.G + rh;
+    if (hi == 0) {
+        if (a.splits > 1)
+            a.split_lse[sr] = sum == 0.f ? -__builtin_inff() : lse;
+        else
+            a.lse[rh] = sum == 0.f ? __builtin_inff() : lse;
+    }
+    uint16_t *out = (uint16_t *)a.od + (int64_t)(row0 + c / a.G) * a.o_row +
+                    (h * a.G + c % a.G) * a.o_head;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+        const float16v o = acc[d] * inv * vscale;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int dim = d * 32 + 8 * q + 4 * hi;
+            if (dim >= D) continue;
+            if (a.splits > 1) {
+                *(float4v *)(a.split_o + sr * D + dim) =
+                    float4v{o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]};
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) out[dim + i] = row_bits(o[4 * q + i], a.dtype);
+            }
+        }
+    }
+}
+
+// Joins the splits of the keys: a wave to a (row, head) of a sequence of many rows.
+__global__ __launch_bounds__(kThreads) void k_prompt_join(AttnArgs a)
+{
+    const int lane = threadIdx.x & 63, heads = a.H * a.G;
+    const int64_t w = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    const int64_t per = (int64_t)a.q.max_new * heads;
+    const int s = (int)(w / per);
+    if (s >= a.q.n_seqs) return;
+    int row0;
+    const int n = seq_rows(a.q, s, &row0), r = (int)(w % per / heads), head = (int)(w % heads);
+    if (n * a.G <= a.few || r >= n) return;
+    const int64_t rh = column(a, head / a.G, row0 + r, head % a.G);
+    const int64_t step = (int64_t)a.q.n_rows * heads;
+    float M = -__builtin_inff(), L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < a.splits; ++k) M = fmaxf(M, a.split_lse[rh + k * step]);
+    for (int k = 0; k < a.splits; ++k) {
+        const float z = a.split_lse[rh + k * step];
+        const float f = z == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(z - M);
+        L += f;
+        for (int e = 0; e < 4; ++e) {
+            const float x = a.split_o[(rh + k * step) * a.D + min(e * 64 + lane, a.D - 1)];
+            acc[e] += f == 0.f ? 0.f : f * x;
+        }
+    }
+    for (int e = 0; e < 4; ++e)
+        if (e * 64 + lane < a.D)
+            ((uint16_t *)a.od)[(row0 + r) * a.o_row + head * a.o_head + e * 64 + lane] =
+                row_bits(L == 0.f ? 0.f : acc[e] / L, a.dtype);
+    if (lane == 0) a.lse[rh] = L == 0.f ? __builtin_inff() : M + __builtin_amdgcn_logf(L);
+}
+
+// Weights of the sequences of many rows: a wave to a block of 64 slots of a
+// (sequence, kv head) holds its keys as matrix operands, forms the scores of all
+// columns that see it again, 32 at a time, and adds up their probabilities; a
+// workgroup's four waves take neighbouring blocks, so that one read of the
+// queries serves them from the cache.
 template <int FMT, int ND>
 __global__ __launch_bounds__(kThreads) void k_attend_colsum(AttnArgs a)
 {
-    __shared__ float part[kWaves][kBlock];
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    const int g = lane >> 4, c16 = lane & 15;
-    const int64_t w = blockIdx.x;
-    const int h = (int)(w % a.H);
-    const int64_t sb = w / a.H;
-    const int j = (int)(sb % a.blocks), s = (int)(sb / a.blocks);
-    const int len = seq_length(a.q, s);
-    if (j * kBlock >= len) return;
-    const int id = a.q.table[s * a.q.table_stride + j];
-    if ((unsigned)id >= (unsigned)a.n_blocks) return;
+    constexpr int DP = ND * 64, KS = DP / 16;
+    const int lane = threadIdx.x & 63;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int hi = lane >> 5, c32 = lane & 31;
+    const uint32_t groups = (uint32_t)(a.blocks + kWaves - 1) / kWaves;
+    uint32_t at = blockIdx.x;
+    const int j = (int)(at % groups) * kWaves + wv;
+    at /= groups;
+    const int h = (int)(at % (uint32_t)a.H), s = (int)(at / (uint32_t)a.H);
     int row0;
-    const int n = seq_rows(a.q, s, &row0);
+    const int n = seq_rows(a.q, s, &row0), len = seq_length(a.q, s);
     const int cols = n * a.G, before = len - n, D = a.D;
+    if (cols <= a.few || j * kBlock >= len) return;
+    const int id = uniform(a.q.table + s * a.q.table_stride + j);
+    if ((unsigned)id >= (unsigned)a.n_blocks) return;
     const int64_t bh = (int64_t)id * a.H + h;
-    const uint8_t *kp = a.kc + bh * kBlock * D;
-    uint4 kk[4][ND];
-    for (int t = 0; t < 4; ++t)
-        for (int c = 0; c < ND; ++c) {
-            const int d = c * 64 + g * 16;
-            kk[t][c] = d < D ? *(const uint4 *)(kp + (t * 16 + c16) * D + d) : uint4{0, 0, 0, 0};
+    half8v kf[2][KS];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            // (dims past the last: their query is 0)
+            const uint2 x = *(const uint2 *)(a.kc + (bh * kBlock + u * 32 + c32) * D +
+                                             min(k * 16 + hi * 8, D - 8));
+            kf[u][k] = halves8<FMT>(x.x, x.y);
         }
-    const float ksc = a.ks[bh];
-    const int slot0 = j * kBlock + 4 * g;
-    float4v sum[4];
-    for (int t = 0; t < 4; ++t) sum[t] = float4v{0.f, 0.f, 0.f, 0.f};
-    // rows that see the block's first slot
-    const int first = max(0, j * kBlock - before) * a.G / 16;
-    for (int ct = first + wv; ct * 16 < cols; ct += kWaves) {
-        const int c = ct * 16 + c16;
-        const bool valid = c < cols;
-        const int row = row0 + (valid ? c / a.G : 0), head = h * a.G + (valid ? c % a.G : 0);
-        half8v qf[ND][2];
-        float fac;
-        load_query<ND>(a, row, head, valid, g, qf, &fac);
-        fac *= a.scale * ksc;
-        const int lim = valid ? before + c / a.G + 1 : 0;
-        const float lse = valid ? a.lse[(int64_t)row * a.H * a.G + head] : 0.f;
-        for (int t = 0; t < 4; ++t) {
-            float4v sc = {0.f, 0.f, 0.f, 0.f};
-            for (int x = 0; x < ND; ++x) {
-                sc = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves8<FMT>(kk[t][x].x, kk[t][x].y),
-                                                            qf[x][0], sc, 0, 0, 0);
-                sc = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves8<FMT>(kk[t][x].z, kk[t][x].w),
-                                                            qf[x][1], sc, 0, 0, 0);
+    const float ksc = uniform(a.ks + bh);
+    const int slot0 = j * kBlock + 4 * hi;
+    float16v sum[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[u][i] = 0.f;
+    const int64_t all = (int64_t)a.q.n_rows * a.G, base = column(a, h, row0, 0);
+    const half8v *qp = (const half8v *)a.qh + ((int64_t)h * (DP / 8 - 1) + hi) * all + base;
+    half8v qn[KS];
+    float facn, lsen;
+    auto fetch = [&](int ct) {                   // (past the last column it is read again)
+        const int c = min(ct * 32 + c32, cols - 1);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) qn[k] = qp[2 * k * all + c];
+        facn = a.qfac[base + c];
+        lsen = a.lse[base + c];
+    };
+    const int first = max(0, j * kBlock - before) * a.G / 32;   // tile that sees the first slot
+    const int tiles = (cols + 31) / 32;
+    fetch(min(first, tiles - 1));
+    for (int ct = first; ct < tiles; ++ct) {
+        half8v qf[KS];
+#pragma unroll
+        for (int k = 0; k < KS; ++k) qf[k] = qn[k];
+        const int c = ct * 32 + c32;
+        const float fac = facn * ksc, lse = c < cols ? lsen : __builtin_inff();
+        fetch(min(ct + 1, tiles - 1));
+        const bool masked = (j + 1) * kBlock > before + ct * 32 / a.G + 1 || ct + 1 == tiles;
+        const int lim = masked && c < cols ? before + c / a.G + 1 : 0;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            float16v sc;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+                sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[u][k], qf[k], sc, 0, 0, 0);
+            if (masked)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float p = __builtin_amdgcn_exp2f(fmaf(sc[i], fac, -lse));
+                    sum[u][i] += slot0 + u * 32 + (i & 3) + 8 * (i >> 2) < lim ? p : 0.f;
+                }
+            else
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    sum[u][i] += __builtin_amdgcn_exp2f(fmaf(sc[i], fac, -lse));
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float x = sum[u][i];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) x += __shfl_xor(x, o);
+            const int slot = u * 32 + (i & 3) + 8 * (i >> 2) + 4 * hi;
+            if (c32 == 0 && j * kBlock + slot < len) {
+                float *w = a.weight + bh * kBlock + slot;
+                *w = a.decay == 0.f ? x : a.decay * *w + x;
             }
-            for (int i = 0; i < 4; ++i)
-                if (slot0 + t * 16 + i < lim) sum[t][i] += __builtin_amdgcn_exp2f(sc[i] * fac - lse);
         }
-    }
-    for (int t = 0; t < 4; ++t)
-        for (int i = 0; i < 4; ++i) {
-            float x = sum[t][i];
-            for (int o = 1; o < 16; o <<= 1) x += __shfl_xor(x, o);
-            if (c16 == 0) part[wv][t * 16 + 4 * g + i] = x;
-        }
-    __syncthreads();
-    const int o = threadIdx.x;
-    if (o < kBlock && j * kBlock + o < len) {
-        float x = 0.f;
-        for (int k = 0; k < kWaves; ++k) x += part[k][o];
-        float *at = a.weight + bh * kBlock + o;
-        *at = a.decay == 0.f ? x : a.decay * *at + x;
-    }
 }
 
 // -- host -------------------------------------------------------------------
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
-constexpr int kRowsMax = 64;     // columns for which scores are kept for the weights
+constexpr int kFew = 64;         // columns of a sequence that k_attend_rows takes
 
 struct Plan {
-    int nt, tile, workers, cols, blocks;
-    size_t part_o, part_lse, lse, s, total;
+    int nt, tile, workers, cols, blocks, splits;
+    bool few, many;              // which sequences there can be
+    size_t part_o, part_lse, lse, s, qh, qfac, split_o, split_lse, total;
 };
 
 Plan plan_of(const qlm_kv_cache *c, const qlm_kv_batch *b, int32_t n_heads, bool weights)
@@ -691,18 +1058,42 @@ Plan plan_of(const qlm_kv_cache *c, const qlm_kv_batch *b, int32_t n_heads, bool
     Plan p{};
     const int64_t cols = (int64_t)b->max_new * (n_heads / c->n_kv_heads);
     p.cols = (int)std::min<int64_t>(cols, INT32_MAX);
+    p.many = cols > kFew;
+    p.few = !p.many || b->n_rows != (int64_t)b->n_seqs * b->max_new;
     p.nt = cols <= 16 ? 1 : 2;
     p.tile = 16 * p.nt;
     p.blocks = std::max(1, (b->max_length + kBlock - 1) / kBlock);
     // as many waves as the registers of 256 CUs hold at once
     p.workers = c->head_dim <= 128 && p.nt == 1 ? 2048 : 1024;
-    p.part_o = 0;
-    p.part_lse = p.part_o + align256((size_t)2 * p.workers * p.tile * c->head_dim * 4);
-    p.lse = p.part_lse + align256((size_t)2 * p.workers * p.tile * 4);
-    p.s = p.lse + align256((size_t)b->n_rows * n_heads * 4);
-    p.total = p.s;
-    if (weights && cols <= kRowsMax)
-        p.total += align256((size_t)b->n_seqs * p.blocks * c->n_kv_heads * p.cols * kBlock * 4);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += align256(bytes);
+        return here;
+    };
+    p.lse = take((size_t)b->n_rows * n_heads * 4);
+    if (p.few) {
+        p.part_o = take((size_t)2 * p.workers * p.tile * c->head_dim * 4);
+        p.part_lse = take((size_t)2 * p.workers * p.tile * 4);
+        if (weights)
+            p.s = take((size_t)b->n_seqs * p.blocks * c->n_kv_heads * std::min(p.cols, kFew) *
+                       kBlock * 4);
+    }
+    p.splits = 1;
+    if (p.many) {
+        // two workgroups to a CU; eight blocks to a split at least
+        const int64_t wg = ((int64_t)b->n_rows * n_heads + 127) / 128;
+        p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(wg, 1),
+                                                               p.blocks / 8));
+        const size_t rh = (size_t)b->n_rows * n_heads;
+        p.qh = take(rh * ((c->head_dim + 63) / 64 == 3 ? 4 : (c->head_dim + 63) / 64) * 128);
+        p.qfac = take(rh * 4);
+        if (p.splits > 1) {
+            p.split_o = take(rh * p.splits * c->head_dim * 4);
+            p.split_lse = take(rh * p.splits * 4);
+        }
+    }
+    p.total = at;
     return p;
 }
 
@@ -721,14 +1112,32 @@ template <int FMT> void launch_rows(const AttnArgs &a, int nt, int64_t grid, hip
         nt == 1 ? launch_rows<FMT, 4, 1>(a, grid, st) : launch_rows<FMT, 4, 2>(a, grid, st);
 }
 
-template <int FMT> void launch_colsum(const AttnArgs &a, int64_t grid, hipStream_t st)
+template <int FMT, int ND> void launch_prompt(const AttnArgs &a, hipStream_t st)
 {
-    if (a.D <= 64)
-        k_attend_colsum<FMT, 1><<<(unsigned)grid, kThreads, 0, st>>>(a);
-    else if (a.D <= 128)
-        k_attend_colsum<FMT, 2><<<(unsigned)grid, kThreads, 0, st>>>(a);
+    const dim3 grid((unsigned)((int64_t)a.q.n_seqs * a.H * ((a.cols + 127) / 128)), a.splits);
+    if (a.D == ND * 64)
+        k_attend_prompt<FMT, ND, true><<<grid, kThreads, 0, st>>>(a);
     else
-        k_attend_colsum<FMT, 4><<<(unsigned)grid, kThreads, 0, st>>>(a);
+        k_attend_prompt<FMT, ND, false><<<grid, kThreads, 0, st>>>(a);
+}
+
+template <int ND> void launch_many(const AttnArgs &a, bool e4m3, hipStream_t st)
+{
+    const int64_t rh = (int64_t)a.q.n_rows * a.H * a.G;
+    k_query_half<ND><<<(unsigned)((rh + kWaves - 1) / kWaves), kThreads, 0, st>>>(a);
+    if (e4m3)
+        launch_prompt<QLM_KV_E4M3, ND>(a, st);
+    else
+        launch_prompt<QLM_KV_INT8, ND>(a, st);
+}
+
+template <int ND> void launch_colsum(const AttnArgs &a, bool e4m3, hipStream_t st)
+{
+    const unsigned grid = (unsigned)((int64_t)a.q.n_seqs * a.H * ((a.blocks + kWaves - 1) / kWaves));
+    if (e4m3)
+        k_attend_colsum<QLM_KV_E4M3, ND><<<grid, kThreads, 0, st>>>(a);
+    else
+        k_attend_colsum<QLM_KV_INT8, ND><<<grid, kThreads, 0, st>>>(a);
 }
 
 }  // namespace
@@ -799,17 +1208,26 @@ int qlm_kv_attention(const qlm_kv_cache *cache, const qlm_kv_batch *batch,
     a.part_o = (float *)(base + p.part_o);
     a.part_lse = (float *)(base + p.part_lse);
     a.lse = (float *)(base + p.lse);
-    const bool kept = query->accumulate && p.cols <= kRowsMax;
-    a.s = kept ? (float *)(base + p.s) : nullptr;
+    a.s = query->accumulate && p.few ? (float *)(base + p.s) : nullptr;
+    a.few = kFew;
+    a.qh = (uint16_t *)(base + p.qh);
+    a.qfac = (float *)(base + p.qfac);
+    a.splits = p.splits;
+    a.split_o = (float *)(base + p.split_o);
+    a.split_lse = (float *)(base + p.split_lse);
     a.decay = query->weight_decay;
 
     const bool e4m3 = cache->format == QLM_KV_E4M3;
     const int64_t sh = (int64_t)batch->n_seqs * a.H;
-    const int64_t units = sh * ((p.cols + p.tile - 1) / p.tile) * p.blocks;
-    if (units > INT32_MAX || sh * p.cols > INT32_MAX)
+    const int64_t few = std::min(p.cols, kFew);
+    const int64_t units = sh * ((few + p.tile - 1) / p.tile) * p.blocks;
+    if (units > INT32_MAX || sh * few > INT32_MAX ||
+        sh * (((int64_t)p.cols + 127) / 128) > INT32_MAX ||
+        (int64_t)batch->max_new * batch->n_seqs * query->n_heads > INT32_MAX ||
+        (int64_t)batch->n_rows * query->n_heads > INT32_MAX)
         return fail(QLM_ERR_CAPACITY, "too many rows or blocks in one call");
     hipError_t e;
-    if (batch->n_rows > 0) {
+    if (batch->n_rows > 0 && p.few) {
         const int64_t wg = (std::min<int64_t>(p.workers, units) + kWaves - 1) / kWaves;
         if (e4m3)
             launch_rows<QLM_KV_E4M3>(a, p.nt, wg, stream);
@@ -817,22 +1235,32 @@ int qlm_kv_attention(const qlm_kv_cache *cache, const qlm_kv_batch *batch,
             launch_rows<QLM_KV_INT8>(a, p.nt, wg, stream);
         if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_attend_rows launch");
         // few columns: a workgroup to each, their parts may be many
-        if (sh * p.cols <= 2048)
-            k_attend_join<kWaves><<<(unsigned)(sh * p.cols), kThreads, 0, stream>>>(a);
+        if (sh * few <= 2048)
+            k_attend_join<kWaves><<<(unsigned)(sh * few), kThreads, 0, stream>>>(a);
         else
-            k_attend_join<1><<<(unsigned)(sh * ((p.cols + kWaves - 1) / kWaves)), kThreads, 0,
+            k_attend_join<1><<<(unsigned)(sh * ((few + kWaves - 1) / kWaves)), kThreads, 0,
                                stream>>>(a);
         if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_attend_join launch");
     }
+    if (batch->n_rows > 0 && p.many) {
+        a.D <= 64 ? launch_many<1>(a, e4m3, stream)
+                  : a.D <= 128 ? launch_many<2>(a, e4m3, stream) : launch_many<4>(a, e4m3, stream);
+        if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_attend_prompt launch");
+        if (p.splits > 1) {
+            const int64_t w = (int64_t)batch->n_seqs * batch->max_new * query->n_heads;
+            k_prompt_join<<<(unsigned)((w + kWaves - 1) / kWaves), kThreads, 0, stream>>>(a);
+            if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_prompt_join launch");
+        }
+    }
     if (query->accumulate && batch->max_length > 0) {
-        if (kept) {
+        if (p.few) {
             const int64_t wg = (sh * p.blocks + kWaves - 1) / kWaves;
             k_attend_weights<<<(unsigned)wg, kThreads, 0, stream>>>(a);
-        } else if (e4m3) {
-            launch_colsum<QLM_KV_E4M3>(a, sh * p.blocks, stream);
-        } else {
-            launch_colsum<QLM_KV_INT8>(a, sh * p.blocks, stream);
         }
+        if (p.many && batch->n_rows > 0)
+            a.D <= 64 ? launch_colsum<1>(a, e4m3, stream)
+                      : a.D <= 128 ? launch_colsum<2>(a, e4m3, stream)
+                                   : launch_colsum<4>(a, e4m3, stream);
         if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "weight launch");
     }
     return QLM_OK;
