@@ -670,16 +670,18 @@ __global__ __launch_bounds__(kThreads, ND <= 2 ? 2 : 1) void k_attend_prompt(Att
     constexpr int DP = ND * 64, KS = DP / 16, DT = DP / 32;
     constexpr int KP = kBlock * 8 + 8;               // halves between chunks of 8 dims
     __shared__ uint4 ldsk[2][KS * 2 * KP / 8], ldsv[2][kBlock * DP / 8];
-    __shared__ int some_nan[3];                      // of blocks j, j + 1, j + 2 in turn
+    // blocks j, j + 1, j + 2 in turn: whether any value is not a number, and which
+    // slots of a dim are not
+    __shared__ int some_nan[3];
+    __shared__ unsigned long long nan_at[3][FMT == QLM_KV_E4M3 ? DP : 1];
     const int t = threadIdx.x, lane = t & 63;
     const int wv = __builtin_amdgcn_readfirstlane(t >> 6);
     const int hi = lane >> 5, c32 = lane & 31;
-    const uint32_t most = (uint32_t)(a.cols + 127) / 128;
-    uint32_t at = blockIdx.x;
-    // (the last rows see most: they come first)
-    const int ct = (int)(most - 1 - at % most);
-    at /= most;
-    const int h = (int)(at % (uint32_t)a.H), s = (int)(at / (uint32_t)a.H), sp = blockIdx.y;
+    const uint32_t most = (uint32_t)(a.cols + 127) / 128, heads = (uint32_t)(a.q.n_seqs * a.H);
+    // (the last rows see most: they come first, of every sequence)
+    const int ct = (int)(most - 1 - blockIdx.x / heads);
+    const uint32_t sh = blockIdx.x % heads;
+    const int h = (int)(sh % (uint32_t)a.H), s = (int)(sh / (uint32_t)a.H), sp = blockIdx.y;
     int row0;
     const int n = seq_rows(a.q, s, &row0);
     const int cols = n * a.G, col0 = ct * 128;
@@ -732,7 +734,6 @@ __global__ __launch_bounds__(kThreads, ND <= 2 ? 2 : 1) void k_attend_prompt(Att
     auto stage = [&](int buf, int j, bool mapped) {
         _Float16 *ks = (_Float16 *)ldsk[buf], *vs = (_Float16 *)ldsv[buf];
         const bool masked = (j + 1) * kBlock > lo_lim || !mapped;
-        uint32_t nans = 0;
 #pragma unroll
         for (int i = 0; i < ND; ++i) {
             const int e = t + kThreads * i, tok = e / (DP / 16), ch = e % (DP / 16);
@@ -746,7 +747,14 @@ __global__ __launch_bounds__(kThreads, ND <= 2 ? 2 : 1) void k_attend_prompt(Att
                     const int left = mapped ? hi_lim - (j * kBlock + q * 16 + 4 * g) : 0;
                     x[q] = left <= 0 ? 0u : left < 4 ? x[q] & (0xffffffffu >> (8 * (4 - left)))
                                                      : x[q];
-                    if (FMT == QLM_KV_E4M3) nans |= nan_bytes(x[q]);
+                    const uint32_t z = FMT == QLM_KV_E4M3 ? nan_bytes(x[q]) : 0;
+                    if (z) {                     // (taken out here, given to whom sees it below)
+                        x[q] &= ~z;
+                        some_nan[j % 3] = 1;
+                        atomicOr(&nan_at[j % 3][d],
+                                 (unsigned long long)((z & 1) | (z >> 7 & 2) | (z >> 14 & 4) |
+                                                      (z >> 21 & 8)) << (q * 16 + 4 * g));
+                    }
                 }
                 half2v lo, up;
                 halves4<FMT>(x[q], &lo, &up);
@@ -755,9 +763,12 @@ __global__ __launch_bounds__(kThreads, ND <= 2 ? 2 : 1) void k_attend_prompt(Att
                     half4v{lo[0], lo[1], up[0], up[1]};
             }
         }
-        if (FMT == QLM_KV_E4M3 && masked && nans) some_nan[j % 3] = 1;
     };
-    if (t < 3) some_nan[t] = 0;
+    auto no_nans = [&](int r) {
+        if (t == 0) some_nan[r] = 0;
+        if (FMT == QLM_KV_E4M3 && t < DP) nan_at[r][t] = 0;
+    };
+    for (int r = 0; r < 3; ++r) no_nans(r);
     __syncthreads();
     bool mapped = false;
     if (b0 < b1) {
@@ -833,49 +844,30 @@ __global__ __launch_bounds__(kThreads, ND <= 2 ? 2 : 1) void k_attend_prompt(Att
                     sums[i & 3] += p;
                     pb[2 * u + (i >> 3)][i & 7] = (_Float16)p;
                 }
-            l += ((sums[0] + sums[1]) + (sums[2] + sums[3])) / vrel;
-            if (FMT == QLM_KV_E4M3 && masked && some_nan[j % 3]) {
-                // not-a-numbers that some columns see: taken out, and given to those
+            l += ((sums[0] + sums[1]) + (sums[2] + sums[3])) * __builtin_amdgcn_rcpf(vrel);
 #pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    float16v cnt;
+            for (int d = 0; d < DT; ++d) {
+                if (!FULL && d * 32 >= D) break;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) cnt[i] = 0.f;
+                for (int q = 0; q < 4; ++q) {
+                    const half8v x = *(const half8v *)(vs + ((q * 2 + hi) * DP + d * 32 + c32) * 8);
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, pb[q], acc[d], 0, 0, 0);
+                }
+            }
+            if (FMT == QLM_KV_E4M3 && some_nan[j % 3]) {
+                const int n_seen = min(max(lim - j * kBlock, 0), kBlock);
+                const unsigned long long seen = n_seen ? ~0ull >> (kBlock - n_seen) : 0;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        half8v x = *(const half8v *)(vs + ((q * 2 + hi) * DP + d * 32 + c32) * 8);
-                        half8v z, seen;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const bool bad = x[e] != x[e];
-                            z[e] = bad ? (_Float16)1.f : (_Float16)0.f;
-                            x[e] = bad ? (_Float16)0.f : x[e];
-                            seen[e] = slot0 + q * 16 + (e & 3) + 8 * (e >> 2) < lim
-                                          ? (_Float16)1.f : (_Float16)0.f;
-                        }
-                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, pb[q], acc[d], 0, 0, 0);
-                        cnt = __builtin_amdgcn_mfma_f32_32x32x16_f16(z, seen, cnt, 0, 0, 0);
-                    }
+                for (int d = 0; d < DT; ++d)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        acc[d][i] += cnt[i] > 0.f ? __builtin_nanf("") : 0.f;
-                }
-            } else {
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    if (!FULL && d * 32 >= D) break;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const half8v x =
-                            *(const half8v *)(vs + ((q * 2 + hi) * DP + d * 32 + c32) * 8);
-                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, pb[q], acc[d], 0, 0, 0);
-                    }
-                }
+                        if (nan_at[j % 3][d * 32 + (i & 3) + 8 * (i >> 2) + 4 * hi] & seen)
+                            acc[d][i] = __builtin_nanf("");
             }
         }
         if (j + 1 < b1) stage(buf ^ 1, j + 1, mapped);
         // (read in the last round, set in the next one: a barrier lies on either side)
-        if (t == 0) some_nan[(j + 2) % 3] = 0;
+        if ((j + 2) * kBlock > lo_lim) no_nans((j + 2) % 3);
         __syncthreads();
     }
 
@@ -942,22 +934,21 @@ __global__ __launch_bounds__(kThreads) void k_prompt_join(AttnArgs a)
     if (lane == 0) a.lse[rh] = L == 0.f ? __builtin_inff() : M + __builtin_amdgcn_logf(L);
 }
 
-// Weights of the sequences of many rows: a wave to a block of 64 slots of a
-// (sequence, kv head) holds its keys as matrix operands, forms the scores of all
-// columns that see it again, 32 at a time, and adds up their probabilities; a
-// workgroup's four waves take neighbouring blocks, so that one read of the
-// queries serves them from the cache.
+// Weights of the sequences of many rows: a workgroup to a block of 64 slots of a
+// (sequence, kv head).  Its waves hold the block's keys as matrix operands, form
+// the scores of the columns that see it again, a wave every fourth 32, the next
+// ones' queries on their way meanwhile, and add up their probabilities.
 template <int FMT, int ND>
-__global__ __launch_bounds__(kThreads) void k_attend_colsum(AttnArgs a)
+__global__ __launch_bounds__(kThreads, ND <= 2 ? 2 : 1) void k_attend_colsum(AttnArgs a)
 {
+    __shared__ float part[kWaves][kBlock];
     constexpr int DP = ND * 64, KS = DP / 16;
     const int lane = threadIdx.x & 63;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hi = lane >> 5, c32 = lane & 31;
-    const uint32_t groups = (uint32_t)(a.blocks + kWaves - 1) / kWaves;
     uint32_t at = blockIdx.x;
-    const int j = (int)(at % groups) * kWaves + wv;
-    at /= groups;
+    const int j = (int)(at % (uint32_t)a.blocks);
+    at /= (uint32_t)a.blocks;
     const int h = (int)(at % (uint32_t)a.H), s = (int)(at / (uint32_t)a.H);
     int row0;
     const int n = seq_rows(a.q, s, &row0), len = seq_length(a.q, s);
@@ -996,14 +987,14 @@ __global__ __launch_bounds__(kThreads) void k_attend_colsum(AttnArgs a)
     };
     const int first = max(0, j * kBlock - before) * a.G / 32;   // tile that sees the first slot
     const int tiles = (cols + 31) / 32;
-    fetch(min(first, tiles - 1));
-    for (int ct = first; ct < tiles; ++ct) {
+    fetch(min(first + wv, tiles - 1));
+    for (int ct = first + wv; ct < tiles; ct += kWaves) {
         half8v qf[KS];
 #pragma unroll
         for (int k = 0; k < KS; ++k) qf[k] = qn[k];
         const int c = ct * 32 + c32;
         const float fac = facn * ksc, lse = c < cols ? lsen : __builtin_inff();
-        fetch(min(ct + 1, tiles - 1));
+        fetch(min(ct + kWaves, tiles - 1));
         const bool masked = (j + 1) * kBlock > before + ct * 32 / a.G + 1 || ct + 1 == tiles;
         const int lim = masked && c < cols ? before + c / a.G + 1 : 0;
 #pragma unroll
@@ -1034,11 +1025,15 @@ __global__ __launch_bounds__(kThreads) void k_attend_colsum(AttnArgs a)
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) x += __shfl_xor(x, o);
             const int slot = u * 32 + (i & 3) + 8 * (i >> 2) + 4 * hi;
-            if (c32 == 0 && j * kBlock + slot < len) {
-                float *w = a.weight + bh * kBlock + slot;
-                *w = a.decay == 0.f ? x : a.decay * *w + x;
-            }
+            if (c32 == 0) part[wv][slot] = x;
         }
+    __syncthreads();
+    const int slot = threadIdx.x;
+    if (slot < kBlock && j * kBlock + slot < len) {
+        const float x = (part[0][slot] + part[1][slot]) + (part[2][slot] + part[3][slot]);
+        float *w = a.weight + bh * kBlock + slot;
+        *w = a.decay == 0.f ? x : a.decay * *w + x;
+    }
 }
 
 // -- host -------------------------------------------------------------------
@@ -1133,7 +1128,7 @@ template <int ND> void launch_many(const AttnArgs &a, bool e4m3, hipStream_t st)
 
 template <int ND> void launch_colsum(const AttnArgs &a, bool e4m3, hipStream_t st)
 {
-    const unsigned grid = (unsigned)((int64_t)a.q.n_seqs * a.H * ((a.blocks + kWaves - 1) / kWaves));
+    const unsigned grid = (unsigned)((int64_t)a.q.n_seqs * a.H * a.blocks);
     if (e4m3)
         k_attend_colsum<QLM_KV_E4M3, ND><<<grid, kThreads, 0, st>>>(a);
     else
@@ -1222,7 +1217,7 @@ int qlm_kv_attention(const qlm_kv_cache *cache, const qlm_kv_batch *batch,
     const int64_t few = std::min(p.cols, kFew);
     const int64_t units = sh * ((few + p.tile - 1) / p.tile) * p.blocks;
     if (units > INT32_MAX || sh * few > INT32_MAX ||
-        sh * (((int64_t)p.cols + 127) / 128) > INT32_MAX ||
+        sh * (((int64_t)p.cols + 127) / 128) > INT32_MAX || sh * p.blocks > INT32_MAX ||
         (int64_t)batch->max_new * batch->n_seqs * query->n_heads > INT32_MAX ||
         (int64_t)batch->n_rows * query->n_heads > INT32_MAX)
         return fail(QLM_ERR_CAPACITY, "too many rows or blocks in one call");
