@@ -3,12 +3,14 @@
 //
 // A code c becomes the number 16 + c by placing its four bits at the top of a
 // mantissa under the exponent of 16 (exact in half precision and bfloat16, one
-// shift and one and-or for two codes).  With X = x as it came and one group's
-// sums S = sum of x, T[n] = sum of (16 + c[n]) x, both by the matrix
-// instructions (S with a matrix of ones), the group's part of the output is
-//   s[n] (T[n] - (16 + z[n]) S),
-// formed in single precision; so no weight is ever rounded.  An x that is not
-// finite makes its row's outputs not finite.
+// shift and one and-or for two codes).  No weight is ever rounded:
+//  - up to 16 rows, with one group's sums S = sum of x, T[n] = sum of (16 + c[n]) x,
+//    both by the matrix instructions (S with a matrix of ones), the group's part of
+//    the output is s[n] (T[n] - (16 + z[n]) S), formed in single precision;
+//  - for more rows 16 + z is taken off in half precision (exact: -15 .. 15), once for
+//    all of them, and the part is s[n] T[n].  Rows of bfloat16 are first scaled by
+//    powers of two to fit halves.
+// An x that is not finite makes its row's outputs not finite.
 //
 // Packed: for each 16 outputs and each 128 inputs one chunk of 1024 bytes of
 // codes in the order of the matrix operand (lane l of 64: output l % 16, and for
@@ -54,12 +56,21 @@ __global__ __launch_bounds__(64) void k_w4_pack(PackArgs a)
     uint8_t *chunk = a.packed + (int64_t)blockIdx.x * chunk_bytes(a.group);
     const int n = tile * 16 + l % 16;
     uint32_t w[4] = {0, 0, 0, 0};
-    for (int j = 0; j < 4; ++j)
-        for (int e = 0; e < 8; ++e) {
-            const int k = kb * kStep + j * 32 + (l / 16) * 8 + e;
-            const uint32_t c = n < a.N && k < a.K ? a.codes[(int64_t)n * a.K + k] & 15u : 0u;
-            w[j] |= c << (16 * (e & 1) + 4 * (e >> 1));
+    const bool wide = a.K % 8 == 0 && (uintptr_t)a.codes % 8 == 0;
+    for (int j = 0; j < 4; ++j) {
+        const int k = kb * kStep + j * 32 + (l / 16) * 8;
+        const uint8_t *p = a.codes + (int64_t)n * a.K + k;
+        uint8_t c[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (n < a.N && wide && k < a.K) {
+            const uint2 x = *(const uint2 *)p;
+            for (int e = 0; e < 8; ++e) c[e] = (uint8_t)((e < 4 ? x.x : x.y) >> (8 * (e & 3)));
+        } else if (n < a.N) {
+            for (int e = 0; e < 8; ++e)
+                if (k + e < a.K) c[e] = p[e];
         }
+        for (int e = 0; e < 8; ++e)
+            w[j] |= (uint32_t)(c[e] & 15u) << (16 * (e & 1) + 4 * (e >> 1));
+    }
     *(uint4 *)(chunk + 16 * l) = uint4{w[0], w[1], w[2], w[3]};
     const int per = kStep / a.group, groups = (a.K + a.group - 1) / a.group;
     for (int i = l; i < per * 16; i += 64) {
@@ -83,14 +94,23 @@ template <bool BF> __device__ inline float4v mfma(uint4 x, uint4 y, float4v c)
                                                   __builtin_bit_cast(half8v, y), c, 0, 0, 0);
 }
 
+// The exponent of 16 for two numbers, in a register (an and-or takes one constant
+// from the scalar side only).
+template <bool BF> __device__ inline uint32_t sixteen()
+{
+    uint32_t c = BF ? 0x41804180u : 0x4c004c00u;
+    asm("" : "+v"(c));
+    return c;
+}
+
 // The eight codes of a dword as 16 + c.
-template <bool BF> __device__ inline uint4 operand(uint32_t w)
+template <bool BF> __device__ inline uint4 operand(uint32_t w, uint32_t c)
 {
     if (BF)
-        return {(w << 3 & 0x00780078u) | 0x41804180u, (w >> 1 & 0x00780078u) | 0x41804180u,
-                (w >> 5 & 0x00780078u) | 0x41804180u, (w >> 9 & 0x00780078u) | 0x41804180u};
-    return {(w << 6 & 0x03c003c0u) | 0x4c004c00u, (w << 2 & 0x03c003c0u) | 0x4c004c00u,
-            (w >> 2 & 0x03c003c0u) | 0x4c004c00u, (w >> 6 & 0x03c003c0u) | 0x4c004c00u};
+        return {(w << 3 & 0x00780078u) | c, (w >> 1 & 0x00780078u) | c,
+                (w >> 5 & 0x00780078u) | c, (w >> 9 & 0x00780078u) | c};
+    return {(w << 6 & 0x03c003c0u) | c, (w << 2 & 0x03c003c0u) | c,
+            (w >> 2 & 0x03c003c0u) | c, (w >> 6 & 0x03c003c0u) | c};
 }
 
 template <bool BF> __device__ inline uint4 ones()
@@ -123,6 +143,8 @@ struct MatArgs {
     int64_t x_stride, out_stride;
     int32_t N, K, M, tiles, steps;
     int32_t wide;                    // x may be read 16 bytes at a time
+    int32_t bf;                      // out is bfloat16 (k_w4_wide)
+    const float *fac;                // [M] what takes the rows' scaling out, or NULL
     int32_t per_stage;               // thin: steps of x held at once (a multiple of kWaves)
     int32_t splits, per_split;       // wide form: splits of K, steps of one
     float *part;                     // [split][M][N]
@@ -156,6 +178,7 @@ template <bool BF, int GROUP> __global__ __launch_bounds__(kThreads) void k_w4_t
     const uint8_t *base = a.packed + (int64_t)tile * a.steps * cb;
     const int ld = a.per_stage * kStep + 8;      // elements of a row in shared memory
     const int mine = c16 < a.M ? c16 : 0;
+    const uint32_t c16f = sixteen<BF>();
     float4v sum = {0.f, 0.f, 0.f, 0.f};
     uint4 cw[PF], mw[PF][PER];
     auto fetch = [&](int u, int kb) {
@@ -190,7 +213,7 @@ template <bool BF, int GROUP> __global__ __launch_bounds__(kThreads) void k_w4_t
                     float4v t = {0.f, 0.f, 0.f, 0.f}, S = {0.f, 0.f, 0.f, 0.f};
                     for (int j = q * SUB; j < (q + 1) * SUB; ++j) {
                         const uint4 b = *(const uint4 *)(xp + 32 * j);
-                        t = mfma<BF>(operand<BF>(w[j]), b, t);
+                        t = mfma<BF>(operand<BF>(w[j], c16f), b, t);
                         S = mfma<BF>(ones<BF>(), b, S);
                     }
                     sum = add_group(sum, t, S[0], mw[u][q]);
@@ -211,12 +234,41 @@ template <bool BF, int GROUP> __global__ __launch_bounds__(kThreads) void k_w4_t
     if (m < a.M && n < a.N) a.out[m * a.out_stride + n] = out_bits(v, BF);
 }
 
-// More rows: one workgroup to 64 outputs (16 a wave) and 16 NT rows; x passes
-// through shared memory a step at a time, in two buffers.
-template <bool BF, int GROUP, int NT>
-__global__ __launch_bounds__(kThreads) void k_w4_wide(MatArgs a)
+// Rows of bfloat16 as halves: scaled by a power of two to below 2^15.  A
+// workgroup to a row.
+__global__ __launch_bounds__(kThreads) void k_w4_half(MatArgs a, uint16_t *xh, float *fac, int ld)
 {
-    constexpr int PER = kStep / GROUP, SUB = 4 / PER, LD = kStep + 8;
+    __shared__ uint32_t part[kWaves];
+    const uint16_t *p = a.x + blockIdx.x * a.x_stride;
+    uint32_t top = 0;                       // greatest exponent of a finite element
+    for (int k = threadIdx.x; k < a.K; k += kThreads) {
+        const uint32_t e = (uint32_t)(p[k] >> 7) & 0xff;
+        top = e < 255 ? max(top, e) : top;
+    }
+    for (int o = 32; o; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = top;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) top = max(top, part[w]);
+    const int up = min(15 - ((int)top - 126), 126);
+    const float by = ldexpf(1.f, up);
+    for (int k = threadIdx.x; k < ld; k += kThreads) {
+        const float x = k < a.K ? __builtin_bit_cast(float, (uint32_t)p[k] << 16) : 0.f;
+        xh[(int64_t)blockIdx.x * ld + k] = __builtin_bit_cast(uint16_t, (_Float16)(x * by));
+    }
+    if (threadIdx.x == 0) fac[blockIdx.x] = ldexpf(1.f, -up);
+}
+
+__device__ inline uint16_t wide_out(const MatArgs &a, float v, int m)
+{
+    return out_bits(a.fac ? v * a.fac[m] : v, a.bf);
+}
+
+// More rows: one workgroup to 64 outputs (16 a wave) and 16 NT rows of halves; x
+// passes through shared memory two steps at a time, in two buffers; the weights of
+// the two steps after the present ones are on their way.
+template <int GROUP, int NT> __global__ __launch_bounds__(kThreads, 2) void k_w4_wide(MatArgs a)
+{
+    constexpr int PER = kStep / GROUP, SUB = 4 / PER, LD = 2 * kStep + 8;
     __shared__ uint4 lds[2][NT * 16 * LD / 8];
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
     const int g = lane >> 4, c16 = lane & 15;
@@ -225,82 +277,115 @@ __global__ __launch_bounds__(kThreads) void k_w4_wide(MatArgs a)
     const int cb = chunk_bytes(GROUP);
     const bool mine = tile < a.tiles;
     const uint8_t *base = a.packed + (int64_t)(mine ? tile : 0) * a.steps * cb;
+    const uint32_t c16f = sixteen<false>();
     float4v sum[NT];
+#pragma unroll
     for (int t = 0; t < NT; ++t) sum[t] = float4v{0.f, 0.f, 0.f, 0.f};
-    uint4 cw, mw[PER], xr[NT];
-    auto fetch_w = [&](int kb) {
-        const uint8_t *p = base + (int64_t)kb * cb;
-        cw = *(const uint4 *)(p + 16 * lane);
-        for (int q = 0; q < PER; ++q) mw[q] = *(const uint4 *)(p + 1024 + 64 * q + 16 * g);
+    uint4 cw[2], mw[2][PER], xr[2 * NT];
+    uint16_t zw[2][PER];
+    auto fetch_w = [&](int u, int kb) {          // (past the last step it is read again)
+        const uint8_t *p = base + (int64_t)min(kb, k1 - 1) * cb;
+        cw[u] = *(const uint4 *)(p + 16 * lane);
+#pragma unroll
+        for (int q = 0; q < PER; ++q) {
+            mw[u][q] = *(const uint4 *)(p + 1024 + 64 * q + 16 * g);
+            zw[u][q] = *(const uint16_t *)(p + 1024 + 64 * q + 4 * c16 + 2);
+        }
     };
-    // thread t stages row t / 16 of each 16 rows, inputs 8 (t % 16) on
+    // thread t stages row t / 16 of each 16 rows, inputs 8 (t % 16) on of each step;
+    // rows past the last are the last again (their outputs are not written)
     const int sr = threadIdx.x >> 4, sk = 8 * (threadIdx.x & 15);
     auto fetch_x = [&](int kb) {
-        for (int t = 0; t < NT; ++t) {
-            const int r = m0 + t * 16 + sr;
-            xr[t] = r < a.M ? x8(a, r, kb * kStep + sk) : uint4{0, 0, 0, 0};
+        const bool whole = a.wide && (kb + 2) * kStep <= a.K;
+#pragma unroll
+        for (int t = 0; t < 2 * NT; ++t) {
+            const int r = min(m0 + (t >> 1) * 16 + sr, a.M - 1), k = (kb + (t & 1)) * kStep + sk;
+            if (whole)
+                xr[t] = *(const uint4 *)(a.x + r * a.x_stride + k);
+            else
+                xr[t] = x8(a, r, k);
         }
     };
     auto stage = [&](int buf) {
         uint16_t *xs = (uint16_t *)lds[buf];
-        for (int t = 0; t < NT; ++t) *(uint4 *)(xs + (t * 16 + sr) * LD + sk) = xr[t];
+#pragma unroll
+        for (int t = 0; t < 2 * NT; ++t)
+            *(uint4 *)(xs + ((t >> 1) * 16 + sr) * LD + (t & 1) * kStep + sk) = xr[t];
     };
     if (k0 < k1) {
-        fetch_w(k0);
         fetch_x(k0);
+        fetch_w(0, k0);
+        fetch_w(1, k0 + 1);
         stage(0);
     }
     __syncthreads();
-    for (int kb = k0; kb < k1; ++kb) {
-        const int buf = (kb - k0) & 1;
-        const uint4 w4 = cw;
-        uint4 m4[PER];
-        for (int q = 0; q < PER; ++q) m4[q] = mw[q];
-        if (kb + 1 < k1) {
-            fetch_w(kb + 1);
-            fetch_x(kb + 1);
-        }
+    for (int kb = k0; kb < k1; kb += 2) {
+        const int buf = ((kb - k0) >> 1) & 1;
+        if (kb + 2 < k1) fetch_x(kb + 2);
         const uint16_t *xs = (const uint16_t *)lds[buf];
-        const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
-        for (int q = 0; q < PER; ++q) {
-            float4v t[NT], S[NT];
-            for (int k = 0; k < NT; ++k) t[k] = S[k] = float4v{0.f, 0.f, 0.f, 0.f};
-            for (int j = q * SUB; j < (q + 1) * SUB; ++j) {
-                const uint4 o = operand<BF>(w[j]);
-                for (int k = 0; k < NT; ++k) {
-                    const uint4 b = *(const uint4 *)(xs + (k * 16 + c16) * LD + 32 * j + 8 * g);
-                    t[k] = mfma<BF>(o, b, t[k]);
-                    S[k] = mfma<BF>(ones<BF>(), b, S[k]);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if (kb + u >= k1) break;
+            const uint32_t w[4] = {cw[u].x, cw[u].y, cw[u].z, cw[u].w};
+#pragma unroll
+            for (int q = 0; q < PER; ++q) {
+                const half2v z = __builtin_bit_cast(half2v, (uint32_t)zw[u][q] * 0x10001u);
+                float4v t[NT];
+#pragma unroll
+                for (int k = 0; k < NT; ++k) t[k] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = q * SUB; j < (q + 1) * SUB; ++j) {
+                    uint4 o = operand<false>(w[j], c16f);
+                    o.x = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, o.x) - z);
+                    o.y = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, o.y) - z);
+                    o.z = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, o.z) - z);
+                    o.w = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, o.w) - z);
+#pragma unroll
+                    for (int k = 0; k < NT; ++k) {
+                        const uint4 b = *(const uint4 *)(xs + (k * 16 + c16) * LD + u * kStep +
+                                                         32 * j + 8 * g);
+                        t[k] = mfma<false>(o, b, t[k]);
+                    }
                 }
+                const uint32_t m[4] = {mw[u][q].x, mw[u][q].y, mw[u][q].z, mw[u][q].w};
+#pragma unroll
+                for (int k = 0; k < NT; ++k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        sum[k][i] = fmaf((float)__builtin_bit_cast(half2v, m[i])[0], t[k][i],
+                                         sum[k][i]);
             }
-            for (int k = 0; k < NT; ++k) sum[k] = add_group(sum[k], t[k], S[k][0], m4[q]);
+            fetch_w(u, kb + u + 2);
         }
-        if (kb + 1 < k1) stage(buf ^ 1);
+        if (kb + 2 < k1) stage(buf ^ 1);
         __syncthreads();
     }
     if (!mine) return;
+#pragma unroll
     for (int k = 0; k < NT; ++k) {
         const int m = m0 + k * 16 + c16;
         if (m >= a.M) continue;
+#pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int n = tile * 16 + 4 * g + i;
             if (n >= a.N) continue;
             if (a.splits > 1)
                 a.part[((int64_t)sp * a.M + m) * a.N + n] = sum[k][i];
             else
-                a.out[m * a.out_stride + n] = out_bits(sum[k][i], BF);
+                a.out[m * a.out_stride + n] = wide_out(a, sum[k][i], m);
         }
     }
 }
 
-__global__ __launch_bounds__(kThreads) void k_w4_join(MatArgs a, int bf)
+__global__ __launch_bounds__(kThreads) void k_w4_join(MatArgs a)
 {
     const int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     const int64_t all = (int64_t)a.M * a.N;
     if (e >= all) return;
     float v = 0.f;
     for (int s = 0; s < a.splits; ++s) v += a.part[s * all + e];
-    a.out[e / a.N * a.out_stride + e % a.N] = out_bits(v, bf);
+    const int m = (int)(e / a.N), n = (int)(e % a.N);
+    a.out[m * a.out_stride + n] = wide_out(a, v, m);
 }
 
 // -- host -------------------------------------------------------------------
@@ -332,34 +417,53 @@ void split_of(const qlm_w4 *w, int rows, int *splits, int *per)
     *splits = (steps + *per - 1) / *per;
 }
 
-template <bool BF, int GROUP> void launch(MatArgs a, int rows, hipStream_t st)
+template <bool BF, int GROUP> void launch_thin(MatArgs a, hipStream_t st)
 {
-    if (rows <= kThinRows) {
-        // as much of x as 64 KiB hold
-        const int most = (65536 / rows - 16) / (2 * kStep) / kWaves * kWaves;
-        a.per_stage = std::min(most, (a.steps + kWaves - 1) / kWaves * kWaves);
-        const int bytes = std::max(rows * (a.per_stage * kStep + 8) * 2, kWaves * 1024);
-        k_w4_thin<BF, GROUP><<<a.tiles, kThreads, bytes, st>>>(a);
-        return;
-    }
-    const int nt = std::min(4, (rows + 15) / 16);
-    const dim3 grid((a.tiles + kWaves - 1) / kWaves, (rows + 16 * nt - 1) / (16 * nt), a.splits);
-    if (nt == 2)
-        k_w4_wide<BF, GROUP, 2><<<grid, kThreads, 0, st>>>(a);
-    else if (nt == 3)
-        k_w4_wide<BF, GROUP, 3><<<grid, kThreads, 0, st>>>(a);
-    else
-        k_w4_wide<BF, GROUP, 4><<<grid, kThreads, 0, st>>>(a);
+    // as much of x as 64 KiB hold
+    const int most = (65536 / a.M - 16) / (2 * kStep) / kWaves * kWaves;
+    a.per_stage = std::min(most, (a.steps + kWaves - 1) / kWaves * kWaves);
+    const int bytes = std::max(a.M * (a.per_stage * kStep + 8) * 2, kWaves * 1024);
+    k_w4_thin<BF, GROUP><<<a.tiles, kThreads, bytes, st>>>(a);
 }
 
-template <bool BF> void launch(const MatArgs &a, int group, int rows, hipStream_t st)
+template <int GROUP> void launch(const MatArgs &a, hipStream_t st)
 {
-    if (group == 32)
-        launch<BF, 32>(a, rows, st);
-    else if (group == 64)
-        launch<BF, 64>(a, rows, st);
+    if (a.M <= kThinRows) {
+        if (a.bf)
+            launch_thin<true, GROUP>(a, st);
+        else
+            launch_thin<false, GROUP>(a, st);
+        return;
+    }
+    const int nt = std::min(4, (a.M + 15) / 16);
+    const dim3 grid((a.tiles + kWaves - 1) / kWaves, (a.M + 16 * nt - 1) / (16 * nt), a.splits);
+    if (nt == 2)
+        k_w4_wide<GROUP, 2><<<grid, kThreads, 0, st>>>(a);
+    else if (nt == 3)
+        k_w4_wide<GROUP, 3><<<grid, kThreads, 0, st>>>(a);
     else
-        launch<BF, 128>(a, rows, st);
+        k_w4_wide<GROUP, 4><<<grid, kThreads, 0, st>>>(a);
+}
+
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+
+// Workspace of the form for more rows: parts of the splits, then halves of x.
+struct Layout {
+    size_t xh, fac, total;
+    int ld;
+};
+
+Layout layout_of(const qlm_w4 *w, int rows)
+{
+    Layout l{};
+    if (rows <= kThinRows) return l;
+    int splits, per;
+    split_of(w, rows, &splits, &per);
+    l.ld = (w->n_in + 2 * kStep - 1) / (2 * kStep) * 2 * kStep;
+    l.xh = splits > 1 ? align256((size_t)splits * rows * w->n_out * 4) : 0;
+    l.fac = l.xh + align256((size_t)rows * l.ld * 2);
+    l.total = l.fac + align256((size_t)rows * 4);
+    return l;
 }
 
 }  // namespace
@@ -400,9 +504,7 @@ int qlm_w4_pack(const qlm_w4 *weight, const uint8_t *codes, const void *scale,
 size_t qlm_w4_workspace_bytes(const qlm_w4 *weight, int32_t n_rows)
 {
     if (!weight || n_rows < 1 || weight->n_out < 1 || weight->n_in < 1) return 0;
-    int splits, per;
-    split_of(weight, n_rows, &splits, &per);
-    return splits > 1 ? (size_t)splits * n_rows * weight->n_out * 4 : 0;
+    return layout_of(weight, n_rows).total;
 }
 
 int qlm_w4_matmul(const qlm_w4 *weight, const void *x, int64_t x_stride, void *out,
@@ -421,6 +523,8 @@ int qlm_w4_matmul(const qlm_w4 *weight, const void *x, int64_t x_stride, void *o
     if (x == out) return fail(QLM_ERR_ARG, "out may not alias x");
     if (x_stride < weight->n_in || out_stride < weight->n_out)
         return fail(QLM_ERR_ARG, "x_stride and out_stride must be >= the row's length");
+    if (((int64_t)n_rows * weight->n_out + kThreads - 1) / kThreads > INT32_MAX)
+        return fail(QLM_ERR_CAPACITY, "too many outputs in one call");
     const size_t need = qlm_w4_workspace_bytes(weight, n_rows);
     if (need && (!ws || (uintptr_t)ws % 256))
         return fail(QLM_ERR_WORKSPACE, "workspace must be non-NULL and 256-byte aligned");
@@ -437,18 +541,31 @@ int qlm_w4_matmul(const qlm_w4 *weight, const void *x, int64_t x_stride, void *o
     a.tiles = (a.N + 15) / 16;
     a.steps = (a.K + kStep - 1) / kStep;
     a.wide = (uintptr_t)x % 16 == 0 && x_stride % 8 == 0;
+    a.bf = dtype == QLM_BF16;
     split_of(weight, n_rows, &a.splits, &a.per_split);
     a.part = (float *)ws;
-    if (dtype == QLM_BF16)
-        launch<true>(a, weight->group, n_rows, stream);
+    hipError_t e;
+    if (a.bf && n_rows > kThinRows) {
+        const Layout l = layout_of(weight, n_rows);
+        uint16_t *xh = (uint16_t *)((char *)ws + l.xh);
+        float *fac = (float *)((char *)ws + l.fac);
+        k_w4_half<<<n_rows, kThreads, 0, stream>>>(a, xh, fac, l.ld);
+        if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_w4_half launch");
+        a.x = xh;
+        a.x_stride = a.K = l.ld;
+        a.wide = 1;
+        a.fac = fac;
+    }
+    if (weight->group == 32)
+        launch<32>(a, stream);
+    else if (weight->group == 64)
+        launch<64>(a, stream);
     else
-        launch<false>(a, weight->group, n_rows, stream);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return hip_fail(e, "w4 launch");
+        launch<128>(a, stream);
+    if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "w4 launch");
     if (a.splits > 1) {
         const int64_t grid = ((int64_t)a.M * a.N + kThreads - 1) / kThreads;
-        if (grid > INT32_MAX) return fail(QLM_ERR_CAPACITY, "too many outputs in one call");
-        k_w4_join<<<(unsigned)grid, kThreads, 0, stream>>>(a, dtype == QLM_BF16);
+        k_w4_join<<<(unsigned)grid, kThreads, 0, stream>>>(a);
         if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_w4_join launch");
     }
     return QLM_OK;
