@@ -125,14 +125,6 @@ __device__ inline int value_place(int t) { return ((t >> 4) << 2) | (t & 3); }
 // The slot at place p of group g.
 __device__ inline int value_slot(int g, int p) { return ((p >> 2) << 4) | (g << 2) | (p & 3); }
 
-// A row's element as a float.
-__device__ inline float row_value(const void *p, int64_t at, int dtype)
-{
-    const uint16_t u = ((const uint16_t *)p)[at];
-    if (dtype == QLM_BF16) return __builtin_bit_cast(float, (uint32_t)u << 16);
-    return (float)__builtin_bit_cast(_Float16, u);
-}
-
 // The bits of a row's element: rounded to nearest, ties to even.
 __device__ inline uint16_t row_bits(float v, int dtype)
 {

@@ -150,16 +150,67 @@ struct AppendArgs {
     Seqs q;
     const void *k, *v;
     int64_t k_row, k_head, v_row, v_head;
-    int32_t k_type, v_type;
+    int32_t k_type, v_type, k_wide, v_wide;   // wide: may be read 16 bytes at a time
     const int32_t *first;
     int32_t touched;      // blocks a sequence's new slots may lie in
 };
 
-// One workgroup for each (sequence, block that takes new slots, kv head).
-template <int FMT> __global__ __launch_bounds__(kThreads) void k_append(AppendArgs a)
+// Eight dims of a row as bits, 16 bytes at once where they are aligned.
+__device__ inline uint4 row_bits8(const void *p, int64_t at, bool wide)
 {
+    const uint16_t *u = (const uint16_t *)p + at;
+    if (wide) return *(const uint4 *)u;
+    return {u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16, u[4] | (uint32_t)u[5] << 16,
+            u[6] | (uint32_t)u[7] << 16};
+}
+
+__device__ inline float bits_value(uint32_t u, int dtype)
+{
+    if (dtype == QLM_BF16) return __builtin_bit_cast(float, u << 16);
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)u);
+}
+
+// The greatest finite magnitude of eight dims, as bits (magnitudes order as integers).
+__device__ inline uint32_t magnitude8(uint4 x, int dtype)
+{
+    const uint32_t inf = dtype == QLM_BF16 ? 0x7f80u : 0x7c00u;
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    uint32_t top = 0;
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t m = (w[i >> 1] >> (16 * (i & 1))) & 0x7fffu;
+        top = max(top, m < inf ? m : 0u);
+    }
+    return top;
+}
+
+// Eight dims as codes over `scale` (a power of two nearly always: a product then).
+template <int FMT> __device__ inline uint2 codes8(uint4 x, int dtype, float scale, bool exact)
+{
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    const float by = 1.f / scale;
+    uint32_t o[2] = {0, 0};
+    for (int i = 0; i < 8; ++i) {
+        const float v = bits_value((w[i >> 1] >> (16 * (i & 1))) & 0xffff, dtype);
+        o[i >> 2] |= code_of<FMT>(exact ? v * by : v / scale) << (8 * (i & 3));
+    }
+    return {o[0], o[1]};
+}
+
+__device__ inline bool power_of_two(float x)
+{
+    return (__builtin_bit_cast(uint32_t, x) & 0x7fffffu) == 0;
+}
+
+// One workgroup for each (sequence, block that takes new slots, kv head).  A
+// thread holds eight dims of every (32 / ND)-th slot: read once, for the largest magnitude,
+// then written as codes; values pass through shared memory into their order, and
+// the groups of slots that take any are read and written whole.
+template <int FMT, int ND> __global__ __launch_bounds__(kThreads) void k_append(AppendArgs a)
+{
+    constexpr int DP = 64 * ND, CH = DP / 8, ROWS = kThreads / CH, PASS = kBlock / ROWS;
     __shared__ float red[2 * kThreads / 64];
-    const int t = threadIdx.x, nt = blockDim.x;
+    __shared__ uint4 vl4[4 * DP];
+    const int t = threadIdx.x;
     const uint32_t bt = blockIdx.x / (uint32_t)a.c.H, h = blockIdx.x % (uint32_t)a.c.H;
     const int tb = (int)(bt % (uint32_t)a.touched), s = (int)(bt / (uint32_t)a.touched);
     int row0;
@@ -174,67 +225,92 @@ template <int FMT> __global__ __launch_bounds__(kThreads) void k_append(AppendAr
 
     const int D = a.c.D;
     const int o0 = lo - j * kBlock, o1 = hi - j * kBlock;   // slots [o0, o1) are new
-    const int64_t kbase = (int64_t)h * a.k_head, vbase = (int64_t)h * a.v_head;
     const int64_t r0 = (int64_t)row0 + (lo - start);        // row of slot o0
-    float ak = 0.f, av = 0.f;
-    for (int e = t; e < (o1 - o0) * D; e += nt) {
-        const int64_t r = r0 + e / D;
-        const int d = e % D;
-        ak = fmaxf(ak, finite_abs(row_value(a.k, kbase + r * a.k_row + d, a.k_type)));
-        av = fmaxf(av, finite_abs(row_value(a.v, vbase + r * a.v_row + d, a.v_type)));
-    }
-    max2(ak, av, red);
     const int64_t bh = (int64_t)id * a.c.H + h;
     const bool fresh = o0 == 0;
     const float oldk = fresh ? 0.f : a.c.ks[bh], oldv = fresh ? 0.f : a.c.vs[bh];
+    const int d = 8 * (t % CH), slot0 = t / CH;
+    const bool in_d = d < D;
+    uint4 kx[PASS], vx[PASS];
+#pragma unroll
+    for (int p = 0; p < PASS; ++p) {
+        // (a slot or dim that is not new is read as one that is: neither counts nor is
+        // written)
+        const int64_t r = r0 + min(max(slot0 + p * ROWS, o0), o1 - 1) - o0;
+        const int dd = min(d, D - 8);
+        kx[p] = row_bits8(a.k, (int64_t)h * a.k_head + r * a.k_row + dd, a.k_wide);
+        vx[p] = row_bits8(a.v, (int64_t)h * a.v_head + r * a.v_row + dd, a.v_wide);
+    }
+    uint32_t tk = 0, tv = 0;
+#pragma unroll
+    for (int p = 0; p < PASS; ++p) {
+        tk = max(tk, magnitude8(kx[p], a.k_type));
+        tv = max(tv, magnitude8(vx[p], a.v_type));
+    }
+    float ak = bits_value(tk, a.k_type), av = bits_value(tv, a.v_type);
+    max2(ak, av, red);                              // (its barrier: all have the old scales)
     const float newk = fmaxf(oldk, scale_for<FMT>(ak)), newv = fmaxf(oldv, scale_for<FMT>(av));
-    __syncthreads();                                // every thread has read the old scales
     if (t == 0) {
         a.c.ks[bh] = newk;
         a.c.vs[bh] = newv;
     }
-
-    // keys: four dims of a slot at a time
-    uint8_t *kc = a.c.kc + bh * kBlock * D;
-    const bool growk = !fresh && newk > oldk;
-    const float ratiok = oldk / newk;
-    const int s0 = growk ? 0 : o0, s1 = growk ? kBlock : o1;
-    for (int e = t; e < (s1 - s0) * (D / 4); e += nt) {
-        const int o = s0 + e / (D / 4), d = 4 * (e % (D / 4));
-        uint32_t w = 0;
+    const bool growk = !fresh && newk > oldk, growv = !fresh && newv > oldv;
+    const bool exk = power_of_two(newk), exv = power_of_two(newv);
+    uint8_t *kc = a.c.kc + bh * kBlock * D, *vc = a.c.vc + bh * kBlock * D;
+    uint8_t *vl = (uint8_t *)vl4;
+    // (a decode step's one token: as bytes, without reading the group they stand in)
+    const bool few = o1 - o0 == 1 && !growv;
+#pragma unroll
+    for (int p = 0; p < PASS; ++p) {
+        const int o = slot0 + p * ROWS;
+        if (!in_d) continue;
+        uint2 *to = (uint2 *)(kc + o * D + d);
         if (o >= o0 && o < o1) {
-            for (int b = 0; b < 4; ++b)
-                w |= code_of<FMT>(row_value(a.k, kbase + (r0 + o - o0) * a.k_row + d + b,
-                                            a.k_type) / newk) << (8 * b);
-        } else {
-            w = requant4<FMT>(*(const uint32_t *)(kc + o * D + d), ratiok);
+            *to = codes8<FMT>(kx[p], a.k_type, newk, exk);
+            const uint2 c = codes8<FMT>(vx[p], a.v_type, newv, exv);
+            uint8_t *at = few ? vc + (value_group(o) * D + d) * 16 + value_place(o)
+                              : vl + (value_group(o) * DP + d) * 16 + value_place(o);
+            for (int e = 0; e < 8; ++e) at[16 * e] = (uint8_t)((e < 4 ? c.x : c.y) >> (8 * (e & 3)));
+        } else if (growk) {
+            const uint2 w = *to;
+            *to = uint2{requant4<FMT>(w.x, oldk / newk), requant4<FMT>(w.y, oldk / newk)};
         }
-        *(uint32_t *)(kc + o * D + d) = w;
     }
-    // values: four places of a dim at a time
-    uint8_t *vc = a.c.vc + bh * kBlock * D;
-    const bool growv = !fresh && newv > oldv;
-    const float ratiov = oldv / newv;
-    for (int e = t; e < 16 * D; e += nt) {
-        const int p = 4 * (e & 3), d = (e >> 2) % D, g = (e >> 2) / D;
-        const int o = value_slot(g, p);             // slots o .. o + 3
-        if (!growv && (o + 4 <= o0 || o >= o1)) continue;
-        uint8_t *at4 = vc + (g * D + d) * 16 + p;
-        uint32_t w = 0;
-        bool all = true;
-        for (int b = 0; b < 4; ++b) all = all && o + b >= o0 && o + b < o1;
-        if (!all) {
-            w = *(const uint32_t *)at4;
-            if (growv) w = requant4<FMT>(w, ratiov);
-        }
-        for (int b = 0; b < 4; ++b)
-            if (o + b >= o0 && o + b < o1) {
-                const float x = row_value(a.v, vbase + (r0 + o + b - o0) * a.v_row + d, a.v_type);
-                w = (w & ~(0xffu << (8 * b))) | code_of<FMT>(x / newv) << (8 * b);
+    if (!few) __syncthreads();
+    // four dims' 16 bytes at a time: which of a group's places are new
+#pragma unroll
+    for (int e0 = 0; e0 < 4 * DP; e0 += kThreads) {
+        if (few) break;
+        const int e = e0 + t, g = e / DP, dim = e % DP;   // (g is uniform over a wave)
+        if (dim >= D) continue;
+        uint32_t take[4];
+        bool any = false, all = true;
+        for (int q = 0; q < 4; ++q) {
+            take[q] = 0;
+            for (int i = 0; i < 4; ++i) {
+                const int o = 16 * q + 4 * g + i;
+                const bool in = o >= o0 && o < o1;
+                any = any || in;
+                all = all && in;
+                take[q] |= in ? 0xffu << (8 * i) : 0u;
             }
-        *(uint32_t *)at4 = w;
+        }
+        if (!any && !growv) continue;
+        uint4 *to = (uint4 *)(vc + (g * D + dim) * 16);
+        uint4 w = vl4[e];
+        if (!all) {
+            const uint4 was = *to;
+            uint32_t x[4] = {was.x, was.y, was.z, was.w};
+            const uint32_t y[4] = {w.x, w.y, w.z, w.w};
+            for (int q = 0; q < 4; ++q) {
+                if (growv) x[q] = requant4<FMT>(x[q], oldv / newv);
+                x[q] = (x[q] & ~take[q]) | (y[q] & take[q]);
+            }
+            w = uint4{x[0], x[1], x[2], x[3]};
+        }
+        *to = w;
     }
-    for (int o = o0 + t; o < o1; o += nt) {
+    for (int o = o0 + t; o < o1; o += kThreads) {
         if (a.c.pos)
             a.c.pos[bh * kBlock + o] =
                 a.first ? a.first[s] + (j * kBlock + o - start) : j * kBlock + o;
@@ -713,7 +789,12 @@ int qlm_kv_append(const qlm_kv_cache *cache, const qlm_kv_batch *batch, const ql
     a.touched = (int32_t)(most < have ? most : have);
     const int64_t grid = (int64_t)batch->n_seqs * a.touched * a.c.H;
     if (grid > INT32_MAX) return fail(QLM_ERR_CAPACITY, "too many blocks in one append");
-    auto kern = cache->format == QLM_KV_E4M3 ? k_append<QLM_KV_E4M3> : k_append<QLM_KV_INT8>;
+    a.k_wide = (uintptr_t)a.k % 16 == 0 && a.k_row % 8 == 0 && a.k_head % 8 == 0;
+    a.v_wide = (uintptr_t)a.v % 16 == 0 && a.v_row % 8 == 0 && a.v_head % 8 == 0;
+    const bool e4m3 = cache->format == QLM_KV_E4M3;
+    auto kern = a.c.D <= 64    ? e4m3 ? k_append<QLM_KV_E4M3, 1> : k_append<QLM_KV_INT8, 1>
+                : a.c.D <= 128 ? e4m3 ? k_append<QLM_KV_E4M3, 2> : k_append<QLM_KV_INT8, 2>
+                               : e4m3 ? k_append<QLM_KV_E4M3, 4> : k_append<QLM_KV_INT8, 4>;
     kern<<<(unsigned)grid, kThreads, 0, stream>>>(a);
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? QLM_OK : hip_fail(e, "k_append launch");
