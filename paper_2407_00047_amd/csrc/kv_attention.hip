@@ -88,51 +88,67 @@ __device__ inline uint32_t nan_bytes(uint32_t w)
     return (z >> 7) * 0xffu;
 }
 
-// One query row's dims as matrix operands: for chunk c and half m the dims
-// c * 64 + g * 16 + m * 8 .. + 8.  A row of bfloat16 is scaled by a power of
-// two so that it fits halves; *unscale takes that out of the score.
+// One query row's dims as they came: of chunk c the dims c * 64 + g * 16 .. + 16.
+template <int ND> struct Query {
+    uint4 u[ND][2];
+};
+
 template <int ND>
 __device__ inline void load_query(const AttnArgs &a, int64_t row, int head, bool valid, int g,
-                                  half8v (&qf)[ND][2], float *unscale)
+                                  Query<ND> &q)
 {
-    *unscale = 1.f;
     const uint16_t *p = (const uint16_t *)a.qd + row * a.q_row + head * a.q_head;
-    uint16_t u[ND][16];
-    for (int c = 0; c < ND; ++c) {
-        const int d = c * 64 + g * 16;
-        if (!valid || d >= a.D) {
-            for (int e = 0; e < 16; ++e) u[c][e] = 0;
-        } else if (a.wide) {
-            *(uint4 *)&u[c][0] = *(const uint4 *)(p + d);
-            *(uint4 *)&u[c][8] = *(const uint4 *)(p + d + 8);
-        } else {
-            for (int e = 0; e < 16; ++e) u[c][e] = p[d + e];
+    for (int c = 0; c < ND; ++c)
+        for (int m = 0; m < 2; ++m) {
+            const int d = c * 64 + g * 16 + m * 8;
+            uint4 x = {0, 0, 0, 0};
+            if (valid && d < a.D) {
+                if (a.wide) {
+                    x = *(const uint4 *)(p + d);
+                } else {
+                    const uint16_t *e = p + d;
+                    x = uint4{e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16,
+                              e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16};
+                }
+            }
+            q.u[c][m] = x;
         }
-    }
+}
+
+// The row as matrix operands: half m of chunk c holds the dims c * 64 + g * 16 +
+// m * 8 .. + 8.  A row of bfloat16 is scaled by a power of two so that it fits
+// halves; the result takes that out of the score.
+template <int ND>
+__device__ inline float query_halves(const AttnArgs &a, const Query<ND> &q, half8v (&qf)[ND][2])
+{
     if (a.dtype == QLM_F16) {
         for (int c = 0; c < ND; ++c)
-            for (int m = 0; m < 2; ++m)
-                for (int e = 0; e < 8; ++e)
-                    qf[c][m][e] = __builtin_bit_cast(_Float16, u[c][m * 8 + e]);
-        return;
+            for (int m = 0; m < 2; ++m) qf[c][m] = __builtin_bit_cast(half8v, q.u[c][m]);
+        return 1.f;
     }
     uint32_t top = 0;                     // greatest exponent of a finite element
     for (int c = 0; c < ND; ++c)
-        for (int e = 0; e < 16; ++e) {
-            const uint32_t x = (u[c][e] >> 7) & 0xff;
-            top = x < 255 ? max(top, x) : top;
+        for (int m = 0; m < 2; ++m) {
+            const uint32_t w[4] = {q.u[c][m].x, q.u[c][m].y, q.u[c][m].z, q.u[c][m].w};
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t x = (w[e >> 1] >> (16 * (e & 1) + 7)) & 0xff;
+                top = x < 255 ? max(top, x) : top;
+            }
         }
     top = max(top, (uint32_t)__shfl_xor((int)top, 16));
     top = max(top, (uint32_t)__shfl_xor((int)top, 32));
     // |q| < 2^(top - 126): to below 2^15
     const int up = min(15 - ((int)top - 126), 126);
     const float by = ldexpf(1.f, up);
-    *unscale = ldexpf(1.f, -up);
     for (int c = 0; c < ND; ++c)
-        for (int m = 0; m < 2; ++m)
+        for (int m = 0; m < 2; ++m) {
+            const uint32_t w[4] = {q.u[c][m].x, q.u[c][m].y, q.u[c][m].z, q.u[c][m].w};
             for (int e = 0; e < 8; ++e)
                 qf[c][m][e] = (_Float16)(
-                    __builtin_bit_cast(float, (uint32_t)u[c][m * 8 + e] << 16) * by);
+                    __builtin_bit_cast(float, e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16) *
+                    by);
+        }
+    return ldexpf(1.f, -up);
 }
 
 // -- few query rows ---------------------------------------------------------
@@ -245,23 +261,41 @@ __global__ __launch_bounds__(kThreads, ND * NT <= 2 ? 2 : 1) void k_attend_rows(
     __shared__ int pre[kThreads], wave_sum[kWaves];
     const int lane = threadIdx.x & 63;
     const int g = lane >> 4, c16 = lane & 15;
-    const int all = __builtin_amdgcn_readfirstlane(unit_prefix(a, pre, wave_sum));
-    const int each = units_each(a, all);
     const int worker = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + (threadIdx.x >> 6));
-    if ((int64_t)worker * each >= all) return;
-    const int u0 = worker * each, u1 = min(all, u0 + each);
-
-    // the chunk of sequences that holds unit u0, then the sequence, then the item
-    int chunk = 0;
-    for (int k = 0; k < kWaves; ++k) chunk += __popcll(__ballot(pre[k * 64 + lane] <= u0));
-    chunk = __builtin_amdgcn_readfirstlane(chunk) - 1;
     Cursor cur;
-    cur.enter(a, chunk * ((a.q.n_seqs + kThreads - 1) / kThreads));
-    int left = u0 - __builtin_amdgcn_readfirstlane(pre[chunk]);
-    while (left >= cur.nb * cur.tiles * a.H) {
-        left -= cur.nb * cur.tiles * a.H;
-        cur.enter(a, cur.s + 1);
+    int all, each, u0, left;
+    if (a.q.n_seqs <= 64) {                      // a lane to a sequence: no barrier, one read
+        const Units un = lane < a.q.n_seqs ? units_of(a, lane) : Units{0, 0};
+        int run = un.nb * un.tiles * a.H;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(run, o);
+            run += lane >= o ? v : 0;
+        }
+        all = __builtin_amdgcn_readlane(run, 63);
+        each = units_each(a, all);
+        if ((int64_t)worker * each >= all) return;
+        u0 = worker * each;
+        cur.s = __popcll(__ballot(run <= u0));
+        cur.nb = __builtin_amdgcn_readlane(un.nb, cur.s);
+        cur.tiles = __builtin_amdgcn_readlane(un.tiles, cur.s);
+        left = u0 - (cur.s ? __builtin_amdgcn_readlane(run, cur.s - 1) : 0);
+    } else {
+        all = __builtin_amdgcn_readfirstlane(unit_prefix(a, pre, wave_sum));
+        each = units_each(a, all);
+        if ((int64_t)worker * each >= all) return;
+        u0 = worker * each;
+        // the chunk of sequences that holds unit u0, then the sequence
+        int chunk = 0;
+        for (int k = 0; k < kWaves; ++k) chunk += __popcll(__ballot(pre[k * 64 + lane] <= u0));
+        chunk = __builtin_amdgcn_readfirstlane(chunk) - 1;
+        cur.enter(a, chunk * ((a.q.n_seqs + kThreads - 1) / kThreads));
+        left = u0 - __builtin_amdgcn_readfirstlane(pre[chunk]);
+        while (left >= cur.nb * cur.tiles * a.H) {
+            left -= cur.nb * cur.tiles * a.H;
+            cur.enter(a, cur.s + 1);
+        }
     }
+    const int u1 = min(all, u0 + each);
     cur.h = left / (cur.nb * cur.tiles);
     cur.tile = left / cur.nb % cur.tiles;
     cur.block = left % cur.nb;
@@ -283,6 +317,45 @@ __global__ __launch_bounds__(kThreads, ND * NT <= 2 ? 2 : 1) void k_attend_rows(
         for (int d = 0; d < DT; ++d) vv[d] = *(const uint4 *)(vp + voff[d]);
     };
     int id = cur.block_id(a);
+
+    half8v qf[NT][ND][2];
+    float fac[NT], m[NT], l[NT], vscale;
+    int lim[NT];
+    float4v acc[NT][DT];
+    int row0, cols, col0, before, hi_lim, lo_lim;
+    // a new item: its rows and limits, its queries on their way
+    auto rows_of = [&](Query<ND> (&raw)[NT]) {
+        int n = 1;
+        row0 = cur.s;
+        if (a.q.row_start) {
+            row0 = max(0, min(uniform(a.q.row_start + cur.s), a.q.n_rows));
+            n = min(max(row0, min(uniform(a.q.row_start + cur.s + 1), a.q.n_rows)) - row0,
+                    a.q.max_new);
+        }
+        before = max(0, min(uniform(a.q.lengths + cur.s), a.q.max_length)) - n;
+        cols = n * a.G;
+        col0 = cur.tile * NT * 16;
+        hi_lim = before + min(cols - 1, col0 + NT * 16 - 1) / a.G + 1;
+        lo_lim = before + col0 / a.G + 1;
+        for (int k = 0; k < NT; ++k) {
+            const int c = col0 + k * 16 + c16;
+            const bool valid = c < cols;
+            load_query<ND>(a, row0 + (valid ? c / a.G : 0),
+                           cur.h * a.G + (valid ? c % a.G : 0), valid, g, raw[k]);
+            lim[k] = valid ? before + c / a.G + 1 : 0;
+        }
+    };
+    auto begin = [&](const Query<ND> (&raw)[NT]) {
+        vscale = 1e-38f;                         // the values' common scale so far
+        for (int k = 0; k < NT; ++k) {
+            fac[k] = query_halves<ND>(a, raw[k], qf[k]) * a.scale;
+            m[k] = -__builtin_inff();
+            l[k] = 0.f;
+            for (int d = 0; d < DT; ++d) acc[k][d] = float4v{0.f, 0.f, 0.f, 0.f};
+        }
+    };
+    Query<ND> raw[NT];
+    rows_of(raw);
     int64_t bh = cur.row(a, id);
     load_keys(bh);
     load_values(bh);
@@ -290,49 +363,16 @@ __global__ __launch_bounds__(kThreads, ND * NT <= 2 ? 2 : 1) void k_attend_rows(
     Cursor nxt = cur;
     nxt.next(a);
     int id1 = nxt.block_id(a);
-
-    half8v qf[NT][ND][2];
-    float fac[NT], m[NT], l[NT], vscale = 0.f;
-    int lim[NT];
-    float4v acc[NT][DT];
+    begin(raw);
     int seg0 = u0;                               // first unit of the item at hand
-    int row0 = 0, cols = 0, col0 = 0, before = 0, hi_lim = 0, lo_lim = 0;
-    for (int k = 0; k < NT; ++k) {
-        fac[k] = m[k] = l[k] = 0.f;
-        lim[k] = 0;
-        for (int d = 0; d < DT; ++d) acc[k][d] = float4v{0.f, 0.f, 0.f, 0.f};
-        for (int c = 0; c < ND; ++c)
-            for (int x = 0; x < 2; ++x) qf[k][c][x] = half8v{0, 0, 0, 0, 0, 0, 0, 0};
-    }
 
     for (int u = u0; u < u1; ++u) {
         const int s = cur.s, h = cur.h, j = cur.block;
-        if (u == u0 || j == 0) {                 // a new item
+        if (j == 0 && u != u0) {
             seg0 = u;
-            int n = 1;
-            row0 = s;
-            if (a.q.row_start) {
-                row0 = max(0, min(uniform(a.q.row_start + s), a.q.n_rows));
-                n = min(max(row0, min(uniform(a.q.row_start + s + 1), a.q.n_rows)) - row0,
-                        a.q.max_new);
-            }
-            before = max(0, min(uniform(a.q.lengths + s), a.q.max_length)) - n;
-            cols = n * a.G;
-            col0 = cur.tile * NT * 16;
-            hi_lim = before + min(cols - 1, col0 + NT * 16 - 1) / a.G + 1;
-            lo_lim = before + col0 / a.G + 1;
-            vscale = 1e-38f;                     // the values' common scale so far
-            for (int k = 0; k < NT; ++k) {
-                const int c = col0 + k * 16 + c16;
-                const bool valid = c < cols;
-                load_query<ND>(a, row0 + (valid ? c / a.G : 0), h * a.G + (valid ? c % a.G : 0),
-                               valid, g, qf[k], &fac[k]);
-                fac[k] *= a.scale;
-                lim[k] = valid ? before + c / a.G + 1 : 0;
-                m[k] = -__builtin_inff();
-                l[k] = 0.f;
-                for (int d = 0; d < DT; ++d) acc[k][d] = float4v{0.f, 0.f, 0.f, 0.f};
-            }
+            Query<ND> raw[NT];
+            rows_of(raw);
+            begin(raw);
         }
         const bool mapped = (unsigned)id < (unsigned)a.n_blocks, more = u + 1 < u1;
         const int64_t bh1 = nxt.row(a, id1);
@@ -1055,7 +1095,7 @@ Plan plan_of(const qlm_kv_cache *c, const qlm_kv_batch *b, int32_t n_heads, bool
     p.cols = (int)std::min<int64_t>(cols, INT32_MAX);
     p.many = cols > kFew;
     p.few = !p.many || b->n_rows != (int64_t)b->n_seqs * b->max_new;
-    p.nt = cols <= 16 ? 1 : 2;
+    p.nt = cols <= 16 || c->head_dim > 128 ? 1 : 2;      // (two would not fit the registers)
     p.tile = 16 * p.nt;
     p.blocks = std::max(1, (b->max_length + kBlock - 1) / kBlock);
     // as many waves as the registers of 256 CUs hold at once
@@ -1104,7 +1144,7 @@ template <int FMT> void launch_rows(const AttnArgs &a, int nt, int64_t grid, hip
     else if (a.D <= 128)
         nt == 1 ? launch_rows<FMT, 2, 1>(a, grid, st) : launch_rows<FMT, 2, 2>(a, grid, st);
     else
-        nt == 1 ? launch_rows<FMT, 4, 1>(a, grid, st) : launch_rows<FMT, 4, 2>(a, grid, st);
+        launch_rows<FMT, 4, 1>(a, grid, st);
 }
 
 template <int FMT, int ND> void launch_prompt(const AttnArgs &a, hipStream_t st)
