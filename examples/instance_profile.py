@@ -1,0 +1,211 @@
+#!/usr/bin/env python3
+"""A hardware profile measured on this GPU, and the plan it leads to.
+
+The scheduler's estimator needs, for every class of instances and every model,
+the seconds of a prompt (P), the seconds of a decode step (d) and the tokens that
+the memory holds (GPU) -- Sec. 6, "Offline profiling".  Here an instance of this
+GPU is run instead of described: a stack of decoder layers with random 4-bit
+weights (qlm.w4_matmul) over an 8-bit token cache (qlm.kv_append,
+qlm.kv_attention) whose sequences give up their least attended tokens when they
+pass a budget (qlm.kv_evict).  The measured numbers go through qlm.apply_profile
+into the tables of a scheduling problem, and qlm.best_plan picks a plan.
+
+    python examples/instance_profile.py [--layers 32] [--batch 32] ...
+"""
+from __future__ import annotations
+
+import argparse
+import os
+import sys
+import time
+
+import numpy as np
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+from paper_2407_00047_amd import qlm, workload  # noqa: E402
+
+BLOCK = qlm.KV_BLOCK
+
+
+class Model:
+    """Sizes of a decoder layer and its 4-bit weights (one layer's, used by every
+    layer: the time of a step does not depend on their values)."""
+
+    def __init__(self, hidden, heads, kv_heads, dim, inner, group=128, seed=0):
+        self.hidden, self.heads, self.kv_heads, self.dim = hidden, heads, kv_heads, dim
+        self.inner = inner
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+
+        def matrix(n_out, n_in):
+            codes = torch.randint(0, 16, (n_out, n_in), generator=gen, device="cuda",
+                                  dtype=torch.uint8)
+            groups = -(-n_in // group)
+            scale = torch.full((n_out, groups), 0.2 * n_in ** -0.5, device="cuda").half()
+            zero = torch.randint(7, 9, (n_out, groups), generator=gen, device="cuda",
+                                 dtype=torch.uint8)
+            return qlm.w4_pack(codes, scale, zero, group)
+
+        self.qkv = matrix((heads + 2 * kv_heads) * dim, hidden)
+        self.out = matrix(hidden, heads * dim)
+        self.up = matrix(inner, hidden)
+        self.down = matrix(hidden, inner)
+
+    def weight_bytes(self, layers):
+        return layers * sum(m.packed.numel() for m in (self.qkv, self.out, self.up, self.down))
+
+    def token_bytes(self, layers):
+        """Cache bytes of a token: codes of keys and values, its position and weight,
+        its part of the block scales."""
+        return layers * self.kv_heads * (2 * self.dim + 8 + 8 / BLOCK)
+
+
+class Instance:
+    """Sequences in decode on one model: their cache, a block table and lengths."""
+
+    def __init__(self, model, layers, batch, most):
+        self.model, self.layers, self.batch = model, layers, batch
+        self.width = -(-most // BLOCK)
+        n = batch * self.width
+        self.caches = [qlm.DeviceKvCache.empty(n, model.kv_heads, model.dim)
+                       for _ in range(layers)]
+        order = torch.randperm(n, device="cuda").int()
+        self.table = order.view(batch, self.width).contiguous()
+        self.lengths = torch.zeros(batch, dtype=torch.int32, device="cuda")
+        self.next = torch.zeros(batch, dtype=torch.int32, device="cuda")   # next position
+        self.ws = {}
+
+    def _workspace(self, name, need, make):
+        """One workspace for each use, grown when a larger one is needed: the
+        calls of a step share it in the order of the stream."""
+        if name not in self.ws or self.ws[name].numel() < need:
+            self.ws[name] = make()
+        return self.ws[name]
+
+    def _matmul(self, x, w):
+        ws = self._workspace("w4", qlm.w4_workspace_bytes(w, x.shape[0]),
+                             lambda: qlm.w4_workspace(w, x.shape[0]))
+        return qlm.w4_matmul(x, w, ws=ws)
+
+    def forward(self, x, new):
+        """x [batch * new, hidden] through the layers; `new` tokens a sequence."""
+        m = self.model
+        self.lengths += new
+        start = torch.arange(self.batch + 1, dtype=torch.int32, device="cuda") * new
+        batch = qlm.KvBatch(self.table, self.lengths, start, self.batch * new, new)
+        for cache in self.caches:
+            qkv = self._matmul(x, m.qkv).view(-1, m.heads + 2 * m.kv_heads, m.dim)
+            q = qkv[:, :m.heads]
+            k, v = qkv[:, m.heads:m.heads + m.kv_heads], qkv[:, m.heads + m.kv_heads:]
+            qlm.kv_append(cache, batch, k, v, self.next)
+            need = qlm.kv_attention_workspace_bytes(cache, batch, m.heads, True)
+            ws = self._workspace("attention", need,
+                                 lambda: qlm.kv_attention_workspace(cache, batch, m.heads, True))
+            att = qlm.kv_attention(cache, batch, q, weight_decay=1.0, ws=ws)
+            x = x + self._matmul(att.view(x.shape[0], -1), m.out)
+            x = x + self._matmul(torch.nn.functional.silu(self._matmul(x, m.up)), m.down)
+        self.next += new
+        return x
+
+    def evict(self, budget, recent):
+        batch = qlm.KvBatch(self.table, self.lengths)
+        need = qlm.kv_evict_workspace_bytes(self.caches[0], batch, budget)
+        ws = self._workspace("evict", need,
+                             lambda: qlm.kv_evict_workspace(self.caches[0], batch, budget))
+        out = torch.empty_like(self.lengths)
+        for cache in self.caches:
+            qlm.kv_evict(cache, batch, budget, recent, out=out, ws=ws)
+        self.lengths.copy_(out)
+
+
+def measure(model, layers, batch, prompt, budget, recent, steps, memory):
+    """The profile's numbers for this model on this GPU: prefill and decode
+    seconds, and the tokens that `memory` bytes hold beside the weights."""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    inst = Instance(model, layers, batch, max(prompt, budget) + 2 * BLOCK)
+    rnd = lambda n: torch.randn((n, model.hidden), generator=gen, device="cuda",  # noqa: E731
+                                dtype=torch.bfloat16)
+
+    def timed(f):
+        torch.cuda.synchronize()
+        t = time.perf_counter()
+        f()
+        torch.cuda.synchronize()
+        return time.perf_counter() - t
+
+    x = rnd(batch * prompt)
+    inst.forward(x, prompt)                        # first use: workspaces, memory
+    inst.lengths.zero_()
+    inst.next.zero_()
+    prefill = timed(lambda: inst.forward(x, prompt)) / batch
+
+    y = rnd(batch)
+
+    def decode():
+        for _ in range(steps):
+            inst.forward(y, 1)
+            if int(inst.next[0]) % BLOCK == 0:     # a block is full: cut to the budget
+                inst.evict(budget, recent)
+
+    inst.evict(budget, recent)
+    inst.forward(y, 1)
+    seconds = timed(decode) / steps
+    assert bool(torch.isfinite(inst.forward(y, 1)).all())
+    return {"prefill": prefill, "decode_time": seconds,
+            "kv_tokens": (memory - model.weight_bytes(layers)) / model.token_bytes(layers),
+            "lengths": inst.lengths}
+
+
+def main(argv=None):
+    ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
+    ap.add_argument("--layers", type=int, default=16)
+    ap.add_argument("--hidden", type=int, default=4096)
+    ap.add_argument("--heads", type=int, default=32)
+    ap.add_argument("--kv-heads", type=int, default=8)
+    ap.add_argument("--dim", type=int, default=128)
+    ap.add_argument("--inner", type=int, default=16384)
+    ap.add_argument("--batch", type=int, default=32)
+    ap.add_argument("--prompt", type=int, default=1000)
+    ap.add_argument("--budget", type=int, default=1024)
+    ap.add_argument("--recent", type=int, default=128)
+    ap.add_argument("--steps", type=int, default=64)
+    ap.add_argument("--memory-gb", type=float, default=288.0)
+    ap.add_argument("--plans", type=int, default=4096)
+    a = ap.parse_args(argv)
+
+    # two models that take turns on the instances of one class: the second of half
+    # the layers
+    model = Model(a.hidden, a.heads, a.kv_heads, a.dim, a.inner)
+    layers = [a.layers, max(1, a.layers // 2)]
+    got = [measure(model, n, a.batch, a.prompt, a.budget, a.recent, a.steps, a.memory_gb * 1e9)
+           for n in layers]
+    for n, g in zip(layers, got):
+        print("%2d layers: prefill %.2f ms a prompt of %d, decode step %.3f ms (batch %d), "
+              "%.3g tokens of cache" % (n, 1e3 * g["prefill"], a.prompt, 1e3 * g["decode_time"],
+                                        a.batch, g["kv_tokens"]), flush=True)
+
+    problem = workload.make_problem("mixed")
+    plans = workload.make_plans(problem, 0, a.plans)
+    dpr, dpl = qlm.DeviceProblem(problem), qlm.DevicePlans.from_host(plans)
+    one = lambda key: np.array([g[key] for g in got], np.float32)  # noqa: E731
+    classes = problem["n_classes"]
+    per_class = lambda v: np.tile(v, (classes, 1))  # noqa: E731
+    profile = {"prefill": one("prefill"), "decode_time": per_class(one("decode_time")),
+               # (the step measured holds a.batch sequences of a.budget tokens; one over the
+               # whole memory takes in proportion longer)
+               "ineff": per_class(one("kv_tokens") / (a.batch * a.budget)),
+               "max_tokens": np.full(2, 1000, np.float32),
+               "kv_tokens": per_class(one("kv_tokens")),
+               "mean_tokens": np.full(2, a.budget, np.float32)}
+    loaded = np.arange(problem["n_instances"]) % problem["n_models"]
+    measured, _ = qlm.apply_profile(dpr, profile, inst_model=loaded)
+    index, score = qlm.best_plan(measured, dpl)
+    print("throughput of an instance: %s tokens/s" %
+          ", ".join("%.0f" % t for t in measured.inst_tput.cpu().tolist()[:2]))
+    print("best of %d plans: %d, %.1f of %d requests expected to miss their SLO"
+          % (a.plans, int(index), float(score), dpr.total_requests), flush=True)
+    return {"profile": profile, "best": int(index), "score": float(score), "measured": got}
+
+
+if __name__ == "__main__":
+    main()

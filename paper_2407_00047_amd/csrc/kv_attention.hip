@@ -5,6 +5,10 @@
 #include <algorithm>
 #include <string>
 
+// A score is rounded before the maximum is taken off it, as the maximum was (a fused
+// multiply-add would leave the rounding error of a large score in the exponent).
+#pragma clang fp contract(off)
+
 namespace {
 
 using namespace qlm_kv;
@@ -13,10 +17,26 @@ using qlm_internal::hip_fail;
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr float kLog2e = 1.44269504088896340736f;
-// p is held as 2^(s - m + kRaise): s may pass the running maximum m by kSlack
-// before the sums are rescaled, so p < 2^14 fits a half, and a p down to
-// 2^-20 of the maximum is a normal one.
-constexpr float kRaise = 6.f, kSlack = 8.f;
+// p = 2^(s - m), in which s may pass the running maximum m by kSlack before the
+// sums are rescaled.  As a half it is held kRaised times as large: p < 2^14 then
+// fits, and a p down to 2^-20 of the maximum is a normal one.
+constexpr float kSlack = 8.f, kRaised = 64.f;
+
+// A column's running maximum m and its sum l of 2^(s - m), apart: their common
+// logarithm would lose the sum beside a large maximum.  Of a finished column
+// what gives p = 2^(s - top) sum; {0, 0} where nothing is seen.
+struct TopSum {
+    float top, sum;
+};
+__device__ inline TopSum finished(float m, float l)
+{
+    return l == 0.f ? TopSum{0.f, 0.f} : TopSum{m, 1.f / l};
+}
+// The weight of a part in a join whose greatest maximum is M.
+__device__ inline float part_weight(TopSum p, float M)
+{
+    return p.sum == 0.f ? 0.f : p.sum * __builtin_amdgcn_exp2f(p.top - M);
+}
 
 struct AttnArgs {
     const uint8_t *kc, *vc;
@@ -33,15 +53,17 @@ struct AttnArgs {
     int32_t tile;                        // columns of a tile (k_attend_rows)
     int32_t workers;                     // waves that share the units (k_attend_rows)
     int32_t cols, blocks;                // max_new * G, ceil(max_length / 64)
-    float *part_o, *part_lse;            // [2 worker + which][tile]([D])
-    float *lse;                          // [kv head][row][G], log2 units; +inf: nothing seen
+    float *part_o;                       // [2 worker + which][tile][D] outputs, normalised
+    TopSum *part_ts;                     // [2 worker + which][tile] their m and l
+    TopSum *done;                        // [kv head][row][G] finished columns
     float *s;                            // [seq][block][head][few][64] scores, or NULL
     float decay;
     // sequences of many rows
     uint16_t *qh;                        // [kv head][8 ND][row][G][8] queries as halves
     float *qfac;                         // [kv head][row][G] what takes their scaling out
     int32_t splits;                      // of the keys
-    float *split_o, *split_lse;          // [split][kv head][row][G]([D])
+    float *split_o;                      // [split][kv head][row][G][D], as part_o
+    TopSum *split_ts;                    // [split][kv head][row][G]
 };
 
 // Column of head e of a row among all rows of kv head h.
@@ -437,10 +459,10 @@ __global__ __launch_bounds__(kThreads, ND * NT <= 2 ? 2 : 1) void k_attend_rows(
                 for (int d = 0; d < DT; ++d) acc[k][d] *= al;
             vscale = vsc;
         }
-        const float vrel = vsc / vscale;
+        const float vrel = vsc / vscale * kRaised;
         half8v pb[NT][2];
         for (int k = 0; k < NT; ++k) {
-            const float base = m[k] == -__builtin_inff() ? 0.f : m[k] - kRaise;
+            const float base = m[k] == -__builtin_inff() ? 0.f : m[k];
             for (int t = 0; t < 4; ++t)
                 for (int i = 0; i < 4; ++i) {
                     const float p = __builtin_amdgcn_exp2f(sc[k][t][i] - base);
@@ -502,18 +524,16 @@ __global__ __launch_bounds__(kThreads, ND * NT <= 2 ? 2 : 1) void k_attend_rows(
             const int64_t part = 2 * (int64_t)worker + (seg0 == u0 ? 0 : 1);
             for (int k = 0; k < NT; ++k) {
                 const float sum = group_sum(l[k]);
-                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                const float inv = sum == 0.f ? 0.f : 1.f / (kRaised * sum);
                 const int c = col0 + k * 16 + c16;
                 if (c >= cols) continue;
                 const int64_t row = row0 + c / a.G;
                 const int head = h * a.G + c % a.G;
-                const float lse = m[k] - kRaise + __builtin_amdgcn_logf(sum);
                 if (g == 0) {
                     if (whole)
-                        a.lse[column(a, h, row, c % a.G)] = sum == 0.f ? __builtin_inff() : lse;
+                        a.done[column(a, h, row, c % a.G)] = finished(m[k], sum);
                     else
-                        a.part_lse[part * a.tile + k * 16 + c16] =
-                            sum == 0.f ? -__builtin_inff() : lse;
+                        a.part_ts[part * a.tile + k * 16 + c16] = {m[k], sum};
                 }
                 for (int d = 0; d < DT; ++d) {
                     if (d * 16 >= D) break;
@@ -584,19 +604,19 @@ template <int WPC> __global__ __launch_bounds__(kThreads) void k_attend_join(Att
         return (2 * (int64_t)w + (w == w0 && u0 % each ? 1 : 0)) * a.tile + c % a.tile;
     };
     if (mine) {
-        for (int w = w0 + lane; w <= w1; w += 64) M = fmaxf(M, a.part_lse[place(w)]);
+        for (int w = w0 + lane; w <= w1; w += 64) M = fmaxf(M, a.part_ts[place(w)].top);
         for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
         for (int b = w0 + wv % WPC; b <= w1; b += 4 * WPC) {
-            float f[4], x[4][4];
+            TopSum f[4];
+            float x[4][4];
             for (int k = 0; k < 4; ++k) {
                 const int64_t at = place(min(b + k * WPC, w1));
-                f[k] = a.part_lse[at];
+                f[k] = a.part_ts[at];
                 for (int e = 0; e < 4; ++e)
                     x[k][e] = a.part_o[at * a.D + min(e * 64 + lane, a.D - 1)];
             }
             for (int k = 0; k < 4; ++k) {
-                const float z = b + k * WPC > w1 || f[k] == -__builtin_inff()
-                                    ? 0.f : __builtin_amdgcn_exp2f(f[k] - M);
+                const float z = b + k * WPC > w1 ? 0.f : part_weight(f[k], M);
                 L += z;
                 for (int e = 0; e < 4; ++e) acc[e] += z == 0.f ? 0.f : z * x[k][e];
             }
@@ -622,8 +642,7 @@ template <int WPC> __global__ __launch_bounds__(kThreads) void k_attend_join(Att
             ((uint16_t *)a.od)[row * a.o_row + head * a.o_head + e * 64 + lane] =
                 row_bits(L == 0.f ? 0.f : acc[e] / L, a.dtype);
     if (lane == 0)
-        a.lse[column(a, h, row, c % a.G)] =
-            L == 0.f ? __builtin_inff() : M + __builtin_amdgcn_logf(L);
+        a.done[column(a, h, row, c % a.G)] = finished(M, L);
 }
 
 // Weights from the scores that k_attend_rows left: a wave to a (sequence,
@@ -644,13 +663,14 @@ __global__ __launch_bounds__(kThreads) void k_attend_weights(AttnArgs a)
     const int n = seq_rows(a.q, s, &row0);
     if (n * a.G > a.few) return;                 // (k_attend_colsum)
     const float *sc = a.s + w * min(a.cols, a.few) * kBlock + lane;
-    const float *lse = a.lse + column(a, h, row0, 0);
+    const TopSum *done = a.done + column(a, h, row0, 0);
     float sum = 0.f;
     const int before = len - n;
     for (int t = 0; t < n; ++t) {
         if (before + t < j * kBlock) continue;    // (the row's scores were not formed)
         for (int e = 0; e < a.G; ++e)
-            sum += __builtin_amdgcn_exp2f(sc[(t * a.G + e) * kBlock] - lse[t * a.G + e]);
+            sum += __builtin_amdgcn_exp2f(sc[(t * a.G + e) * kBlock] - done[t * a.G + e].top) *
+                   done[t * a.G + e].sum;
     }
     if (j * kBlock + lane >= len) return;
     float *at = a.weight + ((int64_t)id * a.H + h) * kBlock + lane;
@@ -870,21 +890,20 @@ __global__ __launch_bounds__(kThreads, ND <= 2 ? 2 : 1) void k_attend_prompt(Att
                 for (int d = 0; d < DT; ++d) acc[d] *= al;
                 vscale = vs1;
             }
-            // p times the block's part of the common scale; the sum takes it out again
-            const float vrel = fmaxf(vs1 / vscale, 1e-30f);
-            const float base = (m == -__builtin_inff() ? 0.f : m - kRaise) -
-                               __builtin_amdgcn_logf(vrel);
+            const float vrel = vs1 / vscale * kRaised;
+            const float base = m == -__builtin_inff() ? 0.f : m;
             half8v pb[4];
             float sums[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(sc[u][i], f, -base));
+                    const float x = sc[u][i] * f;
+                    const float p = __builtin_amdgcn_exp2f(x - base);
                     sums[i & 3] += p;
-                    pb[2 * u + (i >> 3)][i & 7] = (_Float16)p;
+                    pb[2 * u + (i >> 3)][i & 7] = (_Float16)(p * vrel);
                 }
-            l += ((sums[0] + sums[1]) + (sums[2] + sums[3])) * __builtin_amdgcn_rcpf(vrel);
+            l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
                 if (!FULL && d * 32 >= D) break;
@@ -913,15 +932,14 @@ __global__ __launch_bounds__(kThreads, ND <= 2 ? 2 : 1) void k_attend_prompt(Att
 
     float l0, l1;
     swap32(l, &l0, &l1);
-    const float sum = l0 + l1, inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float sum = l0 + l1, inv = sum == 0.f ? 0.f : 1.f / (kRaised * sum);
     if (!valid) return;
-    const float lse = m - kRaise + __builtin_amdgcn_logf(sum);
     const int64_t sr = (int64_t)sp * a.q.n_rows * a.H * a.G + rh;
     if (hi == 0) {
         if (a.splits > 1)
-            a.split_lse[sr] = sum == 0.f ? -__builtin_inff() : lse;
+            a.split_ts[sr] = {m, sum};
         else
-            a.lse[rh] = sum == 0.f ? __builtin_inff() : lse;
+            a.done[rh] = finished(m, sum);
     }
     uint16_t *out = (uint16_t *)a.od + (int64_t)(row0 + c / a.G) * a.o_row +
                     (h * a.G + c % a.G) * a.o_head;
@@ -957,10 +975,9 @@ __global__ __launch_bounds__(kThreads) void k_prompt_join(AttnArgs a)
     const int64_t rh = column(a, head / a.G, row0 + r, head % a.G);
     const int64_t step = (int64_t)a.q.n_rows * heads;
     float M = -__builtin_inff(), L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < a.splits; ++k) M = fmaxf(M, a.split_lse[rh + k * step]);
+    for (int k = 0; k < a.splits; ++k) M = fmaxf(M, a.split_ts[rh + k * step].top);
     for (int k = 0; k < a.splits; ++k) {
-        const float z = a.split_lse[rh + k * step];
-        const float f = z == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(z - M);
+        const float f = part_weight(a.split_ts[rh + k * step], M);
         L += f;
         for (int e = 0; e < 4; ++e) {
             const float x = a.split_o[(rh + k * step) * a.D + min(e * 64 + lane, a.D - 1)];
@@ -971,7 +988,7 @@ __global__ __launch_bounds__(kThreads) void k_prompt_join(AttnArgs a)
         if (e * 64 + lane < a.D)
             ((uint16_t *)a.od)[(row0 + r) * a.o_row + head * a.o_head + e * 64 + lane] =
                 row_bits(L == 0.f ? 0.f : acc[e] / L, a.dtype);
-    if (lane == 0) a.lse[rh] = L == 0.f ? __builtin_inff() : M + __builtin_amdgcn_logf(L);
+    if (lane == 0) a.done[rh] = finished(M, L);
 }
 
 // Weights of the sequences of many rows: a workgroup to a block of 64 slots of a
@@ -1017,13 +1034,14 @@ __global__ __launch_bounds__(kThreads, ND <= 2 ? 2 : 1) void k_attend_colsum(Att
     const int64_t all = (int64_t)a.q.n_rows * a.G, base = column(a, h, row0, 0);
     const half8v *qp = (const half8v *)a.qh + ((int64_t)h * (DP / 8 - 1) + hi) * all + base;
     half8v qn[KS];
-    float facn, lsen;
+    float facn;
+    TopSum tsn;
     auto fetch = [&](int ct) {                   // (past the last column it is read again)
         const int c = min(ct * 32 + c32, cols - 1);
 #pragma unroll
         for (int k = 0; k < KS; ++k) qn[k] = qp[2 * k * all + c];
         facn = a.qfac[base + c];
-        lsen = a.lse[base + c];
+        tsn = a.done[base + c];
     };
     const int first = max(0, j * kBlock - before) * a.G / 32;   // tile that sees the first slot
     const int tiles = (cols + 31) / 32;
@@ -1033,7 +1051,8 @@ __global__ __launch_bounds__(kThreads, ND <= 2 ? 2 : 1) void k_attend_colsum(Att
 #pragma unroll
         for (int k = 0; k < KS; ++k) qf[k] = qn[k];
         const int c = ct * 32 + c32;
-        const float fac = facn * ksc, lse = c < cols ? lsen : __builtin_inff();
+        const float fac = facn * ksc;
+        const TopSum ts = c < cols ? tsn : TopSum{0.f, 0.f};
         fetch(min(ct + kWaves, tiles - 1));
         const bool masked = (j + 1) * kBlock > before + ct * 32 / a.G + 1 || ct + 1 == tiles;
         const int lim = masked && c < cols ? before + c / a.G + 1 : 0;
@@ -1048,13 +1067,16 @@ __global__ __launch_bounds__(kThreads, ND <= 2 ? 2 : 1) void k_attend_colsum(Att
             if (masked)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(sc[i], fac, -lse));
+                    const float x = sc[i] * fac;
+                    const float p = __builtin_amdgcn_exp2f(x - ts.top) * ts.sum;
                     sum[u][i] += slot0 + u * 32 + (i & 3) + 8 * (i >> 2) < lim ? p : 0.f;
                 }
             else
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    sum[u][i] += __builtin_amdgcn_exp2f(fmaf(sc[i], fac, -lse));
+                for (int i = 0; i < 16; ++i) {
+                    const float x = sc[i] * fac;
+                    sum[u][i] = fmaf(__builtin_amdgcn_exp2f(x - ts.top), ts.sum, sum[u][i]);
+                }
         }
     }
 #pragma unroll
@@ -1085,7 +1107,7 @@ constexpr int kFew = 64;         // columns of a sequence that k_attend_rows tak
 struct Plan {
     int nt, tile, workers, cols, blocks, splits;
     bool few, many;              // which sequences there can be
-    size_t part_o, part_lse, lse, s, qh, qfac, split_o, split_lse, total;
+    size_t part_o, part_ts, done, s, qh, qfac, split_o, split_ts, total;
 };
 
 Plan plan_of(const qlm_kv_cache *c, const qlm_kv_batch *b, int32_t n_heads, bool weights)
@@ -1106,10 +1128,10 @@ Plan plan_of(const qlm_kv_cache *c, const qlm_kv_batch *b, int32_t n_heads, bool
         at += align256(bytes);
         return here;
     };
-    p.lse = take((size_t)b->n_rows * n_heads * 4);
+    p.done = take((size_t)b->n_rows * n_heads * sizeof(TopSum));
     if (p.few) {
         p.part_o = take((size_t)2 * p.workers * p.tile * c->head_dim * 4);
-        p.part_lse = take((size_t)2 * p.workers * p.tile * 4);
+        p.part_ts = take((size_t)2 * p.workers * p.tile * sizeof(TopSum));
         if (weights)
             p.s = take((size_t)b->n_seqs * p.blocks * c->n_kv_heads * std::min(p.cols, kFew) *
                        kBlock * 4);
@@ -1125,7 +1147,7 @@ Plan plan_of(const qlm_kv_cache *c, const qlm_kv_batch *b, int32_t n_heads, bool
         p.qfac = take(rh * 4);
         if (p.splits > 1) {
             p.split_o = take(rh * p.splits * c->head_dim * 4);
-            p.split_lse = take(rh * p.splits * 4);
+            p.split_ts = take(rh * p.splits * sizeof(TopSum));
         }
     }
     p.total = at;
@@ -1241,15 +1263,15 @@ int qlm_kv_attention(const qlm_kv_cache *cache, const qlm_kv_batch *batch,
     a.blocks = p.blocks;
     char *base = (char *)ws;
     a.part_o = (float *)(base + p.part_o);
-    a.part_lse = (float *)(base + p.part_lse);
-    a.lse = (float *)(base + p.lse);
+    a.part_ts = (TopSum *)(base + p.part_ts);
+    a.done = (TopSum *)(base + p.done);
     a.s = query->accumulate && p.few ? (float *)(base + p.s) : nullptr;
     a.few = kFew;
     a.qh = (uint16_t *)(base + p.qh);
     a.qfac = (float *)(base + p.qfac);
     a.splits = p.splits;
     a.split_o = (float *)(base + p.split_o);
-    a.split_lse = (float *)(base + p.split_lse);
+    a.split_ts = (TopSum *)(base + p.split_ts);
     a.decay = query->weight_decay;
 
     const bool e4m3 = cache->format == QLM_KV_E4M3;

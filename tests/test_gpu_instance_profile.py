@@ -1,0 +1,49 @@
+"""The instance operators used together: the example that measures a hardware
+profile, at a small size, and a layer's decode against its prompt."""
+import importlib.util
+import os
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def example():
+    spec = importlib.util.spec_from_file_location(
+        "instance_profile", os.path.join(ROOT, "examples", "instance_profile.py"))
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    return mod
+
+
+def test_example_runs(example):
+    got = example.main(["--layers", "2", "--hidden", "256", "--heads", "4", "--kv-heads", "2",
+                        "--dim", "64", "--inner", "512", "--batch", "3", "--prompt", "150",
+                        "--budget", "128", "--recent", "16", "--steps", "70", "--plans", "256"])
+    assert 0 <= got["best"] < 256 and got["score"] >= 0
+    for g in got["measured"]:
+        assert g["prefill"] > 0 and g["decode_time"] > 0 and g["kv_tokens"] > 0
+        # every block that filled up was followed by a cut to the budget
+        lengths = g["lengths"].cpu().numpy()
+        assert (lengths >= 128).all() and (lengths < 128 + 64 + 2).all()
+    assert np.isfinite(got["profile"]["decode_time"]).all()
+
+
+def test_prompt_and_steps_agree(example):
+    """The same tokens as one prompt and one after another: the outputs differ by the
+    rounding of codes under other block scales (powers of two: of e4m3 codes only
+    subnormals round anew) and of bfloat16, which the layer's few products pass on."""
+    import torch
+    model = example.Model(128, 4, 2, 32, 256)
+    x = torch.randn((40, 128), device="cuda", dtype=torch.bfloat16)
+    whole = example.Instance(model, 1, 1, 64).forward(x, 40)
+    step = example.Instance(model, 1, 1, 64)
+    rows = torch.cat([step.forward(x[i:i + 1], 1) for i in range(40)])
+    d = (whole.float() - rows.float()).abs()
+    # a bfloat16 rounding of each of five results in a row, and of the e4m3 codes'
+    # values (2^-4 of a subnormal step) far below it
+    assert float(d.max()) <= 6 * 2.0 ** -8 * float(whole.float().abs().max())

@@ -283,6 +283,26 @@ def test_attend_wide_ranges(torch, qlm):
             check(qlm.kv_attention(s.cache, s.batch(), q), want, bound, "bf16", (fmt, spread))
 
 
+@pytest.mark.parametrize("n", [1, 3, 40, 200])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_attend_large_scores(torch, qlm, fmt, n):
+    """Scores far from zero (to 1e12): outputs stay inside the values' range, and every
+    row's and head's weights still add up to one."""
+    s = Setup(torch, qlm, [1100], 1, 64, fmt, seed=n)
+    k, _ = s.rows(1100, 1, "bf16", 30.0)
+    v, _ = s.rows(1100, 1, "bf16")
+    qlm.kv_append(s.cache, s.batch([1100]), k, v)
+    top = float(ko.Cache.read(s.cache, fmt).sequence(s.table[0], 1100, 0)[1].max())
+    for spread in (1e2, 1e4, 1e6, 1e10):
+        q, _ = s.rows(n, 4, "bf16", spread)
+        for scale in (0.125, -0.125):
+            out = qlm.kv_attention(s.cache, s.batch([n]), q, scale=scale, weight_decay=0.0)
+            assert bool(out.isfinite().all()) and float(out.abs().max()) <= 1.01 * abs(top) + 5
+            total = float(s.cache.weight.nan_to_num(0.0).double().sum())
+            # (a sum of up to 1100 single-precision terms each)
+            assert abs(total - 4 * n) <= 4 * n * 1100 * 2.0 ** -22, (spread, scale, total)
+
+
 def test_unmapped_blocks(torch, qlm):
     """A block number outside the pool names no slots: the others are attended."""
     s = Setup(torch, qlm, [300, 64], 1, 64, "e4m3", seed=13)
