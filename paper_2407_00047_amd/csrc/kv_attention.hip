@@ -559,6 +559,11 @@ __global__ __launch_bounds__(kThreads, ND * NT <= 2 ? 2 : 1) void k_attend_rows(
     }
 }
 
+__device__ inline float lane_value(float x, int lane)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+}
+
 // Adds up the parts of the columns whose units several workers held, and gives
 // the columns that see nothing their zeros: WPC waves to a column, the parts in
 // turn.
@@ -569,9 +574,9 @@ template <int WPC> __global__ __launch_bounds__(kThreads) void k_attend_join(Att
     constexpr int CPG = kWaves / WPC;            // columns of a workgroup
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
     const int groups = (min(a.cols, a.few) + CPG - 1) / CPG;
-    const int64_t sh = blockIdx.x / groups;
-    const int c = (int)(blockIdx.x % groups) * CPG + wv / WPC;
-    const int s = (int)(sh / a.H), h = (int)(sh % a.H);
+    const uint32_t sh = blockIdx.x / (uint32_t)groups;
+    const int c = (int)(blockIdx.x % (uint32_t)groups) * CPG + wv / WPC;
+    const int s = (int)(sh / (uint32_t)a.H), h = (int)(sh % (uint32_t)a.H);
     // units of the sequences before, and of all
     int lo = 0, all = 0;
     for (int k = threadIdx.x; k < a.q.n_seqs; k += kThreads) {
@@ -650,28 +655,29 @@ template <int WPC> __global__ __launch_bounds__(kThreads) void k_attend_join(Att
 __global__ __launch_bounds__(kThreads) void k_attend_weights(AttnArgs a)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-    const int h = (int)(w % a.H);
-    const int64_t sb = w / a.H;
-    const int j = (int)(sb % a.blocks), s = (int)(sb / a.blocks);
+    // (fewer than 2^31 waves: checked on the host)
+    const uint32_t w = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + (threadIdx.x >> 6));
+    const int h = (int)(w % (uint32_t)a.H);
+    const uint32_t sb = w / (uint32_t)a.H;
+    const int j = (int)(sb % (uint32_t)a.blocks), s = (int)(sb / (uint32_t)a.blocks);
     if (s >= a.q.n_seqs) return;
     const int len = seq_length(a.q, s);
     if (j * kBlock >= len) return;
-    const int id = a.q.table[s * a.q.table_stride + j];
+    const int id = uniform(a.q.table + s * a.q.table_stride + j);
     if ((unsigned)id >= (unsigned)a.n_blocks) return;
     int row0;
     const int n = seq_rows(a.q, s, &row0);
-    if (n * a.G > a.few) return;                 // (k_attend_colsum)
-    const float *sc = a.s + w * min(a.cols, a.few) * kBlock + lane;
-    const TopSum *done = a.done + column(a, h, row0, 0);
+    const int cols = n * a.G;
+    if (cols > a.few) return;                    // (k_attend_colsum)
+    const float *sc = a.s + (int64_t)w * min(a.cols, a.few) * kBlock + lane;
+    const TopSum mine = lane < cols ? a.done[column(a, h, row0, lane)] : TopSum{0.f, 0.f};
+    // rows that see the block's first slot (of the others no scores were formed)
+    const int c0 = min(max(0, j * kBlock - (len - n)), n) * a.G;
     float sum = 0.f;
-    const int before = len - n;
-    for (int t = 0; t < n; ++t) {
-        if (before + t < j * kBlock) continue;    // (the row's scores were not formed)
-        for (int e = 0; e < a.G; ++e)
-            sum += __builtin_amdgcn_exp2f(sc[(t * a.G + e) * kBlock] - done[t * a.G + e].top) *
-                   done[t * a.G + e].sum;
-    }
+#pragma unroll 4
+    for (int c = c0; c < cols; ++c)
+        sum += __builtin_amdgcn_exp2f(sc[c * kBlock] - lane_value(mine.top, c)) *
+               lane_value(mine.sum, c);
     if (j * kBlock + lane >= len) return;
     float *at = a.weight + ((int64_t)id * a.H + h) * kBlock + lane;
     *at = a.decay == 0.f ? sum : a.decay * *at + sum;
