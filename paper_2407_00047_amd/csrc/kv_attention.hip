@@ -1282,6 +1282,8 @@ int qlm_kv_attention(const qlm_kv_cache *cache, const qlm_kv_batch *batch,
 
     const bool e4m3 = cache->format == QLM_KV_E4M3;
     const int64_t sh = (int64_t)batch->n_seqs * a.H;
+    if ((int64_t)batch->max_new * a.G > (1 << 30))
+        return fail(QLM_ERR_CAPACITY, "too many query rows and heads in one sequence");
     const int64_t few = std::min(p.cols, kFew);
     const int64_t units = sh * ((few + p.tile - 1) / p.tile) * p.blocks;
     if (units > INT32_MAX || sh * few > INT32_MAX ||

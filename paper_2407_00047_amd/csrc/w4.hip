@@ -35,6 +35,7 @@ typedef _Float16 half8v __attribute__((ext_vector_type(8)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
 typedef float float4v __attribute__((ext_vector_type(4)));
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 
 constexpr int kStep = 128;           // inputs of a chunk
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
@@ -171,7 +172,8 @@ template <bool BF, int GROUP> __global__ __launch_bounds__(kThreads) void k_w4_t
     constexpr int PER = kStep / GROUP, SUB = 4 / PER, PF = 4;
     extern __shared__ uint4 lds[];
     uint16_t *xs = (uint16_t *)lds;
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, c16 = lane & 15;
     const int tile = blockIdx.x;
     const int cb = chunk_bytes(GROUP);
@@ -184,8 +186,8 @@ template <bool BF, int GROUP> __global__ __launch_bounds__(kThreads) void k_w4_t
     auto fetch = [&](int u, int kb) {
         if (kb < a.steps) {
             const uint8_t *p = base + (int64_t)kb * cb;
-            cw[u] = *(const uint4 *)(p + 16 * lane);
-            for (int q = 0; q < PER; ++q) mw[u][q] = *(const uint4 *)(p + 1024 + 64 * q + 16 * g);
+            cw[u] = *(const uint4 *)(p + 16u * lane);
+            for (int q = 0; q < PER; ++q) mw[u][q] = *(const uint4 *)(p + 1024 + 64 * q + 16u * g);
         }
     };
     for (int u = 0; u < PF; ++u) fetch(u, wv + u * kWaves);
@@ -234,14 +236,14 @@ template <bool BF, int GROUP> __global__ __launch_bounds__(kThreads) void k_w4_t
     if (m < a.M && n < a.N) a.out[m * a.out_stride + n] = out_bits(v, BF);
 }
 
-// Rows of bfloat16 as halves: scaled by a power of two to below 2^15.  A
-// workgroup to a row.
+// Rows for k_w4_wide: halves, 16-byte aligned, zeros up to a whole number of stages.
+// Rows of bfloat16 are scaled by a power of two to below 2^15.  A workgroup to a row.
 __global__ __launch_bounds__(kThreads) void k_w4_half(MatArgs a, uint16_t *xh, float *fac, int ld)
 {
     __shared__ uint32_t part[kWaves];
     const uint16_t *p = a.x + blockIdx.x * a.x_stride;
     uint32_t top = 0;                       // greatest exponent of a finite element
-    for (int k = threadIdx.x; k < a.K; k += kThreads) {
+    for (int k = threadIdx.x; k < a.K && a.bf; k += kThreads) {
         const uint32_t e = (uint32_t)(p[k] >> 7) & 0xff;
         top = e < 255 ? max(top, e) : top;
     }
@@ -252,10 +254,12 @@ __global__ __launch_bounds__(kThreads) void k_w4_half(MatArgs a, uint16_t *xh, f
     const int up = min(15 - ((int)top - 126), 126);
     const float by = ldexpf(1.f, up);
     for (int k = threadIdx.x; k < ld; k += kThreads) {
-        const float x = k < a.K ? __builtin_bit_cast(float, (uint32_t)p[k] << 16) : 0.f;
-        xh[(int64_t)blockIdx.x * ld + k] = __builtin_bit_cast(uint16_t, (_Float16)(x * by));
+        const uint16_t u = k < a.K ? p[k] : 0;
+        const float x = __builtin_bit_cast(float, (uint32_t)u << 16);
+        xh[(int64_t)blockIdx.x * ld + k] =
+            a.bf ? __builtin_bit_cast(uint16_t, (_Float16)(x * by)) : u;
     }
-    if (threadIdx.x == 0) fac[blockIdx.x] = ldexpf(1.f, -up);
+    if (threadIdx.x == 0) fac[blockIdx.x] = a.bf ? ldexpf(1.f, -up) : 1.f;
 }
 
 __device__ inline uint16_t wide_out(const MatArgs &a, float v, int m)
@@ -270,7 +274,8 @@ template <int GROUP, int NT> __global__ __launch_bounds__(kThreads, 2) void k_w4
 {
     constexpr int PER = kStep / GROUP, SUB = 4 / PER, LD = 2 * kStep + 8;
     __shared__ uint4 lds[2][NT * 16 * LD / 8];
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, c16 = lane & 15;
     const int tile = blockIdx.x * kWaves + wv, m0 = blockIdx.y * NT * 16, sp = blockIdx.z;
     const int k0 = sp * a.per_split, k1 = min(a.steps, k0 + a.per_split);
@@ -281,36 +286,36 @@ template <int GROUP, int NT> __global__ __launch_bounds__(kThreads, 2) void k_w4
     float4v sum[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) sum[t] = float4v{0.f, 0.f, 0.f, 0.f};
-    uint4 cw[2], mw[2][PER], xr[2 * NT];
+    uint4 cw[2], mw[2][PER];
+    uint4v xr[2 * NT];
     uint16_t zw[2][PER];
     auto fetch_w = [&](int u, int kb) {          // (past the last step it is read again)
         const uint8_t *p = base + (int64_t)min(kb, k1 - 1) * cb;
-        cw[u] = *(const uint4 *)(p + 16 * lane);
+        cw[u] = *(const uint4 *)(p + 16u * lane);
 #pragma unroll
         for (int q = 0; q < PER; ++q) {
-            mw[u][q] = *(const uint4 *)(p + 1024 + 64 * q + 16 * g);
-            zw[u][q] = *(const uint16_t *)(p + 1024 + 64 * q + 4 * c16 + 2);
+            mw[u][q] = *(const uint4 *)(p + 1024 + 64 * q + 16u * g);
+            zw[u][q] = *(const uint16_t *)(p + 1024 + 64 * q + 2 + 4u * c16);
         }
     };
     // thread t stages row t / 16 of each 16 rows, inputs 8 (t % 16) on of each step;
     // rows past the last are the last again (their outputs are not written)
     const int sr = threadIdx.x >> 4, sk = 8 * (threadIdx.x & 15);
-    auto fetch_x = [&](int kb) {
-        const bool whole = a.wide && (kb + 2) * kStep <= a.K;
+    // (no branch: the waits for the weights would count loads that may not be there)
+    const uint16_t *xp[NT];
 #pragma unroll
-        for (int t = 0; t < 2 * NT; ++t) {
-            const int r = min(m0 + (t >> 1) * 16 + sr, a.M - 1), k = (kb + (t & 1)) * kStep + sk;
-            if (whole)
-                xr[t] = *(const uint4 *)(a.x + r * a.x_stride + k);
-            else
-                xr[t] = x8(a, r, k);
-        }
+    for (int t = 0; t < NT; ++t)
+        xp[t] = a.x + (int64_t)min(m0 + t * 16 + sr, a.M - 1) * a.x_stride + sk;
+    auto fetch_x = [&](int kb) {
+#pragma unroll
+        for (int t = 0; t < 2 * NT; ++t)
+            xr[t] = *(const uint4v *)(xp[t >> 1] + kb * kStep + (t & 1) * kStep);
     };
     auto stage = [&](int buf) {
         uint16_t *xs = (uint16_t *)lds[buf];
 #pragma unroll
         for (int t = 0; t < 2 * NT; ++t)
-            *(uint4 *)(xs + ((t >> 1) * 16 + sr) * LD + (t & 1) * kStep + sk) = xr[t];
+            *(uint4v *)(xs + ((t >> 1) * 16 + sr) * LD + (t & 1) * kStep + sk) = xr[t];
     };
     if (k0 < k1) {
         fetch_x(k0);
@@ -321,12 +326,12 @@ template <int GROUP, int NT> __global__ __launch_bounds__(kThreads, 2) void k_w4
     __syncthreads();
     for (int kb = k0; kb < k1; kb += 2) {
         const int buf = ((kb - k0) >> 1) & 1;
-        if (kb + 2 < k1) fetch_x(kb + 2);
+        fetch_x(kb + 2 < k1 ? kb + 2 : kb);
         const uint16_t *xs = (const uint16_t *)lds[buf];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            if (kb + u >= k1) break;
             const uint32_t w[4] = {cw[u].x, cw[u].y, cw[u].z, cw[u].w};
+            const uint32_t on = kb + u < k1 ? 0xffffu : 0u;   // (past the last step: scales of 0)
 #pragma unroll
             for (int q = 0; q < PER; ++q) {
                 const half2v z = __builtin_bit_cast(half2v, (uint32_t)zw[u][q] * 0x10001u);
@@ -347,7 +352,8 @@ template <int GROUP, int NT> __global__ __launch_bounds__(kThreads, 2) void k_w4
                         t[k] = mfma<false>(o, b, t[k]);
                     }
                 }
-                const uint32_t m[4] = {mw[u][q].x, mw[u][q].y, mw[u][q].z, mw[u][q].w};
+                const uint32_t m[4] = {mw[u][q].x & on, mw[u][q].y & on, mw[u][q].z & on,
+                                       mw[u][q].w & on};
 #pragma unroll
                 for (int k = 0; k < NT; ++k)
 #pragma unroll
@@ -357,7 +363,7 @@ template <int GROUP, int NT> __global__ __launch_bounds__(kThreads, 2) void k_w4
             }
             fetch_w(u, kb + u + 2);
         }
-        if (kb + 2 < k1) stage(buf ^ 1);
+        stage(buf ^ 1);
         __syncthreads();
     }
     if (!mine) return;
@@ -545,16 +551,16 @@ int qlm_w4_matmul(const qlm_w4 *weight, const void *x, int64_t x_stride, void *o
     split_of(weight, n_rows, &a.splits, &a.per_split);
     a.part = (float *)ws;
     hipError_t e;
-    if (a.bf && n_rows > kThinRows) {
+    // (halves that are aligned and fill whole stages are read where they are)
+    if (n_rows > kThinRows && (a.bf || !a.wide || a.K % (2 * kStep))) {
         const Layout l = layout_of(weight, n_rows);
         uint16_t *xh = (uint16_t *)((char *)ws + l.xh);
         float *fac = (float *)((char *)ws + l.fac);
         k_w4_half<<<n_rows, kThreads, 0, stream>>>(a, xh, fac, l.ld);
         if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_w4_half launch");
         a.x = xh;
-        a.x_stride = a.K = l.ld;
-        a.wide = 1;
-        a.fac = fac;
+        a.x_stride = l.ld;
+        a.fac = a.bf ? fac : nullptr;
     }
     if (weight->group == 32)
         launch<32>(a, stream);

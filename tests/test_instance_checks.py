@@ -116,6 +116,21 @@ def test_attention_checks(qlm, lib):
         assert call(**bad) == qlm.QLM_ERR_WORKSPACE, bad
 
 
+def test_attention_capacity(qlm, lib):
+    """Sizes whose index arithmetic would not fit are refused, whatever the workspace."""
+    c = cache(qlm)
+    q = qlm.KvQuery(rows(qlm), rows(qlm, data=A + 4096), 2 << 10, 0.1, 0, 0.0)
+    huge = batch(qlm, n_seqs=1, n_rows=1, max_new=1 << 21, row_start=A)
+    assert lib.qlm_kv_attention(P(c), P(huge), P(q), A, 1 << 62, None) == qlm.QLM_ERR_CAPACITY
+    many = batch(qlm, n_seqs=1 << 20, n_rows=1 << 20, max_length=1 << 20, table_stride=1 << 14)
+    assert lib.qlm_kv_attention(P(c), P(many), P(q), A, 1 << 62, None) == qlm.QLM_ERR_CAPACITY
+    assert lib.qlm_kv_evict(P(c), P(many), 64 << 14, 0, A, A, 1 << 62, None) == \
+        qlm.QLM_ERR_CAPACITY
+    assert lib.qlm_kv_append(P(c), P(batch(qlm, n_seqs=1 << 20, n_rows=1 << 20, max_new=1 << 20,
+                                           max_length=1 << 20, table_stride=1 << 14, row_start=A)),
+                             P(rows(qlm)), P(rows(qlm)), None, None) == qlm.QLM_ERR_CAPACITY
+
+
 def test_evict_checks(qlm, lib):
     c, b = cache(qlm), batch(qlm)
     need = lib.qlm_kv_evict_workspace_bytes(P(c), P(b), 64)
