@@ -64,6 +64,8 @@ struct AttnArgs {
     int32_t splits;                      // of the keys
     float *split_o;                      // [split][kv head][row][G][D], as part_o
     TopSum *split_ts;                    // [split][kv head][row][G]
+    int32_t shares;                      // of a block's columns (k_attend_colsum)
+    float *share;                        // [share][seq][block][kv head][64] weights
 };
 
 // Column of head e of a row among all rows of kv head h.
@@ -1050,16 +1052,17 @@ __global__ __launch_bounds__(kThreads, ND <= 2 ? 2 : 1) void k_attend_colsum(Att
         tsn = a.done[base + c];
     };
     const int first = max(0, j * kBlock - before) * a.G / 32;   // tile that sees the first slot
-    const int tiles = (cols + 31) / 32;
-    fetch(min(first + wv, tiles - 1));
-    for (int ct = first + wv; ct < tiles; ct += kWaves) {
+    const int tiles = (cols + 31) / 32, step = kWaves * a.shares;
+    const int from = first + wv + kWaves * (int)blockIdx.y;
+    fetch(min(from, tiles - 1));
+    for (int ct = from; ct < tiles; ct += step) {
         half8v qf[KS];
 #pragma unroll
         for (int k = 0; k < KS; ++k) qf[k] = qn[k];
         const int c = ct * 32 + c32;
         const float fac = facn * ksc;
         const TopSum ts = c < cols ? tsn : TopSum{0.f, 0.f};
-        fetch(min(ct + kWaves, tiles - 1));
+        fetch(min(ct + step, tiles - 1));
         const bool masked = (j + 1) * kBlock > before + ct * 32 / a.G + 1 || ct + 1 == tiles;
         const int lim = masked && c < cols ? before + c / a.G + 1 : 0;
 #pragma unroll
@@ -1097,11 +1100,37 @@ __global__ __launch_bounds__(kThreads, ND <= 2 ? 2 : 1) void k_attend_colsum(Att
         }
     __syncthreads();
     const int slot = threadIdx.x;
-    if (slot < kBlock && j * kBlock + slot < len) {
-        const float x = (part[0][slot] + part[1][slot]) + (part[2][slot] + part[3][slot]);
+    if (slot >= kBlock || j * kBlock + slot >= len) return;
+    const float x = (part[0][slot] + part[1][slot]) + (part[2][slot] + part[3][slot]);
+    if (a.shares > 1) {
+        const int64_t all = (int64_t)a.q.n_seqs * a.blocks * a.H;
+        a.share[((blockIdx.y * all) + ((int64_t)s * a.blocks + j) * a.H + h) * kBlock + slot] = x;
+    } else {
         float *w = a.weight + bh * kBlock + slot;
         *w = a.decay == 0.f ? x : a.decay * *w + x;
     }
+}
+
+// Adds up the shares of the columns: a wave to a (sequence, block, kv head), a
+// lane to a slot.
+__global__ __launch_bounds__(kThreads) void k_colsum_join(AttnArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const uint32_t w = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + (threadIdx.x >> 6));
+    const int h = (int)(w % (uint32_t)a.H);
+    const uint32_t sb = w / (uint32_t)a.H;
+    const int j = (int)(sb % (uint32_t)a.blocks), s = (int)(sb / (uint32_t)a.blocks);
+    if (s >= a.q.n_seqs) return;
+    int row0;
+    const int len = seq_length(a.q, s);
+    if (seq_rows(a.q, s, &row0) * a.G <= a.few || j * kBlock + lane >= len) return;
+    const int id = uniform(a.q.table + s * a.q.table_stride + j);
+    if ((unsigned)id >= (unsigned)a.n_blocks) return;
+    const int64_t all = (int64_t)a.q.n_seqs * a.blocks * a.H;
+    float x = 0.f;
+    for (int k = 0; k < a.shares; ++k) x += a.share[(k * all + w) * kBlock + lane];
+    float *at = a.weight + ((int64_t)id * a.H + h) * kBlock + lane;
+    *at = a.decay == 0.f ? x : a.decay * *at + x;
 }
 
 // -- host -------------------------------------------------------------------
@@ -1111,9 +1140,9 @@ size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 constexpr int kFew = 64;         // columns of a sequence that k_attend_rows takes
 
 struct Plan {
-    int nt, tile, workers, cols, blocks, splits;
+    int nt, tile, workers, cols, blocks, splits, shares;
     bool few, many;              // which sequences there can be
-    size_t part_o, part_ts, done, s, qh, qfac, split_o, split_ts, total;
+    size_t part_o, part_ts, done, s, qh, qfac, split_o, split_ts, share, total;
 };
 
 Plan plan_of(const qlm_kv_cache *c, const qlm_kv_batch *b, int32_t n_heads, bool weights)
@@ -1144,16 +1173,25 @@ Plan plan_of(const qlm_kv_cache *c, const qlm_kv_batch *b, int32_t n_heads, bool
     }
     p.splits = 1;
     if (p.many) {
-        // two workgroups to a CU; eight blocks to a split at least
+        // two workgroups to a CU; three blocks to a split at least (one prompt of 571
+        // tokens over 10 blocks: 11 us and 4 for the join, 25 in one)
         const int64_t wg = ((int64_t)b->n_rows * n_heads + 127) / 128;
         p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(wg, 1),
-                                                               p.blocks / 8));
+                                                               p.blocks / 3));
         const size_t rh = (size_t)b->n_rows * n_heads;
         p.qh = take(rh * ((c->head_dim + 63) / 64 == 3 ? 4 : (c->head_dim + 63) / 64) * 128);
         p.qfac = take(rh * 4);
         if (p.splits > 1) {
             p.split_o = take(rh * p.splits * c->head_dim * 4);
             p.split_ts = take(rh * p.splits * sizeof(TopSum));
+        }
+        if (weights) {
+            // a block's columns shared by up to 16 workgroups where the blocks are few,
+            // 256 columns each at least
+            const int64_t sbh = (int64_t)b->n_seqs * p.blocks * c->n_kv_heads;
+            p.shares = (int)std::min<int64_t>(
+                std::min<int64_t>(16, std::max<int64_t>(1, 4096 / sbh)), (cols + 255) / 256);
+            if (p.shares > 1) p.share = take((size_t)p.shares * sbh * kBlock * 4);
         }
     }
     p.total = at;
@@ -1196,7 +1234,7 @@ template <int ND> void launch_many(const AttnArgs &a, bool e4m3, hipStream_t st)
 
 template <int ND> void launch_colsum(const AttnArgs &a, bool e4m3, hipStream_t st)
 {
-    const unsigned grid = (unsigned)((int64_t)a.q.n_seqs * a.H * a.blocks);
+    const dim3 grid((unsigned)((int64_t)a.q.n_seqs * a.H * a.blocks), a.shares);
     if (e4m3)
         k_attend_colsum<QLM_KV_E4M3, ND><<<grid, kThreads, 0, st>>>(a);
     else
@@ -1278,6 +1316,8 @@ int qlm_kv_attention(const qlm_kv_cache *cache, const qlm_kv_batch *batch,
     a.splits = p.splits;
     a.split_o = (float *)(base + p.split_o);
     a.split_ts = (TopSum *)(base + p.split_ts);
+    a.shares = p.shares;
+    a.share = (float *)(base + p.share);
     a.decay = query->weight_decay;
 
     const bool e4m3 = cache->format == QLM_KV_E4M3;
@@ -1326,6 +1366,11 @@ int qlm_kv_attention(const qlm_kv_cache *cache, const qlm_kv_batch *batch,
             a.D <= 64 ? launch_colsum<1>(a, e4m3, stream)
                       : a.D <= 128 ? launch_colsum<2>(a, e4m3, stream)
                                    : launch_colsum<4>(a, e4m3, stream);
+        if (p.many && batch->n_rows > 0 && p.shares > 1) {
+            if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_attend_colsum launch");
+            k_colsum_join<<<(unsigned)((sh * p.blocks + kWaves - 1) / kWaves), kThreads, 0,
+                            stream>>>(a);
+        }
         if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "weight launch");
     }
     return QLM_OK;
