@@ -589,12 +589,15 @@ int qlm_kv_append(const qlm_kv_cache *cache, const qlm_kv_batch *batch, const ql
  * (the old weight is not read when weight_decay is 0).  Slots that a row does
  * not see have no part in its result, whatever they hold.  Scores, their
  * maxima and sums, weights and outputs are formed in single precision from
- * exact products; p is rounded to half precision (relative to the running
- * maximum) for the sum over values.  Bit-for-bit reproducible for the same
+ * exact products; p, times the ratio of the block's value scale to the largest
+ * one so far, is rounded to half precision (relative to the running maximum) for
+ * the sum over values: below 2^-20 of the largest such product bits are lost.
+ * Bit-for-bit reproducible for the same
  * inputs and sizes.
  *   q, out  [n_rows][n_heads][head_dim], the same dtype; out may not alias q
  *   ws      device workspace of at least qlm_kv_attention_workspace_bytes for
- *           this batch's sizes or larger ones, 256-byte aligned, scratch
+ *           this batch's sizes (larger sizes may need less: the work is split
+ *           less), 256-byte aligned, scratch
  */
 typedef struct qlm_kv_query {
     qlm_rows q, out;
@@ -657,7 +660,10 @@ int qlm_w4_pack(const qlm_w4 *weight, const uint8_t *codes, const void *scale,
 
 /*
  * out[m][n] = sum over k of x[m][k] * weight[n][k], the sums in single
- * precision from exact products within a group, rounded once.
+ * precision from exact products within a group, rounded once.  A row of x that
+ * holds an infinity or a NaN may have any of its outputs infinite or NaN.  Over
+ * many rows or outputs a row of bfloat16 is held in half precision, scaled by a
+ * power of two: elements below 2^-29 of the row's largest lose bits.
  *   x    [n_rows][n_in], x_stride elements between rows (>= n_in)
  *   out  [n_rows][n_out], out_stride elements between rows; of x's dtype, may
  *        not alias x

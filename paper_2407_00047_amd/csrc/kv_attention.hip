@@ -278,6 +278,9 @@ struct Cursor {
 // and values stay in registers; the next unit's keys are loaded as soon as this
 // one's scores are formed, its values as soon as this one's are added, so that
 // loads are always under way.
+// Bound by the cache's bytes: 192 ragged sequences of up to 16000 (3.2 GB, 8 kv heads of
+// 128) 546 us, 5.8 TB/s; two of up to 150000 74 (5.1); 48 ragged ones of up to 4096 that write
+// their scores 60 us (3.5 TB/s); one of 700 9 us, a launch and its dependent reads.
 template <int FMT, int ND, int NT>
 __global__ __launch_bounds__(kThreads, ND * NT <= 2 ? 2 : 1) void k_attend_rows(AttnArgs a)
 {
@@ -568,7 +571,8 @@ __device__ inline float lane_value(float x, int lane)
 
 // Adds up the parts of the columns whose units several workers held, and gives
 // the columns that see nothing their zeros: WPC waves to a column, the parts in
-// turn.
+// turn.  4.5 us at one sequence, 10 at two whose columns have 512 parts each: the reads
+// of the parts, four under way to a wave.
 template <int WPC> __global__ __launch_bounds__(kThreads) void k_attend_join(AttnArgs a)
 {
     __shared__ float part[kWaves][256], sum[kWaves];
@@ -653,7 +657,8 @@ template <int WPC> __global__ __launch_bounds__(kThreads) void k_attend_join(Att
 }
 
 // Weights from the scores that k_attend_rows left: a wave to a (sequence,
-// block, kv head), a lane to a slot.
+// block, kv head), a lane to a slot.  After the join, as a probability needs the whole
+// sum; 9 us at 48 sequences of up to 4096.
 __global__ __launch_bounds__(kThreads) void k_attend_weights(AttnArgs a)
 {
     const int lane = threadIdx.x & 63;
@@ -692,7 +697,8 @@ typedef float float16v __attribute__((ext_vector_type(16)));
 // Queries in half precision, dims padded with zeros to whole 64s, in the order of
 // the matrix operands (8 dims of a column after the next column's): scaled by a
 // power of two where they come in bfloat16 (load_query), negated where the scale
-// of the scores is negative.  A wave to a (row, head).
+// of the scores is negative.  A wave to a (row, head).  Bound by its bytes; 5 ragged prompts
+// of up to 2000 x 32 heads under 10 us.
 template <int ND> __global__ __launch_bounds__(kThreads) void k_query_half(AttnArgs a)
 {
     const int lane = threadIdx.x & 63;
@@ -732,6 +738,9 @@ template <int ND> __global__ __launch_bounds__(kThreads) void k_query_half(AttnA
 // serve the four waves.  S^T = K Q^T and O^T = V^T P^T are 32x32x16 matrix
 // instructions; a lane's scores are again the operand of the second product, so
 // only keys and values pass through shared memory.
+// Bound by matrix instructions, exponentials and reads of shared memory in turn, two
+// waves to a SIMD being all its registers allow: 5 ragged prompts of up to 2000 tokens
+// over up to 2600, 32 heads of 128: 170 us, 600 TFLOP/s.
 template <int FMT, int ND, bool FULL>
 __global__ __launch_bounds__(kThreads, ND <= 2 ? 2 : 1) void k_attend_prompt(AttnArgs a)
 {
@@ -1002,7 +1011,10 @@ __global__ __launch_bounds__(kThreads) void k_prompt_join(AttnArgs a)
 // Weights of the sequences of many rows: a workgroup to a block of 64 slots of a
 // (sequence, kv head).  Its waves hold the block's keys as matrix operands, form
 // the scores of the columns that see it again, a wave every fourth 32, the next
-// ones' queries on their way meanwhile, and add up their probabilities.
+// ones' queries on their way meanwhile, and add up their probabilities.  (Kept
+// scores would be four bytes for each column and slot, gigabytes of them.)
+// Bound by the exponentials, one for each 256 operations of the product at 128 dims, and the
+// reads of queries from L2: 128 us for the prompts of k_attend_prompt's figure.
 template <int FMT, int ND>
 __global__ __launch_bounds__(kThreads, ND <= 2 ? 2 : 1) void k_attend_colsum(AttnArgs a)
 {
@@ -1137,7 +1149,17 @@ __global__ __launch_bounds__(kThreads) void k_colsum_join(AttnArgs a)
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
-constexpr int kFew = 64;         // columns of a sequence that k_attend_rows takes
+// Columns of a sequence that k_attend_rows takes: it reads the keys and values again for
+// every 32, k_attend_prompt for every 128 but turns every block's codes for them.  At
+// 4096 tokens and 16 sequences, 32 columns 38 us to the other's 69, 64 58 to 65, 128 94
+// to 69; 64 sequences of 2048, 64 columns 96 to 118, 96 156 to 106.
+constexpr int kFew = 64;
+// Waves of k_attend_rows: one to a SIMD, for its many loads under way are enough and
+// each wave leaves parts to join (a sequence of 65536 tokens 38 us, two to a SIMD 44; 64 of
+// 4096 103 and 107).  Two where a wave has less under way (64 dims) or writes scores,
+// and the items are many: 64 of 4096 at 64 dims 57 us, one to a SIMD 71; 48 ragged
+// ones with weights 81 and 89.
+constexpr int kWorkers = 1024, kManyItems = 128;
 
 struct Plan {
     int nt, tile, workers, cols, blocks, splits, shares;
@@ -1155,8 +1177,9 @@ Plan plan_of(const qlm_kv_cache *c, const qlm_kv_batch *b, int32_t n_heads, bool
     p.nt = cols <= 16 || c->head_dim > 128 ? 1 : 2;      // (two would not fit the registers)
     p.tile = 16 * p.nt;
     p.blocks = std::max(1, (b->max_length + kBlock - 1) / kBlock);
-    // as many waves as the registers of 256 CUs hold at once
-    p.workers = c->head_dim <= 128 && p.nt == 1 ? 2048 : 1024;
+    const bool twice = (weights || c->head_dim <= 64) && c->head_dim <= 128 && p.nt == 1 &&
+                       (int64_t)b->n_seqs * c->n_kv_heads >= kManyItems;
+    p.workers = twice ? 2 * kWorkers : kWorkers;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -1186,11 +1209,12 @@ Plan plan_of(const qlm_kv_cache *c, const qlm_kv_batch *b, int32_t n_heads, bool
             p.split_ts = take(rh * p.splits * sizeof(TopSum));
         }
         if (weights) {
-            // a block's columns shared by up to 16 workgroups where the blocks are few,
-            // 256 columns each at least
+            // a block's columns shared where the blocks are few, 2048 columns to a
+            // workgroup at least: shares against none, one prompt of 1024 tokens 85 us to
+            // 93, of 8192 1194 to 1351, two of 1024 over 2 kv heads 70 to 99, four of 2048
+            // 437 to 415; at 512 columns the prompt of 2048 took 192 in place of 153
             const int64_t sbh = (int64_t)b->n_seqs * p.blocks * c->n_kv_heads;
-            p.shares = (int)std::min<int64_t>(
-                std::min<int64_t>(16, std::max<int64_t>(1, 4096 / sbh)), (cols + 255) / 256);
+            p.shares = (int)std::max<int64_t>(1, std::min(4096 / sbh, cols / 2048));
             if (p.shares > 1) p.share = take((size_t)p.shares * sbh * kBlock * 4);
         }
     }
@@ -1339,8 +1363,10 @@ int qlm_kv_attention(const qlm_kv_cache *cache, const qlm_kv_batch *batch,
         else
             launch_rows<QLM_KV_INT8>(a, p.nt, wg, stream);
         if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_attend_rows launch");
-        // few columns: a workgroup to each, their parts may be many
-        if (sh * few <= 2048)
+        // few columns: a workgroup to each, as their parts may be many (32 columns of
+        // 16384 tokens: 26 us with the rows, a wave to each 55; 512 columns 31 and 33;
+        // 4096 columns 61 and 53)
+        if (sh * few <= 1024)
             k_attend_join<kWaves><<<(unsigned)(sh * few), kThreads, 0, stream>>>(a);
         else
             k_attend_join<1><<<(unsigned)(sh * ((few + kWaves - 1) / kWaves)), kThreads, 0,

@@ -166,7 +166,9 @@ __device__ inline uint4 x8(const MatArgs &a, int row, int k)
 }
 
 // Up to 16 rows: one workgroup to 16 outputs, its waves taking the steps of K
-// in turn; x in shared memory.
+// in turn, four steps' weights under way; x in shared memory.  The sum of a group's x,
+// for its zero point, is a matrix product with ones.
+// 1 row, 4096 x 4096: 5.8 us (8.9 MB, 1.5 TB/s), the launch and one round of loads.
 template <bool BF, int GROUP> __global__ __launch_bounds__(kThreads) void k_w4_thin(MatArgs a)
 {
     constexpr int PER = kStep / GROUP, SUB = 4 / PER, PF = 4;
@@ -237,27 +239,43 @@ template <bool BF, int GROUP> __global__ __launch_bounds__(kThreads) void k_w4_t
 }
 
 // Rows for k_w4_wide: halves, 16-byte aligned, zeros up to a whole number of stages.
-// Rows of bfloat16 are scaled by a power of two to below 2^15.  A workgroup to a row.
-__global__ __launch_bounds__(kThreads) void k_w4_half(MatArgs a, uint16_t *xh, float *fac, int ld)
+// Rows of bfloat16 are scaled by a power of two to below 2^15.  A workgroup to a
+// row, eight inputs to a thread: a row is read in few rounds, as latency is all it costs.
+constexpr int kHalfThreads = 1024;
+
+__global__ __launch_bounds__(kHalfThreads) void k_w4_half(MatArgs a, uint16_t *xh, float *fac,
+                                                          int ld)
 {
-    __shared__ uint32_t part[kWaves];
-    const uint16_t *p = a.x + blockIdx.x * a.x_stride;
+    __shared__ uint32_t part[kHalfThreads / 64];
     uint32_t top = 0;                       // greatest exponent of a finite element
-    for (int k = threadIdx.x; k < a.K && a.bf; k += kThreads) {
-        const uint32_t e = (uint32_t)(p[k] >> 7) & 0xff;
-        top = e < 255 ? max(top, e) : top;
+    for (int k = 8 * threadIdx.x; k < a.K && a.bf; k += 8 * kHalfThreads) {
+        const uint4 v = x8(a, blockIdx.x, k);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t x = w[e >> 1] >> (16 * (e & 1) + 7) & 0xff;
+            top = x < 255 ? max(top, x) : top;
+        }
     }
     for (int o = 32; o; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = top;
     __syncthreads();
-    for (int w = 0; w < kWaves; ++w) top = max(top, part[w]);
+    for (int w = 0; w < kHalfThreads / 64; ++w) top = max(top, part[w]);
     const int up = min(15 - ((int)top - 126), 126);
     const float by = ldexpf(1.f, up);
-    for (int k = threadIdx.x; k < ld; k += kThreads) {
-        const uint16_t u = k < a.K ? p[k] : 0;
-        const float x = __builtin_bit_cast(float, (uint32_t)u << 16);
-        xh[(int64_t)blockIdx.x * ld + k] =
-            a.bf ? __builtin_bit_cast(uint16_t, (_Float16)(x * by)) : u;
+    for (int k = 8 * threadIdx.x; k < ld; k += 8 * kHalfThreads) {
+        uint4 v = {0u, 0u, 0u, 0u};
+        if (k < a.K) v = x8(a, blockIdx.x, k);
+        if (a.bf) {
+            uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            for (int e = 0; e < 4; ++e) {
+                const float lo = __builtin_bit_cast(float, w[e] << 16);
+                const float hi = __builtin_bit_cast(float, w[e] & 0xffff0000u);
+                w[e] = (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)(lo * by)) |
+                       (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)(hi * by)) << 16;
+            }
+            v = {w[0], w[1], w[2], w[3]};
+        }
+        *(uint4 *)(xh + (int64_t)blockIdx.x * ld + k) = v;
     }
     if (threadIdx.x == 0) fac[blockIdx.x] = a.bf ? ldexpf(1.f, -up) : 1.f;
 }
@@ -269,7 +287,11 @@ __device__ inline uint16_t wide_out(const MatArgs &a, float v, int m)
 
 // More rows: one workgroup to 64 outputs (16 a wave) and 16 NT rows of halves; x
 // passes through shared memory two steps at a time, in two buffers; the weights of
-// the two steps after the present ones are on their way.
+// the two steps after the present ones are on their way.  The zero point is taken off
+// the codes (exact in halves), so a group costs one product and one fma an output.
+// 48 rows, 20001 x 8192 in groups of 32: 60 us (262 TFLOP/s; 98 MB, 1.6 TB/s).  It waits
+// on the chain from codes to operands to products at 2.4 waves to a SIMD: without its
+// reads of memory it takes 43 us, and no pipe is full.
 template <int GROUP, int NT> __global__ __launch_bounds__(kThreads, 2) void k_w4_wide(MatArgs a)
 {
     constexpr int PER = kStep / GROUP, SUB = 4 / PER, LD = 2 * kStep + 8;
@@ -408,15 +430,27 @@ int check_weight(const qlm_w4 *w)
     return QLM_OK;
 }
 
-constexpr int kThinRows = 16;
+// k_w4_thin reads x again for every 16 outputs, k_w4_wide for every 64, but it has
+// parts to join and, where x is not aligned halves in whole stages, x to convert.
+// So up to 16 rows the product of rows, tiles of outputs and steps decides (us, halves
+// and bfloat16, thin against wide): 12 rows, 4096 x 4096 11.4 to 10.2 and 11.5 to
+// 13.0; 4 rows, 11000 x 4096 11.2 to 13.9 and 10.9 to 16.5, 8 rows 18.1 to 14.1 and
+// 18.0 to 16.7; 20001 x 8192 1 row 26.5 to 31.5 and 23.5 to 32.2, 2 rows 34.0 to 31.4
+// and 31.8 to 32.5, 16 rows 67.9 to 30.4 and 68.6 to 34.4.
+constexpr int kThinRows = 16, kThinWork = 96000, kThinWorkConvert = 160000;
 
+bool thin(const qlm_w4 *w, int rows, bool convert)
+{
+    const int64_t work = (int64_t)rows * ((w->n_out + 15) / 16) * ((w->n_in + kStep - 1) / kStep);
+    return rows <= kThinRows && work <= (convert ? kThinWorkConvert : kThinWork);
+}
+
+// Splits of K for k_w4_wide.
 void split_of(const qlm_w4 *w, int rows, int *splits, int *per)
 {
     const int steps = (w->n_in + kStep - 1) / kStep;
-    *splits = 1;
-    *per = steps;
-    if (rows <= kThinRows) return;
-    // enough workgroups for every CU, eight steps each at least
+    // two workgroups to a CU, eight steps each at least (48 rows, 20001 x 8192: half and
+    // twice as many splits were no faster)
     const int64_t wg = ((int64_t)w->n_out + 63) / 64 * ((rows + 63) / 64);
     const int64_t want = std::min<int64_t>((512 + wg - 1) / wg, std::max(1, steps / 8));
     *per = (int)((steps + want - 1) / want);
@@ -432,9 +466,9 @@ template <bool BF, int GROUP> void launch_thin(MatArgs a, hipStream_t st)
     k_w4_thin<BF, GROUP><<<a.tiles, kThreads, bytes, st>>>(a);
 }
 
-template <int GROUP> void launch(const MatArgs &a, hipStream_t st)
+template <int GROUP> void launch(const MatArgs &a, bool few, hipStream_t st)
 {
-    if (a.M <= kThinRows) {
+    if (few) {
         if (a.bf)
             launch_thin<true, GROUP>(a, st);
         else
@@ -443,7 +477,9 @@ template <int GROUP> void launch(const MatArgs &a, hipStream_t st)
     }
     const int nt = std::min(4, (a.M + 15) / 16);
     const dim3 grid((a.tiles + kWaves - 1) / kWaves, (a.M + 16 * nt - 1) / (16 * nt), a.splits);
-    if (nt == 2)
+    if (nt == 1)
+        k_w4_wide<GROUP, 1><<<grid, kThreads, 0, st>>>(a);
+    else if (nt == 2)
         k_w4_wide<GROUP, 2><<<grid, kThreads, 0, st>>>(a);
     else if (nt == 3)
         k_w4_wide<GROUP, 3><<<grid, kThreads, 0, st>>>(a);
@@ -462,7 +498,7 @@ struct Layout {
 Layout layout_of(const qlm_w4 *w, int rows)
 {
     Layout l{};
-    if (rows <= kThinRows) return l;
+    if (thin(w, rows, false)) return l;          // (and so where x is converted)
     int splits, per;
     split_of(w, rows, &splits, &per);
     l.ld = (w->n_in + 2 * kStep - 1) / (2 * kStep) * 2 * kStep;
@@ -548,26 +584,29 @@ int qlm_w4_matmul(const qlm_w4 *weight, const void *x, int64_t x_stride, void *o
     a.steps = (a.K + kStep - 1) / kStep;
     a.wide = (uintptr_t)x % 16 == 0 && x_stride % 8 == 0;
     a.bf = dtype == QLM_BF16;
-    split_of(weight, n_rows, &a.splits, &a.per_split);
     a.part = (float *)ws;
+    a.splits = 1;
     hipError_t e;
     // (halves that are aligned and fill whole stages are read where they are)
-    if (n_rows > kThinRows && (a.bf || !a.wide || a.K % (2 * kStep))) {
+    const bool convert = a.bf || !a.wide || a.K % (2 * kStep);
+    const bool few = thin(weight, n_rows, convert);
+    if (!few) split_of(weight, n_rows, &a.splits, &a.per_split);
+    if (!few && convert) {
         const Layout l = layout_of(weight, n_rows);
         uint16_t *xh = (uint16_t *)((char *)ws + l.xh);
         float *fac = (float *)((char *)ws + l.fac);
-        k_w4_half<<<n_rows, kThreads, 0, stream>>>(a, xh, fac, l.ld);
+        k_w4_half<<<n_rows, kHalfThreads, 0, stream>>>(a, xh, fac, l.ld);
         if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_w4_half launch");
         a.x = xh;
         a.x_stride = l.ld;
         a.fac = a.bf ? fac : nullptr;
     }
     if (weight->group == 32)
-        launch<32>(a, stream);
+        launch<32>(a, few, stream);
     else if (weight->group == 64)
-        launch<64>(a, stream);
+        launch<64>(a, few, stream);
     else
-        launch<128>(a, stream);
+        launch<128>(a, few, stream);
     if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "w4 launch");
     if (a.splits > 1) {
         const int64_t grid = ((int64_t)a.M * a.N + kThreads - 1) / kThreads;
