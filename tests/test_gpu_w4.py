@@ -111,6 +111,25 @@ def test_not_finite_rows(torch, qlm):
         check(got[keep], want, bound, "f16")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("k,group,pad", [(5120, 128, 0), (5000, 32, 0), (5120, 64, 8),
+                                         (5120, 128, 3)])
+@pytest.mark.parametrize("m", [1, 9, 10, 15, 16])
+def test_few_rows_many_outputs(torch, qlm, m, k, group, pad, dtype):
+    """Up to 16 rows on either side of the sizes from which x is shared by 64 outputs."""
+    n = 4100
+    host, dev = matrix(torch, n, k, group)
+    w = qlm.w4_pack(*dev, group=group)
+    x, xh = rows(torch, m, k, dtype, pad=pad)
+    want, bound = ko.w4(xh, *host, group)
+    got = qlm.w4_matmul(x, w)
+    check(got, want, bound, dtype)
+    assert torch.equal(got, qlm.w4_matmul(x, w))
+    x[0, 3] = float("nan")
+    again = qlm.w4_matmul(x, w)
+    assert not again[:1].isfinite().any() and torch.equal(again[1:], got[1:])
+
+
 def test_repeats_stream_graph(torch, qlm):
     """The same bits again, on another stream, and in a replayed graph."""
     _, dev = matrix(torch, 500, 2048, 128)
