@@ -25,6 +25,7 @@
 
 #include "internal.h"
 #include "qlm.h"
+#include "w4_split.h"
 
 namespace {
 
@@ -37,7 +38,8 @@ typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 
-constexpr int kStep = 128;           // inputs of a chunk
+using qlm_w4_host::kStep;            // inputs of a chunk
+using qlm_w4_host::split_of;
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 
 __host__ __device__ inline int chunk_bytes(int group) { return 1024 + 64 * (kStep / group); }
@@ -323,7 +325,8 @@ template <int GROUP, int NT> __global__ __launch_bounds__(kThreads, 2) void k_w4
     // thread t stages row t / 16 of each 16 rows, inputs 8 (t % 16) on of each step;
     // rows past the last are the last again (their outputs are not written)
     const int sr = threadIdx.x >> 4, sk = 8 * (threadIdx.x & 15);
-    // (no branch: the waits for the weights would count loads that may not be there)
+    // (no branch: the waits for the weights would count loads that may not be there.  Both
+    // steps of a pair are read: splits begin at whole pairs, and rows hold whole pairs)
     const uint16_t *xp[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -353,7 +356,8 @@ template <int GROUP, int NT> __global__ __launch_bounds__(kThreads, 2) void k_w4
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const uint32_t w[4] = {cw[u].x, cw[u].y, cw[u].z, cw[u].w};
-            const uint32_t on = kb + u < k1 ? 0xffffu : 0u;   // (past the last step: scales of 0)
+            // (past the last step: x is zeros, and scales of 0, as they may be infinite)
+            const uint32_t on = kb + u < k1 ? 0xffffu : 0u;
 #pragma unroll
             for (int q = 0; q < PER; ++q) {
                 const half2v z = __builtin_bit_cast(half2v, (uint32_t)zw[u][q] * 0x10001u);
@@ -445,18 +449,6 @@ bool thin(const qlm_w4 *w, int rows, bool convert)
     return rows <= kThinRows && work <= (convert ? kThinWorkConvert : kThinWork);
 }
 
-// Splits of K for k_w4_wide.
-void split_of(const qlm_w4 *w, int rows, int *splits, int *per)
-{
-    const int steps = (w->n_in + kStep - 1) / kStep;
-    // two workgroups to a CU, eight steps each at least (48 rows, 20001 x 8192: half and
-    // twice as many splits were no faster)
-    const int64_t wg = ((int64_t)w->n_out + 63) / 64 * ((rows + 63) / 64);
-    const int64_t want = std::min<int64_t>((512 + wg - 1) / wg, std::max(1, steps / 8));
-    *per = (int)((steps + want - 1) / want);
-    *splits = (steps + *per - 1) / *per;
-}
-
 template <bool BF, int GROUP> void launch_thin(MatArgs a, hipStream_t st)
 {
     // as much of x as 64 KiB hold
@@ -500,7 +492,7 @@ Layout layout_of(const qlm_w4 *w, int rows)
     Layout l{};
     if (thin(w, rows, false)) return l;          // (and so where x is converted)
     int splits, per;
-    split_of(w, rows, &splits, &per);
+    split_of(w->n_out, w->n_in, rows, &splits, &per);
     l.ld = (w->n_in + 2 * kStep - 1) / (2 * kStep) * 2 * kStep;
     l.xh = splits > 1 ? align256((size_t)splits * rows * w->n_out * 4) : 0;
     l.fac = l.xh + align256((size_t)rows * l.ld * 2);
@@ -590,7 +582,7 @@ int qlm_w4_matmul(const qlm_w4 *weight, const void *x, int64_t x_stride, void *o
     // (halves that are aligned and fill whole stages are read where they are)
     const bool convert = a.bf || !a.wide || a.K % (2 * kStep);
     const bool few = thin(weight, n_rows, convert);
-    if (!few) split_of(weight, n_rows, &a.splits, &a.per_split);
+    if (!few) split_of(weight->n_out, weight->n_in, n_rows, &a.splits, &a.per_split);
     if (!few && convert) {
         const Layout l = layout_of(weight, n_rows);
         uint16_t *xh = (uint16_t *)((char *)ws + l.xh);

@@ -130,6 +130,37 @@ def test_few_rows_many_outputs(torch, qlm, m, k, group, pad, dtype):
     assert not again[:1].isfinite().any() and torch.equal(again[1:], got[1:])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n,k,counts", [(83, 2816, (8, 33, 300)), (83, 2700, (40,)),
+                                        (4096, 11008, (8, 32, 64)), (3584, 18944, (8, 32, 64)),
+                                        (6144, 8192, (8, 32, 64))])
+def test_split_ends(torch, qlm, n, k, counts, dtype):
+    """Inputs split so that the last share would end inside a pair of steps: x is the front
+    of a larger tensor whose every other element is a not-a-number, on the right and
+    below, and none of them is read; a row that is a not-a-number leaves the others as they are."""
+    group = 128
+    host, dev = matrix(torch, n, k, group)
+    w = qlm.w4_pack(*dev, group=group)
+    x, xh = rows(torch, max(counts), k, dtype)
+    want, bound = ko.w4(xh, *host, group)
+    for m in counts:
+        outs = []
+        for right in (0, 256):
+            big = torch.full((m + 2, k + right), float("nan"), dtype=x.dtype, device="cuda")
+            view = big[:m, :k]
+            view.copy_(x[:m])
+            ws = torch.full((qlm.w4_workspace_bytes(w, m),), 255, dtype=torch.uint8,
+                            device="cuda")
+            outs.append(qlm.w4_matmul(view, w, ws=ws))
+            check(outs[-1], want[:m], bound[:m], dtype, (m, right))
+        assert torch.equal(outs[0], outs[1])
+        view[m // 2] = float("nan")
+        got = qlm.w4_matmul(view, w)
+        assert not got[m // 2].isfinite().any()
+        keep = torch.arange(m, device="cuda") != m // 2
+        assert torch.equal(got[keep], outs[1][keep])
+
+
 def test_repeats_stream_graph(torch, qlm):
     """The same bits again, on another stream, and in a replayed graph."""
     _, dev = matrix(torch, 500, 2048, 128)
