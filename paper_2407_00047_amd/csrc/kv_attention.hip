@@ -920,7 +920,10 @@ __global__ __launch_bounds__(kThreads, ND <= 2 ? 2 : 1) void k_attend_prompt(Att
             }
             float top, other;
             swap32(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), &top, &other);
-            const float f = fac * ks1;
+            // (an unseen slot's -inf is multiplied too: the factor may not vanish, as it
+            // would with queries and keys of zeros, both at their least scale.  Scores stay
+            // below 2^-80 at the one it is held to)
+            const float f = fmaxf(fac * ks1, 1e-37f);
             top = fmaxf(top, other) * f;
             if (__any(top > m + kSlack)) {
                 const float mn = fmaxf(m, top);

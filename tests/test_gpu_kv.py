@@ -303,6 +303,32 @@ def test_attend_large_scores(torch, qlm, fmt, n):
             assert abs(total - 4 * n) <= 4 * n * 1100 * 2.0 ** -22, (spread, scale, total)
 
 
+@pytest.mark.parametrize("fmt,dtype", [("e4m3", "bf16"), ("int8", "bf16"), ("e4m3", "f16"),
+                                       ("int8", "f16")])
+@pytest.mark.parametrize("counts", [[1, 1, 0], [30, 9, 12], [200, 70, 90]])
+def test_attend_nothing_to_tell_apart(torch, qlm, fmt, dtype, counts):
+    """Queries of zeros or next to them, keys of zeros or next to them, a scale of zero:
+    every seen slot has the same part, and the unseen ones none."""
+    lengths = [200, 130, 100]
+    for keys, spread, scale in ((0.0, 0.0, 0.125), (0.0, 1.0, 0.125), (1.0, 0.0, -0.125),
+                                (1e-7, 1e-4, 0.125), (1.0, 1.0, 0.0), (0.0, 1.0, 0.0)):
+        s = Setup(torch, qlm, lengths, 2, 64, fmt, seed=sum(counts))
+        k, kx = s.rows(sum(lengths), 2, dtype, keys)
+        v, vx = s.rows(sum(lengths), 2, dtype)
+        ora = ko.Cache.read(s.cache, fmt)
+        qlm.kv_append(s.cache, s.batch(lengths), k, v)
+        ora.append(s.table, lengths, lengths, kx, vx)
+        q, qx = s.rows(sum(counts), 8, dtype, spread)
+        label = (keys, spread, scale)
+        want, bound, wb = ora.attend(s.table, lengths, counts, qx, scale, 0.0)
+        got = qlm.kv_attention(s.cache, s.batch(counts), q, scale=scale, weight_decay=0.0)
+        check(got, want, bound, dtype, label)
+        now = s.cache.weight.double().cpu().numpy()
+        assert (np.isnan(now) == np.isnan(ora.weight)).all(), label
+        off = np.abs(now - ora.weight) - wb
+        assert not (off > 0).any(), (label, float(np.nanmax(off)))
+
+
 def test_unmapped_blocks(torch, qlm):
     """A block number outside the pool names no slots: the others are attended."""
     s = Setup(torch, qlm, [300, 64], 1, 64, "e4m3", seed=13)
