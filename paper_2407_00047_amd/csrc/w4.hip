@@ -6,7 +6,9 @@
 // shift and one and-or for two codes).  No weight is ever rounded:
 //  - up to 16 rows, with one group's sums S = sum of x, T[n] = sum of (16 + c[n]) x,
 //    both by the matrix instructions (S with a matrix of ones), the group's part of
-//    the output is s[n] (T[n] - (16 + z[n]) S), formed in single precision;
+//    the output is s[n] (T[n] - (16 + z[n]) S), formed in single precision.  Of bfloat16
+//    both sums are taken 2^-13 times as large, by the constants' exponents: T of 128
+//    inputs would pass single precision's range from x = 2^116 on;
 //  - for more rows 16 + z is taken off in half precision (exact: -15 .. 15), once for
 //    all of them, and the part is s[n] T[n].  Rows of bfloat16 are first scaled by
 //    powers of two to fit halves.
@@ -97,16 +99,18 @@ template <bool BF> __device__ inline float4v mfma(uint4 x, uint4 y, float4v c)
                                                   __builtin_bit_cast(half8v, y), c, 0, 0, 0);
 }
 
-// The exponent of 16 for two numbers, in a register (an and-or takes one constant
-// from the scalar side only).
+constexpr float kRaise = 8192.f;     // takes out the 2^-13 of bfloat16's sums
+
+// The exponent of 16 (of bfloat16, of 16 * 2^-13) for two numbers, in a register (an
+// and-or takes one constant from the scalar side only).
 template <bool BF> __device__ inline uint32_t sixteen()
 {
-    uint32_t c = BF ? 0x41804180u : 0x4c004c00u;
+    uint32_t c = BF ? 0x3b003b00u : 0x4c004c00u;
     asm("" : "+v"(c));
     return c;
 }
 
-// The eight codes of a dword as 16 + c.
+// The eight codes of a dword as 16 + c (times 2^-13 of bfloat16).
 template <bool BF> __device__ inline uint4 operand(uint32_t w, uint32_t c)
 {
     if (BF)
@@ -116,19 +120,21 @@ template <bool BF> __device__ inline uint4 operand(uint32_t w, uint32_t c)
             (w >> 2 & 0x03c003c0u) | c, (w >> 6 & 0x03c003c0u) | c};
 }
 
+// Ones (2^-13 of bfloat16).
 template <bool BF> __device__ inline uint4 ones()
 {
-    const uint32_t o = BF ? 0x3f803f80u : 0x3c003c00u;
+    const uint32_t o = BF ? 0x39003900u : 0x3c003c00u;
     return {o, o, o, o};
 }
 
-// sum += scale (t - zero S) for the four outputs of a lane
-__device__ inline float4v add_group(float4v sum, float4v t, float S, uint4 meta)
+// sum += scale (t - zero S) for the four outputs of a lane (the 2^-13 is taken out of
+// the scale: the sum then keeps small rows' bits, and t - zero S may not fit without)
+template <bool BF> __device__ inline float4v add_group(float4v sum, float4v t, float S, uint4 meta)
 {
     const uint32_t w[4] = {meta.x, meta.y, meta.z, meta.w};
     for (int i = 0; i < 4; ++i) {
         const half2v h = __builtin_bit_cast(half2v, w[i]);
-        sum[i] = fmaf((float)h[0], fmaf(-(float)h[1], S, t[i]), sum[i]);
+        sum[i] = fmaf(BF ? (float)h[0] * kRaise : (float)h[0], fmaf(-(float)h[1], S, t[i]), sum[i]);
     }
     return sum;
 }
@@ -222,7 +228,7 @@ template <bool BF, int GROUP> __global__ __launch_bounds__(kThreads) void k_w4_t
                         t = mfma<BF>(operand<BF>(w[j], c16f), b, t);
                         S = mfma<BF>(ones<BF>(), b, S);
                     }
-                    sum = add_group(sum, t, S[0], mw[u][q]);
+                    sum = add_group<BF>(sum, t, S[0], mw[u][q]);
                 }
                 fetch(u, kb + kWaves * PF);
             }

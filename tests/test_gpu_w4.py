@@ -97,6 +97,26 @@ def test_magnitudes(torch, qlm):
         check(qlm.w4_matmul(x, w), want, bound, "bf16")
 
 
+@pytest.mark.parametrize("m", [1, 4, 16, 20])
+def test_largest_magnitudes(torch, qlm, m):
+    """Rows of bfloat16 up to its largest value, beside one down at its least normal ones:
+    outputs that fit are finite, whichever form the number of rows takes."""
+    for group in (32, 128):
+        host, dev = matrix(torch, 40, 300, group)
+        dev[1].mul_(2.0 ** -9)
+        host = (host[0], dev[1].double().cpu().numpy(), host[2])
+        w = qlm.w4_pack(*dev, group=group)
+        x, _ = rows(torch, m, 300, "bf16")
+        size = torch.tensor([3e37, 1e-36, 1e38, 1e36], device="cuda", dtype=torch.float64)
+        x.copy_((x.double() * size[torch.arange(m, device="cuda") % 4][:, None])
+                .clamp(-3.3e38, 3.3e38))
+        if m == 1:
+            x.abs_()                         # (sums that no sign keeps small)
+        want, bound = ko.w4(x.double().cpu().numpy(), *host, group)
+        assert (np.abs(want) < 3e38).all()
+        check(qlm.w4_matmul(x, w), want, bound, "bf16", group)
+
+
 def test_not_finite_rows(torch, qlm):
     """A row that is not finite spoils itself alone."""
     host, dev = matrix(torch, 50, 256, 64)
