@@ -716,6 +716,14 @@ def _rows(t, n_rows, heads, dim, what):
     return t.data_ptr(), row, head, _row_type(t, what)
 
 
+def _refuse_place(index, **tensors):
+    """Names the tensor that is not on GPU `index`, that of the call's cache or matrix
+    (-1 of host memory): a kernel would follow its address."""
+    for name, t in tensors.items():
+        if index < 0 or (t is not None and t.get_device() != index):
+            raise ValueError("%s must be on the GPU, together with the call's other tensors" % name)
+
+
 def _raw_stream(stream):
     if stream is not None:
         return stream.cuda_stream
@@ -754,6 +762,9 @@ class DeviceKvCache:
                 continue
             if tuple(x.shape) != shape or x.dtype != dtype or not x.is_contiguous():
                 raise ValueError("%s must be contiguous %s of %s" % (name, shape, dtype))
+            if x.device != k_codes.device:
+                raise ValueError("%s must be where k_codes is" % name)
+        self.index = k_codes.get_device()
         self.n_blocks, self.n_kv_heads, self.head_dim = int(nb), int(h), int(d)
         self.k_codes, self.v_codes = k_codes, v_codes
         self.k_scale, self.v_scale = k_scale, v_scale
@@ -801,6 +812,9 @@ class KvBatch:
             raise ValueError("row_start must be [n_seqs + 1]")
         if row_start is not None and n_rows is None:
             raise ValueError("n_rows is required with row_start")
+        if any(x is not None and x.device != lengths.device for x in (block_table, row_start)):
+            raise ValueError("block_table and row_start must be where lengths is")
+        self.index = lengths.get_device()
         width = int(block_table.shape[1])
         if max_length is None:
             max_length = width * KV_BLOCK
@@ -827,6 +841,10 @@ def kv_append(cache: DeviceKvCache, batch: KvBatch, k, v, first_position=None, s
         raise ValueError("first_position must be [n_seqs] int32")
     rk = _rows(k, batch.n_rows, cache.n_kv_heads, cache.head_dim, "k")
     rv = _rows(v, batch.n_rows, cache.n_kv_heads, cache.head_dim, "v")
+    if not 0 <= cache.index == batch.index == k.get_device() == v.get_device() or \
+            (first_position is not None and first_position.get_device() != cache.index):
+        _refuse_place(cache.index, cache=cache.k_codes, batch=batch.lengths, k=k, v=v,
+                      first_position=first_position)
     rc = (_lib or library()).qlm_kv_append(
         cache._ref, batch._ref, _ROWS.pack(*rk), _ROWS.pack(*rv),
         None if first_position is None else first_position.data_ptr(), _raw_stream(stream))
@@ -867,6 +885,8 @@ def kv_attention(cache: DeviceKvCache, batch: KvBatch, q, scale=None, weight_dec
     query = _KV_QUERY.pack(*rq, *_rows(out, batch.n_rows, heads, dim, "out"), heads,
                            dim ** -0.5 if scale is None else scale, weight_decay is not None,
                            weight_decay or 0.0)
+    if not 0 <= cache.index == batch.index == q.get_device() == out.get_device() == ws.get_device():
+        _refuse_place(cache.index, cache=cache.k_codes, batch=batch.lengths, q=q, out=out, ws=ws)
     rc = (_lib or library()).qlm_kv_attention(cache._ref, batch._ref, query, ws.data_ptr(),
                                               ws.numel(), _raw_stream(stream))
     if rc:
@@ -897,6 +917,8 @@ def kv_evict(cache: DeviceKvCache, batch: KvBatch, budget: int, recent: int = 0,
         raise ValueError("out must be [n_seqs] int32")
     if ws is None:
         ws = kv_evict_workspace(cache, batch, budget)
+    if not 0 <= cache.index == batch.index == out.get_device() == ws.get_device():
+        _refuse_place(cache.index, cache=cache.k_codes, batch=batch.lengths, out=out, ws=ws)
     rc = (_lib or library()).qlm_kv_evict(cache._ref, batch._ref, budget, recent, out.data_ptr(),
                                           ws.data_ptr(), ws.numel(), _raw_stream(stream))
     if rc:
@@ -910,6 +932,7 @@ class W4:
 
     def __init__(self, packed, n_out, n_in, group):
         self.packed, self.n_out, self.n_in, self.group = packed, n_out, n_in, group
+        self.index = packed.get_device()
         self.struct = W4Struct(n_out, n_in, group, _ptr(packed))
         self._ref = ctypes.byref(self.struct)
 
@@ -934,6 +957,7 @@ def w4_pack(codes, scale, zero=None, group=None, stream=None):
     if zero is not None and (zero.shape != scale.shape or zero.dtype != torch.uint8 or
                              not zero.is_contiguous()):
         raise ValueError("zero must be contiguous uint8 of scale's shape")
+    _refuse_place(codes.get_device(), codes=codes, scale=scale, zero=zero)
     packed = torch.empty(int(library().qlm_w4_packed_bytes(n, k, group)), dtype=torch.uint8,
                          device=codes.device)
     w = W4(packed, n, k, group)
@@ -968,6 +992,8 @@ def w4_matmul(x, weight: W4, out=None, ws=None, stream=None):
         ws = w4_workspace(weight, n)
     # (the stride of a matrix of one row says nothing)
     xs, os_ = (x.stride(0), out.stride(0)) if n > 1 else (weight.n_in, weight.n_out)
+    if not 0 <= weight.index == x.get_device() == out.get_device() == ws.get_device():
+        _refuse_place(weight.index, weight=weight.packed, x=x, out=out, ws=ws)
     rc = (_lib or library()).qlm_w4_matmul(weight._ref, x.data_ptr(), xs, out.data_ptr(), os_, n,
                                            kind, ws.data_ptr(), ws.numel(), _raw_stream(stream))
     if rc:

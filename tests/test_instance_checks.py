@@ -224,3 +224,72 @@ def test_binding_refusals(qlm):
             qlm.w4_matmul(x, w)
     with pytest.raises(ValueError):
         qlm.w4_matmul(half(2, 64), w, out=half(2, 15))
+
+
+def test_host_tensors_are_refused(qlm, monkeypatch):
+    """Tensors of the right shape and type in host memory: their addresses reach no kernel."""
+    import torch
+    reached = []
+
+    class Library:
+        """The sizes as they are; no call of a kernel."""
+
+        def __getattr__(self, name):
+            if name.endswith("_bytes"):
+                return getattr(real, name)
+            return lambda *args: reached.append(name) or 0
+
+    real = qlm.library()
+    monkeypatch.setattr(qlm, "_lib", Library())
+    monkeypatch.setattr(qlm, "_raw_stream", lambda stream: None)
+    monkeypatch.setattr(qlm, "_stream", lambda stream: None)
+    i32 = dict(dtype=torch.int32)
+    half = lambda *s: torch.zeros(s, dtype=torch.float16)  # noqa: E731
+    c = qlm.DeviceKvCache.empty(4, 2, 32, device="cpu")
+    b = qlm.KvBatch(torch.zeros((2, 3), **i32), torch.zeros(2, **i32))
+    u8 = torch.zeros((4, 64), dtype=torch.uint8)
+    w = qlm.W4(torch.zeros(1024 + 128, dtype=torch.uint8), 16, 64, 64)
+    calls = [lambda: qlm.kv_append(c, b, half(2, 2, 32), half(2, 2, 32)),
+             lambda: qlm.kv_attention(c, b, half(2, 4, 32)),
+             lambda: qlm.kv_evict(c, b, 64),
+             lambda: qlm.w4_pack(u8, half(4, 2)),
+             lambda: qlm.w4_matmul(half(2, 64), w)]
+    for call in calls:
+        with pytest.raises(ValueError, match="must be on the GPU"):
+            call()
+    assert not reached
+    # a cache or a batch in two places
+    with pytest.raises(ValueError, match="must be where"):
+        qlm.DeviceKvCache(c.k_codes, c.v_codes, c.k_scale, c.v_scale.to("meta"))
+    with pytest.raises(ValueError, match="must be where"):
+        qlm.KvBatch(torch.zeros((2, 3), device="meta", **i32), torch.zeros(2, **i32))
+
+
+@pytest.mark.gpu
+def test_host_tensors_beside_device_tensors(qlm):
+    """One tensor of a call left in host memory."""
+    import torch
+    i32 = dict(dtype=torch.int32)
+    half = lambda *s, dev="cuda": torch.zeros(s, dtype=torch.float16, device=dev)  # noqa: E731
+    c = qlm.DeviceKvCache.empty(4, 2, 32)
+    there = torch.zeros((2, 3), device="cuda", **i32), torch.zeros(2, device="cuda", **i32)
+    b, host = qlm.KvBatch(*there), qlm.KvBatch(*(x.cpu() for x in there))
+    k, q, hk, hq = half(2, 2, 32), half(2, 4, 32), half(2, 2, 32, dev="cpu"), half(2, 4, 32, dev="cpu")
+    w = qlm.w4_pack(torch.zeros((4, 64), dtype=torch.uint8, device="cuda"), half(4, 2))
+    ws = torch.zeros(1 << 25, dtype=torch.uint8)
+    calls = [lambda: qlm.kv_append(c, host, k, k), lambda: qlm.kv_append(c, b, hk, k),
+             lambda: qlm.kv_append(c, b, k, hk),
+             lambda: qlm.kv_append(c, b, k, k, torch.zeros(2, **i32)),
+             lambda: qlm.kv_attention(c, host, q), lambda: qlm.kv_attention(c, b, hq),
+             lambda: qlm.kv_attention(c, b, q, out=hq), lambda: qlm.kv_attention(c, b, q, ws=ws),
+             lambda: qlm.kv_evict(c, host, 64),
+             lambda: qlm.kv_evict(c, b, 64, out=torch.zeros(2, **i32)),
+             lambda: qlm.kv_evict(c, b, 64, ws=ws),
+             lambda: qlm.w4_pack(torch.zeros((4, 64), dtype=torch.uint8, device="cuda"),
+                                 half(4, 2, dev="cpu")),
+             lambda: qlm.w4_matmul(half(2, 64, dev="cpu"), w),
+             lambda: qlm.w4_matmul(half(2, 64), w, out=half(2, 4, dev="cpu")),
+             lambda: qlm.w4_matmul(half(2, 64), w, ws=ws)]
+    for call in calls:
+        with pytest.raises(ValueError, match="must be on the GPU"):
+            call()
