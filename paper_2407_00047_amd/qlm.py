@@ -716,6 +716,22 @@ def _rows(t, n_rows, heads, dim, what):
     return t.data_ptr(), row, head, _row_type(t, what)
 
 
+def _allocated(stream, make, returned=True):
+    """What `make` allocates for a call on `stream` (None: the current one).  The
+    allocator hands memory out again in the order of the stream it was allocated on, and
+    that must be the stream whose kernels use it: not memory that the current one still
+    works in, nor given away by it while the call is queued.  What the caller gets is kept
+    from reuse until the current stream has passed the point where it was dropped, too."""
+    if stream is None:
+        return make()
+    import torch
+    with torch.cuda.stream(stream):
+        t = make()
+    if returned:
+        t.record_stream(torch.cuda.current_stream())
+    return t
+
+
 def _refuse_place(index, **tensors):
     """Names the tensor that is not on GPU `index`, that of the call's cache or matrix
     (-1 of host memory): a kernel would follow its address."""
@@ -877,11 +893,12 @@ def kv_attention(cache: DeviceKvCache, batch: KvBatch, q, scale=None, weight_dec
     heads, dim = q.shape[1], cache.head_dim
     rq = _rows(q, batch.n_rows, heads, dim, "q")
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = _allocated(stream, lambda: torch.empty(q.shape, dtype=q.dtype, device=q.device))
     elif out.shape != q.shape or out.dtype != q.dtype:
         raise ValueError("out must have q's shape and type")
     if ws is None:
-        ws = kv_attention_workspace(cache, batch, heads, weight_decay is not None)
+        ws = _allocated(stream, lambda: kv_attention_workspace(cache, batch, heads,
+                                                               weight_decay is not None), False)
     query = _KV_QUERY.pack(*rq, *_rows(out, batch.n_rows, heads, dim, "out"), heads,
                            dim ** -0.5 if scale is None else scale, weight_decay is not None,
                            weight_decay or 0.0)
@@ -912,11 +929,11 @@ def kv_evict(cache: DeviceKvCache, batch: KvBatch, budget: int, recent: int = 0,
     batch's own lengths)."""
     if out is None:
         import torch
-        out = torch.empty_like(batch.lengths)
+        out = _allocated(stream, lambda: torch.empty_like(batch.lengths))
     elif out.dtype != batch.lengths.dtype or out.numel() != batch.n_seqs or not out.is_contiguous():
         raise ValueError("out must be [n_seqs] int32")
     if ws is None:
-        ws = kv_evict_workspace(cache, batch, budget)
+        ws = _allocated(stream, lambda: kv_evict_workspace(cache, batch, budget), False)
     if not 0 <= cache.index == batch.index == out.get_device() == ws.get_device():
         _refuse_place(cache.index, cache=cache.k_codes, batch=batch.lengths, out=out, ws=ws)
     rc = (_lib or library()).qlm_kv_evict(cache._ref, batch._ref, budget, recent, out.data_ptr(),
@@ -958,8 +975,8 @@ def w4_pack(codes, scale, zero=None, group=None, stream=None):
                              not zero.is_contiguous()):
         raise ValueError("zero must be contiguous uint8 of scale's shape")
     _refuse_place(codes.get_device(), codes=codes, scale=scale, zero=zero)
-    packed = torch.empty(int(library().qlm_w4_packed_bytes(n, k, group)), dtype=torch.uint8,
-                         device=codes.device)
+    nbytes = int(library().qlm_w4_packed_bytes(n, k, group))
+    packed = _allocated(stream, lambda: torch.empty(nbytes, dtype=torch.uint8, device=codes.device))
     w = W4(packed, n, k, group)
     _check(library().qlm_w4_pack(w._ref, _ptr(codes), _ptr(scale), _ptr(zero), _stream(stream)))
     return w
@@ -984,12 +1001,13 @@ def w4_matmul(x, weight: W4, out=None, ws=None, stream=None):
     kind = _row_type(x, "x")
     n = x.shape[0]
     if out is None:
-        out = torch.empty((n, weight.n_out), dtype=x.dtype, device=x.device)
+        out = _allocated(stream, lambda: torch.empty((n, weight.n_out), dtype=x.dtype,
+                                                     device=x.device))
     elif tuple(out.shape) != (n, weight.n_out) or out.dtype != x.dtype or \
             (out.stride(1) != 1 and weight.n_out > 1):
         raise ValueError("out must be [rows, %d] of x's type with contiguous rows" % weight.n_out)
     if ws is None:
-        ws = w4_workspace(weight, n)
+        ws = _allocated(stream, lambda: w4_workspace(weight, n), False)
     # (the stride of a matrix of one row says nothing)
     xs, os_ = (x.stride(0), out.stride(0)) if n > 1 else (weight.n_in, weight.n_out)
     if not 0 <= weight.index == x.get_device() == out.get_device() == ws.get_device():

@@ -265,6 +265,99 @@ def test_host_tensors_are_refused(qlm, monkeypatch):
         qlm.KvBatch(torch.zeros((2, 3), device="meta", **i32), torch.zeros(2, **i32))
 
 
+def test_memory_of_the_calls_stream(qlm, monkeypatch):
+    """Outputs and workspaces that a call allocates itself are memory of the stream that it
+    runs on, whose order decides when the allocator hands them out again; what the caller gets
+    is also recorded on the stream that was current."""
+    import contextlib
+
+    import torch
+    current, made, recorded, launched = ["main"], [], [], []
+
+    class Library:
+        def __getattr__(self, name):
+            if name.endswith("_bytes"):
+                return lambda *args: 64
+            return lambda *args: launched.append(name) or 0
+
+    @contextlib.contextmanager
+    def on(stream):
+        current.append(stream)
+        yield
+        current.pop()
+
+    def noted(make):
+        return lambda *a, **k: (made.append(current[-1]), make(*a, **k))[1]
+
+    i32 = dict(dtype=torch.int32)
+    half = lambda *s: torch.zeros(s, dtype=torch.float16)  # noqa: E731
+    c = qlm.DeviceKvCache.empty(4, 2, 32, device="cpu")
+    b = qlm.KvBatch(torch.zeros((2, 3), **i32), torch.zeros(2, **i32))
+    u8 = torch.zeros((4, 64), dtype=torch.uint8)
+    w = qlm.W4(torch.zeros(1024 + 128, dtype=torch.uint8), 16, 64, 64)
+    monkeypatch.setattr(qlm, "_lib", Library())
+    for name in ("_raw_stream", "_stream"):
+        monkeypatch.setattr(qlm, name, lambda stream: None)
+    monkeypatch.setattr(qlm, "_refuse_place", lambda *a, **k: None)   # (no GPU here)
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: current[-1])
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: recorded.append(s))
+    for name in ("empty", "empty_like"):
+        monkeypatch.setattr(torch, name, noted(getattr(torch, name)))
+    calls = [(lambda s: qlm.kv_attention(c, b, half(2, 4, 32), stream=s), 2),
+             (lambda s: qlm.kv_evict(c, b, 64, stream=s), 2),
+             (lambda s: qlm.w4_pack(u8, half(4, 2), stream=s), 1),
+             (lambda s: qlm.w4_matmul(half(2, 64), w, stream=s), 2)]
+    for call, n in calls:
+        for stream, where in ((None, "main"), ("side", "side")):
+            made.clear(), recorded.clear(), launched.clear()
+            call(stream)
+            assert made == [where] * n and len(launched) == 1
+            assert recorded == (["main"] if stream else [])
+
+
+@pytest.mark.gpu
+def test_memory_beside_another_stream(qlm):
+    """Calls on a stream of their own that allocate for themselves, while the current stream
+    allocates and writes memory of the same sizes: results as on the current stream."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    rnd = lambda *s: torch.randn(s, generator=gen, device="cuda").half()  # noqa: E731
+    lengths = torch.tensor([3000, 2000], dtype=torch.int32, device="cuda")
+    table = torch.arange(100, dtype=torch.int32, device="cuda").view(2, 50)
+    caches = [qlm.DeviceKvCache.empty(100, 2, 64) for _ in range(2)]
+    start = torch.tensor([0, 3000, 5000], dtype=torch.int32, device="cuda")
+    k, v, q = rnd(5000, 2, 64), rnd(5000, 2, 64), rnd(2, 8, 64)
+    codes = torch.randint(0, 16, (700, 1024), generator=gen, device="cuda", dtype=torch.uint8)
+    scale, x = rnd(700, 8), rnd(40, 1024)
+    b = qlm.KvBatch(table, lengths)
+    side = torch.cuda.Stream()
+
+    def steps(cache, stream):
+        got = [qlm.kv_attention(cache, b, q, weight_decay=0.0, stream=stream)]
+        disturb()
+        got.append(qlm.kv_evict(cache, b, 512, 32, stream=stream))
+        disturb()
+        w = qlm.w4_pack(codes, scale, stream=stream)
+        got.append(qlm.w4_matmul(x, w, stream=stream))
+        disturb()
+        return got + [cache.weight, w.packed]
+
+    def disturb():
+        for n in (qlm.kv_attention_workspace_bytes(caches[0], b, 8, True),
+                  qlm.kv_evict_workspace_bytes(caches[0], b, 512), 2 * 8 * 64 * 2, 1 << 18):
+            torch.empty(n, dtype=torch.uint8, device="cuda").fill_(255)
+
+    for cache in caches:
+        cache.weight.zero_()
+        qlm.kv_append(cache, qlm.KvBatch(table, lengths, start, 5000, 3000), k, v)
+    want = steps(caches[0], None)
+    side.wait_stream(torch.cuda.current_stream())
+    got = steps(caches[1], side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 @pytest.mark.gpu
 def test_host_tensors_beside_device_tensors(qlm):
     """One tensor of a call left in host memory."""
