@@ -29,10 +29,12 @@ BLOCK = qlm.KV_BLOCK
 
 
 class Model:
-    """Sizes of a decoder layer and its 4-bit weights (one layer's, used by every
-    layer: the time of a step does not depend on their values)."""
+    """Sizes of a decoder layer and the 4-bit weights of a stack of them.  Every
+    layer has the same codes, as the time of a step does not depend on them, in memory
+    of its own: a step reads each layer's weights anew, where one layer's would come from the
+    last-level cache (90 MB at the sizes below, of 256)."""
 
-    def __init__(self, hidden, heads, kv_heads, dim, inner, group=128, seed=0):
+    def __init__(self, hidden, heads, kv_heads, dim, inner, group=128, seed=0, layers=1):
         self.hidden, self.heads, self.kv_heads, self.dim = hidden, heads, kv_heads, dim
         self.inner = inner
         gen = torch.Generator(device="cuda").manual_seed(seed)
@@ -46,13 +48,14 @@ class Model:
                                  dtype=torch.uint8)
             return qlm.w4_pack(codes, scale, zero, group)
 
-        self.qkv = matrix((heads + 2 * kv_heads) * dim, hidden)
-        self.out = matrix(hidden, heads * dim)
-        self.up = matrix(inner, hidden)
-        self.down = matrix(hidden, inner)
+        first = (matrix((heads + 2 * kv_heads) * dim, hidden), matrix(hidden, heads * dim),
+                 matrix(inner, hidden), matrix(hidden, inner))
+        copy = lambda m: qlm.W4(m.packed.clone(), m.n_out, m.n_in, m.group)  # noqa: E731
+        # (qkv, out, up, down) of each layer
+        self.layers = [first] + [tuple(copy(m) for m in first) for _ in range(layers - 1)]
 
     def weight_bytes(self, layers):
-        return layers * sum(m.packed.numel() for m in (self.qkv, self.out, self.up, self.down))
+        return layers * sum(m.packed.numel() for m in self.layers[0])
 
     def token_bytes(self, layers):
         """Cache bytes of a token: codes of keys and values, its position and weight,
@@ -64,6 +67,8 @@ class Instance:
     """Sequences in decode on one model: their cache, a block table and lengths."""
 
     def __init__(self, model, layers, batch, most):
+        if layers > len(model.layers):
+            raise ValueError("the model has %d layers" % len(model.layers))
         self.model, self.layers, self.batch = model, layers, batch
         self.width = -(-most // BLOCK)
         n = batch * self.width
@@ -93,8 +98,8 @@ class Instance:
         self.lengths += new
         start = torch.arange(self.batch + 1, dtype=torch.int32, device="cuda") * new
         batch = qlm.KvBatch(self.table, self.lengths, start, self.batch * new, new)
-        for cache in self.caches:
-            qkv = self._matmul(x, m.qkv).view(-1, m.heads + 2 * m.kv_heads, m.dim)
+        for cache, (w_qkv, w_out, w_up, w_down) in zip(self.caches, m.layers):
+            qkv = self._matmul(x, w_qkv).view(-1, m.heads + 2 * m.kv_heads, m.dim)
             q = qkv[:, :m.heads]
             k, v = qkv[:, m.heads:m.heads + m.kv_heads], qkv[:, m.heads + m.kv_heads:]
             qlm.kv_append(cache, batch, k, v, self.next)
@@ -102,8 +107,8 @@ class Instance:
             ws = self._workspace("attention", need,
                                  lambda: qlm.kv_attention_workspace(cache, batch, m.heads, True))
             att = qlm.kv_attention(cache, batch, q, weight_decay=1.0, ws=ws)
-            x = x + self._matmul(att.view(x.shape[0], -1), m.out)
-            x = x + self._matmul(torch.nn.functional.silu(self._matmul(x, m.up)), m.down)
+            x = x + self._matmul(att.view(x.shape[0], -1), w_out)
+            x = x + self._matmul(torch.nn.functional.silu(self._matmul(x, w_up)), w_down)
         self.next += new
         return x
 
@@ -175,7 +180,7 @@ def main(argv=None):
 
     # two models that take turns on the instances of one class: the second of half
     # the layers
-    model = Model(a.hidden, a.heads, a.kv_heads, a.dim, a.inner)
+    model = Model(a.hidden, a.heads, a.kv_heads, a.dim, a.inner, layers=a.layers)
     layers = [a.layers, max(1, a.layers // 2)]
     got = [measure(model, n, a.batch, a.prompt, a.budget, a.recent, a.steps, a.memory_gb * 1e9)
            for n in layers]

@@ -47,3 +47,20 @@ def test_prompt_and_steps_agree(example):
     # a bfloat16 rounding of each of five results in a row, and of the e4m3 codes'
     # values (2^-4 of a subnormal step) far below it
     assert float(d.max()) <= 6 * 2.0 ** -8 * float(whole.float().abs().max())
+
+
+def test_layers_have_weights_of_their_own(example, monkeypatch):
+    """A step reads as many weights as the layers count: no layer's come a second time."""
+    seen = []
+    real = example.qlm.w4_matmul
+
+    def noted(x, w, **more):
+        seen.append(w.packed.data_ptr())
+        return real(x, w, **more)
+
+    monkeypatch.setattr(example.qlm, "w4_matmul", noted)
+    example.main(["--layers", "3", "--hidden", "128", "--heads", "4", "--kv-heads", "2",
+                  "--dim", "32", "--inner", "256", "--batch", "2", "--prompt", "20",
+                  "--budget", "64", "--recent", "8", "--steps", "2", "--plans", "64"])
+    # the first pass: a prompt through three layers of four matrices
+    assert len(set(seen[:12])) == 12 and set(seen) == set(seen[:12])
