@@ -78,6 +78,7 @@ class Instance:
         self.table = order.view(batch, self.width).contiguous()
         self.lengths = torch.zeros(batch, dtype=torch.int32, device="cuda")
         self.next = torch.zeros(batch, dtype=torch.int32, device="cuda")   # next position
+        self.position = 0                                # the same, known to the host
         self.ws = {}
 
     def _workspace(self, name, need, make):
@@ -110,7 +111,23 @@ class Instance:
             x = x + self._matmul(att.view(x.shape[0], -1), w_out)
             x = x + self._matmul(torch.nn.functional.silu(self._matmul(x, w_up)), w_down)
         self.next += new
+        self.position += new
         return x
+
+    def restart(self):
+        """Every sequence without a token again."""
+        self.lengths.zero_()
+        self.next.zero_()
+        self.position = 0
+
+    def decode(self, x, steps, budget, recent):
+        """Steps of one token a sequence, queued without waiting for the GPU; a block that
+        is full is followed by a cut to the budget."""
+        for _ in range(steps):
+            y = self.forward(x, 1)
+            if self.position % BLOCK == 0:
+                self.evict(budget, recent)
+        return y
 
     def evict(self, budget, recent):
         batch = qlm.KvBatch(self.table, self.lengths)
@@ -140,21 +157,14 @@ def measure(model, layers, batch, prompt, budget, recent, steps, memory):
 
     x = rnd(batch * prompt)
     inst.forward(x, prompt)                        # first use: workspaces, memory
-    inst.lengths.zero_()
-    inst.next.zero_()
+    inst.restart()
     prefill = timed(lambda: inst.forward(x, prompt)) / batch
 
     y = rnd(batch)
 
-    def decode():
-        for _ in range(steps):
-            inst.forward(y, 1)
-            if int(inst.next[0]) % BLOCK == 0:     # a block is full: cut to the budget
-                inst.evict(budget, recent)
-
     inst.evict(budget, recent)
     inst.forward(y, 1)
-    seconds = timed(decode) / steps
+    seconds = timed(lambda: inst.decode(y, steps, budget, recent)) / steps
     assert bool(torch.isfinite(inst.forward(y, 1)).all())
     return {"prefill": prefill, "decode_time": seconds,
             "kv_tokens": (memory - model.weight_bytes(layers)) / model.token_bytes(layers),

@@ -64,3 +64,25 @@ def test_layers_have_weights_of_their_own(example, monkeypatch):
                   "--budget", "64", "--recent", "8", "--steps", "2", "--plans", "64"])
     # the first pass: a prompt through three layers of four matrices
     assert len(set(seen[:12])) == 12 and set(seen) == set(seen[:12])
+
+
+def test_decode_does_not_wait(example, monkeypatch):
+    """Decode steps and cuts are queued without a read of device memory, whose wait would
+    be timed with them; lengths and positions as counted by the host."""
+    import torch
+    monkeypatch.undo()                   # (the tests' filling of fresh memory waits for it)
+    model = example.Model(128, 4, 2, 32, 256, layers=2)
+    inst = example.Instance(model, 2, 3, 192)
+    x = torch.randn((3, 128), device="cuda", dtype=torch.bfloat16)
+    inst.forward(x.repeat_interleave(60, 0), 60)
+    inst.evict(64, 8)
+    inst.decode(x, 1, 64, 8)
+    torch.cuda.synchronize()
+    torch.cuda.set_sync_debug_mode("error")
+    try:
+        inst.decode(x, 80, 64, 8)
+    finally:
+        torch.cuda.set_sync_debug_mode("default")
+    assert inst.position == 141 and inst.next.cpu().tolist() == [141] * 3
+    # cut to 64 at 128 tokens, then 13 more
+    assert inst.lengths.cpu().tolist() == [77] * 3
