@@ -139,4 +139,8 @@ int check_batch(const qlm_kv_batch *b);
 int check_rows(const qlm_rows *r, const char *what);
 int check_workspace(const void *ws, size_t have, size_t need);
 
+// Whether so many workgroups can be launched: fewer than 2^32 threads in a dimension.  Asked
+// of every launch of a call before the first one, as a call is done whole or not at all.
+inline bool can_launch(int64_t groups, int threads) { return groups < (1ll << 32) / threads; }
+
 }  // namespace qlm_kv

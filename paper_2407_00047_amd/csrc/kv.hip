@@ -732,18 +732,23 @@ template <int FMT, int ND> void launch_move(const EvictArgs &a, int waves, unsig
         k_evict_move<FMT, ND, 4><<<grid, 256, bytes, st>>>(a);
 }
 
-template <int FMT> void launch_move(const EvictArgs &a, int max_length, unsigned grid, hipStream_t st)
+template <int FMT> void launch_move(const EvictArgs &a, int waves, unsigned grid, hipStream_t st)
 {
-    // two waves to a block where at most a quarter of its slots can fall free (4 of
-    // 64, 8192 blocks: 31 us, four waves 36), four where more can (48 of 64, 3072
-    // blocks: 48 us, two waves 62)
-    const int waves = max_length - a.budget <= a.budget / 4 ? 2 : 4;
     if (a.c.D <= 64)
         launch_move<FMT, 1>(a, waves, grid, st);
     else if (a.c.D <= 128)
         launch_move<FMT, 2>(a, waves, grid, st);
     else
         launch_move<FMT, 4>(a, waves, grid, st);
+}
+
+// Waves to a block of k_evict_move.
+int move_waves(int max_length, int budget)
+{
+    // two waves to a block where at most a quarter of its slots can fall free (4 of
+    // 64, 8192 blocks: 31 us, four waves 36), four where more can (48 of 64, 3072
+    // blocks: 48 us, two waves 62)
+    return max_length - budget <= budget / 4 ? 2 : 4;
 }
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
@@ -796,7 +801,7 @@ int qlm_kv_append(const qlm_kv_cache *cache, const qlm_kv_batch *batch, const ql
     const int64_t have = ((int64_t)batch->max_length + kBlock - 1) / kBlock;
     a.touched = (int32_t)(most < have ? most : have);
     const int64_t grid = (int64_t)batch->n_seqs * a.touched * a.c.H;
-    if (grid > INT32_MAX) return fail(QLM_ERR_CAPACITY, "too many blocks in one append");
+    if (!can_launch(grid, kThreads)) return fail(QLM_ERR_CAPACITY, "too many blocks in one append");
     a.k_wide = (uintptr_t)a.k % 16 == 0 && a.k_row % 8 == 0 && a.k_head % 8 == 0;
     a.v_wide = (uintptr_t)a.v % 16 == 0 && a.v_row % 8 == 0 && a.v_head % 8 == 0;
     const bool e4m3 = cache->format == QLM_KV_E4M3;
@@ -851,8 +856,10 @@ int qlm_kv_evict(const qlm_kv_cache *cache, const qlm_kv_batch *batch, int32_t b
     a.out = lengths_out;
     const int64_t sh = (int64_t)batch->n_seqs * a.c.H;
     const int64_t grid = sh * (budget / kBlock);
-    if (grid > INT32_MAX) return fail(QLM_ERR_CAPACITY, "too many blocks in one eviction");
     const int blocks = a.slots / kBlock;        // of the longest sequence
+    const int waves = move_waves(batch->max_length, budget);
+    if (!can_launch(grid, 64 * waves) || !can_launch(sh, blocks <= 4 * 8 ? 256 : 1024))
+        return fail(QLM_ERR_CAPACITY, "too many blocks in one eviction");
     const unsigned n = (unsigned)sh;
     // few blocks: four waves, more workgroups to a CU (64 sequences of 2048, 8 heads, with
     // the move 21 us; sixteen waves 26; 128 of 512 17 and 35; 8 of 1024 11 and 11)
@@ -869,9 +876,9 @@ int qlm_kv_evict(const qlm_kv_cache *cache, const qlm_kv_batch *batch, int32_t b
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return hip_fail(e, "k_evict_select launch");
     if (cache->format == QLM_KV_E4M3)
-        launch_move<QLM_KV_E4M3>(a, batch->max_length, (unsigned)grid, stream);
+        launch_move<QLM_KV_E4M3>(a, waves, (unsigned)grid, stream);
     else
-        launch_move<QLM_KV_INT8>(a, batch->max_length, (unsigned)grid, stream);
+        launch_move<QLM_KV_INT8>(a, waves, (unsigned)grid, stream);
     e = hipGetLastError();
     return e == hipSuccess ? QLM_OK : hip_fail(e, "k_evict_move launch");
 }

@@ -1387,6 +1387,17 @@ int qlm_kv_attention(const qlm_kv_cache *cache, const qlm_kv_batch *batch,
         (int64_t)batch->max_new * batch->n_seqs * query->n_heads > INT32_MAX ||
         (int64_t)batch->n_rows * query->n_heads > INT32_MAX)
         return fail(QLM_ERR_CAPACITY, "too many rows or blocks in one call");
+    const bool weights = query->accumulate && batch->max_length > 0;
+    const int64_t row_groups = ((int64_t)batch->n_rows * a.G + kQueryCols - 1) / kQueryCols;
+    const int64_t joined = (int64_t)batch->n_seqs * batch->max_new * query->n_heads;
+    if ((p.few && !can_launch(sh * ((few + kWaves - 1) / kWaves), kThreads)) ||
+        (p.few && weights && !can_launch((sh * p.blocks + kWaves - 1) / kWaves, kThreads)) ||
+        (p.many && batch->n_rows > 0 &&
+         (!can_launch(row_groups * a.H, kThreads) ||
+          !can_launch(sh * (((int64_t)p.cols + 127) / 128), kThreads) ||
+          (p.splits > 1 && !can_launch((joined + kWaves - 1) / kWaves, kThreads)) ||
+          (weights && !can_launch(sh * p.blocks, kThreads)))))
+        return fail(QLM_ERR_CAPACITY, "too many rows or blocks in one call: a launch of 2^32 threads");
     hipError_t e;
     if (batch->n_rows > 0 && p.few) {
         const int64_t wg = (std::min<int64_t>(p.workers, units) + kWaves - 1) / kWaves;
@@ -1415,7 +1426,7 @@ int qlm_kv_attention(const qlm_kv_cache *cache, const qlm_kv_batch *batch,
             if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_prompt_join launch");
         }
     }
-    if (query->accumulate && batch->max_length > 0) {
+    if (weights) {
         if (p.few) {
             const int64_t wg = (sh * p.blocks + kWaves - 1) / kWaves;
             k_attend_weights<<<(unsigned)wg, kThreads, 0, stream>>>(a);

@@ -535,7 +535,8 @@ int qlm_w4_pack(const qlm_w4 *weight, const uint8_t *codes, const void *scale,
     a.scale = (const uint16_t *)scale;
     a.packed = (uint8_t *)weight->packed;
     const int64_t grid = (int64_t)a.tiles * a.steps;
-    if (grid > INT32_MAX) return fail(QLM_ERR_CAPACITY, "the matrix is too large");
+    // (a launch holds fewer than 2^32 threads)
+    if (grid >= (1ll << 32) / 64) return fail(QLM_ERR_CAPACITY, "the matrix is too large");
     k_w4_pack<<<(unsigned)grid, 64, 0, (hipStream_t)stream_>>>(a);
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? QLM_OK : hip_fail(e, "k_w4_pack launch");

@@ -131,6 +131,38 @@ def test_attention_capacity(qlm, lib):
                              P(rows(qlm)), P(rows(qlm)), None, None) == qlm.QLM_ERR_CAPACITY
 
 
+def test_launches_of_too_many_threads(qlm, lib):
+    """A call whose last launch would have 2^32 threads is refused before its first one."""
+    big = 1 << 62
+    q = qlm.KvQuery(rows(qlm), rows(qlm, data=A + 4096), 8, 0.1, 1, 0.0)
+    c = cache(qlm, n_kv_heads=8)
+    # the weights of prompts: a workgroup of 256 to each of 8 heads and 2^21 blocks
+    b = batch(qlm, n_seqs=1, n_rows=100, max_new=100, max_length=1 << 27, table_stride=1 << 21,
+              row_start=A)
+    assert lib.qlm_kv_attention(P(c), P(b), P(q), A, big, None) == qlm.QLM_ERR_CAPACITY
+    assert b"threads" in lib.qlm_last_error()
+    # prompts: to each of 8 heads, 16 sequences and 2^17 tiles of 128 columns
+    b = batch(qlm, n_seqs=16, n_rows=17, max_new=1 << 24, max_length=100, row_start=A)
+    assert lib.qlm_kv_attention(P(c), P(b), P(q), A, big, None) == qlm.QLM_ERR_CAPACITY
+    # queries: to each 32 columns
+    b = batch(qlm, n_seqs=1, n_rows=1 << 24, max_new=1 << 23, max_length=100, row_start=A)
+    q4 = qlm.KvQuery(rows(qlm), rows(qlm, data=A + 4096), 64, 0.1, 0, 0.0)
+    assert lib.qlm_kv_attention(P(c), P(b), P(q4), A, big, None) == qlm.QLM_ERR_CAPACITY
+    # appends: to each of 8 heads and 2^21 blocks
+    b = batch(qlm, n_seqs=128, n_rows=1 << 20, max_new=1 << 20, max_length=1 << 20,
+              table_stride=1 << 14, row_start=A)
+    assert lib.qlm_kv_append(P(c), P(b), P(rows(qlm)), P(rows(qlm)), None, None) == \
+        qlm.QLM_ERR_CAPACITY
+    # evictions: two waves to each of 8 heads and 2^22 blocks; sixteen to each of 2^22 heads
+    b = batch(qlm, n_seqs=1 << 8, n_rows=1 << 8, max_length=1 << 20, table_stride=1 << 14)
+    assert lib.qlm_kv_evict(P(c), P(b), 1 << 20, 0, A, A, big, None) == qlm.QLM_ERR_CAPACITY
+    b = batch(qlm, n_seqs=1 << 19, n_rows=1 << 19, max_length=1 << 12, table_stride=1 << 6)
+    assert lib.qlm_kv_evict(P(c), P(b), 64, 0, A, A, big, None) == qlm.QLM_ERR_CAPACITY
+    # packing: a wave to each 16 outputs and 128 inputs
+    w = qlm.W4Struct(1 << 24, 1 << 13, 128, A)
+    assert lib.qlm_w4_pack(P(w), A, A, None, None) == qlm.QLM_ERR_CAPACITY
+
+
 def test_evict_checks(qlm, lib):
     c, b = cache(qlm), batch(qlm)
     need = lib.qlm_kv_evict_workspace_bytes(P(c), P(b), 64)
