@@ -597,7 +597,11 @@ int qlm_kv_append(const qlm_kv_cache *cache, const qlm_kv_batch *batch, const ql
  *   q, out  [n_rows][n_heads][head_dim], the same dtype; out may not alias q
  *   ws      device workspace of at least qlm_kv_attention_workspace_bytes for
  *           this batch's sizes (larger sizes may need less: the work is split
- *           less), 256-byte aligned, scratch
+ *           less), 256-byte aligned, scratch.  Most of it, with `accumulate`, are
+ *           the scores of sequences of few rows, 256 bytes for each row, head and
+ *           block of the longest sequence; with sequences of more than 64 rows and
+ *           heads to a kv head beside them 16 KiB for each kv head and block, up to
+ *           4 GiB (or one sequence's, where that is more) at a time
  */
 typedef struct qlm_kv_query {
     qlm_rows q, out;

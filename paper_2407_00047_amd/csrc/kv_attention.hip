@@ -1193,8 +1193,16 @@ constexpr int kFew = 64;
 // ones with weights 81 and 89.
 constexpr int kWorkers = 1024, kManyItems = 128;
 
+// Scores held at once where prompts and few rows share a call.  A sequence of few rows
+// then has room for kFew columns in every block up to the longest one's, whatever it uses:
+// 192 sequences of 16000 slots beside a prompt would need 6.4 GB.  The sequences go in as many
+// passes as the scores do; a pass costs some 35 us (that call, 64 heads: 1466 us in one, 1502
+// in two, 1535 in three; 128 of 12000, 32 heads, 3.2 GB: 688 in one, 729 in two).
+constexpr int64_t kScoreBytes = 4ll << 30;
+
 struct Plan {
     int nt, tile, workers, cols, blocks, splits, shares;
+    int at_once;                 // sequences of few rows in a pass
     bool few, many;              // which sequences there can be
     size_t part_o, part_ts, done, s, qh, qfac, split_o, split_ts, share, total;
 };
@@ -1212,6 +1220,7 @@ Plan plan_of(const qlm_kv_cache *c, const qlm_kv_batch *b, int32_t n_heads, bool
     const bool twice = (weights || c->head_dim <= 64) && c->head_dim <= 128 && p.nt == 1 &&
                        (int64_t)b->n_seqs * c->n_kv_heads >= kManyItems;
     p.workers = twice ? 2 * kWorkers : kWorkers;
+    p.at_once = b->n_seqs;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -1222,9 +1231,12 @@ Plan plan_of(const qlm_kv_cache *c, const qlm_kv_batch *b, int32_t n_heads, bool
     if (p.few) {
         p.part_o = take((size_t)2 * p.workers * p.tile * c->head_dim * 4);
         p.part_ts = take((size_t)2 * p.workers * p.tile * sizeof(TopSum));
-        if (weights)
-            p.s = take((size_t)b->n_seqs * p.blocks * c->n_kv_heads * std::min(p.cols, kFew) *
-                       kBlock * 4);
+        if (weights) {
+            const int64_t one = (int64_t)p.blocks * c->n_kv_heads * std::min(p.cols, kFew) * kBlock * 4;
+            if (p.many)
+                p.at_once = (int)std::max<int64_t>(1, std::min<int64_t>(b->n_seqs, kScoreBytes / one));
+            p.s = take((size_t)p.at_once * one);
+        }
     }
     p.splits = 1;
     if (p.many) {
@@ -1399,22 +1411,38 @@ int qlm_kv_attention(const qlm_kv_cache *cache, const qlm_kv_batch *batch,
           (weights && !can_launch(sh * p.blocks, kThreads)))))
         return fail(QLM_ERR_CAPACITY, "too many rows or blocks in one call: a launch of 2^32 threads");
     hipError_t e;
-    if (batch->n_rows > 0 && p.few) {
-        const int64_t wg = (std::min<int64_t>(p.workers, units) + kWaves - 1) / kWaves;
-        if (e4m3)
-            launch_rows<QLM_KV_E4M3>(a, p.nt, wg, stream);
-        else
-            launch_rows<QLM_KV_INT8>(a, p.nt, wg, stream);
-        if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_attend_rows launch");
-        // few columns: a workgroup to each, as their parts may be many (32 columns of
-        // 16384 tokens: 26 us with the rows, a wave to each 55; 512 columns 31 and 33;
-        // 4096 columns 61 and 53)
-        if (sh * few <= 1024)
-            k_attend_join<kWaves><<<(unsigned)(sh * few), kThreads, 0, stream>>>(a);
-        else
-            k_attend_join<1><<<(unsigned)(sh * ((few + kWaves - 1) / kWaves)), kThreads, 0,
-                               stream>>>(a);
-        if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_attend_join launch");
+    for (int s0 = 0; p.few && s0 < batch->n_seqs; s0 += p.at_once) {
+        AttnArgs f = a;                          // the pass's sequences
+        f.q.n_seqs = std::min(p.at_once, batch->n_seqs - s0);
+        if (s0 > 0) {                            // (rows are counted through row_start then)
+            f.q.table += s0 * f.q.table_stride;
+            f.q.lengths += s0;
+            f.q.row_start += s0;
+        }
+        const int64_t fh = (int64_t)f.q.n_seqs * a.H;
+        if (batch->n_rows > 0) {
+            const int64_t fu = fh * ((few + p.tile - 1) / p.tile) * p.blocks;
+            const int64_t wg = (std::min<int64_t>(p.workers, fu) + kWaves - 1) / kWaves;
+            if (e4m3)
+                launch_rows<QLM_KV_E4M3>(f, p.nt, wg, stream);
+            else
+                launch_rows<QLM_KV_INT8>(f, p.nt, wg, stream);
+            if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_attend_rows launch");
+            // few columns: a workgroup to each, as their parts may be many (32 columns of
+            // 16384 tokens: 26 us with the rows, a wave to each 55; 512 columns 31 and 33;
+            // 4096 columns 61 and 53)
+            if (fh * few <= 1024)
+                k_attend_join<kWaves><<<(unsigned)(fh * few), kThreads, 0, stream>>>(f);
+            else
+                k_attend_join<1><<<(unsigned)(fh * ((few + kWaves - 1) / kWaves)), kThreads, 0,
+                                   stream>>>(f);
+            if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_attend_join launch");
+        }
+        if (weights) {
+            k_attend_weights<<<(unsigned)((fh * p.blocks + kWaves - 1) / kWaves), kThreads, 0,
+                               stream>>>(f);
+            if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_attend_weights launch");
+        }
     }
     if (batch->n_rows > 0 && p.many) {
         a.D <= 64 ? launch_many<1>(a, e4m3, stream)
@@ -1426,21 +1454,16 @@ int qlm_kv_attention(const qlm_kv_cache *cache, const qlm_kv_batch *batch,
             if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_prompt_join launch");
         }
     }
-    if (weights) {
-        if (p.few) {
-            const int64_t wg = (sh * p.blocks + kWaves - 1) / kWaves;
-            k_attend_weights<<<(unsigned)wg, kThreads, 0, stream>>>(a);
-        }
-        if (p.many && batch->n_rows > 0)
-            a.D <= 64 ? launch_colsum<1>(a, e4m3, stream)
-                      : a.D <= 128 ? launch_colsum<2>(a, e4m3, stream)
-                                   : launch_colsum<4>(a, e4m3, stream);
-        if (p.many && batch->n_rows > 0 && p.shares > 1) {
-            if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_attend_colsum launch");
+    if (weights && p.many && batch->n_rows > 0) {
+        a.D <= 64 ? launch_colsum<1>(a, e4m3, stream)
+                  : a.D <= 128 ? launch_colsum<2>(a, e4m3, stream)
+                               : launch_colsum<4>(a, e4m3, stream);
+        if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_attend_colsum launch");
+        if (p.shares > 1) {
             k_colsum_join<<<(unsigned)((sh * p.blocks + kWaves - 1) / kWaves), kThreads, 0,
                             stream>>>(a);
+            if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_colsum_join launch");
         }
-        if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "weight launch");
     }
     return QLM_OK;
 }

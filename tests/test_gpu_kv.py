@@ -233,6 +233,30 @@ def test_attend_rows_and_weights(torch, qlm, fmt, dtype, d, kv, g, counts):
     assert torch.equal(got, qlm.kv_attention(s.cache, b, q, scale=scale))
 
 
+@pytest.mark.parametrize("counts", [[1, 0, 70, 1, 3, 1, 0, 1, 2], [200, 1, 1, 1, 1, 1, 1, 1, 1],
+                                    [1, 2, 3, 4, 5, 6, 7, 8, 90]])
+def test_attend_scores_in_passes(torch, qlm, counts):
+    """Prompts beside few rows whose scores, sized for 2^20 slots of 4 heads, are formed for
+    four sequences at a time."""
+    kv, d, g = 4, 64, 2
+    s = Setup(torch, qlm, [300, 65, 130, 1, 64, 700, 90, 2, 128], kv, d, "e4m3", seed=sum(counts))
+    ora = s.fill()
+    wide = torch.full((9, 1 << 14), -1, dtype=torch.int32, device="cuda")
+    wide[:, :s.table.shape[1]] = s.dev_table
+    s.dev_table = wide
+    b = s.batch(counts)
+    q, qx = s.rows(sum(counts), kv * g, "bf16", 1.5)
+    for decay in (0.0, 0.5):
+        want, bound, wb = ora.attend(s.table, s.lengths, counts, qx, 0.125, decay)
+        check(qlm.kv_attention(s.cache, b, q, scale=0.125, weight_decay=decay), want, bound, "bf16",
+              decay)
+        now = s.cache.weight.double().cpu().numpy()
+        assert (np.isnan(now) == np.isnan(ora.weight)).all()
+        off = np.abs(now - ora.weight) - wb
+        assert not (off > 0).any(), (decay, float(np.nanmax(off)))
+        ora.weight = now
+
+
 @pytest.mark.parametrize("fmt,g,n", [("e4m3", 8, 1), ("int8", 2, 1), ("e4m3", 4, 4)])
 def test_attend_long(torch, qlm, fmt, g, n):
     """Long axes, split over workgroups and joined."""

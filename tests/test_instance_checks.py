@@ -131,6 +131,25 @@ def test_attention_capacity(qlm, lib):
                              P(rows(qlm)), P(rows(qlm)), None, None) == qlm.QLM_ERR_CAPACITY
 
 
+def test_workspace_of_prompts_beside_steps(qlm, lib):
+    """One prompt joins a decode step whose weights are kept: the scores' room does not
+    grow with the sequences without end."""
+    c = cache(qlm, n_blocks=48000, n_kv_heads=8, head_dim=128)
+    need = lib.qlm_kv_attention_workspace_bytes
+
+    def mixed(seqs, length):
+        b = batch(qlm, n_seqs=seqs, n_rows=seqs - 1 + 2000, max_new=2000, max_length=length,
+                  table_stride=length // 64, row_start=A)
+        return need(P(c), P(b), 64, 1)
+
+    assert mixed(48, 4096) < 1 << 30
+    for seqs, length in ((192, 16000), (1000, 16000), (192, 100032)):
+        # (beside the scores: rows laid out, parts and splits)
+        assert mixed(seqs, length) < (4 << 30) + (1 << 28)
+    # one sequence's scores are the least
+    assert mixed(3, 1 << 22) < (8 << 30) + (1 << 28)
+
+
 def test_launches_of_too_many_threads(qlm, lib):
     """A call whose last launch would have 2^32 threads is refused before its first one."""
     big = 1 << 62
