@@ -6,9 +6,11 @@
 // shift and one and-or for two codes).  No weight is ever rounded:
 //  - up to 16 rows, with one group's sums S = sum of x, T[n] = sum of (16 + c[n]) x,
 //    both by the matrix instructions (S with a matrix of ones), the group's part of
-//    the output is s[n] (T[n] - (16 + z[n]) S), formed in single precision.  Of bfloat16
-//    both sums are taken 2^-13 times as large, by the constants' exponents: T of 128
-//    inputs would pass single precision's range from x = 2^116 on;
+//    the output is s[n] (T[n] - (16 + z[n]) S), formed in single precision: T is up to some six
+//    times the sum of |c - z| |x|, whose bits the difference loses.  Of bfloat16 all is held
+//    times 2^-kDown, by the constants' exponents, and the output raised again: a T
+//    of x from 2^116 on would pass single precision's range.  What the smallest numbers lose
+//    by that, 2^-138 an addition, is below the least bfloat16 (2^-133);
 //  - for more rows 16 + z is taken off in half precision (exact: -15 .. 15), once for
 //    all of them, and the part is s[n] T[n].  Rows of bfloat16 are first scaled by
 //    powers of two to fit halves.
@@ -99,18 +101,19 @@ template <bool BF> __device__ inline float4v mfma(uint4 x, uint4 y, float4v c)
                                                   __builtin_bit_cast(half8v, y), c, 0, 0, 0);
 }
 
-constexpr float kRaise = 8192.f;     // takes out the 2^-13 of bfloat16's sums
+// 31 GROUP 2^-kDown < 1: the sum of a group's (16 + c) x is finite with every x.
+template <bool BF, int GROUP> constexpr int kDown = !BF ? 0 : GROUP == 32 ? 10 : GROUP == 64 ? 11 : 12;
 
-// The exponent of 16 (of bfloat16, of 16 * 2^-13) for two numbers, in a register (an
-// and-or takes one constant from the scalar side only).
-template <bool BF> __device__ inline uint32_t sixteen()
+// The exponent of 16 * 2^-kDown for two numbers, in a register (an and-or takes one constant
+// from the scalar side only).
+template <bool BF, int GROUP> __device__ inline uint32_t sixteen()
 {
-    uint32_t c = BF ? 0x3b003b00u : 0x4c004c00u;
+    uint32_t c = BF ? (127 + 4 - kDown<BF, GROUP>) * 0x00800080u : 0x4c004c00u;
     asm("" : "+v"(c));
     return c;
 }
 
-// The eight codes of a dword as 16 + c (times 2^-13 of bfloat16).
+// The eight codes of a dword as 16 + c (times 2^-kDown).
 template <bool BF> __device__ inline uint4 operand(uint32_t w, uint32_t c)
 {
     if (BF)
@@ -120,21 +123,20 @@ template <bool BF> __device__ inline uint4 operand(uint32_t w, uint32_t c)
             (w >> 2 & 0x03c003c0u) | c, (w >> 6 & 0x03c003c0u) | c};
 }
 
-// Ones (2^-13 of bfloat16).
-template <bool BF> __device__ inline uint4 ones()
+// Ones (times 2^-kDown).
+template <bool BF, int GROUP> __device__ inline uint4 ones()
 {
-    const uint32_t o = BF ? 0x39003900u : 0x3c003c00u;
+    const uint32_t o = BF ? (127 - kDown<BF, GROUP>) * 0x00800080u : 0x3c003c00u;
     return {o, o, o, o};
 }
 
-// sum += scale (t - zero S) for the four outputs of a lane (the 2^-13 is taken out of
-// the scale: the sum then keeps small rows' bits, and t - zero S may not fit without)
-template <bool BF> __device__ inline float4v add_group(float4v sum, float4v t, float S, uint4 meta)
+// sum += scale (t - zero S) for the four outputs of a lane
+__device__ inline float4v add_group(float4v sum, float4v t, float S, uint4 meta)
 {
     const uint32_t w[4] = {meta.x, meta.y, meta.z, meta.w};
     for (int i = 0; i < 4; ++i) {
         const half2v h = __builtin_bit_cast(half2v, w[i]);
-        sum[i] = fmaf(BF ? (float)h[0] * kRaise : (float)h[0], fmaf(-(float)h[1], S, t[i]), sum[i]);
+        sum[i] = fmaf((float)h[0], fmaf(-(float)h[1], S, t[i]), sum[i]);
     }
     return sum;
 }
@@ -190,7 +192,7 @@ template <bool BF, int GROUP> __global__ __launch_bounds__(kThreads) void k_w4_t
     const uint8_t *base = a.packed + (int64_t)tile * a.steps * cb;
     const int ld = a.per_stage * kStep + 8;      // elements of a row in shared memory
     const int mine = c16 < a.M ? c16 : 0;
-    const uint32_t c16f = sixteen<BF>();
+    const uint32_t c16f = sixteen<BF, GROUP>();
     float4v sum = {0.f, 0.f, 0.f, 0.f};
     uint4 cw[PF], mw[PF][PER];
     auto fetch = [&](int u, int kb) {
@@ -226,9 +228,9 @@ template <bool BF, int GROUP> __global__ __launch_bounds__(kThreads) void k_w4_t
                     for (int j = q * SUB; j < (q + 1) * SUB; ++j) {
                         const uint4 b = *(const uint4 *)(xp + 32 * j);
                         t = mfma<BF>(operand<BF>(w[j], c16f), b, t);
-                        S = mfma<BF>(ones<BF>(), b, S);
+                        S = mfma<BF>(ones<BF, GROUP>(), b, S);
                     }
-                    sum = add_group<BF>(sum, t, S[0], mw[u][q]);
+                    sum = add_group(sum, t, S[0], mw[u][q]);
                 }
                 fetch(u, kb + kWaves * PF);
             }
@@ -243,7 +245,7 @@ template <bool BF, int GROUP> __global__ __launch_bounds__(kThreads) void k_w4_t
     float v = 0.f;
     for (int w = 0; w < kWaves; ++w) v += red[w * 256 + threadIdx.x];
     const int m = threadIdx.x >> 4, n = tile * 16 + (threadIdx.x & 15);
-    if (m < a.M && n < a.N) a.out[m * a.out_stride + n] = out_bits(v, BF);
+    if (m < a.M && n < a.N) a.out[m * a.out_stride + n] = out_bits(v * (1 << kDown<BF, GROUP>), BF);
 }
 
 // Rows for k_w4_wide: halves, 16-byte aligned, zeros up to a whole number of stages.
@@ -312,7 +314,7 @@ template <int GROUP, int NT> __global__ __launch_bounds__(kThreads, 2) void k_w4
     const int cb = chunk_bytes(GROUP);
     const bool mine = tile < a.tiles;
     const uint8_t *base = a.packed + (int64_t)(mine ? tile : 0) * a.steps * cb;
-    const uint32_t c16f = sixteen<false>();
+    const uint32_t c16f = sixteen<false, GROUP>();
     float4v sum[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) sum[t] = float4v{0.f, 0.f, 0.f, 0.f};
