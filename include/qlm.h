@@ -536,7 +536,9 @@ typedef struct qlm_kv_cache {
  * slot.  A block belongs to one sequence.  The device arrays are not checked by
  * the calls, but nothing is read or written out of bounds for any content:
  * lengths are clamped to [0, max_length], rows to [0, n_rows) and max_new, and
- * block numbers outside [0, n_blocks) name no slots.
+ * block numbers outside [0, n_blocks) name no slots.  Sizes of which a launch
+ * would have 2^32 threads are refused (QLM_ERR_CAPACITY): they grow with n_seqs
+ * n_kv_heads and max_new, budget or max_length, however short the sequences are.
  */
 typedef struct qlm_kv_batch {
     int32_t n_seqs;              /* >= 0                                         */
@@ -589,9 +591,11 @@ int qlm_kv_append(const qlm_kv_cache *cache, const qlm_kv_batch *batch, const ql
  * (the old weight is not read when weight_decay is 0).  Slots that a row does
  * not see have no part in its result, whatever they hold.  Scores, their
  * maxima and sums, weights and outputs are formed in single precision from
- * exact products; p, times the ratio of the block's value scale to the largest
- * one so far, is rounded to half precision (relative to the running maximum) for
- * the sum over values: below 2^-20 of the largest such product bits are lost.
+ * exact products of codes and queries (a row of bfloat16 is held in half precision,
+ * scaled by a power of two: elements below 2^-29 of the row's largest lose bits).
+ * For the sum over values p, times the ratio of the block's value scale to the
+ * largest one so far, is rounded to half precision, 11 bits of it; below 2^-20
+ * of a slot with the greatest score so far and the largest scale, fewer.
  * Bit-for-bit reproducible for the same
  * inputs and sizes.
  *   q, out  [n_rows][n_heads][head_dim], the same dtype; out may not alias q
@@ -664,15 +668,18 @@ int qlm_w4_pack(const qlm_w4 *weight, const uint8_t *codes, const void *scale,
 
 /*
  * out[m][n] = sum over k of x[m][k] * weight[n][k], the sums in single
- * precision from exact products within a group, rounded once.  A row of x that
+ * precision from exact products within a group, rounded once; of few rows a
+ * group's sum is the difference of sums over (16 + c) x and (16 + z) x, whose size
+ * its error goes by.  A row of x that
  * holds an infinity or a NaN may have any of its outputs infinite or NaN.  Over
  * many rows or outputs a row of bfloat16 is held in half precision, scaled by a
  * power of two: elements below 2^-29 of the row's largest lose bits.
  *   x    [n_rows][n_in], x_stride elements between rows (>= n_in)
  *   out  [n_rows][n_out], out_stride elements between rows; of x's dtype, may
  *        not alias x
- *   ws   device workspace of at least qlm_w4_workspace_bytes, 256-byte aligned,
- *        scratch; may be NULL when that is 0
+ *   ws   device workspace of at least qlm_w4_workspace_bytes for this number of
+ *        rows (more rows may need less), 256-byte aligned, scratch; may be NULL
+ *        when that is 0
  */
 size_t qlm_w4_workspace_bytes(const qlm_w4 *weight, int32_t n_rows);
 int qlm_w4_matmul(const qlm_w4 *weight, const void *x, int64_t x_stride, void *out,

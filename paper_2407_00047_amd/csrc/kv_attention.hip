@@ -19,7 +19,10 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr float kLog2e = 1.44269504088896340736f;
 // p = 2^(s - m), in which s may pass the running maximum m by kSlack before the
 // sums are rescaled.  As a half it is held kRaised times as large: p < 2^14 then
-// fits, and a p down to 2^-20 of the maximum is a normal one.
+// fits, and a p down to 2^-20 of the maximum is a normal one.  Half precision because
+// the second product runs on 16-bit matrix instructions as the first does: 2^-11 of each p,
+// below what rounding an output to bfloat16 costs, and seen beside a half's (an error of
+// 0.00027 where rounding alone gives 0.00021: 192 sequences of up to 16000).
 constexpr float kSlack = 8.f, kRaised = 64.f;
 
 // A column's running maximum m and its sum l of 2^(s - m), apart: their common
@@ -141,7 +144,8 @@ __device__ inline void load_query(const AttnArgs &a, int64_t row, int head, bool
 
 // The row as matrix operands: half m of chunk c holds the dims c * 64 + g * 16 +
 // m * 8 .. + 8.  A row of bfloat16 is scaled by a power of two so that it fits
-// halves; the result takes that out of the score.
+// halves, which the codes are turned into by one instruction for two; the result takes that
+// out of the score.  Its elements below 2^-29 of the largest lose bits.
 template <int ND>
 __device__ inline float query_halves(const AttnArgs &a, const Query<ND> &q, half8v (&qf)[ND][2])
 {
@@ -279,8 +283,10 @@ struct Cursor {
 // one's scores are formed, its values as soon as this one's are added, so that
 // loads are always under way.
 // Bound by the cache's bytes: 192 ragged sequences of up to 16000 (3.2 GB, 8 kv heads of
-// 128) 546 us, 5.8 TB/s; two of up to 150000 74 (5.1); 48 ragged ones of up to 4096 that write
-// their scores 60 us (3.5 TB/s); one of 700 9 us, a launch and its dependent reads.
+// 128) 545 us, 5.8 TB/s; two of up to 150000 74 (5.1); 48 ragged ones of up to 4096 that write
+// their scores 60 us (3.5 TB/s: runs are rounded up, there to 7 units where a wave's part
+// is 6.07, and an eighth of the waves has none; the scores are a sixteenth of the bytes); one
+// of 700 9 us, a launch and its dependent reads.
 template <int FMT, int ND, int NT>
 __global__ __launch_bounds__(kThreads, ND * NT <= 2 ? 2 : 1) void k_attend_rows(AttnArgs a)
 {
@@ -696,7 +702,7 @@ typedef float float16v __attribute__((ext_vector_type(16)));
 
 // Queries in half precision, dims padded with zeros to whole 64s, in the order of
 // the matrix operands (8 dims of a column after the next column's): scaled by a
-// power of two where they come in bfloat16 (load_query), negated where the scale
+// power of two where they come in bfloat16 (query_halves), negated where the scale
 // of the scores is negative.  A workgroup to 32 columns of a kv head, 8 dims to a thread, which
 // pass through shared memory into runs of 512 bytes.  Bound by its bytes; 5 ragged
 // prompts of up to 2000, 32 heads of 128 (79 MB) 17 us, 4.7 TB/s; a wave to a
@@ -1045,8 +1051,10 @@ __global__ __launch_bounds__(kThreads) void k_prompt_join(AttnArgs a)
 // the scores of the columns that see it again, a wave every fourth 32, the next
 // ones' queries on their way meanwhile, and add up their probabilities.  (Kept
 // scores would be four bytes for each column and slot, gigabytes of them.)
-// Bound by the exponentials, one for each 256 operations of the product at 128 dims, and the
-// reads of queries from L2: 128 us for the prompts of k_attend_prompt's figure.
+// No one rate bounds it: for the prompts of k_attend_prompt's figure 129 us, of which the
+// product would take 42 at a large product's rate and the 201 million exponentials some 20;
+// a wave forms product, exponentials and sums in turn, two waves to a SIMD, and every
+// workgroup reads its columns' queries from L2 again (0.8 GB in all).
 template <int FMT, int ND>
 __global__ __launch_bounds__(kThreads, ND <= 2 ? 2 : 1) void k_attend_colsum(AttnArgs a)
 {
