@@ -496,7 +496,8 @@ int qlm_apply_profile(const qlm_problem *problem, const qlm_profile *profile,
  * memory holds; these calls are what an MI355X instance spends that time and
  * memory on, so that a class of such instances can be measured instead of
  * described: a token cache held in 8 bits (written, attended to, cut to a
- * budget) and products with 4-bit weights.
+ * budget), products with 4-bit and 8-bit weights, and the verification of drafted
+ * tokens.
  *
  * The cache is a pool of blocks of QLM_KV_BLOCK slots.  For every block and kv
  * head it holds a code of 8 bits for each slot and dim of keys and values, one
@@ -511,7 +512,8 @@ int qlm_apply_profile(const qlm_problem *problem, const qlm_profile *profile,
  */
 #define QLM_KV_BLOCK 64
 
-enum { QLM_F16 = 0, QLM_BF16 = 1 };           /* types of rows                 */
+enum { QLM_F16 = 0, QLM_BF16 = 1,             /* types of rows                 */
+       QLM_F32 = 2 };                         /* only where it is named        */
 enum { QLM_KV_E4M3 = 0, QLM_KV_INT8 = 1 };    /* codes: e4m3 (largest 448),
                                                  two's complement (127)        */
 
@@ -577,6 +579,40 @@ typedef struct qlm_rows {
  */
 int qlm_kv_append(const qlm_kv_cache *cache, const qlm_kv_batch *batch, const qlm_rows *k,
                   const qlm_rows *v, const int32_t *first_position, qlm_stream stream);
+
+/*
+ * qlm_kv_append of keys that are turned by their positions on the way, together
+ * with the rows' queries.  Of a row of a head, with half = rotary_dim / 2, pair i
+ * (0 <= i < half) is the dims (a, b) = (i, i + half), or (2i, 2i + 1) where
+ * `interleaved` is set, and
+ *   x'_a = x_a c - x_b s,   x'_b = x_b c + x_a s,   c = cos[p][i], s = sin[p][i],
+ *   p = position[axis[i]][row], clamped to [0, n_positions)
+ * each product and sum rounded to single precision; the dims from rotary_dim on
+ * stay.  Keys go into their codes from these values without another rounding,
+ * queries are rounded to q_out's type once.  Every axis has a position for each
+ * row (for pictures and video a token's time, row and column, each turning a part
+ * of the pairs); without `position` a row's is the one that the cache keeps for its
+ * slot: first_position[s] + t for row t of sequence s, or its slot's number.
+ * Rows of no sequence, and those past max_new of one, are left as they were in q_out.
+ *   q, q_out  [n_rows][n_heads][head_dim], the same dtype; q_out may be q itself
+ *             (the same data and strides), else it may not overlap q, k or v; both
+ *             NULL with n_heads 0
+ */
+typedef struct qlm_rotary {
+    int32_t rotary_dim;          /* even, 2..head_dim                            */
+    int32_t interleaved;         /* nonzero: neighbouring dims make a pair       */
+    int32_t n_positions;         /* >= 1                                         */
+    int32_t n_axes;              /* 1..4; 1 where position is NULL               */
+    const float *cos, *sin;      /* [n_positions][rotary_dim / 2]                */
+    const int32_t *axis;         /* [rotary_dim / 2] of 0..n_axes-1 (clamped);
+                                    NULL = 0 for every pair                      */
+    const int32_t *position;     /* [n_axes][n_rows] or NULL                     */
+} qlm_rotary;
+
+int qlm_kv_append_rotated(const qlm_kv_cache *cache, const qlm_kv_batch *batch, const qlm_rows *k,
+                          const qlm_rows *v, const qlm_rows *q, const qlm_rows *q_out,
+                          int32_t n_heads, const qlm_rotary *rotary,
+                          const int32_t *first_position, qlm_stream stream);
 
 /*
  * Attention of each sequence's new tokens over its slots, the new ones
@@ -685,6 +721,105 @@ size_t qlm_w4_workspace_bytes(const qlm_w4 *weight, int32_t n_rows);
 int qlm_w4_matmul(const qlm_w4 *weight, const void *x, int64_t x_stride, void *out,
                   int64_t out_stride, int32_t n_rows, int32_t dtype, void *ws, size_t ws_bytes,
                   qlm_stream stream);
+
+/*
+ * Products in 8-bit floating point (e4m3: largest value 448) with a scale for
+ * each block of QLM_F8_BLOCK inputs: of rows for every row, of weights for every
+ * QLM_F8_BLOCK outputs.  Codes of rows and of weights are held in tiles of
+ * QLM_F8_TILE rows and one block of inputs, [tile][block][8][16][16]: input k of row r
+ * of a tile at [k / 16][r][k % 16], the order in which the matrix instructions take
+ * them.  Rows past the last one and inputs past the last one are zeros.
+ *
+ * qlm_f8_pack lays out a matrix once (qlm_f8_packed_bytes bytes, 256-byte aligned).
+ *   codes  [n_out][n_in] e4m3
+ *   scale  [ceil(n_out / 128)][ceil(n_in / 128)]
+ *   weight[n][k] = codes[n][k] * scale[n / 128][k / 128]
+ */
+#define QLM_F8_BLOCK 128
+#define QLM_F8_TILE 16
+
+typedef struct qlm_f8 {
+    int32_t n_out, n_in;         /* 1 .. 2^24 each                               */
+    void *packed;
+} qlm_f8;
+
+size_t qlm_f8_packed_bytes(int32_t n_out, int32_t n_in);
+int qlm_f8_pack(const qlm_f8 *weight, const void *codes, const float *scale, qlm_stream stream);
+
+/*
+ * Rows of 16 bits as codes.  For each row and block of inputs, with a the largest
+ * finite magnitude:  scale = 2^e, the least e >= -100 with a <= 448 2^e, and each
+ * code the nearest to x / scale (ties to even; infinities the largest code, a NaN
+ * stays one).  The tiles' rows past the last one get zeros with scales of 2^-100.
+ *   x  [n_rows][n_in], QLM_F16 or QLM_BF16, x_stride elements between rows (>= n_in)
+ */
+typedef struct qlm_f8_codes {
+    int32_t n_rows;              /* >= 0                                         */
+    int32_t n_in;                /* 1 .. 2^24                                    */
+    void *codes;                 /* tiles as above, 16-byte aligned              */
+    float *scale;                /* [ceil(n_in / 128)][16 ceil(n_rows / 16)]     */
+} qlm_f8_codes;
+
+int qlm_f8_rows(const qlm_f8_codes *rows, const void *x, int64_t x_stride, int32_t dtype,
+                qlm_stream stream);
+
+/*
+ * out[m][n] = sum over blocks b of x_scale[b][m] * w_scale[n / 128][b] *
+ *             (sum over the block of x_code[m][k] * w_code[n][k])
+ * the sums in single precision, rounded once, but for what the matrix instruction
+ * does: it adds the products of eight neighbouring inputs with 13 bits below the
+ * exponent of the largest of them (1.5e-5 to 3e-5 of the outputs' norm over normally
+ * distributed inputs, whatever their number).  A NaN among a row's codes makes
+ * that row's outputs NaN, one among an output's codes that output of every row.
+ *   rows  any scales (qlm_f8_rows writes powers of two)
+ *   out   [n_rows][n_out], out_stride elements between rows; QLM_F16, QLM_BF16 or
+ *         QLM_F32; may not overlap the codes
+ *   ws    device workspace of at least qlm_f8_workspace_bytes for this number of rows
+ *         (more rows may need less), 256-byte aligned, scratch; may be NULL when that
+ *         is 0
+ */
+size_t qlm_f8_workspace_bytes(const qlm_f8 *weight, int32_t n_rows);
+int qlm_f8_matmul(const qlm_f8_codes *rows, const qlm_f8 *weight, void *out, int64_t out_stride,
+                  int32_t dtype, void *ws, size_t ws_bytes, qlm_stream stream);
+
+/*
+ * Verification of drafted tokens.  A sequence's new rows are a token it has and the
+ * tokens drafted to follow it (row_start as for attention: n rows, n - 1 drafts);
+ * target[r] holds the probabilities of the token after row r, draft[r] those that
+ * the token of row r + 1 was drawn from.  With t = tokens[r + 1], drafts are accepted in
+ * their order while
+ *   uniform[r] * draft[r][t] < target[r][t]      (in double precision, exact)
+ * (a t outside the vocabulary is refused).  Then one token is drawn: from weights
+ * w = max(target[r] - draft[r], 0) where the draft behind row r is refused (where these
+ * sum to 0 or are not finite, from w = target[r]), from w = target[r] of the last row r
+ * where none is:
+ *   the least word with (w[0] + .. + w[word]) > u * (sum of w), u = uniform[last row]
+ * in double precision; -1 where the sum is 0 or not finite.  The token is then distributed as
+ * one drawn from the target, whatever the drafts.  Without `draft` the drafts were
+ * chosen, not drawn: draft[r] is 1 at t and 0 elsewhere.  Bit-for-bit reproducible.
+ *   tokens_out   [n_seqs][max_new]: the accepted drafts, the token drawn, -1 from there on
+ *   count        [n_seqs]: accepted drafts + 1; 0 for a sequence without rows
+ *   lengths_out  [n_seqs] or NULL: max(0, length - refused drafts), the slots that
+ *                stay in the cache; may be the batch's own lengths
+ *   ws           device workspace of at least qlm_draft_verify_workspace_bytes,
+ *                256-byte aligned, scratch; may be NULL when that is 0
+ * The batch's block table is not used.
+ */
+typedef struct qlm_draft {
+    int32_t vocab;               /* words, 1 .. 2^24                             */
+    int32_t dtype;               /* QLM_F16, QLM_BF16 or QLM_F32: of both        */
+    const void *target;          /* [n_rows][vocab]                              */
+    const void *draft;           /* [n_rows][vocab] (a sequence's last row is not
+                                    read) or NULL                                */
+    int64_t target_stride, draft_stride;   /* elements between rows, >= vocab    */
+    const int32_t *tokens;       /* [n_rows]                                     */
+    const float *uniform;        /* [n_rows] in [0, 1)                           */
+} qlm_draft;
+
+size_t qlm_draft_verify_workspace_bytes(const qlm_kv_batch *batch, int32_t vocab);
+int qlm_draft_verify(const qlm_kv_batch *batch, const qlm_draft *draft, int32_t *tokens_out,
+                     int32_t *count, int32_t *lengths_out, void *ws, size_t ws_bytes,
+                     qlm_stream stream);
 
 /* Largest G the scoring kernels accept for these M, C, I (on-chip budget). */
 int32_t qlm_max_groups(int32_t n_models, int32_t n_classes, int32_t n_instances,

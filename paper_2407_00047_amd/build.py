@@ -15,7 +15,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 LIB = os.path.join(HERE, "libqlm.so")
 ARCH = "gfx950"
 SOURCES = ["qlm.hip", "search.hip", "fcfs.hip", "profile.hip", "kv.hip", "kv_attention.hip",
-           "w4.hip"]
+           "w4.hip", "f8.hip", "draft.hip"]
 
 HIP_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=" + ARCH, "-fPIC", "-shared",

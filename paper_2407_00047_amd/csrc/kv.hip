@@ -1,5 +1,6 @@
-// kv.hip -- the 8-bit token cache: writing new tokens (qlm_kv_append) and
-// cutting sequences to a budget by accumulated attention weight (qlm_kv_evict).
+// kv.hip -- the 8-bit token cache: writing new tokens (qlm_kv_append, with keys
+// turned by their positions qlm_kv_append_rotated) and cutting sequences to a budget
+// by accumulated attention weight (qlm_kv_evict).
 // The definitions stand in include/qlm.h.
 #include "kv.h"
 
@@ -155,6 +156,70 @@ struct AppendArgs {
     int32_t touched;      // blocks a sequence's new slots may lie in
 };
 
+// Tables and positions of the rotation, and the queries that are turned beside the keys.
+struct TurnArgs {
+    const float *cos, *sin;
+    const int32_t *axis, *position;
+    int32_t half, n_positions, n_axes;
+    int32_t table_wide;             // the tables may be read 16 bytes at a time
+    const void *q;
+    void *q_out;
+    int64_t q_row, q_head, out_row, out_head;
+    int32_t q_type, q_wide, n_heads;
+    int32_t units, pair_units;      // 16 dims of a head each: the pairs' first, then the rest
+    uint32_t key_groups, row_groups;   // workgroups of the keys; of a row's queries
+};
+
+// The place in the tables of pair i of a row (`own`: its position without `position`).
+__device__ inline int64_t table_at(const TurnArgs &t, int n_rows, int row, int own, int i)
+{
+    int p = own;
+    if (t.position) {
+        const int ax = t.axis ? max(0, min(t.axis[i], t.n_axes - 1)) : 0;
+        p = t.position[(int64_t)ax * n_rows + row];
+    }
+    return (int64_t)max(0, min(p, t.n_positions - 1)) * t.half + i;
+}
+
+// cos and sin of N pairs from i on, of which those from `half` on are not read (1 and 0).
+template <int N>
+__device__ inline void angles(const TurnArgs &t, int n_rows, int row, int own, int i, float *c,
+                              float *s)
+{
+    if (t.table_wide && !t.axis && i + N <= t.half) {
+        const int64_t at = table_at(t, n_rows, row, own, i);
+#pragma unroll
+        for (int e = 0; e < N; e += 4) {
+            *(float4v *)(c + e) = *(const float4v *)(t.cos + at + e);
+            *(float4v *)(s + e) = *(const float4v *)(t.sin + at + e);
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const bool in = i + e < t.half;
+        const int64_t at = table_at(t, n_rows, row, own, in ? i + e : 0);
+        c[e] = in ? t.cos[at] : 1.f;
+        s[e] = in ? t.sin[at] : 0.f;
+    }
+}
+
+// The position `place` tokens behind another.
+__device__ inline int position_of(int64_t first, int64_t place)
+{
+    return (int)min(first + place, (int64_t)INT32_MAX);
+}
+
+// A pair turned, each product and sum rounded by itself: a fused product would make the
+// codes depend on which of the two products it takes.
+__device__ inline void turn(float &a, float &b, float c, float s)
+{
+#pragma clang fp contract(off)
+    const float x = a * c - b * s, y = b * c + a * s;
+    a = x;
+    b = y;
+}
+
 // Eight dims of a row as bits, 16 bytes at once where they are aligned.
 __device__ inline uint4 row_bits8(const void *p, int64_t at, bool wide)
 {
@@ -183,6 +248,62 @@ __device__ inline uint32_t magnitude8(uint4 x, int dtype)
     return top;
 }
 
+// Eight values as codes over `scale`.
+template <int FMT> __device__ inline uint2 codes_of(const float *v, float scale, bool exact)
+{
+    const float by = 1.f / scale;
+    uint32_t o[2] = {0, 0};
+    for (int i = 0; i < 8; ++i)
+        o[i >> 2] |= code_of<FMT>(exact ? v[i] * by : v[i] / scale) << (8 * (i & 3));
+    return {o[0], o[1]};
+}
+
+// Eight dims from d on of a row of a head, turned; `x`: the dims as they are, `at`: of dim 0.
+__device__ inline void turned8(const TurnArgs &t, int n_rows, int row, int own, const void *data,
+                               int64_t at, int d, uint4 x, int dtype, bool wide, bool neighbours,
+                               float *y)
+{
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = bits_value((w[e >> 1] >> (16 * (e & 1))) & 0xffff, dtype);
+    if (d >= 2 * t.half) return;
+    float c[8], s[8];
+    if (neighbours) {
+        angles<4>(t, n_rows, row, own, d / 2, c, s);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (d / 2 + e < t.half) turn(y[2 * e], y[2 * e + 1], c[e], s[e]);
+        return;
+    }
+    if (t.half % 8 == 0) {                  // eight pairs: these dims and those half away
+        const bool low = d < t.half;
+        const int i = low ? d : d - t.half;
+        const uint4 o = row_bits8(data, at + (low ? d + t.half : i), wide);
+        const uint32_t u[4] = {o.x, o.y, o.z, o.w};
+        angles<8>(t, n_rows, row, own, i, c, s);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float other = bits_value((u[e >> 1] >> (16 * (e & 1))) & 0xffff, dtype);
+            float a = low ? y[e] : other, b = low ? other : y[e];
+            turn(a, b, c[e], s[e]);
+            y[e] = low ? a : b;
+        }
+        return;
+    }
+    for (int e = 0; e < 8; ++e) {
+        const int dim = d + e;
+        if (dim >= 2 * t.half) break;
+        const bool low = dim < t.half;
+        const int i = low ? dim : dim - t.half;
+        const int64_t k = table_at(t, n_rows, row, own, i);
+        const float other =
+            bits_value(((const uint16_t *)data)[at + (low ? dim + t.half : i)], dtype);
+        float a = low ? y[e] : other, b = low ? other : y[e];
+        turn(a, b, t.cos[k], t.sin[k]);
+        y[e] = low ? a : b;
+    }
+}
+
 // Eight dims as codes over `scale` (a power of two nearly always: a product then).
 template <int FMT> __device__ inline uint2 codes8(uint4 x, int dtype, float scale, bool exact)
 {
@@ -201,6 +322,29 @@ __device__ inline bool power_of_two(float x)
     return (__builtin_bit_cast(uint32_t, x) & 0x7fffffu) == 0;
 }
 
+// The sequence that a row belongs to and its place there; -1 of a row of none.  Found by 64
+// lanes at a time: one read of up to 64 sequences, two of up to 4096.
+__device__ inline int row_seq(const Seqs &q, int row, int *place)
+{
+    int s = row, row0;
+    if (q.row_start) {
+        s = 0;
+        int left = q.n_seqs;
+        for (int step = 1 << 30; step > 1;) {
+            step = (left + 63) / 64;
+            const int64_t at = (int64_t)(threadIdx.x & 63) * step;
+            const uint64_t m = __ballot(at < left && q.row_start[s + min(at, (int64_t)left - 1)] <= row);
+            if (m == 0) return -1;
+            const int last = (63 - __builtin_clzll(m)) * step;
+            s += last;
+            left = min(step, left - last);
+        }
+    }
+    const int n = seq_rows(q, s, &row0);
+    *place = row - row0;
+    return *place >= 0 && *place < n ? s : -1;
+}
+
 // One workgroup for each (sequence, block that takes new slots, kv head).  A
 // thread holds eight dims of every (32 / ND)-th slot: read once, for the largest magnitude,
 // then written as codes; values pass through shared memory into their order, and
@@ -209,7 +353,8 @@ __device__ inline bool power_of_two(float x)
 // dependent reads (length, table, scale, row).  Six ragged prompts of up to 2100 tokens
 // (8 heads of 64, 20 MB): 12.5 us, 1.6 TB/s, the ends of a short launch and the pass
 // through shared memory.
-template <int FMT, int ND> __global__ __launch_bounds__(kThreads) void k_append(AppendArgs a)
+template <int FMT, int ND, int TURN>   // TURN: 1 halves, 2 neighbours make a pair
+__device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
 {
     constexpr int DP = 64 * ND, CH = DP / 8, ROWS = kThreads / CH, PASS = kBlock / ROWS;
     __shared__ float red[2 * kThreads / 64];
@@ -236,6 +381,7 @@ template <int FMT, int ND> __global__ __launch_bounds__(kThreads) void k_append(
     const int d = 8 * (t % CH), slot0 = t / CH;
     const bool in_d = d < D;
     uint4 kx[PASS], vx[PASS];
+    float ky[TURN ? PASS : 1][8];
 #pragma unroll
     for (int p = 0; p < PASS; ++p) {
         // (a slot or dim that is not new is read as one that is: neither counts nor is
@@ -245,13 +391,30 @@ template <int FMT, int ND> __global__ __launch_bounds__(kThreads) void k_append(
         kx[p] = row_bits8(a.k, (int64_t)h * a.k_head + r * a.k_row + dd, a.k_wide);
         vx[p] = row_bits8(a.v, (int64_t)h * a.v_head + r * a.v_row + dd, a.v_wide);
     }
+    if (TURN) {
+        const int64_t own0 = a.first ? a.first[s] : start;
+#pragma unroll
+        for (int p = 0; p < PASS; ++p) {
+            const int64_t r = r0 + min(max(slot0 + p * ROWS, o0), o1 - 1) - o0;
+            turned8(turned, a.q.n_rows, (int)r, position_of(own0, r - row0), a.k,
+                    (int64_t)h * a.k_head + r * a.k_row, min(d, D - 8), kx[p], a.k_type, a.k_wide,
+                    TURN == 2, ky[p]);
+        }
+    }
     uint32_t tk = 0, tv = 0;
+    float ak = 0.f;
 #pragma unroll
     for (int p = 0; p < PASS; ++p) {
-        tk = max(tk, magnitude8(kx[p], a.k_type));
+        if (TURN) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ak = fmaxf(ak, finite_abs(ky[p][e]));
+        } else {
+            tk = max(tk, magnitude8(kx[p], a.k_type));
+        }
         tv = max(tv, magnitude8(vx[p], a.v_type));
     }
-    float ak = bits_value(tk, a.k_type), av = bits_value(tv, a.v_type);
+    if (!TURN) ak = bits_value(tk, a.k_type);
+    float av = bits_value(tv, a.v_type);
     max2(ak, av, red);                              // (its barrier: all have the old scales)
     const float newk = fmaxf(oldk, scale_for<FMT>(ak)), newv = fmaxf(oldv, scale_for<FMT>(av));
     if (t == 0) {
@@ -270,7 +433,7 @@ template <int FMT, int ND> __global__ __launch_bounds__(kThreads) void k_append(
         if (!in_d) continue;
         uint2 *to = (uint2 *)(kc + o * D + d);
         if (o >= o0 && o < o1) {
-            *to = codes8<FMT>(kx[p], a.k_type, newk, exk);
+            *to = TURN ? codes_of<FMT>(ky[p], newk, exk) : codes8<FMT>(kx[p], a.k_type, newk, exk);
             const uint2 c = codes8<FMT>(vx[p], a.v_type, newv, exv);
             uint8_t *at = few ? vc + (value_group(o) * D + d) * 16 + value_place(o)
                               : vl + (value_group(o) * DP + d) * 16 + value_place(o);
@@ -320,6 +483,104 @@ template <int FMT, int ND> __global__ __launch_bounds__(kThreads) void k_append(
                 a.first ? a.first[s] + (j * kBlock + o - start) : j * kBlock + o;
         if (a.c.weight) a.c.weight[bh * kBlock + o] = 0.f;
     }
+}
+
+template <int FMT, int ND> __global__ __launch_bounds__(kThreads) void k_append(AppendArgs a)
+{
+    append<FMT, ND, 0>(a, TurnArgs{});
+}
+
+// Two bytes of a row of queries.
+__device__ inline uint32_t q_bits(const TurnArgs &t, int64_t at)
+{
+    return ((const uint16_t *)t.q)[at];
+}
+
+// The queries of one row, 16 dims a thread: eight pairs, or 16 dims past the pairs.  A thread
+// writes what it read, so that they may be turned in place.
+template <bool NEIGHBOURS> __device__ inline void turn_queries(const AppendArgs &a, const TurnArgs &t)
+{
+    const uint32_t g = blockIdx.x - t.key_groups;
+    const int row = (int)(g / t.row_groups);
+    const int u = (int)(g % t.row_groups) * kThreads + (int)threadIdx.x;
+    int place;
+    const int s = row_seq(a.q, row, &place);
+    if (s < 0 || u >= t.n_heads * t.units) return;
+    const int h = u / t.units, k = u % t.units, D = a.c.D, half = t.half;
+    int64_t own0 = 0;
+    if (!t.position) {
+        int row0;
+        own0 = a.first ? a.first[s] : seq_length(a.q, s) - seq_rows(a.q, s, &row0);
+    }
+    const int own = position_of(own0, place);
+    const int64_t from = row * t.q_row + h * t.q_head, to = row * t.out_row + h * t.out_head;
+    // the unit's 16 dims are n0 from d0 on and n1 from d1 on
+    const bool pairs = k < t.pair_units;
+    int d0, d1, n0 = 8, n1 = 8;
+    if (NEIGHBOURS) {
+        d0 = 16 * k;
+        d1 = d0 + 8;
+    } else if (pairs) {
+        d0 = 8 * k;
+        d1 = half + 8 * k;
+        n0 = n1 = min(8, half - d0);
+    } else {
+        d0 = 2 * half + 16 * (k - t.pair_units);
+        d1 = d0 + 8;
+        n0 = min(8, D - d0);
+        n1 = max(0, min(8, D - d1));
+    }
+    float x[16];
+    if (t.q_wide) {
+        const uint4 lo = row_bits8(t.q, from + d0, true), hi = row_bits8(t.q, from + d1, true);
+        const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            x[e] = bits_value((w[e >> 1] >> (16 * (e & 1))) & 0xffff, t.q_type);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int i = e & 7, d = e < 8 ? d0 : d1;
+            x[e] = i < (e < 8 ? n0 : n1) ? bits_value(q_bits(t, from + d + i), t.q_type) : 0.f;
+        }
+    }
+    if (pairs) {
+        float c[8], s8[8];
+        angles<8>(t, a.q.n_rows, row, own, 8 * k, c, s8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (8 * k + e < half) {
+                if (NEIGHBOURS)
+                    turn(x[2 * e], x[2 * e + 1], c[e], s8[e]);
+                else
+                    turn(x[e], x[e + 8], c[e], s8[e]);
+            }
+    }
+    uint16_t *out = (uint16_t *)t.q_out + to;
+    if (t.q_wide) {
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            w[e] = row_bits(x[2 * e], t.q_type) | (uint32_t)row_bits(x[2 * e + 1], t.q_type) << 16;
+        *(uint4 *)(out + d0) = uint4{w[0], w[1], w[2], w[3]};
+        *(uint4 *)(out + d1) = uint4{w[4], w[5], w[6], w[7]};
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const int i = e & 7, d = e < 8 ? d0 : d1;
+        if (i < (e < 8 ? n0 : n1)) out[d + i] = row_bits(x[e], t.q_type);
+    }
+}
+
+// The keys' workgroups as in k_append, then for each row those of its queries.
+template <int FMT, int ND, bool NEIGHBOURS>
+__global__ __launch_bounds__(kThreads) void k_append_rotated(AppendArgs a, TurnArgs t)
+{
+    if (blockIdx.x < t.key_groups)
+        append<FMT, ND, NEIGHBOURS ? 2 : 1>(a, t);
+    else
+        turn_queries<NEIGHBOURS>(a, t);
 }
 
 // -- eviction ---------------------------------------------------------------
@@ -771,19 +1032,15 @@ EvictLayout evict_layout(const qlm_kv_cache *c, const qlm_kv_batch *b, int32_t b
     return l;
 }
 
-}  // namespace
-
-extern "C" {
-
-int qlm_kv_append(const qlm_kv_cache *cache, const qlm_kv_batch *batch, const qlm_rows *k,
-                  const qlm_rows *v, const int32_t *first_position, qlm_stream stream_)
+// Whether rows may be read and written 16 bytes at a time.
+bool rows_wide(const qlm_rows *r)
 {
-    hipStream_t stream = (hipStream_t)stream_;
-    int rc = check_cache(cache);
-    if (!rc) rc = check_batch(batch);
-    if (rc) return rc;
-    if (batch->n_seqs == 0 || batch->n_rows == 0 || batch->max_length == 0) return QLM_OK;
-    if ((rc = check_rows(k, "k")) || (rc = check_rows(v, "v"))) return rc;
+    return (uintptr_t)r->data % 16 == 0 && r->row_stride % 8 == 0 && r->head_stride % 8 == 0;
+}
+
+AppendArgs append_args(const qlm_kv_cache *cache, const qlm_kv_batch *batch, const qlm_rows *k,
+                       const qlm_rows *v, const int32_t *first_position)
+{
     AppendArgs a{};
     a.c = cache_args(cache);
     a.q = seqs_of(batch);
@@ -800,10 +1057,47 @@ int qlm_kv_append(const qlm_kv_cache *cache, const qlm_kv_batch *batch, const ql
     const int64_t most = ((int64_t)batch->max_new + kBlock - 2) / kBlock + 1;
     const int64_t have = ((int64_t)batch->max_length + kBlock - 1) / kBlock;
     a.touched = (int32_t)(most < have ? most : have);
-    const int64_t grid = (int64_t)batch->n_seqs * a.touched * a.c.H;
+    a.k_wide = rows_wide(k);
+    a.v_wide = rows_wide(v);
+    return a;
+}
+
+int64_t append_groups(const AppendArgs &a, const qlm_kv_batch *batch)
+{
+    return (int64_t)batch->n_seqs * a.touched * a.c.H;
+}
+
+int check_rotary(const qlm_rotary *r, int head_dim)
+{
+    if (!r) return fail(QLM_ERR_ARG, "rotary is NULL");
+    if (r->rotary_dim < 2 || r->rotary_dim > head_dim || r->rotary_dim % 2)
+        return fail(QLM_ERR_ARG, "rotary_dim must be even, in 2..head_dim");
+    if (r->n_positions < 1) return fail(QLM_ERR_ARG, "n_positions must be >= 1");
+    if (r->n_axes < 1 || r->n_axes > 4) return fail(QLM_ERR_ARG, "n_axes must be in 1..4");
+    if (!r->position && r->n_axes != 1)
+        return fail(QLM_ERR_ARG, "position is required with more than one axis");
+    if (!r->cos || !r->sin) return fail(QLM_ERR_ARG, "cos and sin are required");
+    if ((uintptr_t)r->cos % 4 || (uintptr_t)r->sin % 4)
+        return fail(QLM_ERR_ARG, "cos or sin is misaligned");
+    return QLM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int qlm_kv_append(const qlm_kv_cache *cache, const qlm_kv_batch *batch, const qlm_rows *k,
+                  const qlm_rows *v, const int32_t *first_position, qlm_stream stream_)
+{
+    hipStream_t stream = (hipStream_t)stream_;
+    int rc = check_cache(cache);
+    if (!rc) rc = check_batch(batch);
+    if (rc) return rc;
+    if (batch->n_seqs == 0 || batch->n_rows == 0 || batch->max_length == 0) return QLM_OK;
+    if ((rc = check_rows(k, "k")) || (rc = check_rows(v, "v"))) return rc;
+    const AppendArgs a = append_args(cache, batch, k, v, first_position);
+    const int64_t grid = append_groups(a, batch);
     if (!can_launch(grid, kThreads)) return fail(QLM_ERR_CAPACITY, "too many blocks in one append");
-    a.k_wide = (uintptr_t)a.k % 16 == 0 && a.k_row % 8 == 0 && a.k_head % 8 == 0;
-    a.v_wide = (uintptr_t)a.v % 16 == 0 && a.v_row % 8 == 0 && a.v_head % 8 == 0;
     const bool e4m3 = cache->format == QLM_KV_E4M3;
     auto kern = a.c.D <= 64    ? e4m3 ? k_append<QLM_KV_E4M3, 1> : k_append<QLM_KV_INT8, 1>
                 : a.c.D <= 128 ? e4m3 ? k_append<QLM_KV_E4M3, 2> : k_append<QLM_KV_INT8, 2>
@@ -811,6 +1105,74 @@ int qlm_kv_append(const qlm_kv_cache *cache, const qlm_kv_batch *batch, const ql
     kern<<<(unsigned)grid, kThreads, 0, stream>>>(a);
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? QLM_OK : hip_fail(e, "k_append launch");
+}
+
+int qlm_kv_append_rotated(const qlm_kv_cache *cache, const qlm_kv_batch *batch, const qlm_rows *k,
+                          const qlm_rows *v, const qlm_rows *q, const qlm_rows *q_out,
+                          int32_t n_heads, const qlm_rotary *rotary,
+                          const int32_t *first_position, qlm_stream stream_)
+{
+    hipStream_t stream = (hipStream_t)stream_;
+    int rc = check_cache(cache);
+    if (!rc) rc = check_batch(batch);
+    if (!rc) rc = check_rotary(rotary, cache->head_dim);
+    if (rc) return rc;
+    if (n_heads < 0 || n_heads > (1 << 16)) return fail(QLM_ERR_ARG, "n_heads must be in 0..65536");
+    if (n_heads == 0 && (q || q_out)) return fail(QLM_ERR_ARG, "q and q_out must be NULL without heads");
+    if (batch->n_seqs == 0 || batch->n_rows == 0) return QLM_OK;
+    if ((rc = check_rows(k, "k")) || (rc = check_rows(v, "v"))) return rc;
+    if (n_heads > 0) {
+        if ((rc = check_rows(q, "q")) || (rc = check_rows(q_out, "q_out"))) return rc;
+        if (q->dtype != q_out->dtype) return fail(QLM_ERR_ARG, "q and q_out must have one dtype");
+        const bool same = q->data == q_out->data;
+        if (same && (q->row_stride != q_out->row_stride || q->head_stride != q_out->head_stride))
+            return fail(QLM_ERR_ARG, "q_out in the place of q must have its strides");
+        if (q_out->data == k->data || q_out->data == v->data)
+            return fail(QLM_ERR_ARG, "q_out may not overlap k or v");
+    }
+    const AppendArgs a = append_args(cache, batch, k, v, first_position);
+    TurnArgs t{};
+    t.cos = rotary->cos;
+    t.sin = rotary->sin;
+    t.axis = rotary->axis;
+    t.position = rotary->position;
+    t.half = rotary->rotary_dim / 2;
+    t.n_positions = rotary->n_positions;
+    t.n_axes = rotary->n_axes;
+    t.table_wide = t.half % 4 == 0 && (uintptr_t)t.cos % 16 == 0 && (uintptr_t)t.sin % 16 == 0;
+    const bool neighbours = rotary->interleaved != 0;
+    const int64_t keys = batch->max_length > 0 ? append_groups(a, batch) : 0;
+    int64_t grid = keys;
+    t.n_heads = n_heads;
+    t.pair_units = (t.half + 7) / 8;
+    t.units = neighbours ? a.c.D / 16 : t.pair_units + (a.c.D - 2 * t.half + 15) / 16;
+    t.row_groups = (uint32_t)(((int64_t)n_heads * t.units + kThreads - 1) / kThreads);
+    if (n_heads > 0) {
+        t.q = q->data;
+        t.q_out = q_out->data;
+        t.q_row = q->row_stride;
+        t.q_head = q->head_stride;
+        t.out_row = q_out->row_stride;
+        t.out_head = q_out->head_stride;
+        t.q_type = q->dtype;
+        t.q_wide = rows_wide(q) && rows_wide(q_out) && (neighbours || t.half % 8 == 0);
+        grid += (int64_t)batch->n_rows * t.row_groups;
+    }
+    if (!can_launch(grid, kThreads)) return fail(QLM_ERR_CAPACITY, "too many rows in one append");
+    if (grid == 0) return QLM_OK;
+    t.key_groups = (uint32_t)keys;
+    auto pick = [&](auto e4m3, auto int8) { return cache->format == QLM_KV_E4M3 ? e4m3 : int8; };
+    constexpr int E = QLM_KV_E4M3, I = QLM_KV_INT8;
+    auto kern = neighbours
+        ? a.c.D <= 64    ? pick(k_append_rotated<E, 1, true>, k_append_rotated<I, 1, true>)
+          : a.c.D <= 128 ? pick(k_append_rotated<E, 2, true>, k_append_rotated<I, 2, true>)
+                         : pick(k_append_rotated<E, 4, true>, k_append_rotated<I, 4, true>)
+        : a.c.D <= 64    ? pick(k_append_rotated<E, 1, false>, k_append_rotated<I, 1, false>)
+          : a.c.D <= 128 ? pick(k_append_rotated<E, 2, false>, k_append_rotated<I, 2, false>)
+                         : pick(k_append_rotated<E, 4, false>, k_append_rotated<I, 4, false>);
+    kern<<<(unsigned)grid, kThreads, 0, stream>>>(a, t);
+    hipError_t e = hipGetLastError();
+    return e == hipSuccess ? QLM_OK : hip_fail(e, "k_append_rotated launch");
 }
 
 size_t qlm_kv_evict_workspace_bytes(const qlm_kv_cache *cache, const qlm_kv_batch *batch,

@@ -9,7 +9,8 @@ Function names follow the C interface: ``rwt_score``, ``rwt_score_exact``,
 ``validate_problem``, ``search_n_moves``, ``search_workspace_bytes``,
 ``search_moves``, ``search_screen``, ``local_search``, ``seed_plans``,
 ``place_group``; and of a serving instance's decode step ``kv_append``,
-``kv_attention``, ``kv_evict``, ``w4_pack``, ``w4_matmul``.
+``kv_append_rotated``, ``kv_attention``, ``kv_evict``, ``w4_pack``, ``w4_matmul``,
+``f8_pack``, ``f8_rows``, ``f8_matmul``, ``draft_verify``.
 """
 from __future__ import annotations
 
@@ -98,6 +99,29 @@ class W4Struct(ctypes.Structure):
                 ("packed", ctypes.c_void_p)]
 
 
+class F8Struct(ctypes.Structure):
+    _fields_ = [("n_out", ctypes.c_int32), ("n_in", ctypes.c_int32), ("packed", ctypes.c_void_p)]
+
+
+class F8CodesStruct(ctypes.Structure):
+    _fields_ = [("n_rows", ctypes.c_int32), ("n_in", ctypes.c_int32), ("codes", ctypes.c_void_p),
+                ("scale", ctypes.c_void_p)]
+
+
+class RotaryStruct(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("n_positions", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("axis", ctypes.c_void_p),
+                ("position", ctypes.c_void_p)]
+
+
+class DraftStruct(ctypes.Structure):
+    _fields_ = [("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32), ("target", ctypes.c_void_p),
+                ("draft", ctypes.c_void_p), ("target_stride", ctypes.c_int64),
+                ("draft_stride", ctypes.c_int64), ("tokens", ctypes.c_void_p),
+                ("uniform", ctypes.c_void_p)]
+
+
 PROFILE_FIELDS = ("prefill", "decode_time", "ineff", "max_tokens", "kv_tokens", "mean_tokens")
 
 
@@ -170,8 +194,21 @@ def library():
             lib.qlm_w4_workspace_bytes.argtypes = [W, i32]
             lib.qlm_w4_workspace_bytes.restype = ctypes.c_size_t
             lib.qlm_w4_matmul.argtypes = [W, vp, i64, vp, i64, i32, i32, vp, sz, vp]
+            lib.qlm_kv_append_rotated.argtypes = [C, B, vp, vp, vp, vp, i32, vp, vp, vp]
+            F, R = ctypes.POINTER(F8Struct), ctypes.POINTER(F8CodesStruct)
+            lib.qlm_f8_packed_bytes.argtypes = [i32, i32]
+            lib.qlm_f8_packed_bytes.restype = ctypes.c_size_t
+            lib.qlm_f8_pack.argtypes = [F, vp, vp, vp]
+            lib.qlm_f8_rows.argtypes = [R, vp, i64, i32, vp]
+            lib.qlm_f8_workspace_bytes.argtypes = [F, i32]
+            lib.qlm_f8_workspace_bytes.restype = ctypes.c_size_t
+            lib.qlm_f8_matmul.argtypes = [R, F, vp, i64, i32, vp, sz, vp]
+            lib.qlm_draft_verify_workspace_bytes.argtypes = [B, i32]
+            lib.qlm_draft_verify_workspace_bytes.restype = ctypes.c_size_t
+            lib.qlm_draft_verify.argtypes = [B, vp, vp, vp, vp, vp, sz, vp]
             for name in ("qlm_kv_append", "qlm_kv_attention", "qlm_kv_evict", "qlm_w4_pack",
-                         "qlm_w4_matmul"):
+                         "qlm_w4_matmul", "qlm_kv_append_rotated", "qlm_f8_pack", "qlm_f8_rows",
+                         "qlm_f8_matmul", "qlm_draft_verify"):
                 getattr(lib, name).restype = ctypes.c_int
             for name in ("qlm_rwt_score", "qlm_rwt_score_exact", "qlm_best_plan", "qlm_best_plan_static",
                          "qlm_score_form",
@@ -693,6 +730,8 @@ _KV_FORMATS = ("float8_e4m3fn", "int8")
 # (a few microseconds less a call than ctypes objects and torch.cuda.Stream).
 _ROWS = struct.Struct("@Pqqi0P")
 _KV_QUERY = struct.Struct("@Pqqi0PPqqi0Pifif0P")
+_ROTARY = struct.Struct("@iiiiPPPP")
+_DRAFT = struct.Struct("@iiPPqqPP")
 _row_types = {}
 
 
@@ -868,6 +907,78 @@ def kv_append(cache: DeviceKvCache, batch: KvBatch, k, v, first_position=None, s
         _check(rc)
 
 
+class Rotary:
+    """Tables of a rotation by position: ``cos`` and ``sin`` [n_positions, pairs]
+    float32, contiguous; twice the pairs' number of a head's dims turn, dim i with
+    dim i + pairs, or 2i with 2i + 1 where ``interleaved``.  ``axis`` [pairs] int32:
+    which of a token's positions turns the pair (the first one where None)."""
+
+    def __init__(self, cos, sin, interleaved=False, axis=None):
+        import torch
+        for name, x in (("cos", cos), ("sin", sin)):
+            if x.dim() != 2 or x.dtype != torch.float32 or not x.is_contiguous() or \
+                    x.shape != cos.shape:
+                raise ValueError(name + " must be contiguous [n_positions, pairs] float32")
+        if axis is not None and (axis.dtype != torch.int32 or axis.shape != cos.shape[1:] or
+                                 not axis.is_contiguous()):
+            raise ValueError("axis must be [pairs] int32")
+        if any(x is not None and x.device != cos.device for x in (sin, axis)):
+            raise ValueError("sin and axis must be where cos is")
+        self.cos, self.sin, self.axis, self.interleaved = cos, sin, axis, bool(interleaved)
+        self.n_positions, self.pairs = (int(x) for x in cos.shape)
+        self.index = cos.get_device()
+        self._tables = (_ptr(cos), _ptr(sin), _ptr(axis) or 0)
+
+
+def kv_append_rotated(cache: DeviceKvCache, batch: KvBatch, k, v, q, rotary: Rotary,
+                      position=None, first_position=None, out=None, stream=None):
+    """``kv_append`` of keys turned by their positions, together with the rows'
+    queries q [n_rows, n_heads, head_dim] (None: no queries); returns the turned
+    queries (``out``, which may be q itself).  position [axes, n_rows] (or [n_rows])
+    int32: each row's positions on the rotation's axes; None: the position that the
+    cache keeps for its slot, counted from first_position."""
+    if first_position is not None and (first_position.dtype != batch.lengths.dtype or
+                                       first_position.numel() != batch.n_seqs or
+                                       not first_position.is_contiguous()):
+        raise ValueError("first_position must be [n_seqs] int32")
+    axes = 1
+    if position is not None:
+        if position.dtype != batch.lengths.dtype or not position.is_contiguous() or \
+                position.dim() not in (1, 2) or position.shape[-1] != batch.n_rows:
+            raise ValueError("position must be contiguous [axes, %d rows] int32" % batch.n_rows)
+        axes = position.shape[0] if position.dim() == 2 else 1
+    rk = _rows(k, batch.n_rows, cache.n_kv_heads, cache.head_dim, "k")
+    rv = _rows(v, batch.n_rows, cache.n_kv_heads, cache.head_dim, "v")
+    heads, rq, ro = 0, None, None
+    if q is not None:
+        if q.dim() != 3:
+            raise ValueError("q must be [rows, n_heads, head_dim]")
+        heads = q.shape[1]
+        rq = _rows(q, batch.n_rows, heads, cache.head_dim, "q")
+        if out is None:
+            import torch
+            out = _allocated(stream, lambda: torch.empty(q.shape, dtype=q.dtype, device=q.device))
+        elif out.shape != q.shape or out.dtype != q.dtype:
+            raise ValueError("out must have q's shape and type")
+        ro = _rows(out, batch.n_rows, heads, cache.head_dim, "out")
+    elif out is not None:
+        raise ValueError("out is of queries, and there are none")
+    tensors = dict(k=k, v=v, q=q, out=out, rotary=rotary.cos, position=position,
+                   first_position=first_position)
+    if not 0 <= cache.index == batch.index or \
+            any(x is not None and x.get_device() != cache.index for x in tensors.values()):
+        _refuse_place(cache.index, cache=cache.k_codes, batch=batch.lengths, **tensors)
+    rc = (_lib or library()).qlm_kv_append_rotated(
+        cache._ref, batch._ref, _ROWS.pack(*rk), _ROWS.pack(*rv),
+        _ROWS.pack(*rq) if heads else None, _ROWS.pack(*ro) if heads else None, heads,
+        _ROTARY.pack(2 * rotary.pairs, rotary.interleaved, rotary.n_positions, axes,
+                     *rotary._tables, _ptr(position) or 0),
+        None if first_position is None else first_position.data_ptr(), _raw_stream(stream))
+    if rc:
+        _check(rc)
+    return out
+
+
 def kv_attention_workspace_bytes(cache: DeviceKvCache, batch: KvBatch, n_heads: int,
                                  accumulate: bool = False) -> int:
     return int(library().qlm_kv_attention_workspace_bytes(cache._ref, batch._ref, int(n_heads),
@@ -1017,3 +1128,201 @@ def w4_matmul(x, weight: W4, out=None, ws=None, stream=None):
     if rc:
         _check(rc)
     return out
+
+
+F8_BLOCK, F8_TILE = 128, 16
+
+
+class F8:
+    """A matrix of e4m3 weights as the kernels read it (qlm_f8): made by
+    ``f8_pack``."""
+
+    def __init__(self, packed, n_out, n_in):
+        self.packed, self.n_out, self.n_in = packed, n_out, n_in
+        self.index = packed.get_device()
+        self.struct = F8Struct(n_out, n_in, _ptr(packed))
+        self._ref = ctypes.byref(self.struct)
+
+
+class F8Rows:
+    """Rows in e4m3 with a scale for each row and 128 inputs (qlm_f8_codes): made by
+    ``f8_rows``, or from
+
+    codes  [ceil(n_rows / 16), ceil(n_in / 128), 8, 16, 16] float8_e4m3fn: input k of
+           row r of a tile at [k % 128 // 16, r, k % 16], zeros past the last row and
+           input
+    scale  [ceil(n_in / 128), 16 * ceil(n_rows / 16)] float32
+
+    both contiguous."""
+
+    def __init__(self, codes, scale, n_rows, n_in):
+        import torch
+        tiles, blocks = -(-n_rows // F8_TILE), -(-n_in // F8_BLOCK)
+        if tuple(codes.shape) != (tiles, blocks, 8, F8_TILE, 16) or \
+                codes.dtype != torch.float8_e4m3fn or not codes.is_contiguous():
+            raise ValueError("codes must be contiguous [%d, %d, 8, 16, 16] float8_e4m3fn"
+                             % (tiles, blocks))
+        if tuple(scale.shape) != (blocks, tiles * F8_TILE) or scale.dtype != torch.float32 or \
+                not scale.is_contiguous():
+            raise ValueError("scale must be contiguous [%d, %d] float32"
+                             % (blocks, tiles * F8_TILE))
+        if scale.device != codes.device:
+            raise ValueError("scale must be where codes is")
+        self.codes, self.scale, self.n_rows, self.n_in = codes, scale, int(n_rows), int(n_in)
+        self.index = codes.get_device()
+        self.struct = F8CodesStruct(self.n_rows, self.n_in, _ptr(codes), _ptr(scale))
+        self._ref = ctypes.byref(self.struct)
+
+
+def f8_pack(codes, scale, stream=None):
+    """Lays out 8-bit weights code * scale once: ``codes`` [n_out, n_in]
+    float8_e4m3fn, ``scale`` [ceil(n_out / 128), ceil(n_in / 128)] float32."""
+    import torch
+    if codes.dim() != 2 or codes.dtype != torch.float8_e4m3fn or not codes.is_contiguous():
+        raise ValueError("codes must be contiguous [n_out, n_in] float8_e4m3fn")
+    n, k = (int(x) for x in codes.shape)
+    if tuple(scale.shape) != (-(-n // F8_BLOCK), -(-k // F8_BLOCK)) or \
+            scale.dtype != torch.float32 or not scale.is_contiguous():
+        raise ValueError("scale must be contiguous [ceil(n_out / 128), ceil(n_in / 128)] float32")
+    _refuse_place(codes.get_device(), codes=codes, scale=scale)
+    nbytes = int(library().qlm_f8_packed_bytes(n, k))
+    packed = _allocated(stream, lambda: torch.empty(nbytes, dtype=torch.uint8, device=codes.device))
+    w = F8(packed, n, k)
+    _check(library().qlm_f8_pack(w._ref, _ptr(codes), _ptr(scale), _stream(stream)))
+    return w
+
+
+def f8_rows(x, out=None, stream=None):
+    """x [n_rows, n_in] (float16 or bfloat16) as e4m3 codes with a scale for each row
+    and 128 inputs: an F8Rows (``out``, of x's sizes, when given)."""
+    import torch
+    if x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1) or x.shape[1] < 1:
+        raise ValueError("x must be [rows, inputs] with contiguous rows")
+    kind = _row_type(x, "x")
+    n, k = x.shape
+    if out is None:
+        tiles, blocks = -(-n // F8_TILE), -(-k // F8_BLOCK)
+        out = F8Rows(
+            _allocated(stream, lambda: torch.empty((tiles, blocks, 8, F8_TILE, 16),
+                                                   dtype=torch.float8_e4m3fn, device=x.device)),
+            _allocated(stream, lambda: torch.empty((blocks, tiles * F8_TILE), dtype=torch.float32,
+                                                   device=x.device)), n, k)
+    elif out.n_rows != n or out.n_in != k:
+        raise ValueError("out must be of %d rows of %d inputs" % (n, k))
+    if not 0 <= out.index == x.get_device():
+        _refuse_place(x.get_device(), x=x, out=out.codes)
+    # (the stride of a matrix of one row says nothing)
+    rc = (_lib or library()).qlm_f8_rows(out._ref, x.data_ptr(), x.stride(0) if n > 1 else k, kind,
+                                         _raw_stream(stream))
+    if rc:
+        _check(rc)
+    return out
+
+
+def f8_workspace_bytes(weight: F8, n_rows: int) -> int:
+    return int(library().qlm_f8_workspace_bytes(weight._ref, int(n_rows)))
+
+
+def f8_workspace(weight: F8, n_rows: int):
+    import torch
+    return torch.empty(max(f8_workspace_bytes(weight, n_rows), 1), dtype=torch.uint8,
+                       device=weight.packed.device)
+
+
+def _word_type(dtype, what):
+    """The number of a row type, of which float32 is one too."""
+    import torch
+    kind = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}.get(dtype)
+    if kind is None:
+        raise ValueError("%s must be float16, bfloat16 or float32" % what)
+    return kind
+
+
+def f8_matmul(x: F8Rows, weight: F8, out=None, dtype=None, ws=None, stream=None):
+    """Coded rows times the matrix: [n_rows, n_out] of ``dtype`` (bfloat16 when None;
+    out's where out is given)."""
+    import torch
+    if x.n_in != weight.n_in:
+        raise ValueError("x must be rows of %d inputs" % weight.n_in)
+    n = x.n_rows
+    if out is None:
+        dtype = torch.bfloat16 if dtype is None else dtype
+        _word_type(dtype, "dtype")
+        out = _allocated(stream, lambda: torch.empty((n, weight.n_out), dtype=dtype,
+                                                     device=x.codes.device))
+    elif tuple(out.shape) != (n, weight.n_out) or (dtype is not None and out.dtype != dtype) or \
+            (out.stride(1) != 1 and weight.n_out > 1):
+        raise ValueError("out must be [%d, %d] with contiguous rows" % (n, weight.n_out))
+    kind = _word_type(out.dtype, "out")
+    if ws is None:
+        ws = _allocated(stream, lambda: f8_workspace(weight, n), False)
+    if not 0 <= weight.index == x.index == out.get_device() == ws.get_device():
+        _refuse_place(weight.index, weight=weight.packed, x=x.codes, out=out, ws=ws)
+    rc = (_lib or library()).qlm_f8_matmul(x._ref, weight._ref, out.data_ptr(),
+                                           out.stride(0) if n > 1 else weight.n_out, kind,
+                                           ws.data_ptr(), ws.numel(), _raw_stream(stream))
+    if rc:
+        _check(rc)
+    return out
+
+
+def draft_verify_workspace_bytes(batch: KvBatch, vocab: int) -> int:
+    return int(library().qlm_draft_verify_workspace_bytes(batch._ref, int(vocab)))
+
+
+def draft_verify_workspace(batch: KvBatch, vocab: int):
+    import torch
+    return torch.empty(max(draft_verify_workspace_bytes(batch, vocab), 1), dtype=torch.uint8,
+                       device=batch.lengths.device)
+
+
+def draft_verify(batch: KvBatch, tokens, target, draft, uniform, lengths=None, ws=None,
+                 stream=None):
+    """Verifies the drafted tokens of a step.  The batch's rows are a token of each
+    sequence and the drafts behind it; tokens [n_rows] int32; target [n_rows, vocab]
+    the probabilities behind each row, draft the same of the drafting model (None:
+    the drafts were chosen, not drawn), float16, bfloat16 or float32 alike; uniform
+    [n_rows] float32 in [0, 1).  Returns (tokens [n_seqs, max_new] int32: accepted
+    drafts, the token drawn, -1; their number [n_seqs] int32; the lengths that stay
+    in the cache [n_seqs] int32: ``lengths``, which may be the batch's own)."""
+    import torch
+    if target.dim() != 2 or target.shape[0] != batch.n_rows or target.shape[1] < 1 or \
+            (target.stride(1) != 1 and target.shape[1] > 1):
+        raise ValueError("target must be [%d rows, vocab] with contiguous rows" % batch.n_rows)
+    vocab = target.shape[1]
+    kind = _word_type(target.dtype, "target")
+    if draft is not None and (draft.shape != target.shape or draft.dtype != target.dtype or
+                              (draft.stride(1) != 1 and vocab > 1)):
+        raise ValueError("draft must have target's shape and type, with contiguous rows")
+    for name, x, dtype in (("tokens", tokens, torch.int32), ("uniform", uniform, torch.float32)):
+        if x.dtype != dtype or x.numel() != batch.n_rows or not x.is_contiguous():
+            raise ValueError("%s must be [%d rows] %s" % (name, batch.n_rows, dtype))
+    if lengths is None:
+        lengths = _allocated(stream, lambda: torch.empty_like(batch.lengths))
+    elif lengths.dtype != torch.int32 or lengths.numel() != batch.n_seqs or \
+            not lengths.is_contiguous():
+        raise ValueError("lengths must be [n_seqs] int32")
+    device = batch.lengths.device
+    out = _allocated(stream, lambda: torch.empty((batch.n_seqs, batch.max_new), dtype=torch.int32,
+                                                 device=device))
+    count = _allocated(stream, lambda: torch.empty_like(batch.lengths))
+    if ws is None:
+        ws = _allocated(stream, lambda: draft_verify_workspace(batch, vocab), False)
+    tensors = dict(tokens=tokens, target=target, draft=draft, uniform=uniform, lengths=lengths,
+                   ws=ws)
+    if batch.index < 0 or any(x is not None and x.get_device() != batch.index
+                              for x in tensors.values()):
+        _refuse_place(batch.index, batch=batch.lengths, **tensors)
+    # (the stride of a matrix of one row says nothing)
+    one = batch.n_rows <= 1
+    rc = (_lib or library()).qlm_draft_verify(
+        batch._ref,
+        _DRAFT.pack(vocab, kind, target.data_ptr(), _ptr(draft) or 0,
+                    vocab if one else target.stride(0),
+                    vocab if one or draft is None else draft.stride(0), tokens.data_ptr(),
+                    uniform.data_ptr()),
+        out.data_ptr(), count.data_ptr(), lengths.data_ptr(), ws.data_ptr(), ws.numel(),
+        _raw_stream(stream))
+    if rc:
+        _check(rc)
+    return out, count, lengths

@@ -1,0 +1,299 @@
+"""Rows in 8-bit floating point and their products on the GPU: codes and scales value for
+value against the definition, products against 64 bits within the bound of single-precision
+sums."""
+import numpy as np
+import pytest
+
+import kv_oracle as ko
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    assert torch.cuda.is_available()
+    return torch
+
+
+@pytest.fixture(scope="module")
+def qlm():
+    from paper_2407_00047_amd import qlm
+    return qlm
+
+
+def coded(x):
+    """(codes' values, scales [row, block]) of rows in 64 bits."""
+    m, k = x.shape
+    blocks = -(-k // 128)
+    scale = np.empty((m, blocks))
+    codes = np.empty((m, k))
+    for b in range(blocks):
+        part = x[:, 128 * b:128 * (b + 1)]
+        a = np.where(np.isfinite(part), np.abs(part), 0.0).max(axis=1)
+        scale[:, b] = [ko.scale_for(v, "e4m3") for v in a]
+        codes[:, 128 * b:128 * (b + 1)] = ko.encode_value(part / scale[:, b:b + 1], "e4m3")
+    return codes, scale
+
+
+def from_tiles(rows):
+    """An F8Rows as (codes' values, scales [row, block]), past the last row and input too."""
+    import torch
+    c = ko.E4M3[rows.codes.view(torch.uint8).cpu().numpy()]
+    t, b = c.shape[:2]
+    return (c.transpose(0, 3, 1, 2, 4).reshape(16 * t, 128 * b),
+            rows.scale.cpu().numpy().astype(np.float64).T)
+
+
+def to_tiles(torch, codes):
+    """Bytes [row, input] as tiles on the GPU."""
+    m, k = codes.shape
+    t, b = -(-m // 16), -(-k // 128)
+    full = np.zeros((16 * t, 128 * b), np.uint8)
+    full[:m, :k] = codes
+    full = full.reshape(t, 16, b, 8, 16).transpose(0, 2, 3, 1, 4)
+    return torch.from_numpy(np.ascontiguousarray(full)).cuda().view(torch.float8_e4m3fn)
+
+
+def check_rows(torch, qlm, x, view=None):
+    m, k = x.shape
+    got, scale = from_tiles(qlm.f8_rows(x if view is None else view))
+    want, by = coded(x.double().cpu().numpy())
+    same = (got[:m, :k] == want) | (np.isnan(got[:m, :k]) & np.isnan(want))
+    assert same.all(), np.argwhere(~same)[:4].tolist()
+    assert (scale[:m] == by).all()
+    assert (got[m:] == 0).all() and (got[:, k:] == 0).all() and (scale[m:] == 2.0 ** -100).all()
+
+
+@pytest.mark.parametrize("kind", ["bfloat16", "float16"])
+@pytest.mark.parametrize("m", [1, 7, 16, 17, 33])
+@pytest.mark.parametrize("k", [1, 15, 16, 127, 128, 129, 400, 513])
+def test_rows(torch, qlm, m, k, kind):
+    torch.manual_seed(m * 1000 + k)
+    x = torch.randn((m, k), device="cuda") * torch.exp(2 * torch.randn((1, k), device="cuda"))
+    check_rows(torch, qlm, x.to(getattr(torch, kind)))
+
+
+@pytest.mark.parametrize("kind", ["bfloat16", "float16"])
+def test_strided_rows(torch, qlm, kind):
+    torch.manual_seed(1)
+    big = torch.randn((40, 700), device="cuda").to(getattr(torch, kind))
+    for view in (big[:20, 8:400], big[3:20, 1:300], big[::2, :256], big[:, 692:]):
+        check_rows(torch, qlm, view.contiguous(), view)
+
+
+@pytest.mark.parametrize("kind", ["bfloat16", "float16"])
+def test_rows_of_odd_values(torch, qlm, kind):
+    """Not-a-numbers, infinities, zeros, the least and largest numbers, and halves between codes."""
+    dt = getattr(torch, kind)
+    big = torch.finfo(dt).max
+    x = torch.zeros((16, 256), device="cuda", dtype=dt)
+    x[0, 5] = float("nan")
+    x[1, 3], x[1, 4] = float("inf"), 1.0
+    x[2] = -float("inf")
+    x[3, 130] = big
+    x[4] = torch.finfo(dt).tiny
+    x[5, 9] = 2.0 ** -24 if kind == "float16" else 2.0 ** -133
+    x[6, :8] = torch.tensor([448, 449, 17, 19, 21, 1.0625, 1.1875, -17], dtype=dt)
+    x[7, :6] = torch.tensor([224, 2.0 ** -9, 2.0 ** -10, 3 * 2.0 ** -10, 2.0 ** -11, 5 * 2.0 ** -10],
+                            dtype=dt)
+    x[8, :2] = torch.tensor([float("nan"), -float("inf")], dtype=dt)
+    x[9, 128:] = -big
+    check_rows(torch, qlm, x)
+
+
+def product(torch, qlm, m, n, k, dtype, seed=0, out=None, spread=1.0):
+    rng = np.random.default_rng(seed)
+    blocks = -(-k // 128)
+    codes = rng.integers(0, 256, (m, k)).astype(np.uint8)
+    weight = rng.integers(0, 256, (n, k)).astype(np.uint8)
+    for c in (codes, weight):
+        c[(c & 0x7f) == 0x7f] = 0x30
+    xs = np.exp(spread * rng.normal(size=(blocks, -(-m // 16) * 16))).astype(np.float32)
+    ws = (0.01 * np.exp(spread * rng.normal(size=(-(-n // 128), blocks)))).astype(np.float32)
+    x = qlm.F8Rows(to_tiles(torch, codes), torch.from_numpy(xs).cuda(), m, k)
+    w = qlm.f8_pack(torch.from_numpy(weight).cuda().view(torch.float8_e4m3fn),
+                    torch.from_numpy(ws).cuda())
+    ws_ = torch.full((max(1, qlm.f8_workspace_bytes(w, m)),), 255, dtype=torch.uint8, device="cuda")
+    got = qlm.f8_matmul(x, w, out=out, dtype=dtype, ws=ws_)
+    wide = lambda s: np.repeat(s, 128, axis=-1)[..., :k].astype(np.float64)  # noqa: E731
+    xv = ko.E4M3[codes] * wide(xs.T[:m])
+    wv = ko.E4M3[weight] * wide(np.repeat(ws, 128, axis=0)[:n])
+    dev = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    exact = dev(xv) @ dev(wv).t()
+    return got, exact, sizes(dev(xv), dev(wv)), (x, w)
+
+
+def sizes(x, w):
+    """The sum of the products' magnitudes, and of the largest products of groups of eight
+    inputs: the instruction adds the products of eight neighbouring inputs with 13 bits below the exponent
+    of the largest one (test_sums_of_eight): each of the other seven loses less than 2^-13 of
+    that product, which is at most the group's largest |x| times its largest |w|."""
+    import torch
+    k = -(-x.shape[1] // 8) * 8
+    pad = lambda a: torch.nn.functional.pad(a, (0, k - a.shape[1])).abs()  # noqa: E731
+    top = lambda a: pad(a).view(a.shape[0], -1, 8).amax(-1)  # noqa: E731
+    return x.abs() @ w.abs().t(), top(x) @ top(w).t()
+
+
+def bound(torch, exact, size, k, dtype):
+    """What groups of eight lose (sizes); single-precision sums of a block's 128 products (an
+    addition may be cut off instead of rounded: 2^-23 each), the scales' product and the block's
+    (2^-24 each), sums over the blocks, of which some may be joined last; then the output's half
+    step, for a half also where it is subnormal."""
+    blocks = -(-k // 128)
+    e = 7 * 2.0 ** -13 * size[1] + size[0] * (2.0 ** -23 * 128 + 2.0 ** -24 * (blocks + 10))
+    half = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32: 2.0 ** -24}[dtype]
+    return e + half * (exact.abs() + e) + (2.0 ** -25 if dtype == torch.float16 else 0.0)
+
+
+def test_sums_of_eight(torch, qlm):
+    """The arithmetic of the matrix instruction that the bound goes by: beside a product of 1 one
+    of 2^-13 among the same eight inputs is kept, and in another eight one of 2^-18."""
+    one, power = 0x38, {4: 0x18, 9: 0x01}                 # codes of 2^-e
+    for place, a, b in ((1, 4, 4), (7, 9, 4), (8, 9, 9), (64, 9, 9), (127, 9, 9)):
+        x, w = (np.zeros((1, 128), np.uint8) for _ in range(2))
+        x[0, 0] = w[0, 0] = one
+        x[0, place], w[0, place] = power[a], power[b]
+        got = qlm.f8_matmul(
+            qlm.F8Rows(to_tiles(torch, x), torch.ones((1, 16), device="cuda"), 1, 128),
+            qlm.f8_pack(torch.from_numpy(w).cuda().view(torch.float8_e4m3fn),
+                        torch.ones((1, 1), device="cuda")), dtype=torch.float32)
+        assert float(got) - 1.0 == 2.0 ** -(a + b), (place, a, b)
+
+
+SIZES = [(1, 1, 1), (1, 16, 128), (1, 300, 500), (2, 129, 257), (15, 17, 127), (16, 128, 1024),
+         (17, 130, 640), (31, 100, 129), (33, 257, 1000), (48, 64, 2048), (64, 333, 384),
+         (65, 129, 900), (100, 500, 200), (130, 270, 1500), (200, 1000, 300), (257, 255, 130),
+         (300, 700, 2000), (513, 300, 515), (1000, 1100, 256)]
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
+@pytest.mark.parametrize("m,n,k", SIZES)
+def test_products(torch, qlm, m, n, k, dtype):
+    dt = getattr(torch, dtype)
+    got, exact, size, _ = product(torch, qlm, m, n, k, dt, seed=m + n + k, spread=0.3)
+    assert got.dtype == dt and tuple(got.shape) == (m, n)
+    e = (got.double() - exact).abs()
+    lim = bound(torch, exact, size, k, dt)
+    fine = exact.abs() < torch.finfo(dt).max
+    assert bool((e <= lim)[fine].all()), float((e / lim)[fine].max())
+
+
+@pytest.mark.parametrize("m,n,k", [(5, 1000, 8192), (40, 4096, 4096), (128, 2000, 16384),
+                                   (700, 2050, 4100), (2100, 4100, 1100)])
+def test_large_products(torch, qlm, m, n, k):
+    got, exact, size, (x, w) = product(torch, qlm, m, n, k, torch.float32, seed=k)
+    e = (got.double() - exact).abs()
+    assert bool((e <= bound(torch, exact, size, k, torch.float32)).all())
+    again = qlm.f8_matmul(x, w, dtype=torch.float32)
+    assert torch.equal(got, again)                     # (bit for bit the same)
+
+
+@pytest.mark.parametrize("m", [3, 40, 70, 300])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_strided_out(torch, qlm, m, dtype):
+    """Outputs between other columns, which stay; odd strides and starts."""
+    n, k = 203, 384
+    big = torch.full((m + 2, 451), -5.0, dtype=getattr(torch, dtype), device="cuda")
+    out = big[1:m + 1, 7:7 + n]
+    got, exact, size, _ = product(torch, qlm, m, n, k, None, out=out, spread=0.3)
+    assert got.data_ptr() == out.data_ptr()
+    e = (out.double() - exact).abs()
+    assert bool((e <= bound(torch, exact, size, k, out.dtype)).all())
+    big[1:m + 1, 7:7 + n] = -5.0
+    assert bool((big == -5.0).all())
+
+
+@pytest.mark.parametrize("m", [4, 40, 300])
+def test_not_a_numbers(torch, qlm, m):
+    """A code that is none spoils its row, one of the weights its output, and nothing else."""
+    n, k = 150, 300
+    _, exact, size, (x, w) = product(torch, qlm, m, n, k, torch.float32)
+    codes = x.codes.view(torch.uint8)
+    codes[0, 1, 2, 3, 5] = 0x7f                            # row 3
+    w.packed[(0 * 3 + 2) * 2048 + 1 * 256 + 9 * 16 + 4] = 0xff   # output 9, input 256 + 20
+    got = qlm.f8_matmul(x, w, dtype=torch.float32)
+    bad = torch.zeros((m, n), dtype=torch.bool, device="cuda")
+    bad[3], bad[:, 9] = True, True
+    assert torch.equal(got.isnan(), bad)
+    e = (got.double() - exact).abs()
+    assert bool((e <= bound(torch, exact, size, k, torch.float32))[~bad].all())
+
+
+def test_scales_of_any_size(torch, qlm):
+    """Scales down to 2^-100 and up to 2^100, zeros among them."""
+    m, n, k = 20, 40, 256
+    _, _, _, (x, w) = product(torch, qlm, m, n, k, torch.float32, spread=0.0)
+    xs = torch.ones_like(x.scale)
+    xs[0, :4] = torch.tensor([2.0 ** -100, 2.0 ** 100, 0.0, 3.0], device="cuda")
+    base = qlm.f8_matmul(qlm.F8Rows(x.codes, torch.ones_like(xs), m, k), w, dtype=torch.float32)
+    got = qlm.f8_matmul(qlm.F8Rows(x.codes, xs, m, k), w, dtype=torch.float32)
+    second = x.scale.clone().zero_()
+    second[1] = 1.0
+    rest = qlm.f8_matmul(qlm.F8Rows(x.codes, second, m, k), w, dtype=torch.float32)
+    assert torch.equal(got[2], rest[2]) and torch.equal(got[4:], base[4:])
+    first = (base - rest)[1].double() * 2.0 ** 100
+    big = (base.abs() + rest.abs())[1].double() * 2.0 ** 100 * 2.0 ** -20
+    assert bool(((got[1].double() - first).abs() <= big).all())
+
+
+def test_rows_then_product(torch, qlm):
+    """Rows of bfloat16 through both: against the product of what the codes hold."""
+    torch.manual_seed(5)
+    m, n, k = 70, 260, 777
+    x = torch.randn((m, k), device="cuda").bfloat16()
+    w = (torch.randn((n, k), device="cuda") * 100).clamp(-448, 448).to(torch.float8_e4m3fn)
+    ws = torch.rand((3, 7), device="cuda") + 0.5
+    rows = qlm.f8_rows(x)
+    codes, scale = from_tiles(rows)
+    xv = torch.from_numpy(codes * np.repeat(scale, 128, axis=1)).cuda()[:m, :k]
+    wv = w.double() * ws.double().repeat_interleave(128, 0)[:n].repeat_interleave(128, 1)[:, :k]
+    got = qlm.f8_matmul(rows, qlm.f8_pack(w, ws))
+    exact, size = xv @ wv.t(), sizes(xv, wv)
+    assert bool(((got.double() - exact).abs() <= bound(torch, exact, size, k, torch.bfloat16)).all())
+
+
+@pytest.mark.parametrize("m", [0, 1])
+def test_no_rows(torch, qlm, m):
+    w = qlm.f8_pack(torch.zeros((20, 64), device="cuda").to(torch.float8_e4m3fn),
+                    torch.ones((1, 1), device="cuda"))
+    rows = qlm.f8_rows(torch.ones((m, 64), dtype=torch.bfloat16, device="cuda"))
+    out = qlm.f8_matmul(rows, w)
+    assert tuple(out.shape) == (m, 20) and bool((out == 0).all())
+
+
+@pytest.mark.parametrize("m", [5, 100, 300])
+def test_captured_and_replayed(torch, qlm, m):
+    torch.manual_seed(2)
+    n, k = 300, 1100
+    x = torch.randn((m, k), device="cuda").bfloat16()
+    w = qlm.f8_pack((torch.randn((n, k), device="cuda") * 100).clamp(-448, 448).to(torch.float8_e4m3fn),
+                    torch.rand((3, 9), device="cuda"))
+    rows, ws = qlm.f8_rows(x), qlm.f8_workspace(w, m)
+    out = torch.empty((m, n), dtype=torch.bfloat16, device="cuda")
+    qlm.f8_matmul(rows, w, out=out, ws=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        qlm.f8_rows(x, out=rows)
+        qlm.f8_matmul(rows, w, out=out, ws=ws)
+    for i in range(4):
+        x.copy_(torch.randn((m, k), device="cuda"))
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, qlm.f8_matmul(qlm.f8_rows(x), w)), i
+
+
+def test_on_a_side_stream(torch, qlm):
+    torch.manual_seed(3)
+    x = torch.randn((50, 512), device="cuda").bfloat16()
+    w = qlm.f8_pack(torch.randn((100, 512), device="cuda").to(torch.float8_e4m3fn),
+                    torch.rand((1, 4), device="cuda"))
+    want = qlm.f8_matmul(qlm.f8_rows(x), w)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = qlm.f8_matmul(qlm.f8_rows(x, stream=side), w, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
