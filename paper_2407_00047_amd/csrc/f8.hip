@@ -167,6 +167,7 @@ struct MatArgs {
     int64_t out_stride;
     int32_t N, M, blocks, padded;
     int32_t n_tiles, m_tiles;
+    uint32_t grid_n, grid_m;      // workgroups' tiles of outputs and of rows
     int32_t dtype;
 };
 
@@ -201,6 +202,12 @@ __device__ inline void store4(const MatArgs &a, int64_t m, int n, float4v v)
         return;
     }
     uint16_t *p = (uint16_t *)a.out + m * a.out_stride + n;
+    if (n + 4 <= a.N && (uintptr_t)p % 8 == 0) {
+        const uint32_t lo = out_bits(v[0], a.dtype) | out_bits(v[1], a.dtype) << 16;
+        const uint32_t hi = out_bits(v[2], a.dtype) | out_bits(v[3], a.dtype) << 16;
+        *(uint2 *)p = uint2{lo, hi};
+        return;
+    }
     for (int i = 0; i < 4; ++i)
         if (n + i < a.N) p[i] = (uint16_t)out_bits(v[i], a.dtype);
 }
@@ -235,6 +242,125 @@ template <int MT, int W> __global__ __launch_bounds__(64 * W) void k_f8_thin(Mat
         for (int k = 1; k < W; ++k) v += part[k][i][lane];
         const int64_t m = (int64_t)(mt0 + i) * kTile + (lane & 15);
         if (m < a.M) store4(a, m, nt * kTile + 4 * (lane >> 4), v);
+    }
+}
+
+// 16 bytes a lane from memory into shared memory, lane after lane from `to` on (uniform over the
+// wave); done when the loads are waited for.
+__device__ inline void load_lds(const uint8_t *from, uint8_t *to)
+{
+    typedef const uint32_t __attribute__((address_space(1))) *global_ptr;
+    typedef uint32_t __attribute__((address_space(3))) *shared_ptr;
+    __builtin_amdgcn_global_load_lds((global_ptr)(uintptr_t)from, (shared_ptr)(uintptr_t)to, 16, 0,
+                                     0);
+}
+
+// Tiles of (16 NT WN) outputs and (16 MT WM) rows to a workgroup of WN x WM waves.
+template <int NT, int MT, int WN, int WM>
+__global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
+{
+    constexpr int W = WN * WM, TN = NT * WN, TM = MT * WM, PIECES = 2 * (TN + TM);
+    static_assert(PIECES % W == 0, "pieces of a stage are shared evenly");
+    __shared__ __align__(16) uint8_t buf0[1024 * PIECES], buf1[1024 * PIECES];
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wn = wv % WN, wm = wv / WN;
+    // eight dies take runs of tiles of their own, in each four rows' tiles before the next outputs'
+    const uint32_t total = a.grid_n * a.grid_m, per = (total + 7) / 8;
+    const uint32_t id = blockIdx.x % 8 * per + blockIdx.x / 8;
+    if (id >= total) return;
+    const uint32_t group = id / (4 * a.grid_n), in = id % (4 * a.grid_n);
+    const uint32_t high = min(4u, a.grid_m - 4 * group);
+    const int nt0 = (int)(in / high) * TN, mt0 = (int)(4 * group + in % high) * TM;
+
+    const uint8_t *from[PIECES / W];
+#pragma unroll
+    for (int i = 0; i < PIECES / W; ++i) {
+        const int p = i * W + wv, t = p / 2;
+        const int64_t tile = t < TN ? min(nt0 + t, a.n_tiles - 1) : min(mt0 + t - TN, a.m_tiles - 1);
+        from[i] = (t < TN ? a.w : a.x) + tile * a.blocks * kTileBytes + 1024 * (p & 1);
+    }
+    auto fetch = [&](int b, uint8_t *to) {
+#pragma unroll
+        for (int i = 0; i < PIECES / W; ++i)
+            load_lds(from[i] + (int64_t)b * kTileBytes + 16 * lane, to + 1024 * (i * W + wv));
+    };
+    const int nb = min(nt0 + wn * NT, a.n_tiles - 1) / (kBlock / kTile);
+    const float *ws = a.ws + (int64_t)nb * a.blocks;
+    const float *xs[MT];
+    for (int i = 0; i < MT; ++i)
+        xs[i] = a.xs + min(mt0 + wm * MT + i, a.m_tiles - 1) * kTile;
+    float4v acc[NT][MT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) acc[i][j] = float4v{0, 0, 0, 0};
+    float by[MT], w_next, x_next[MT];
+    auto fetch_scales = [&](int b) {
+        w_next = ws[b];
+#pragma unroll
+        for (int j = 0; j < MT; ++j) x_next[j] = (xs[j] + (int64_t)b * a.padded)[lane & 15];
+    };
+    auto scales = [&] {
+#pragma unroll
+        for (int j = 0; j < MT; ++j) by[j] = w_next * x_next[j];
+    };
+    auto step = [&](const uint8_t *cur) {
+        int8v x[MT];
+#pragma unroll
+        for (int j = 0; j < MT; ++j) x[j] = operand(cur + kTileBytes * (TN + wm * MT + j), lane);
+        int8v ahead = operand(cur + kTileBytes * wn * NT, lane);
+        float4v was[MT], now[MT];
+#pragma unroll
+        for (int i = 0; i <= NT; ++i) {
+            const int8v w = ahead;
+            if (i + 1 < NT) ahead = operand(cur + kTileBytes * (wn * NT + i + 1), lane);
+#pragma unroll
+            for (int j = 0; j < MT; ++j) {
+                if (i < NT) now[j] = product(w, x[j]);
+                if (i > 0)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i - 1][j][e] += by[j] * was[j][e];
+            }
+#pragma unroll
+            for (int j = 0; j < MT; ++j) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+                was[j] = now[j];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // One barrier a stage: behind it the stage's loads are there and the other buffer's readers are
+    // done.  No branch stands inside: the additions would move behind it with all their products
+    // held in registers.  (The last loads may be the last block's once more.)
+    const int last = a.blocks - 1;
+    fetch(0, buf0);
+    fetch_scales(0);
+    int b = 0;
+    for (; b < last; b += 2) {
+        __syncthreads();
+        scales();
+        fetch(b + 1, buf1);
+        fetch_scales(b + 1);
+        step(buf0);
+        __syncthreads();
+        scales();
+        fetch(min(b + 2, last), buf0);
+        fetch_scales(min(b + 2, last));
+        step(buf1);
+    }
+    __syncthreads();
+    if (b == last) {
+        scales();
+        step(buf0);
+    }
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {
+        const int64_t m = (int64_t)(mt0 + wm * MT + j) * kTile + (lane & 15);
+        if (m >= a.M) continue;
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+            store4(a, m, (nt0 + wn * NT + i) * kTile + 4 * (lane >> 4), acc[i][j]);
     }
 }
 
@@ -369,6 +495,15 @@ int qlm_f8_matmul(const qlm_f8_codes *rows, const qlm_f8 *weight, void *out, int
     a.m_tiles = (int32_t)tiles_of(a.M);
     a.padded = a.m_tiles * kTile;
     a.dtype = dtype;
+    if (a.m_tiles > 4) {
+        a.grid_n = (a.n_tiles + 15) / 16;
+        a.grid_m = (a.m_tiles + 15) / 16;
+        const int64_t grid = (int64_t)a.grid_n * a.grid_m;
+        if (!can_launch(grid, 512)) return fail(QLM_ERR_CAPACITY, "too many outputs in one call");
+        k_f8_wide<8, 4, 2, 4><<<(unsigned)((grid + 7) / 8 * 8), 512, 0, stream>>>(a);
+        hipError_t e = hipGetLastError();
+        return e == hipSuccess ? QLM_OK : hip_fail(e, "f8 launch");
+    }
     const int mt = a.m_tiles == 1 ? 1 : a.m_tiles == 2 ? 2 : 4;
     const int64_t grid = (int64_t)a.n_tiles * ((a.m_tiles + mt - 1) / mt);
     if (!can_launch(grid, 512)) return fail(QLM_ERR_CAPACITY, "too many outputs in one call");
