@@ -36,6 +36,7 @@ constexpr int kBlock = QLM_F8_BLOCK, kTile = QLM_F8_TILE;
 constexpr int kTileBytes = kBlock * kTile;
 constexpr int kLeastExp = -100;
 constexpr int kMost = 1 << 24;
+constexpr int kCus = 256;
 
 int64_t blocks_of(int n) { return ((int64_t)n + kBlock - 1) / kBlock; }
 int64_t tiles_of(int n) { return ((int64_t)n + kTile - 1) / kTile; }
@@ -168,6 +169,7 @@ struct MatArgs {
     int32_t N, M, blocks, padded;
     int32_t n_tiles, m_tiles;
     uint32_t grid_n, grid_m;      // workgroups' tiles of outputs and of rows
+    int32_t out_wide;             // rows of out may be written 16 bytes at a time
     int32_t dtype;
 };
 
@@ -245,75 +247,132 @@ template <int MT, int W> __global__ __launch_bounds__(64 * W) void k_f8_thin(Mat
     }
 }
 
-// 16 bytes a lane from memory into shared memory, lane after lane from `to` on (uniform over the
-// wave); done when the loads are waited for.
-__device__ inline void load_lds(const uint8_t *from, uint8_t *to)
+// 16 bytes a lane from a buffer into shared memory, lane after lane from `to` on (uniform over the
+// wave); done when the loads are waited for.  Zeros past the buffer's end.
+__device__ inline void load_lds(__amdgpu_buffer_rsrc_t from, int at, int lane_at, uint8_t *to)
 {
-    typedef const uint32_t __attribute__((address_space(1))) *global_ptr;
     typedef uint32_t __attribute__((address_space(3))) *shared_ptr;
-    __builtin_amdgcn_global_load_lds((global_ptr)(uintptr_t)from, (shared_ptr)(uintptr_t)to, 16, 0,
-                                     0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (shared_ptr)(uintptr_t)to, 16, lane_at, at, 0,
+                                             0);
+}
+
+// 16 rows of NT tiles of outputs, turned in shared memory so that a row's outputs are stored side by
+// side: 16 bytes a lane where rows and outputs are whole, else an output a lane.  `lds`: 16 rows of
+// the wave's own, a row's 16-byte pieces p at p ^ row.
+template <int NT, typename T>
+__device__ inline void store_rows(const MatArgs &a, int64_t m0, int n0, const float4v *v,
+                                  uint8_t *lds)
+{
+    constexpr int ROW = 16 * NT * sizeof(T), CHUNKS = ROW / 16, MASK = (CHUNKS < 16 ? CHUNKS : 16) - 1;
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));         // (places that depend on it are not kept from tile to tile)
+    const int r = lane & 15, q = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        const int at = (16 * i + 4 * q) * sizeof(T);
+        uint8_t *to = lds + r * ROW + ((at / 16) ^ (r & MASK)) * 16 + at % 16;
+        if constexpr (sizeof(T) == 4) {
+            *(float4v *)to = v[i];
+        } else {
+            *(uint2 *)to = uint2{out_bits(v[i][0], a.dtype) | out_bits(v[i][1], a.dtype) << 16,
+                                 out_bits(v[i][2], a.dtype) | out_bits(v[i][3], a.dtype) << 16};
+        }
+    }
+    const int rows = (int)min((int64_t)kTile, a.M - m0);
+    T *out = (T *)a.out + m0 * a.out_stride + n0;
+    if (a.out_wide && n0 + 16 * NT <= a.N) {
+        constexpr int PER = 64 / CHUNKS;
+        const int c = lane % CHUNKS;
+#pragma unroll
+        for (int k = 0; k < kTile; k += PER) {
+            const int row = k + lane / CHUNKS;
+            const uint4 w = *(const uint4 *)(lds + row * ROW + (c ^ (row & MASK)) * 16);
+            if (row < rows) *(uint4 *)((uint8_t *)(out + row * a.out_stride) + 16 * c) = w;
+        }
+        return;
+    }
+#pragma unroll 4
+    for (int row = 0; row < rows; ++row)
+#pragma unroll
+        for (int k = 0; k < 16 * NT; k += 64) {
+            const int e = k + lane, at = e * sizeof(T);
+            if (e < 16 * NT && n0 + e < a.N)
+                out[row * a.out_stride + e] =
+                    *(const T *)(lds + row * ROW + ((at / 16) ^ (row & MASK)) * 16 + at % 16);
+        }
 }
 
 // Tiles of (16 NT WN) outputs and (16 MT WM) rows to a workgroup of WN x WM waves.
-template <int NT, int MT, int WN, int WM>
+template <int NT, int MT, int WN, int WM, int SLOTS>
 __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
 {
-    constexpr int W = WN * WM, TN = NT * WN, TM = MT * WM, PIECES = 2 * (TN + TM);
-    static_assert(PIECES % W == 0, "pieces of a stage are shared evenly");
-    __shared__ __align__(16) uint8_t buf0[1024 * PIECES], buf1[1024 * PIECES];
+    constexpr int W = WN * WM, TN = NT * WN, TM = MT * WM;
+    static_assert(2 * TN % W == 0 && 2 * TM % W == 0, "a half's pieces are shared evenly");
+    constexpr int kSlot = kTileBytes * (TN > TM ? TN : TM);
+    __shared__ __align__(16) uint8_t s0[kSlot], s1[kSlot], s2[kSlot], s3[kSlot],
+        s4[SLOTS > 4 ? kSlot : 16], s5[SLOTS > 5 ? kSlot : 16];
+    uint8_t *const slot[6] = {s0, s1, s2, s3, s4, s5};
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wn = wv % WN, wm = wv / WN;
     // eight dies take runs of tiles of their own, in each four rows' tiles before the next outputs'
     const uint32_t total = a.grid_n * a.grid_m, per = (total + 7) / 8;
-    const uint32_t id = blockIdx.x % 8 * per + blockIdx.x / 8;
-    if (id >= total) return;
-    const uint32_t group = id / (4 * a.grid_n), in = id % (4 * a.grid_n);
-    const uint32_t high = min(4u, a.grid_m - 4 * group);
-    const int nt0 = (int)(in / high) * TN, mt0 = (int)(4 * group + in % high) * TM;
+    uint32_t turn = blockIdx.x / 8;
+    const int last = a.blocks - 1;
 
-    const uint8_t *from[PIECES / W];
-#pragma unroll
-    for (int i = 0; i < PIECES / W; ++i) {
-        const int p = i * W + wv, t = p / 2;
-        const int64_t tile = t < TN ? min(nt0 + t, a.n_tiles - 1) : min(mt0 + t - TN, a.m_tiles - 1);
-        from[i] = (t < TN ? a.w : a.x) + tile * a.blocks * kTileBytes + 1024 * (p & 1);
-    }
-    auto fetch = [&](int b, uint8_t *to) {
-#pragma unroll
-        for (int i = 0; i < PIECES / W; ++i)
-            load_lds(from[i] + (int64_t)b * kTileBytes + 16 * lane, to + 1024 * (i * W + wv));
+    // a wave's pieces of a half: half a tile each, of every (W / 2)-th tile
+    static_assert(W % 2 == 0, "a wave's pieces are the same halves of its tiles");
+    constexpr int PN = 2 * TN / W, PM = 2 * TM / W;
+    const int tile_bytes = a.blocks * kTileBytes;
+    int nt0, mt0;
+    __amdgpu_buffer_rsrc_t w_from, x_from;
+    const float *ws, *xs;
+    auto next_tile = [&] {
+        const uint32_t id = blockIdx.x % 8 * per + turn;
+        if (turn >= per || id >= total) return false;
+        turn += gridDim.x / 8;
+        const uint32_t group = id / (4 * a.grid_n), in = id % (4 * a.grid_n);
+        const uint32_t high = min(4u, a.grid_m - 4 * group);
+        nt0 = (int)(in / high) * TN;
+        mt0 = (int)(4 * group + in % high) * TM;
+        auto from = [&](const uint8_t *p, int t0, int tiles, int most) {
+            return __builtin_amdgcn_make_buffer_rsrc((void *)(p + (int64_t)t0 * tile_bytes), 0,
+                                                     min(tiles - t0, most) * tile_bytes, 0x00020000);
+        };
+        w_from = from(a.w, nt0, a.n_tiles, TN);
+        x_from = from(a.x, mt0, a.m_tiles, TM);
+        ws = a.ws + (int64_t)(min(nt0 + wn * NT, a.n_tiles - 1) / (kBlock / kTile)) * a.blocks;
+        xs = a.xs + (int64_t)mt0 * kTile;
+        return true;
     };
-    const int nb = min(nt0 + wn * NT, a.n_tiles - 1) / (kBlock / kTile);
-    const float *ws = a.ws + (int64_t)nb * a.blocks;
-    const float *xs[MT];
-    for (int i = 0; i < MT; ++i)
-        xs[i] = a.xs + min(mt0 + wm * MT + i, a.m_tiles - 1) * kTile;
+    const int lane_at = 16 * lane + 1024 * (wv & 1);
+    // half h of the loads: the weights of block h / 2, then its rows, in slot h % SLOTS
+    auto fetch = [&](bool n, int b, uint8_t *to) {
+        const int at = wv / 2 * tile_bytes + min(b, last) * kTileBytes;
+#pragma unroll
+        for (int i = 0; i < (n ? PN : PM); ++i)
+            load_lds(n ? w_from : x_from, at + i * (W / 2) * tile_bytes, lane_at,
+                     to + 1024 * (i * W + wv));
+    };
     float4v acc[NT][MT];
-#pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int j = 0; j < MT; ++j) acc[i][j] = float4v{0, 0, 0, 0};
     float by[MT], w_next, x_next[MT];
     auto fetch_scales = [&](int b) {
+        b = min(b, last);
         w_next = ws[b];
+        const float *p = xs + (int64_t)b * a.padded;
 #pragma unroll
-        for (int j = 0; j < MT; ++j) x_next[j] = (xs[j] + (int64_t)b * a.padded)[lane & 15];
+        for (int j = 0; j < MT; ++j)
+            x_next[j] = (p + min(wm * MT + j, a.m_tiles - 1 - mt0) * kTile)[lane & 15];
     };
-    auto scales = [&] {
-#pragma unroll
-        for (int j = 0; j < MT; ++j) by[j] = w_next * x_next[j];
-    };
-    auto step = [&](const uint8_t *cur) {
+    auto step = [&](const uint8_t *wt, const uint8_t *xt) {
         int8v x[MT];
 #pragma unroll
-        for (int j = 0; j < MT; ++j) x[j] = operand(cur + kTileBytes * (TN + wm * MT + j), lane);
-        int8v ahead = operand(cur + kTileBytes * wn * NT, lane);
+        for (int j = 0; j < MT; ++j) x[j] = operand(xt + kTileBytes * (wm * MT + j), lane);
+        int8v ahead = operand(wt + kTileBytes * wn * NT, lane);
         float4v was[MT], now[MT];
 #pragma unroll
         for (int i = 0; i <= NT; ++i) {
             const int8v w = ahead;
-            if (i + 1 < NT) ahead = operand(cur + kTileBytes * (wn * NT + i + 1), lane);
+            if (i + 1 < NT) ahead = operand(wt + kTileBytes * (wn * NT + i + 1), lane);
 #pragma unroll
             for (int j = 0; j < MT; ++j) {
                 if (i < NT) now[j] = product(w, x[j]);
@@ -330,37 +389,72 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    // One barrier a stage: behind it the stage's loads are there and the other buffer's readers are
-    // done.  No branch stands inside: the additions would move behind it with all their products
-    // held in registers.  (The last loads may be the last block's once more.)
-    const int last = a.blocks - 1;
-    fetch(0, buf0);
-    fetch_scales(0);
-    int b = 0;
-    for (; b < last; b += 2) {
-        __syncthreads();
-        scales();
-        fetch(b + 1, buf1);
-        fetch_scales(b + 1);
-        step(buf0);
-        __syncthreads();
-        scales();
-        fetch(min(b + 2, last), buf0);
-        fetch_scales(min(b + 2, last));
-        step(buf1);
-    }
-    __syncthreads();
-    if (b == last) {
-        scales();
-        step(buf0);
-    }
+    // Loads run SLOTS - 2 halves ahead.  Behind a block's barrier its own halves are there and
+    // those of the block before have no readers any more.
+    constexpr int AHEAD = SLOTS - 2;
+    auto begin = [&] {
+        fetch_scales(0);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int j = 0; j < MT; ++j) {
-        const int64_t m = (int64_t)(mt0 + wm * MT + j) * kTile + (lane & 15);
-        if (m >= a.M) continue;
+        for (int h = 0; h < AHEAD; ++h) fetch(h % 2 == 0, h / 2, slot[h]);
+    };
+    auto block = [&](int b, int i) {       // i: b's place in a turn of SLOTS blocks
+        // the loads that may be under way still: those of halves past this block's two
+        constexpr int LATER = (AHEAD - 2) / 2 * (PN + PM) + (AHEAD % 2 ? PN : 0);
+        __builtin_amdgcn_s_waitcnt((LATER & 15) | (LATER >> 4) << 14 | 7 << 4 | 15 << 8);
+        __builtin_amdgcn_s_barrier();
+#pragma unroll
+        for (int j = 0; j < MT; ++j) by[j] = w_next * x_next[j];
+        __builtin_amdgcn_sched_barrier(0);
+        fetch_scales(b + 1);
+        __builtin_amdgcn_sched_barrier(0);     // (before the loads: waited for with fewer left)
+#pragma unroll
+        for (int h = AHEAD; h < AHEAD + 2; ++h)
+            fetch(h % 2 == 0, b + h / 2, slot[(2 * i + h) % SLOTS]);
+        __builtin_amdgcn_sched_barrier(0);
+        step(slot[2 * i % SLOTS], slot[(2 * i + 1) % SLOTS]);
+    };
+    if (!next_tile()) return;
+    begin();
+    for (bool more = true; more;) {
 #pragma unroll
         for (int i = 0; i < NT; ++i)
-            store4(a, m, (nt0 + wn * NT + i) * kTile + 4 * (lane >> 4), acc[i][j]);
+#pragma unroll
+            for (int j = 0; j < MT; ++j) acc[i][j] = float4v{0, 0, 0, 0};
+        int b = 0;
+        for (; b + SLOTS <= a.blocks; b += SLOTS)
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i) block(b + i, i);
+#pragma unroll
+        for (int i = 0; i < SLOTS - 1; ++i) {
+            // (the sums are made before the branch: they would move behind it with all their
+            // products held in registers)
+#pragma unroll
+            for (int k = 0; k < NT; ++k)
+#pragma unroll
+                for (int j = 0; j < MT; ++j) asm volatile("" : "+v"(acc[k][j]));
+            if (b + i < a.blocks) block(b + i, i);
+        }
+        // the next tile's first loads are under way while this one's outputs are stored
+        __syncthreads();
+        const int n0 = (nt0 + wn * NT) * kTile, mt = mt0 + wm * MT;
+        more = next_tile();
+        if (more) begin();
+        constexpr int kStage = kTile * 16 * NT * 4, kIn = kSlot / kStage;
+        static_assert(2 * kIn >= W, "the waves' outputs fit the two slots that are not under way");
+        uint8_t *lds = (wv < kIn ? slot[AHEAD] : slot[AHEAD + 1]) + wv % kIn * kStage;
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+            float4v v[NT];
+#pragma unroll
+            for (int i = 0; i < NT; ++i) v[i] = acc[i][j];
+            if (mt + j >= a.m_tiles) break;
+            const int64_t m0 = (int64_t)(mt + j) * kTile;
+            if (a.dtype == QLM_F32)
+                store_rows<NT, float>(a, m0, n0, v, lds);
+            else
+                store_rows<NT, uint16_t>(a, m0, n0, v, lds);
+        }
     }
 }
 
@@ -495,12 +589,15 @@ int qlm_f8_matmul(const qlm_f8_codes *rows, const qlm_f8 *weight, void *out, int
     a.m_tiles = (int32_t)tiles_of(a.M);
     a.padded = a.m_tiles * kTile;
     a.dtype = dtype;
+    const int size = dtype == QLM_F32 ? 4 : 2;
+    a.out_wide = (uintptr_t)out % 16 == 0 && out_stride * size % 16 == 0;
     if (a.m_tiles > 4) {
         a.grid_n = (a.n_tiles + 15) / 16;
         a.grid_m = (a.m_tiles + 15) / 16;
-        const int64_t grid = (int64_t)a.grid_n * a.grid_m;
-        if (!can_launch(grid, 512)) return fail(QLM_ERR_CAPACITY, "too many outputs in one call");
-        k_f8_wide<8, 4, 2, 4><<<(unsigned)((grid + 7) / 8 * 8), 512, 0, stream>>>(a);
+        const int64_t tiles = (int64_t)a.grid_n * a.grid_m;
+        if (tiles > INT32_MAX) return fail(QLM_ERR_CAPACITY, "too many outputs in one call");
+        const int64_t grid = std::min<int64_t>(kCus, (tiles + 7) / 8 * 8);
+        k_f8_wide<8, 4, 2, 4, 5><<<(unsigned)grid, 512, 0, stream>>>(a);
         hipError_t e = hipGetLastError();
         return e == hipSuccess ? QLM_OK : hip_fail(e, "f8 launch");
     }
