@@ -20,6 +20,7 @@
 #include <cstdint>
 #include <string>
 
+#include "f8_plan.h"
 #include "internal.h"
 #include "qlm.h"
 
@@ -32,11 +33,14 @@ typedef float float4v __attribute__((ext_vector_type(4)));
 typedef int int4v __attribute__((ext_vector_type(4)));
 typedef int int8v __attribute__((ext_vector_type(8)));
 
-constexpr int kBlock = QLM_F8_BLOCK, kTile = QLM_F8_TILE;
+using qlm_f8_host::kBlock;
+using qlm_f8_host::kCus;
+using qlm_f8_host::kTile;
+using qlm_f8_host::Plan;
+static_assert(kBlock == QLM_F8_BLOCK && kTile == QLM_F8_TILE, "the header's sizes");
 constexpr int kTileBytes = kBlock * kTile;
 constexpr int kLeastExp = -100;
 constexpr int kMost = 1 << 24;
-constexpr int kCus = 256;
 
 int64_t blocks_of(int n) { return ((int64_t)n + kBlock - 1) / kBlock; }
 int64_t tiles_of(int n) { return ((int64_t)n + kTile - 1) / kTile; }
@@ -170,6 +174,9 @@ struct MatArgs {
     int32_t n_tiles, m_tiles;
     uint32_t grid_n, grid_m;      // workgroups' tiles of outputs and of rows
     int32_t out_wide;             // rows of out may be written 16 bytes at a time
+    // the blocks of inputs in `splits` runs of `per_split`, whose sums stand out_split apart
+    int32_t splits, per_split;
+    int64_t out_split;
     int32_t dtype;
 };
 
@@ -214,8 +221,9 @@ __device__ inline void store4(const MatArgs &a, int64_t m, int n, float4v v)
         if (n + i < a.N) p[i] = (uint16_t)out_bits(v[i], a.dtype);
 }
 
-// 16 outputs of MT tiles of rows to a workgroup, its W waves taking the blocks of inputs in turn.
-template <int MT, int W> __global__ __launch_bounds__(64 * W) void k_f8_thin(MatArgs a)
+// 16 outputs of MT tiles of rows to a workgroup, its W waves taking the blocks of inputs in turn,
+// U of them loaded at once.
+template <int MT, int W, int U> __global__ __launch_bounds__(64 * W) void k_f8_thin(MatArgs a)
 {
     __shared__ float4v part[W][MT][64];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -225,16 +233,39 @@ template <int MT, int W> __global__ __launch_bounds__(64 * W) void k_f8_thin(Mat
     for (int i = 0; i < MT; ++i) acc[i] = float4v{0, 0, 0, 0};
     const uint8_t *w = a.w + (int64_t)nt * a.blocks * kTileBytes;
     const float *ws = a.ws + (int64_t)(nt / (kBlock / kTile)) * a.blocks;
-    for (int b = wv; b < a.blocks; b += W) {
-        const int8v wo = operand(w + (int64_t)b * kTileBytes, lane);
-        const float s = ws[b];
+    const uint8_t *x[MT];
+    const float *xs[MT];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const int mt = min(mt0 + i, a.m_tiles - 1);
-            const int8v xo = operand(a.x + ((int64_t)mt * a.blocks + b) * kTileBytes, lane);
-            const float by = s * a.xs[(int64_t)b * a.padded + mt * kTile + (lane & 15)];
-            const float4v c = product(wo, xo);
-            for (int j = 0; j < 4; ++j) acc[i][j] += by * c[j];
+    for (int i = 0; i < MT; ++i) {
+        const int mt = min(mt0 + i, a.m_tiles - 1);
+        x[i] = a.x + (int64_t)mt * a.blocks * kTileBytes;
+        xs[i] = a.xs + mt * kTile + (lane & 15);
+    }
+    for (int b0 = wv; b0 < a.blocks; b0 += U * W) {
+        int8v wo[U], xo[U][MT];
+        float s[U], t[U][MT];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            // (past the last block it is read again and not used)
+            const int b = min(b0 + u * W, a.blocks - 1);
+            wo[u] = operand(w + (int64_t)b * kTileBytes, lane);
+            s[u] = ws[b];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                xo[u][i] = operand(x[i] + (int64_t)b * kTileBytes, lane);
+                t[u][i] = xs[i][(int64_t)b * a.padded];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (b0 + u * W >= a.blocks) break;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const float4v c = product(wo[u], xo[u][i]);
+                const float by = s[u] * t[u][i];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] += by * c[j];
+            }
         }
     }
     for (int i = 0; i < MT; ++i) part[wv][i][lane] = acc[i];
@@ -256,12 +287,19 @@ __device__ inline void load_lds(__amdgpu_buffer_rsrc_t from, int at, int lane_at
                                              0);
 }
 
+// Waits until at most N of the wave's memory operations are under way.
+template <int N> __device__ inline void wait_loads()
+{
+    static_assert(N < 64, "the counter's bits");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 7 << 4 | 15 << 8);
+}
+
 // 16 rows of NT tiles of outputs, turned in shared memory so that a row's outputs are stored side by
 // side: 16 bytes a lane where rows and outputs are whole, else an output a lane.  `lds`: 16 rows of
 // the wave's own, a row's 16-byte pieces p at p ^ row.
 template <int NT, typename T>
-__device__ inline void store_rows(const MatArgs &a, int64_t m0, int n0, const float4v *v,
-                                  uint8_t *lds)
+__device__ inline void store_rows(const MatArgs &a, int split, int64_t m0, int n0,
+                                  const float4v *v, uint8_t *lds)
 {
     constexpr int ROW = 16 * NT * sizeof(T), CHUNKS = ROW / 16, MASK = (CHUNKS < 16 ? CHUNKS : 16) - 1;
     int lane = threadIdx.x & 63;
@@ -279,7 +317,7 @@ __device__ inline void store_rows(const MatArgs &a, int64_t m0, int n0, const fl
         }
     }
     const int rows = (int)min((int64_t)kTile, a.M - m0);
-    T *out = (T *)a.out + m0 * a.out_stride + n0;
+    T *out = (T *)a.out + split * a.out_split + m0 * a.out_stride + n0;
     if (a.out_wide && n0 + 16 * NT <= a.N) {
         constexpr int PER = 64 / CHUNKS;
         const int c = lane % CHUNKS;
@@ -315,39 +353,43 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wn = wv % WN, wm = wv / WN;
     // eight dies take runs of tiles of their own, in each four rows' tiles before the next outputs'
-    const uint32_t total = a.grid_n * a.grid_m, per = (total + 7) / 8;
+    const uint32_t tiles = a.grid_n * a.grid_m, total = tiles * a.splits, per = (total + 7) / 8;
     uint32_t turn = blockIdx.x / 8;
-    const int last = a.blocks - 1;
 
     // a wave's pieces of a half: half a tile each, of every (W / 2)-th tile
     static_assert(W % 2 == 0, "a wave's pieces are the same halves of its tiles");
     constexpr int PN = 2 * TN / W, PM = 2 * TM / W;
     const int tile_bytes = a.blocks * kTileBytes;
-    int nt0, mt0;
+    int nt0, mt0, split, count;
     __amdgpu_buffer_rsrc_t w_from, x_from;
     const float *ws, *xs;
     auto next_tile = [&] {
         const uint32_t id = blockIdx.x % 8 * per + turn;
         if (turn >= per || id >= total) return false;
         turn += gridDim.x / 8;
-        const uint32_t group = id / (4 * a.grid_n), in = id % (4 * a.grid_n);
+        split = (int)(id / tiles);
+        const int b0 = split * a.per_split;
+        count = min(a.per_split, a.blocks - b0);
+        const uint32_t tile = id % tiles, group = tile / (4 * a.grid_n), in = tile % (4 * a.grid_n);
         const uint32_t high = min(4u, a.grid_m - 4 * group);
         nt0 = (int)(in / high) * TN;
         mt0 = (int)(4 * group + in % high) * TM;
-        auto from = [&](const uint8_t *p, int t0, int tiles, int most) {
-            return __builtin_amdgcn_make_buffer_rsrc((void *)(p + (int64_t)t0 * tile_bytes), 0,
-                                                     min(tiles - t0, most) * tile_bytes, 0x00020000);
+        auto from = [&](const uint8_t *p, int t0, int have, int most) {
+            const int skip = b0 * kTileBytes;
+            return __builtin_amdgcn_make_buffer_rsrc((void *)(p + (int64_t)t0 * tile_bytes + skip), 0,
+                                                     min(have - t0, most) * tile_bytes - skip,
+                                                     0x00020000);
         };
         w_from = from(a.w, nt0, a.n_tiles, TN);
         x_from = from(a.x, mt0, a.m_tiles, TM);
-        ws = a.ws + (int64_t)(min(nt0 + wn * NT, a.n_tiles - 1) / (kBlock / kTile)) * a.blocks;
-        xs = a.xs + (int64_t)mt0 * kTile;
+        ws = a.ws + (int64_t)(min(nt0 + wn * NT, a.n_tiles - 1) / (kBlock / kTile)) * a.blocks + b0;
+        xs = a.xs + (int64_t)b0 * a.padded + (int64_t)mt0 * kTile;
         return true;
     };
     const int lane_at = 16 * lane + 1024 * (wv & 1);
     // half h of the loads: the weights of block h / 2, then its rows, in slot h % SLOTS
     auto fetch = [&](bool n, int b, uint8_t *to) {
-        const int at = wv / 2 * tile_bytes + min(b, last) * kTileBytes;
+        const int at = wv / 2 * tile_bytes + min(b, count - 1) * kTileBytes;
 #pragma unroll
         for (int i = 0; i < (n ? PN : PM); ++i)
             load_lds(n ? w_from : x_from, at + i * (W / 2) * tile_bytes, lane_at,
@@ -356,7 +398,7 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
     float4v acc[NT][MT];
     float by[MT], w_next, x_next[MT];
     auto fetch_scales = [&](int b) {
-        b = min(b, last);
+        b = min(b, count - 1);
         w_next = ws[b];
         const float *p = xs + (int64_t)b * a.padded;
 #pragma unroll
@@ -401,8 +443,10 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
     auto block = [&](int b, int i) {       // i: b's place in a turn of SLOTS blocks
         // the loads that may be under way still: those of halves past this block's two
         constexpr int LATER = (AHEAD - 2) / 2 * (PN + PM) + (AHEAD % 2 ? PN : 0);
-        __builtin_amdgcn_s_waitcnt((LATER & 15) | (LATER >> 4) << 14 | 7 << 4 | 15 << 8);
+        wait_loads<LATER>();
+        asm volatile("" ::: "memory");         // (no read or write moves over the barrier)
         __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
 #pragma unroll
         for (int j = 0; j < MT; ++j) by[j] = w_next * x_next[j];
         __builtin_amdgcn_sched_barrier(0);
@@ -422,7 +466,7 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
 #pragma unroll
             for (int j = 0; j < MT; ++j) acc[i][j] = float4v{0, 0, 0, 0};
         int b = 0;
-        for (; b + SLOTS <= a.blocks; b += SLOTS)
+        for (; b + SLOTS <= count; b += SLOTS)
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i) block(b + i, i);
 #pragma unroll
@@ -433,11 +477,12 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
             for (int k = 0; k < NT; ++k)
 #pragma unroll
                 for (int j = 0; j < MT; ++j) asm volatile("" : "+v"(acc[k][j]));
-            if (b + i < a.blocks) block(b + i, i);
+            if (b + i < count) block(b + i, i);
         }
         // the next tile's first loads are under way while this one's outputs are stored
+        wait_loads<0>();
         __syncthreads();
-        const int n0 = (nt0 + wn * NT) * kTile, mt = mt0 + wm * MT;
+        const int n0 = (nt0 + wn * NT) * kTile, mt = mt0 + wm * MT, part = split;
         more = next_tile();
         if (more) begin();
         constexpr int kStage = kTile * 16 * NT * 4, kIn = kSlot / kStage;
@@ -451,11 +496,23 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
             if (mt + j >= a.m_tiles) break;
             const int64_t m0 = (int64_t)(mt + j) * kTile;
             if (a.dtype == QLM_F32)
-                store_rows<NT, float>(a, m0, n0, v, lds);
+                store_rows<NT, float>(a, part, m0, n0, v, lds);
             else
-                store_rows<NT, uint16_t>(a, m0, n0, v, lds);
+                store_rows<NT, uint16_t>(a, part, m0, n0, v, lds);
         }
     }
+}
+
+// Sums of the runs, in their order, four outputs of a row a thread.
+__global__ __launch_bounds__(256) void k_f8_join(MatArgs a, const float *part, int64_t ld, int64_t run)
+{
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t m = at / (ld / 4);
+    const int n = (int)(at % (ld / 4)) * 4;
+    if (m >= a.M) return;
+    float4v v = *(const float4v *)(part + m * ld + n);
+    for (int k = 1; k < a.splits; ++k) v += *(const float4v *)(part + k * run + m * ld + n);
+    store4(a, m, n, v);
 }
 
 int check_weight(const qlm_f8 *w)
@@ -479,6 +536,18 @@ int check_codes(const qlm_f8_codes *r)
     if ((uintptr_t)r->codes % 16 || (uintptr_t)r->scale % 4)
         return fail(QLM_ERR_ARG, "codes must be 16-byte, scale 4-byte aligned");
     return QLM_OK;
+}
+
+int64_t part_stride(int n_out) { return ((int64_t)n_out + 3) / 4 * 4; }
+
+// GROUPS: workgroups that a compute unit holds.
+template <int NT, int MT, int WN, int WM, int GROUPS> void launch_wide(MatArgs a, hipStream_t stream)
+{
+    a.grid_n = (a.n_tiles + NT * WN - 1) / (NT * WN);
+    a.grid_m = (a.m_tiles + MT * WM - 1) / (MT * WM);
+    const int64_t tiles = (int64_t)a.grid_n * a.grid_m * a.splits;
+    const int64_t grid = std::min<int64_t>(GROUPS * kCus, (tiles + 7) / 8 * 8);
+    k_f8_wide<NT, MT, WN, WM, 5><<<(unsigned)grid, 64 * WN * WM, 0, stream>>>(a);
 }
 
 int64_t code_bytes(int n_out, int n_in) { return tiles_of(n_out) * blocks_of(n_in) * kTileBytes; }
@@ -551,9 +620,9 @@ int qlm_f8_rows(const qlm_f8_codes *rows, const void *x, int64_t x_stride, int32
 
 size_t qlm_f8_workspace_bytes(const qlm_f8 *weight, int32_t n_rows)
 {
-    (void)weight;
-    (void)n_rows;
-    return 0;
+    if (check_weight(weight) || n_rows < 1) return 0;
+    const Plan p = qlm_f8_host::plan_of(weight->n_out, weight->n_in, n_rows);
+    return p.splits > 1 ? (size_t)p.splits * n_rows * part_stride(weight->n_out) * 4 : 0;
 }
 
 int qlm_f8_matmul(const qlm_f8_codes *rows, const qlm_f8 *weight, void *out, int64_t out_stride,
@@ -591,27 +660,48 @@ int qlm_f8_matmul(const qlm_f8_codes *rows, const qlm_f8 *weight, void *out, int
     a.dtype = dtype;
     const int size = dtype == QLM_F32 ? 4 : 2;
     a.out_wide = (uintptr_t)out % 16 == 0 && out_stride * size % 16 == 0;
-    if (a.m_tiles > 4) {
-        a.grid_n = (a.n_tiles + 15) / 16;
-        a.grid_m = (a.m_tiles + 15) / 16;
-        const int64_t tiles = (int64_t)a.grid_n * a.grid_m;
-        if (tiles > INT32_MAX) return fail(QLM_ERR_CAPACITY, "too many outputs in one call");
-        const int64_t grid = std::min<int64_t>(kCus, (tiles + 7) / 8 * 8);
-        k_f8_wide<8, 4, 2, 4, 5><<<(unsigned)grid, 512, 0, stream>>>(a);
+    const Plan p = qlm_f8_host::plan_of(weight->n_out, weight->n_in, rows->n_rows);
+    if (p.side) {
+        a.splits = p.splits;
+        a.per_split = p.per_split;
+        MatArgs o = a;
+        const int64_t ld = part_stride(a.N), run = a.M * ld;
+        if (p.splits > 1) {
+            o.out = ws;
+            o.out_stride = ld;
+            o.out_split = run;
+            o.out_wide = 1;
+            o.dtype = QLM_F32;
+        }
+        const int64_t tiles = (int64_t)((a.N + p.side - 1) / p.side) *
+                              ((a.M + (int64_t)p.side - 1) / p.side) * p.splits;
+        if (tiles > INT32_MAX / 2) return fail(QLM_ERR_CAPACITY, "too many outputs in one call");
+        if (p.side == 64)
+            launch_wide<2, 2, 2, 2, 3>(o, stream);
+        else if (p.side == 128)
+            launch_wide<4, 2, 2, 4, 2>(o, stream);
+        else
+            launch_wide<8, 4, 2, 4, 1>(o, stream);
         hipError_t e = hipGetLastError();
-        return e == hipSuccess ? QLM_OK : hip_fail(e, "f8 launch");
+        if (e != hipSuccess) return hip_fail(e, "k_f8_wide launch");
+        if (p.splits > 1) {
+            const int64_t grid = (a.M * (ld / 4) + 255) / 256;
+            k_f8_join<<<(unsigned)grid, 256, 0, stream>>>(a, (const float *)ws, ld, run);
+            if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_f8_join launch");
+        }
+        return QLM_OK;
     }
     const int mt = a.m_tiles == 1 ? 1 : a.m_tiles == 2 ? 2 : 4;
     const int64_t grid = (int64_t)a.n_tiles * ((a.m_tiles + mt - 1) / mt);
     if (!can_launch(grid, 512)) return fail(QLM_ERR_CAPACITY, "too many outputs in one call");
     if (mt == 1)
-        k_f8_thin<1, 8><<<(unsigned)grid, 512, 0, stream>>>(a);
+        k_f8_thin<1, 8, 4><<<(unsigned)grid, 512, 0, stream>>>(a);
     else if (mt == 2)
-        k_f8_thin<2, 8><<<(unsigned)grid, 512, 0, stream>>>(a);
+        k_f8_thin<2, 8, 4><<<(unsigned)grid, 512, 0, stream>>>(a);
     else
-        k_f8_thin<4, 8><<<(unsigned)grid, 512, 0, stream>>>(a);
+        k_f8_thin<4, 8, 3><<<(unsigned)grid, 512, 0, stream>>>(a);
     hipError_t e = hipGetLastError();
-    return e == hipSuccess ? QLM_OK : hip_fail(e, "f8 launch");
+    return e == hipSuccess ? QLM_OK : hip_fail(e, "k_f8_thin launch");
 }
 
 }  // extern "C"
