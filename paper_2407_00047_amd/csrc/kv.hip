@@ -161,13 +161,13 @@ struct TurnArgs {
     const float *cos, *sin;
     const int32_t *axis, *position;
     int32_t half, n_positions, n_axes;
-    int32_t table_wide;             // the tables may be read 16 bytes at a time
+    int32_t table_wide;             // the tables (and axes) may be read 16 bytes at a time
     const void *q;
     void *q_out;
     int64_t q_row, q_head, out_row, out_head;
     int32_t q_type, q_wide, n_heads;
     int32_t units, pair_units;      // 16 dims of a head each: the pairs' first, then the rest
-    uint32_t key_groups, row_groups;   // workgroups of the keys; of a row's queries
+    uint32_t key_groups, row_items;    // workgroups of the keys; waves of a row's queries
 };
 
 // The place in the tables of pair i of a row (`own`: its position without `position`).
@@ -181,26 +181,34 @@ __device__ inline int64_t table_at(const TurnArgs &t, int n_rows, int row, int o
     return (int64_t)max(0, min(p, t.n_positions - 1)) * t.half + i;
 }
 
-// cos and sin of N pairs from i on, of which those from `half` on are not read (1 and 0).
+// cos and sin of N pairs from i on, of which those from `half` on are not read (1 and 0).  Four
+// neighbouring pairs nearly always turn by one position: their numbers stand side by side.
 template <int N>
 __device__ inline void angles(const TurnArgs &t, int n_rows, int row, int own, int i, float *c,
                               float *s)
 {
-    if (t.table_wide && !t.axis && i + N <= t.half) {
-        const int64_t at = table_at(t, n_rows, row, own, i);
 #pragma unroll
-        for (int e = 0; e < N; e += 4) {
-            *(float4v *)(c + e) = *(const float4v *)(t.cos + at + e);
-            *(float4v *)(s + e) = *(const float4v *)(t.sin + at + e);
+    for (int e0 = 0; e0 < N; e0 += 4) {
+        if (t.table_wide && i + e0 + 4 <= t.half) {
+            bool one = true;
+            if (t.axis) {
+                const int4 ax = *(const int4 *)(t.axis + i + e0);
+                one = ax.x == ax.y && ax.x == ax.z && ax.x == ax.w;
+            }
+            if (one) {
+                const int64_t at = table_at(t, n_rows, row, own, i + e0);
+                *(float4v *)(c + e0) = *(const float4v *)(t.cos + at);
+                *(float4v *)(s + e0) = *(const float4v *)(t.sin + at);
+                continue;
+            }
         }
-        return;
-    }
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-        const bool in = i + e < t.half;
-        const int64_t at = table_at(t, n_rows, row, own, in ? i + e : 0);
-        c[e] = in ? t.cos[at] : 1.f;
-        s[e] = in ? t.sin[at] : 0.f;
+        for (int e = e0; e < e0 + 4; ++e) {
+            const bool in = i + e < t.half;
+            const int64_t at = table_at(t, n_rows, row, own, in ? i + e : 0);
+            c[e] = in ? t.cos[at] : 1.f;
+            s[e] = in ? t.sin[at] : 0.f;
+        }
     }
 }
 
@@ -248,59 +256,75 @@ __device__ inline uint32_t magnitude8(uint4 x, int dtype)
     return top;
 }
 
-// Eight values as codes over `scale`.
+// Eight values as codes over `scale`, clamped (a NaN stays one in e4m3).
 template <int FMT> __device__ inline uint2 codes_of(const float *v, float scale, bool exact)
 {
     const float by = 1.f / scale;
     uint32_t o[2] = {0, 0};
-    for (int i = 0; i < 8; ++i)
-        o[i >> 2] |= code_of<FMT>(exact ? v[i] * by : v[i] / scale) << (8 * (i & 3));
+    if (FMT == QLM_KV_E4M3) {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float x = exact ? v[i] * by : v[i] / scale;
+            y[i] = x != x ? x : __builtin_amdgcn_fmed3f(x, -448.f, 448.f);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int d = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i], y[4 * i + 1], 0, false);
+            o[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i + 2], y[4 * i + 3], d, true);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            o[i >> 2] |= code_of<FMT>(exact ? v[i] * by : v[i] / scale) << (8 * (i & 3));
+    }
     return {o[0], o[1]};
 }
 
-// Eight dims from d on of a row of a head, turned; `x`: the dims as they are, `at`: of dim 0.
-__device__ inline void turned8(const TurnArgs &t, int n_rows, int row, int own, const void *data,
-                               int64_t at, int d, uint4 x, int dtype, bool wide, bool neighbours,
-                               float *y)
+// The two runs of eight dims that a thread holds of a row of a head: whole pairs where dims that
+// make a pair stand eight dims or more apart by eights, else 16 dims side by side.
+__device__ inline void unit_dims(const TurnArgs &t, bool neighbours, int k, int *d0, int *d1)
 {
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    const bool apart = !neighbours && t.half % 8 == 0 && 8 * k < t.half;
+    *d0 = apart ? 8 * k : 16 * k;
+    *d1 = apart ? t.half + 8 * k : 16 * k + 8;
+}
+
+// A unit's dims, turned; lo, hi: the dims as they are, `at`: of the head's dim 0.
+template <bool NEIGHBOURS>
+__device__ inline void turned16(const TurnArgs &t, int n_rows, int row, int own, const void *data,
+                                int64_t at, int k, uint4 lo, uint4 hi, int dtype, float *y)
+{
+    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = bits_value((w[e >> 1] >> (16 * (e & 1))) & 0xffff, dtype);
-    if (d >= 2 * t.half) return;
-    float c[8], s[8];
-    if (neighbours) {
-        angles<4>(t, n_rows, row, own, d / 2, c, s);
+    for (int e = 0; e < 16; ++e) y[e] = bits_value((w[e >> 1] >> (16 * (e & 1))) & 0xffff, dtype);
+    if (NEIGHBOURS || t.half % 8 == 0) {
+        if (8 * k >= t.half) return;
+        float c[8], s[8];
+        angles<8>(t, n_rows, row, own, 8 * k, c, s);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (d / 2 + e < t.half) turn(y[2 * e], y[2 * e + 1], c[e], s[e]);
+        for (int e = 0; e < 8; ++e)
+            if (8 * k + e < t.half) {
+                if (NEIGHBOURS)
+                    turn(y[2 * e], y[2 * e + 1], c[e], s[e]);
+                else
+                    turn(y[e], y[e + 8], c[e], s[e]);
+            }
         return;
     }
-    if (t.half % 8 == 0) {                  // eight pairs: these dims and those half away
-        const bool low = d < t.half;
-        const int i = low ? d : d - t.half;
-        const uint4 o = row_bits8(data, at + (low ? d + t.half : i), wide);
-        const uint32_t u[4] = {o.x, o.y, o.z, o.w};
-        angles<8>(t, n_rows, row, own, i, c, s);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float other = bits_value((u[e >> 1] >> (16 * (e & 1))) & 0xffff, dtype);
-            float a = low ? y[e] : other, b = low ? other : y[e];
-            turn(a, b, c[e], s[e]);
-            y[e] = low ? a : b;
-        }
-        return;
-    }
-    for (int e = 0; e < 8; ++e) {
-        const int dim = d + e;
+#pragma unroll 1
+    for (int e = 0; e < 16; ++e) {
+        const int dim = 16 * k + e;
         if (dim >= 2 * t.half) break;
         const bool low = dim < t.half;
         const int i = low ? dim : dim - t.half;
-        const int64_t k = table_at(t, n_rows, row, own, i);
-        const float other =
-            bits_value(((const uint16_t *)data)[at + (low ? dim + t.half : i)], dtype);
-        float a = low ? y[e] : other, b = low ? other : y[e];
-        turn(a, b, t.cos[k], t.sin[k]);
-        y[e] = low ? a : b;
+        const int64_t p = table_at(t, n_rows, row, own, i);
+        const uint16_t *x = (const uint16_t *)data + at;
+        float p0 = bits_value(x[i], dtype), p1 = bits_value(x[i + t.half], dtype);
+        turn(p0, p1, t.cos[p], t.sin[p]);
+        const float z = low ? p0 : p1;
+#pragma unroll
+        for (int f = 0; f < 16; ++f) y[f] = f == e ? z : y[f];
     }
 }
 
@@ -308,13 +332,10 @@ __device__ inline void turned8(const TurnArgs &t, int n_rows, int row, int own, 
 template <int FMT> __device__ inline uint2 codes8(uint4 x, int dtype, float scale, bool exact)
 {
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    const float by = 1.f / scale;
-    uint32_t o[2] = {0, 0};
-    for (int i = 0; i < 8; ++i) {
-        const float v = bits_value((w[i >> 1] >> (16 * (i & 1))) & 0xffff, dtype);
-        o[i >> 2] |= code_of<FMT>(exact ? v * by : v / scale) << (8 * (i & 3));
-    }
-    return {o[0], o[1]};
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = bits_value((w[i >> 1] >> (16 * (i & 1))) & 0xffff, dtype);
+    return codes_of<FMT>(v, scale, exact);
 }
 
 __device__ inline bool power_of_two(float x)
@@ -381,39 +402,54 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
     const int d = 8 * (t % CH), slot0 = t / CH;
     const bool in_d = d < D;
     uint4 kx[PASS], vx[PASS];
-    float ky[TURN ? PASS : 1][8];
+    // keys that are turned are held by units of 16 dims, twice as many slots at a time
+    constexpr int UROWS = 2 * ROWS, UPASS = PASS / 2;
+    static_assert(!TURN || PASS % 2 == 0, "units of 16 dims take half the passes");
+    const int unit = t % (CH / 2), uslot0 = t / (CH / 2);
+    float ky[TURN ? UPASS : 1][16];
 #pragma unroll
     for (int p = 0; p < PASS; ++p) {
         // (a slot or dim that is not new is read as one that is: neither counts nor is
         // written)
         const int64_t r = r0 + min(max(slot0 + p * ROWS, o0), o1 - 1) - o0;
         const int dd = min(d, D - 8);
-        kx[p] = row_bits8(a.k, (int64_t)h * a.k_head + r * a.k_row + dd, a.k_wide);
+        if (!TURN) kx[p] = row_bits8(a.k, (int64_t)h * a.k_head + r * a.k_row + dd, a.k_wide);
         vx[p] = row_bits8(a.v, (int64_t)h * a.v_head + r * a.v_row + dd, a.v_wide);
     }
+    int ud0 = 0, ud1 = 0;
     if (TURN) {
         const int64_t own0 = a.first ? a.first[s] : start;
+        const int k = min(unit, D / 16 - 1);
+        unit_dims(turned, TURN == 2, k, &ud0, &ud1);
 #pragma unroll
-        for (int p = 0; p < PASS; ++p) {
-            const int64_t r = r0 + min(max(slot0 + p * ROWS, o0), o1 - 1) - o0;
-            turned8(turned, a.q.n_rows, (int)r, position_of(own0, r - row0), a.k,
-                    (int64_t)h * a.k_head + r * a.k_row, min(d, D - 8), kx[p], a.k_type, a.k_wide,
-                    TURN == 2, ky[p]);
+        for (int p = 0; p < UPASS; ++p) {
+            const int64_t r = r0 + min(max(uslot0 + p * UROWS, o0), o1 - 1) - o0;
+            const int64_t at = (int64_t)h * a.k_head + r * a.k_row;
+            kx[2 * p] = row_bits8(a.k, at + ud0, a.k_wide);
+            kx[2 * p + 1] = row_bits8(a.k, at + ud1, a.k_wide);
+        }
+#pragma unroll
+        for (int p = 0; p < UPASS; ++p) {
+            const int64_t r = r0 + min(max(uslot0 + p * UROWS, o0), o1 - 1) - o0;
+            turned16<TURN == 2>(turned, a.q.n_rows, (int)r, position_of(own0, r - row0), a.k,
+                                (int64_t)h * a.k_head + r * a.k_row, k, kx[2 * p], kx[2 * p + 1],
+                                a.k_type, ky[p]);
         }
     }
     uint32_t tk = 0, tv = 0;
     float ak = 0.f;
 #pragma unroll
     for (int p = 0; p < PASS; ++p) {
-        if (TURN) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) ak = fmaxf(ak, finite_abs(ky[p][e]));
-        } else {
-            tk = max(tk, magnitude8(kx[p], a.k_type));
-        }
+        if (!TURN) tk = max(tk, magnitude8(kx[p], a.k_type));
         tv = max(tv, magnitude8(vx[p], a.v_type));
     }
-    if (!TURN) ak = bits_value(tk, a.k_type);
+    if (TURN)
+#pragma unroll
+        for (int p = 0; p < UPASS; ++p)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) ak = fmaxf(ak, finite_abs(ky[p][e]));
+    else
+        ak = bits_value(tk, a.k_type);
     float av = bits_value(tv, a.v_type);
     max2(ak, av, red);                              // (its barrier: all have the old scales)
     const float newk = fmaxf(oldk, scale_for<FMT>(ak)), newv = fmaxf(oldv, scale_for<FMT>(av));
@@ -433,7 +469,7 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
         if (!in_d) continue;
         uint2 *to = (uint2 *)(kc + o * D + d);
         if (o >= o0 && o < o1) {
-            *to = TURN ? codes_of<FMT>(ky[p], newk, exk) : codes8<FMT>(kx[p], a.k_type, newk, exk);
+            if (!TURN) *to = codes8<FMT>(kx[p], a.k_type, newk, exk);
             const uint2 c = codes8<FMT>(vx[p], a.v_type, newv, exv);
             uint8_t *at = few ? vc + (value_group(o) * D + d) * 16 + value_place(o)
                               : vl + (value_group(o) * DP + d) * 16 + value_place(o);
@@ -443,6 +479,14 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
             *to = uint2{requant4<FMT>(w.x, oldk / newk), requant4<FMT>(w.y, oldk / newk)};
         }
     }
+    if (TURN)
+#pragma unroll
+        for (int p = 0; p < UPASS; ++p) {
+            const int o = uslot0 + p * UROWS;
+            if (16 * unit >= D || o < o0 || o >= o1) continue;
+            *(uint2 *)(kc + o * D + ud0) = codes_of<FMT>(ky[p], newk, exk);
+            *(uint2 *)(kc + o * D + ud1) = codes_of<FMT>(ky[p] + 8, newk, exk);
+        }
     if (!few) __syncthreads();
     // four dims' 16 bytes at a time: which of a group's places are new
 #pragma unroll
@@ -496,24 +540,18 @@ __device__ inline uint32_t q_bits(const TurnArgs &t, int64_t at)
     return ((const uint16_t *)t.q)[at];
 }
 
-// The queries of one row, 16 dims a thread: eight pairs, or 16 dims past the pairs.  A thread
-// writes what it read, so that they may be turned in place.
-template <bool NEIGHBOURS> __device__ inline void turn_queries(const AppendArgs &a, const TurnArgs &t)
+// Queries, a wave to 64 units of one row: 16 dims (eight pairs, or 16 dims past the pairs) of HEADS
+// heads, whose angles are the same.  A thread writes what it read, so that they may be turned in
+// place.  All that is read goes by the row, the sequences only decide what is written: with
+// `position` no read waits for another but the tables'.
+template <bool NEIGHBOURS, int HEADS>
+__device__ inline void turn_queries(const AppendArgs &a, const TurnArgs &t, uint32_t g)
 {
-    const uint32_t g = blockIdx.x - t.key_groups;
-    const int row = (int)(g / t.row_groups);
-    const int u = (int)(g % t.row_groups) * kThreads + (int)threadIdx.x;
-    int place;
-    const int s = row_seq(a.q, row, &place);
-    if (s < 0 || u >= t.n_heads * t.units) return;
-    const int h = u / t.units, k = u % t.units, D = a.c.D, half = t.half;
-    int64_t own0 = 0;
-    if (!t.position) {
-        int row0;
-        own0 = a.first ? a.first[s] : seq_length(a.q, s) - seq_rows(a.q, s, &row0);
-    }
-    const int own = position_of(own0, place);
-    const int64_t from = row * t.q_row + h * t.q_head, to = row * t.out_row + h * t.out_head;
+    const int64_t item = (int64_t)g * (kThreads / 64) + (threadIdx.x >> 6);
+    const int row = (int)(item / t.row_items);
+    if (row >= a.q.n_rows) return;
+    const int u = (int)(item % t.row_items) * 64 + (int)(threadIdx.x & 63);
+    const int h0 = u / t.units * HEADS, k = u % t.units, D = a.c.D, half = t.half;
     // the unit's 16 dims are n0 from d0 on and n1 from d1 on
     const bool pairs = k < t.pair_units;
     int d0, d1, n0 = 8, n1 = 8;
@@ -530,57 +568,81 @@ template <bool NEIGHBOURS> __device__ inline void turn_queries(const AppendArgs 
         n0 = min(8, D - d0);
         n1 = max(0, min(8, D - d1));
     }
-    float x[16];
-    if (t.q_wide) {
-        const uint4 lo = row_bits8(t.q, from + d0, true), hi = row_bits8(t.q, from + d1, true);
-        const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    uint4 lo[HEADS], hi[HEADS];
+    if (t.q_wide)
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-            x[e] = bits_value((w[e >> 1] >> (16 * (e & 1))) & 0xffff, t.q_type);
-    } else {
+        for (int r = 0; r < HEADS; ++r) {
+            const int64_t from = row * t.q_row + min(h0 + r, t.n_heads - 1) * t.q_head;
+            lo[r] = row_bits8(t.q, from + d0, true);
+            hi[r] = row_bits8(t.q, from + d1, true);
+        }
+    float c[8], s8[8];
+    if (t.position && pairs) angles<8>(t, a.q.n_rows, row, 0, 8 * k, c, s8);
+    int place;
+    const int s = row_seq(a.q, row, &place);
+    if (s < 0) return;
+    if (!t.position && pairs) {
+        int row0;
+        const int64_t own0 = a.first ? a.first[s] : seq_length(a.q, s) - seq_rows(a.q, s, &row0);
+        angles<8>(t, a.q.n_rows, row, position_of(own0, place), 8 * k, c, s8);
+    }
+#pragma unroll
+    for (int r = 0; r < HEADS; ++r) {
+        if (h0 + r >= t.n_heads) return;
+        const int64_t from = row * t.q_row + (h0 + r) * t.q_head;
+        float x[16];
+        if (t.q_wide) {
+            const uint32_t w[8] = {lo[r].x, lo[r].y, lo[r].z, lo[r].w,
+                                   hi[r].x, hi[r].y, hi[r].z, hi[r].w};
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                x[e] = bits_value((w[e >> 1] >> (16 * (e & 1))) & 0xffff, t.q_type);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int i = e & 7, d = e < 8 ? d0 : d1;
+                x[e] = i < (e < 8 ? n0 : n1) ? bits_value(q_bits(t, from + d + i), t.q_type) : 0.f;
+            }
+        }
+        if (pairs)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (8 * k + e < half) {
+                    if (NEIGHBOURS)
+                        turn(x[2 * e], x[2 * e + 1], c[e], s8[e]);
+                    else
+                        turn(x[e], x[e + 8], c[e], s8[e]);
+                }
+        uint16_t *out = (uint16_t *)t.q_out + row * t.out_row + (h0 + r) * t.out_head;
+        if (t.q_wide) {
+            uint32_t w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                w[e] = row_bits(x[2 * e], t.q_type) |
+                       (uint32_t)row_bits(x[2 * e + 1], t.q_type) << 16;
+            *(uint4 *)(out + d0) = uint4{w[0], w[1], w[2], w[3]};
+            *(uint4 *)(out + d1) = uint4{w[4], w[5], w[6], w[7]};
+            continue;
+        }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const int i = e & 7, d = e < 8 ? d0 : d1;
-            x[e] = i < (e < 8 ? n0 : n1) ? bits_value(q_bits(t, from + d + i), t.q_type) : 0.f;
+            if (i < (e < 8 ? n0 : n1)) out[d + i] = row_bits(x[e], t.q_type);
         }
-    }
-    if (pairs) {
-        float c[8], s8[8];
-        angles<8>(t, a.q.n_rows, row, own, 8 * k, c, s8);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (8 * k + e < half) {
-                if (NEIGHBOURS)
-                    turn(x[2 * e], x[2 * e + 1], c[e], s8[e]);
-                else
-                    turn(x[e], x[e + 8], c[e], s8[e]);
-            }
-    }
-    uint16_t *out = (uint16_t *)t.q_out + to;
-    if (t.q_wide) {
-        uint32_t w[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            w[e] = row_bits(x[2 * e], t.q_type) | (uint32_t)row_bits(x[2 * e + 1], t.q_type) << 16;
-        *(uint4 *)(out + d0) = uint4{w[0], w[1], w[2], w[3]};
-        *(uint4 *)(out + d1) = uint4{w[4], w[5], w[6], w[7]};
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        const int i = e & 7, d = e < 8 ? d0 : d1;
-        if (i < (e < 8 ? n0 : n1)) out[d + i] = row_bits(x[e], t.q_type);
     }
 }
 
+constexpr int kTurnHeads = 4;             // heads a thread takes of many rows
+constexpr int64_t kTurnMany = 4096;       // waves of single heads
+
 // The keys' workgroups as in k_append, then for each row those of its queries.
-template <int FMT, int ND, bool NEIGHBOURS>
+template <int FMT, int ND, bool NEIGHBOURS, int HEADS>
 __global__ __launch_bounds__(kThreads) void k_append_rotated(AppendArgs a, TurnArgs t)
 {
     if (blockIdx.x < t.key_groups)
         append<FMT, ND, NEIGHBOURS ? 2 : 1>(a, t);
     else
-        turn_queries<NEIGHBOURS>(a, t);
+        turn_queries<NEIGHBOURS, HEADS>(a, t, blockIdx.x - t.key_groups);
 }
 
 // -- eviction ---------------------------------------------------------------
@@ -1067,6 +1129,20 @@ int64_t append_groups(const AppendArgs &a, const qlm_kv_batch *batch)
     return (int64_t)batch->n_seqs * a.touched * a.c.H;
 }
 
+template <int FMT, bool NEIGHBOURS>
+void launch_rotated(const AppendArgs &a, const TurnArgs &t, bool many, int64_t grid,
+                    hipStream_t stream)
+{
+    constexpr int H = kTurnHeads;
+    auto kern = a.c.D <= 64    ? many ? k_append_rotated<FMT, 1, NEIGHBOURS, H>
+                                      : k_append_rotated<FMT, 1, NEIGHBOURS, 1>
+                : a.c.D <= 128 ? many ? k_append_rotated<FMT, 2, NEIGHBOURS, H>
+                                      : k_append_rotated<FMT, 2, NEIGHBOURS, 1>
+                : many         ? k_append_rotated<FMT, 4, NEIGHBOURS, H>
+                               : k_append_rotated<FMT, 4, NEIGHBOURS, 1>;
+    kern<<<(unsigned)grid, kThreads, 0, stream>>>(a, t);
+}
+
 int check_rotary(const qlm_rotary *r, int head_dim)
 {
     if (!r) return fail(QLM_ERR_ARG, "rotary is NULL");
@@ -1139,14 +1215,13 @@ int qlm_kv_append_rotated(const qlm_kv_cache *cache, const qlm_kv_batch *batch, 
     t.half = rotary->rotary_dim / 2;
     t.n_positions = rotary->n_positions;
     t.n_axes = rotary->n_axes;
-    t.table_wide = t.half % 4 == 0 && (uintptr_t)t.cos % 16 == 0 && (uintptr_t)t.sin % 16 == 0;
+    t.table_wide = t.half % 4 == 0 && (uintptr_t)t.cos % 16 == 0 && (uintptr_t)t.sin % 16 == 0 &&
+                   (uintptr_t)t.axis % 16 == 0;
     const bool neighbours = rotary->interleaved != 0;
     const int64_t keys = batch->max_length > 0 ? append_groups(a, batch) : 0;
-    int64_t grid = keys;
     t.n_heads = n_heads;
     t.pair_units = (t.half + 7) / 8;
     t.units = neighbours ? a.c.D / 16 : t.pair_units + (a.c.D - 2 * t.half + 15) / 16;
-    t.row_groups = (uint32_t)(((int64_t)n_heads * t.units + kThreads - 1) / kThreads);
     if (n_heads > 0) {
         t.q = q->data;
         t.q_out = q_out->data;
@@ -1156,22 +1231,27 @@ int qlm_kv_append_rotated(const qlm_kv_cache *cache, const qlm_kv_batch *batch, 
         t.out_head = q_out->head_stride;
         t.q_type = q->dtype;
         t.q_wide = rows_wide(q) && rows_wide(q_out) && (neighbours || t.half % 8 == 0);
-        grid += (int64_t)batch->n_rows * t.row_groups;
     }
+    auto items = [&](int heads) {
+        return (uint32_t)(((int64_t)(n_heads + heads - 1) / heads * t.units + 63) / 64);
+    };
+    t.row_items = items(1);
+    const bool many = (int64_t)batch->n_rows * t.row_items > kTurnMany;
+    if (many) t.row_items = items(kTurnHeads);
+    const int64_t queries = ((int64_t)batch->n_rows * t.row_items + kThreads / 64 - 1) / (kThreads / 64);
+    const int64_t grid = keys + queries;
     if (!can_launch(grid, kThreads)) return fail(QLM_ERR_CAPACITY, "too many rows in one append");
     if (grid == 0) return QLM_OK;
     t.key_groups = (uint32_t)keys;
-    auto pick = [&](auto e4m3, auto int8) { return cache->format == QLM_KV_E4M3 ? e4m3 : int8; };
     constexpr int E = QLM_KV_E4M3, I = QLM_KV_INT8;
-    auto kern = neighbours
-        ? a.c.D <= 64    ? pick(k_append_rotated<E, 1, true>, k_append_rotated<I, 1, true>)
-          : a.c.D <= 128 ? pick(k_append_rotated<E, 2, true>, k_append_rotated<I, 2, true>)
-                         : pick(k_append_rotated<E, 4, true>, k_append_rotated<I, 4, true>)
-        : a.c.D <= 64    ? pick(k_append_rotated<E, 1, false>, k_append_rotated<I, 1, false>)
-          : a.c.D <= 128 ? pick(k_append_rotated<E, 2, false>, k_append_rotated<I, 2, false>)
-                         : pick(k_append_rotated<E, 4, false>, k_append_rotated<I, 4, false>);
-    kern<<<(unsigned)grid, kThreads, 0, stream>>>(a, t);
-    hipError_t e = hipGetLastError();
+    const bool e4m3 = cache->format == E;
+    if (neighbours)
+        e4m3 ? launch_rotated<E, true>(a, t, many, grid, stream)
+             : launch_rotated<I, true>(a, t, many, grid, stream);
+    else
+        e4m3 ? launch_rotated<E, false>(a, t, many, grid, stream)
+             : launch_rotated<I, false>(a, t, many, grid, stream);
+    const hipError_t e = hipGetLastError();
     return e == hipSuccess ? QLM_OK : hip_fail(e, "k_append_rotated launch");
 }
 

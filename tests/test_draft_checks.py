@@ -73,8 +73,8 @@ def test_rotated_append_checks(qlm, lib):
         assert call(**bad) == qlm.QLM_ERR_ARG, bad
     # nothing to write: no device work
     assert call(b=batch(qlm, n_seqs=0, n_rows=0), k=None, v=None, q=None, out=None) == qlm.QLM_OK
-    # a workgroup of 256 to each row of queries
-    huge = batch(qlm, n_seqs=1, n_rows=1 << 24, max_new=1, row_start=A)
+    # a workgroup of 256 to each four rows of queries
+    huge = batch(qlm, n_seqs=1, n_rows=1 << 26, max_new=1, row_start=A)
     assert call(b=huge) == qlm.QLM_ERR_CAPACITY
 
 
