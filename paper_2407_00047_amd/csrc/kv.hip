@@ -170,12 +170,12 @@ struct TurnArgs {
     uint32_t key_groups, row_items;    // workgroups of the keys; waves of a row's queries
 };
 
-// The place in the tables of pair i of a row (`own`: its position without `position`).
+// The place in the tables of pair i of a row (`own`: its position where there is one axis).
 __device__ inline int64_t table_at(const TurnArgs &t, int n_rows, int row, int own, int i)
 {
     int p = own;
-    if (t.position) {
-        const int ax = t.axis ? max(0, min(t.axis[i], t.n_axes - 1)) : 0;
+    if (t.axis && t.position) {
+        const int ax = max(0, min(t.axis[i], t.n_axes - 1));
         p = t.position[(int64_t)ax * n_rows + row];
     }
     return (int64_t)max(0, min(p, t.n_positions - 1)) * t.half + i;
@@ -347,23 +347,27 @@ __device__ inline bool power_of_two(float x)
 // lanes at a time: one read of up to 64 sequences, two of up to 4096.
 __device__ inline int row_seq(const Seqs &q, int row, int *place)
 {
-    int s = row, row0;
-    if (q.row_start) {
-        s = 0;
-        int left = q.n_seqs;
-        for (int step = 1 << 30; step > 1;) {
-            step = (left + 63) / 64;
-            const int64_t at = (int64_t)(threadIdx.x & 63) * step;
-            const uint64_t m = __ballot(at < left && q.row_start[s + min(at, (int64_t)left - 1)] <= row);
-            if (m == 0) return -1;
-            const int last = (63 - __builtin_clzll(m)) * step;
-            s += last;
-            left = min(step, left - last);
-        }
+    if (!q.row_start) {
+        *place = 0;
+        return row < q.n_seqs ? row : -1;
     }
-    const int n = seq_rows(q, s, &row0);
-    *place = row - row0;
-    return *place >= 0 && *place < n ? s : -1;
+    int s = 0, left = q.n_seqs, first = 0, next = 0;
+    for (int step = 1 << 30; step > 1;) {
+        step = (left + 63) / 64;
+        const int64_t at = (int64_t)(threadIdx.x & 63) * step;
+        const int32_t *p = q.row_start + s + min(at, (int64_t)left - 1);
+        const int mine = p[0], after = p[1];
+        const uint64_t m = __ballot(at < left && mine <= row);
+        if (m == 0) return -1;
+        const int lane = 63 - __builtin_clzll(m);
+        first = __builtin_amdgcn_readlane(mine, lane);
+        next = __builtin_amdgcn_readlane(after, lane);
+        s += lane * step;
+        left = min(step, left - lane * step);
+    }
+    const int r0 = max(0, min(first, q.n_rows)), r1 = max(r0, min(next, q.n_rows));
+    *place = row - r0;
+    return *place >= 0 && *place < min(r1 - r0, q.max_new) ? s : -1;
 }
 
 // One workgroup for each (sequence, block that takes new slots, kv head).  A
@@ -391,14 +395,11 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
     const int lo = max(max(start, 0), j * kBlock), hi = min(len, (j + 1) * kBlock);
     if (n == 0 || lo >= hi) return;
     const int id = a.q.table[s * a.q.table_stride + j];
-    if ((unsigned)id >= (unsigned)a.c.n_blocks) return;
 
     const int D = a.c.D;
     const int o0 = lo - j * kBlock, o1 = hi - j * kBlock;   // slots [o0, o1) are new
     const int64_t r0 = (int64_t)row0 + (lo - start);        // row of slot o0
-    const int64_t bh = (int64_t)id * a.c.H + h;
     const bool fresh = o0 == 0;
-    const float oldk = fresh ? 0.f : a.c.ks[bh], oldv = fresh ? 0.f : a.c.vs[bh];
     const int d = 8 * (t % CH), slot0 = t / CH;
     const bool in_d = d < D;
     uint4 kx[PASS], vx[PASS];
@@ -416,26 +417,33 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
         if (!TURN) kx[p] = row_bits8(a.k, (int64_t)h * a.k_head + r * a.k_row + dd, a.k_wide);
         vx[p] = row_bits8(a.v, (int64_t)h * a.v_head + r * a.v_row + dd, a.v_wide);
     }
-    int ud0 = 0, ud1 = 0;
+    int ud0 = 0, ud1 = 0, own[TURN ? UPASS : 1];
+    const int unit_in = min(unit, D / 16 - 1);
     if (TURN) {
         const int64_t own0 = a.first ? a.first[s] : start;
-        const int k = min(unit, D / 16 - 1);
-        unit_dims(turned, TURN == 2, k, &ud0, &ud1);
+        unit_dims(turned, TURN == 2, unit_in, &ud0, &ud1);
 #pragma unroll
         for (int p = 0; p < UPASS; ++p) {
             const int64_t r = r0 + min(max(uslot0 + p * UROWS, o0), o1 - 1) - o0;
             const int64_t at = (int64_t)h * a.k_head + r * a.k_row;
+            own[p] = turned.position ? turned.position[r] : position_of(own0, r - row0);
             kx[2 * p] = row_bits8(a.k, at + ud0, a.k_wide);
             kx[2 * p + 1] = row_bits8(a.k, at + ud1, a.k_wide);
         }
+    }
+    // (all that goes by the rows is under way before the block's number is waited for)
+    __builtin_amdgcn_sched_barrier(0);
+    if ((unsigned)id >= (unsigned)a.c.n_blocks) return;
+    const int64_t bh = (int64_t)id * a.c.H + h;
+    const float oldk = fresh ? 0.f : a.c.ks[bh], oldv = fresh ? 0.f : a.c.vs[bh];
+    if (TURN)
 #pragma unroll
         for (int p = 0; p < UPASS; ++p) {
             const int64_t r = r0 + min(max(uslot0 + p * UROWS, o0), o1 - 1) - o0;
-            turned16<TURN == 2>(turned, a.q.n_rows, (int)r, position_of(own0, r - row0), a.k,
-                                (int64_t)h * a.k_head + r * a.k_row, k, kx[2 * p], kx[2 * p + 1],
-                                a.k_type, ky[p]);
+            turned16<TURN == 2>(turned, a.q.n_rows, (int)r, own[p], a.k,
+                                (int64_t)h * a.k_head + r * a.k_row, unit_in, kx[2 * p],
+                                kx[2 * p + 1], a.k_type, ky[p]);
         }
-    }
     uint32_t tk = 0, tv = 0;
     float ak = 0.f;
 #pragma unroll
@@ -542,8 +550,7 @@ __device__ inline uint32_t q_bits(const TurnArgs &t, int64_t at)
 
 // Queries, a wave to 64 units of one row: 16 dims (eight pairs, or 16 dims past the pairs) of HEADS
 // heads, whose angles are the same.  A thread writes what it read, so that they may be turned in
-// place.  All that is read goes by the row, the sequences only decide what is written: with
-// `position` no read waits for another but the tables'.
+// place.  Rows and positions are read by the row's number beside the search for its sequence.
 template <bool NEIGHBOURS, int HEADS>
 __device__ inline void turn_queries(const AppendArgs &a, const TurnArgs &t, uint32_t g)
 {
@@ -576,16 +583,15 @@ __device__ inline void turn_queries(const AppendArgs &a, const TurnArgs &t, uint
             lo[r] = row_bits8(t.q, from + d0, true);
             hi[r] = row_bits8(t.q, from + d1, true);
         }
-    float c[8], s8[8];
-    if (t.position && pairs) angles<8>(t, a.q.n_rows, row, 0, 8 * k, c, s8);
-    int place;
+    int own = t.position ? t.position[row] : 0, place;
     const int s = row_seq(a.q, row, &place);
     if (s < 0) return;
-    if (!t.position && pairs) {
+    if (!t.position) {
         int row0;
-        const int64_t own0 = a.first ? a.first[s] : seq_length(a.q, s) - seq_rows(a.q, s, &row0);
-        angles<8>(t, a.q.n_rows, row, position_of(own0, place), 8 * k, c, s8);
+        own = position_of(a.first ? a.first[s] : seq_length(a.q, s) - seq_rows(a.q, s, &row0), place);
     }
+    float c[8], s8[8];
+    if (pairs) angles<8>(t, a.q.n_rows, row, own, 8 * k, c, s8);
 #pragma unroll
     for (int r = 0; r < HEADS; ++r) {
         if (h0 + r >= t.n_heads) return;
@@ -637,7 +643,7 @@ constexpr int64_t kTurnMany = 4096;       // waves of single heads
 
 // The keys' workgroups as in k_append, then for each row those of its queries.
 template <int FMT, int ND, bool NEIGHBOURS, int HEADS>
-__global__ __launch_bounds__(kThreads) void k_append_rotated(AppendArgs a, TurnArgs t)
+__global__ __launch_bounds__(kThreads, ND <= 2 ? 4 : 2) void k_append_rotated(AppendArgs a, TurnArgs t)
 {
     if (blockIdx.x < t.key_groups)
         append<FMT, ND, NEIGHBOURS ? 2 : 1>(a, t);
