@@ -195,7 +195,7 @@ def library():
             lib.qlm_w4_workspace_bytes.restype = ctypes.c_size_t
             lib.qlm_w4_matmul.argtypes = [W, vp, i64, vp, i64, i32, i32, vp, sz, vp]
             lib.qlm_kv_append_rotated.argtypes = [C, B, vp, vp, vp, vp, i32, vp, vp, vp]
-            F, R = ctypes.POINTER(F8Struct), ctypes.POINTER(F8CodesStruct)
+            F, R = ctypes.POINTER(F8Struct), vp                  # (coded rows packed as bytes)
             lib.qlm_f8_packed_bytes.argtypes = [i32, i32]
             lib.qlm_f8_packed_bytes.restype = ctypes.c_size_t
             lib.qlm_f8_pack.argtypes = [F, vp, vp, vp]
@@ -732,7 +732,9 @@ _ROWS = struct.Struct("@Pqqi0P")
 _KV_QUERY = struct.Struct("@Pqqi0PPqqi0Pifif0P")
 _ROTARY = struct.Struct("@iiiiPPPP")
 _DRAFT = struct.Struct("@iiPPqqPP")
+_F8_CODES = struct.Struct("@iiPP")
 _row_types = {}
+_word_types = {}
 
 
 def _row_type(t, what):
@@ -941,38 +943,41 @@ def kv_append_rotated(cache: DeviceKvCache, batch: KvBatch, k, v, q, rotary: Rot
                                        first_position.numel() != batch.n_seqs or
                                        not first_position.is_contiguous()):
         raise ValueError("first_position must be [n_seqs] int32")
-    axes = 1
+    n, kv, dim = batch.n_rows, cache.n_kv_heads, cache.head_dim
+    axes, at = 1, 0
     if position is not None:
+        shape = position.shape
         if position.dtype != batch.lengths.dtype or not position.is_contiguous() or \
-                position.dim() not in (1, 2) or position.shape[-1] != batch.n_rows:
-            raise ValueError("position must be contiguous [axes, %d rows] int32" % batch.n_rows)
-        axes = position.shape[0] if position.dim() == 2 else 1
-    rk = _rows(k, batch.n_rows, cache.n_kv_heads, cache.head_dim, "k")
-    rv = _rows(v, batch.n_rows, cache.n_kv_heads, cache.head_dim, "v")
-    heads, rq, ro = 0, None, None
+                len(shape) not in (1, 2) or shape[-1] != n:
+            raise ValueError("position must be contiguous [axes, %d rows] int32" % n)
+        axes, at = shape[0] if len(shape) == 2 else 1, position.data_ptr()
+    rk, rv = _rows(k, n, kv, dim, "k"), _rows(v, n, kv, dim, "v")
+    index, heads, rq, ro = cache.index, 0, None, None
+    here = 0 <= index == batch.index == rotary.index == k.get_device() == v.get_device() and \
+        (position is None or position.get_device() == index) and \
+        (first_position is None or first_position.get_device() == index)
     if q is not None:
         if q.dim() != 3:
             raise ValueError("q must be [rows, n_heads, head_dim]")
         heads = q.shape[1]
-        rq = _rows(q, batch.n_rows, heads, cache.head_dim, "q")
+        rq = _rows(q, n, heads, dim, "q")
         if out is None:
             import torch
             out = _allocated(stream, lambda: torch.empty(q.shape, dtype=q.dtype, device=q.device))
         elif out.shape != q.shape or out.dtype != q.dtype:
             raise ValueError("out must have q's shape and type")
-        ro = _rows(out, batch.n_rows, heads, cache.head_dim, "out")
+        ro = _rows(out, n, heads, dim, "out")
+        here = here and q.get_device() == index == out.get_device()
     elif out is not None:
         raise ValueError("out is of queries, and there are none")
-    tensors = dict(k=k, v=v, q=q, out=out, rotary=rotary.cos, position=position,
-                   first_position=first_position)
-    if not 0 <= cache.index == batch.index or \
-            any(x is not None and x.get_device() != cache.index for x in tensors.values()):
-        _refuse_place(cache.index, cache=cache.k_codes, batch=batch.lengths, **tensors)
+    if not here:
+        _refuse_place(index, cache=cache.k_codes, batch=batch.lengths, k=k, v=v, q=q, out=out,
+                      rotary=rotary.cos, position=position, first_position=first_position)
     rc = (_lib or library()).qlm_kv_append_rotated(
         cache._ref, batch._ref, _ROWS.pack(*rk), _ROWS.pack(*rv),
         _ROWS.pack(*rq) if heads else None, _ROWS.pack(*ro) if heads else None, heads,
         _ROTARY.pack(2 * rotary.pairs, rotary.interleaved, rotary.n_positions, axes,
-                     *rotary._tables, _ptr(position) or 0),
+                     *rotary._tables, at),
         None if first_position is None else first_position.data_ptr(), _raw_stream(stream))
     if rc:
         _check(rc)
@@ -1168,10 +1173,26 @@ class F8Rows:
                              % (blocks, tiles * F8_TILE))
         if scale.device != codes.device:
             raise ValueError("scale must be where codes is")
-        self.codes, self.scale, self.n_rows, self.n_in = codes, scale, int(n_rows), int(n_in)
+        self._hold(codes, scale, int(n_rows), int(n_in))
+
+    def _hold(self, codes, scale, n_rows, n_in):
+        self.codes, self.scale, self.n_rows, self.n_in = codes, scale, n_rows, n_in
         self.index = codes.get_device()
-        self.struct = F8CodesStruct(self.n_rows, self.n_in, _ptr(codes), _ptr(scale))
-        self._ref = ctypes.byref(self.struct)
+        self._struct = _F8_CODES.pack(n_rows, n_in, codes.data_ptr(), scale.data_ptr())
+
+    @classmethod
+    def _empty(cls, n_rows, n_in, device, stream):
+        """Room for so many rows, as a call on `stream` allocates it."""
+        import torch
+        tiles, blocks = -(-n_rows // F8_TILE), -(-n_in // F8_BLOCK)
+        rows = cls.__new__(cls)
+        rows._hold(_allocated(stream, lambda: torch.empty((tiles, blocks, 8, F8_TILE, 16),
+                                                          dtype=torch.float8_e4m3fn,
+                                                          device=device)),
+                   _allocated(stream, lambda: torch.empty((blocks, tiles * F8_TILE),
+                                                          dtype=torch.float32, device=device)),
+                   n_rows, n_in)
+        return rows
 
 
 def f8_pack(codes, scale, stream=None):
@@ -1201,19 +1222,14 @@ def f8_rows(x, out=None, stream=None):
     kind = _row_type(x, "x")
     n, k = x.shape
     if out is None:
-        tiles, blocks = -(-n // F8_TILE), -(-k // F8_BLOCK)
-        out = F8Rows(
-            _allocated(stream, lambda: torch.empty((tiles, blocks, 8, F8_TILE, 16),
-                                                   dtype=torch.float8_e4m3fn, device=x.device)),
-            _allocated(stream, lambda: torch.empty((blocks, tiles * F8_TILE), dtype=torch.float32,
-                                                   device=x.device)), n, k)
+        out = F8Rows._empty(n, k, x.device, stream)
     elif out.n_rows != n or out.n_in != k:
         raise ValueError("out must be of %d rows of %d inputs" % (n, k))
     if not 0 <= out.index == x.get_device():
         _refuse_place(x.get_device(), x=x, out=out.codes)
     # (the stride of a matrix of one row says nothing)
-    rc = (_lib or library()).qlm_f8_rows(out._ref, x.data_ptr(), x.stride(0) if n > 1 else k, kind,
-                                         _raw_stream(stream))
+    rc = (_lib or library()).qlm_f8_rows(out._struct, x.data_ptr(), x.stride(0) if n > 1 else k,
+                                         kind, _raw_stream(stream))
     if rc:
         _check(rc)
     return out
@@ -1231,8 +1247,10 @@ def f8_workspace(weight: F8, n_rows: int):
 
 def _word_type(dtype, what):
     """The number of a row type, of which float32 is one too."""
-    import torch
-    kind = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}.get(dtype)
+    if not _word_types:
+        import torch
+        _word_types.update({torch.float16: 0, torch.bfloat16: 1, torch.float32: 2})
+    kind = _word_types.get(dtype)
     if kind is None:
         raise ValueError("%s must be float16, bfloat16 or float32" % what)
     return kind
@@ -1258,7 +1276,7 @@ def f8_matmul(x: F8Rows, weight: F8, out=None, dtype=None, ws=None, stream=None)
         ws = _allocated(stream, lambda: f8_workspace(weight, n), False)
     if not 0 <= weight.index == x.index == out.get_device() == ws.get_device():
         _refuse_place(weight.index, weight=weight.packed, x=x.codes, out=out, ws=ws)
-    rc = (_lib or library()).qlm_f8_matmul(x._ref, weight._ref, out.data_ptr(),
+    rc = (_lib or library()).qlm_f8_matmul(x._struct, weight._ref, out.data_ptr(),
                                            out.stride(0) if n > 1 else weight.n_out, kind,
                                            ws.data_ptr(), ws.numel(), _raw_stream(stream))
     if rc:
@@ -1286,41 +1304,43 @@ def draft_verify(batch: KvBatch, tokens, target, draft, uniform, lengths=None, w
     drafts, the token drawn, -1; their number [n_seqs] int32; the lengths that stay
     in the cache [n_seqs] int32: ``lengths``, which may be the batch's own)."""
     import torch
-    if target.dim() != 2 or target.shape[0] != batch.n_rows or target.shape[1] < 1 or \
-            (target.stride(1) != 1 and target.shape[1] > 1):
-        raise ValueError("target must be [%d rows, vocab] with contiguous rows" % batch.n_rows)
-    vocab = target.shape[1]
+    n, seqs, index = batch.n_rows, batch.n_seqs, batch.index
+    shape, stride = target.shape, target.stride()
+    if len(shape) != 2 or shape[0] != n or shape[1] < 1 or (stride[1] != 1 and shape[1] > 1):
+        raise ValueError("target must be [%d rows, vocab] with contiguous rows" % n)
+    vocab = shape[1]
     kind = _word_type(target.dtype, "target")
-    if draft is not None and (draft.shape != target.shape or draft.dtype != target.dtype or
-                              (draft.stride(1) != 1 and vocab > 1)):
-        raise ValueError("draft must have target's shape and type, with contiguous rows")
-    for name, x, dtype in (("tokens", tokens, torch.int32), ("uniform", uniform, torch.float32)):
-        if x.dtype != dtype or x.numel() != batch.n_rows or not x.is_contiguous():
-            raise ValueError("%s must be [%d rows] %s" % (name, batch.n_rows, dtype))
-    if lengths is None:
-        lengths = _allocated(stream, lambda: torch.empty_like(batch.lengths))
-    elif lengths.dtype != torch.int32 or lengths.numel() != batch.n_seqs or \
-            not lengths.is_contiguous():
-        raise ValueError("lengths must be [n_seqs] int32")
+    near, apart = 0, vocab
+    if draft is not None:
+        if draft.shape != shape or draft.dtype != target.dtype or \
+                (draft.stride(1) != 1 and vocab > 1):
+            raise ValueError("draft must have target's shape and type, with contiguous rows")
+        near, apart = draft.data_ptr(), draft.stride(0)
+    if tokens.dtype != torch.int32 or tokens.numel() != n or not tokens.is_contiguous():
+        raise ValueError("tokens must be [%d rows] int32" % n)
+    if uniform.dtype != torch.float32 or uniform.numel() != n or not uniform.is_contiguous():
+        raise ValueError("uniform must be [%d rows] float32" % n)
     device = batch.lengths.device
-    out = _allocated(stream, lambda: torch.empty((batch.n_seqs, batch.max_new), dtype=torch.int32,
+    if lengths is None:
+        lengths = _allocated(stream, lambda: torch.empty((seqs,), dtype=torch.int32, device=device))
+    elif lengths.dtype != torch.int32 or lengths.numel() != seqs or not lengths.is_contiguous():
+        raise ValueError("lengths must be [n_seqs] int32")
+    out = _allocated(stream, lambda: torch.empty((seqs, batch.max_new), dtype=torch.int32,
                                                  device=device))
-    count = _allocated(stream, lambda: torch.empty_like(batch.lengths))
+    count = _allocated(stream, lambda: torch.empty((seqs,), dtype=torch.int32, device=device))
     if ws is None:
         ws = _allocated(stream, lambda: draft_verify_workspace(batch, vocab), False)
-    tensors = dict(tokens=tokens, target=target, draft=draft, uniform=uniform, lengths=lengths,
-                   ws=ws)
-    if batch.index < 0 or any(x is not None and x.get_device() != batch.index
-                              for x in tensors.values()):
-        _refuse_place(batch.index, batch=batch.lengths, **tensors)
+    if not 0 <= index == tokens.get_device() == target.get_device() == uniform.get_device() == \
+            lengths.get_device() == ws.get_device() or \
+            (draft is not None and draft.get_device() != index):
+        _refuse_place(index, batch=batch.lengths, tokens=tokens, target=target, draft=draft,
+                      uniform=uniform, lengths=lengths, ws=ws)
     # (the stride of a matrix of one row says nothing)
-    one = batch.n_rows <= 1
+    one = n <= 1
     rc = (_lib or library()).qlm_draft_verify(
         batch._ref,
-        _DRAFT.pack(vocab, kind, target.data_ptr(), _ptr(draft) or 0,
-                    vocab if one else target.stride(0),
-                    vocab if one or draft is None else draft.stride(0), tokens.data_ptr(),
-                    uniform.data_ptr()),
+        _DRAFT.pack(vocab, kind, target.data_ptr(), near, vocab if one else stride[0],
+                    vocab if one else apart, tokens.data_ptr(), uniform.data_ptr()),
         out.data_ptr(), count.data_ptr(), lengths.data_ptr(), ws.data_ptr(), ws.numel(),
         _raw_stream(stream))
     if rc:
