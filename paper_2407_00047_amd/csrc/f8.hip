@@ -388,12 +388,10 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
     };
     const int lane_at = 16 * lane + 1024 * (wv & 1);
     // half h of the loads: the weights of block h / 2, then its rows, in slot h % SLOTS
-    auto fetch = [&](bool n, int b, uint8_t *to) {
+    auto fetch = [&](bool n, int i, int b, uint8_t *to) {       // piece i of a half
         const int at = wv / 2 * tile_bytes + min(b, count - 1) * kTileBytes;
-#pragma unroll
-        for (int i = 0; i < (n ? PN : PM); ++i)
-            load_lds(n ? w_from : x_from, at + i * (W / 2) * tile_bytes, lane_at,
-                     to + 1024 * (i * W + wv));
+        load_lds(n ? w_from : x_from, at + i * (W / 2) * tile_bytes, lane_at,
+                 to + 1024 * (i * W + wv));
     };
     float4v acc[NT][MT];
     float by[MT], w_next, x_next[MT];
@@ -405,7 +403,9 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
         for (int j = 0; j < MT; ++j)
             x_next[j] = (p + min(wm * MT + j, a.m_tiles - 1 - mt0) * kTile)[lane & 15];
     };
-    auto step = [&](const uint8_t *wt, const uint8_t *xt) {
+    // A block's products; `more` starts the loads of later ones, a few at a time: all at once they
+    // would hold the waves up until the last is on its way.
+    auto step = [&](const uint8_t *wt, const uint8_t *xt, auto more) {
         int8v x[MT];
 #pragma unroll
         for (int j = 0; j < MT; ++j) x[j] = operand(xt + kTileBytes * (wm * MT + j), lane);
@@ -415,6 +415,7 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
         for (int i = 0; i <= NT; ++i) {
             const int8v w = ahead;
             if (i + 1 < NT) ahead = operand(wt + kTileBytes * (wn * NT + i + 1), lane);
+            if (i < NT) more(i);
 #pragma unroll
             for (int j = 0; j < MT; ++j) {
                 if (i < NT) now[j] = product(w, x[j]);
@@ -438,7 +439,9 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
         fetch_scales(0);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int h = 0; h < AHEAD; ++h) fetch(h % 2 == 0, h / 2, slot[h]);
+        for (int h = 0; h < AHEAD; ++h)
+#pragma unroll
+            for (int i = 0; i < (h % 2 ? PM : PN); ++i) fetch(h % 2 == 0, i, h / 2, slot[h]);
     };
     auto block = [&](int b, int i) {       // i: b's place in a turn of SLOTS blocks
         // the loads that may be under way still: those of halves past this block's two
@@ -452,11 +455,16 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
         __builtin_amdgcn_sched_barrier(0);
         fetch_scales(b + 1);
         __builtin_amdgcn_sched_barrier(0);     // (before the loads: waited for with fewer left)
+        step(slot[2 * i % SLOTS], slot[(2 * i + 1) % SLOTS], [&](int k) {
+            // the rows of the next block, then the weights of the one after it
+            static_assert(AHEAD == 3, "the halves that follow");
 #pragma unroll
-        for (int h = AHEAD; h < AHEAD + 2; ++h)
-            fetch(h % 2 == 0, b + h / 2, slot[(2 * i + h) % SLOTS]);
-        __builtin_amdgcn_sched_barrier(0);
-        step(slot[2 * i % SLOTS], slot[(2 * i + 1) % SLOTS]);
+            for (int p = k * (PN + PM) / NT; p < (k + 1) * (PN + PM) / NT; ++p)
+                if (p < PM)
+                    fetch(false, p, b + 1, slot[(2 * i + 3) % SLOTS]);
+                else
+                    fetch(true, p - PM, b + 2, slot[(2 * i + 4) % SLOTS]);
+        });
     };
     if (!next_tile()) return;
     begin();
