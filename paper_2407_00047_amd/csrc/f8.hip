@@ -174,6 +174,7 @@ struct MatArgs {
     int32_t n_tiles, m_tiles;
     uint32_t grid_n, grid_m;      // workgroups' tiles of outputs and of rows
     int32_t out_wide;             // rows of out may be written 16 bytes at a time
+    int32_t out_past;             // ... past the caches
     // the blocks of inputs in `splits` runs of `per_split`, whose sums stand out_split apart
     int32_t splits, per_split;
     int64_t out_split;
@@ -325,7 +326,13 @@ __device__ inline void store_rows(const MatArgs &a, int split, int64_t m0, int n
         for (int k = 0; k < kTile; k += PER) {
             const int row = k + lane / CHUNKS;
             const uint4 w = *(const uint4 *)(lds + row * ROW + (c ^ (row & MASK)) * 16);
-            if (row < rows) *(uint4 *)((uint8_t *)(out + row * a.out_stride) + 16 * c) = w;
+            int4v *to = (int4v *)((uint8_t *)(out + row * a.out_stride) + 16 * c);
+            const int4v v4 = {(int)w.x, (int)w.y, (int)w.z, (int)w.w};
+            if (row >= rows) continue;
+            if (a.out_past)
+                __builtin_nontemporal_store(v4, to);
+            else
+                *to = v4;
         }
         return;
     }
@@ -668,6 +675,9 @@ int qlm_f8_matmul(const qlm_f8_codes *rows, const qlm_f8 *weight, void *out, int
     a.dtype = dtype;
     const int size = dtype == QLM_F32 ? 4 : 2;
     a.out_wide = (uintptr_t)out % 16 == 0 && out_stride * size % 16 == 0;
+    // outputs that the second-level caches (32 MiB) do not hold would only push the operands out of
+    // them: 8192 x 16384 x 4096 476 us through the caches, 464 past them
+    a.out_past = (int64_t)a.M * a.N * size > (64 << 20);
     const Plan p = qlm_f8_host::plan_of(weight->n_out, weight->n_in, rows->n_rows);
     if (p.side) {
         a.splits = p.splits;
@@ -679,6 +689,7 @@ int qlm_f8_matmul(const qlm_f8_codes *rows, const qlm_f8 *weight, void *out, int
             o.out_stride = ld;
             o.out_split = run;
             o.out_wide = 1;
+            o.out_past = 0;
             o.dtype = QLM_F32;
         }
         const int64_t tiles = (int64_t)((a.N + p.side - 1) / p.side) *
