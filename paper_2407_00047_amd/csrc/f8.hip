@@ -36,6 +36,7 @@ typedef int int8v __attribute__((ext_vector_type(8)));
 using qlm_f8_host::kBlock;
 using qlm_f8_host::kCus;
 using qlm_f8_host::kTile;
+using qlm_f8_host::parts_of;
 using qlm_f8_host::Plan;
 static_assert(kBlock == QLM_F8_BLOCK && kTile == QLM_F8_TILE, "the header's sizes");
 constexpr int kTileBytes = kBlock * kTile;
@@ -565,6 +566,60 @@ template <int NT, int MT, int WN, int WM, int GROUPS> void launch_wide(MatArgs a
     k_f8_wide<NT, MT, WN, WM, 5><<<(unsigned)grid, 64 * WN * WM, 0, stream>>>(a);
 }
 
+// Tiles of rows that a workgroup of k_f8_thin takes.
+int thin_rows(const MatArgs &a) { return a.m_tiles == 1 ? 1 : a.m_tiles == 2 ? 2 : 4; }
+
+int64_t thin_groups(const MatArgs &a)
+{
+    return (int64_t)a.n_tiles * ((a.m_tiles + thin_rows(a) - 1) / thin_rows(a));
+}
+
+// Whether a form's launches can be made.
+bool fits(const MatArgs &a, const Plan &p)
+{
+    if (!p.side) return can_launch(thin_groups(a), 512);
+    const int64_t tiles = (int64_t)((a.N + p.side - 1) / p.side) *
+                          ((a.M + (int64_t)p.side - 1) / p.side) * p.splits;
+    return tiles <= INT32_MAX / 2 && can_launch((a.M * (part_stride(a.N) / 4) + 255) / 256, 256);
+}
+
+hipError_t launch(MatArgs a, const Plan &p, void *ws, hipStream_t stream)
+{
+    if (!p.side) {
+        const unsigned grid = (unsigned)thin_groups(a);
+        if (thin_rows(a) == 1)
+            k_f8_thin<1, 8, 4><<<grid, 512, 0, stream>>>(a);
+        else if (thin_rows(a) == 2)
+            k_f8_thin<2, 8, 4><<<grid, 512, 0, stream>>>(a);
+        else
+            k_f8_thin<4, 8, 3><<<grid, 512, 0, stream>>>(a);
+        return hipGetLastError();
+    }
+    a.splits = p.splits;
+    a.per_split = p.per_split;
+    MatArgs o = a;
+    const int64_t ld = part_stride(a.N), run = a.M * ld;
+    if (p.splits > 1) {
+        o.out = ws;
+        o.out_stride = ld;
+        o.out_split = run;
+        o.out_wide = 1;
+        o.out_past = 0;
+        o.dtype = QLM_F32;
+    }
+    if (p.side == 64)
+        launch_wide<2, 2, 2, 2, 3>(o, stream);
+    else if (p.side == 128)
+        launch_wide<4, 2, 2, 4, 2>(o, stream);
+    else
+        launch_wide<8, 4, 2, 4, 1>(o, stream);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits == 1) return e;
+    k_f8_join<<<(unsigned)((a.M * (ld / 4) + 255) / 256), 256, 0, stream>>>(a, (const float *)ws, ld,
+                                                                          run);
+    return hipGetLastError();
+}
+
 int64_t code_bytes(int n_out, int n_in) { return tiles_of(n_out) * blocks_of(n_in) * kTileBytes; }
 
 }  // namespace
@@ -636,7 +691,7 @@ int qlm_f8_rows(const qlm_f8_codes *rows, const void *x, int64_t x_stride, int32
 size_t qlm_f8_workspace_bytes(const qlm_f8 *weight, int32_t n_rows)
 {
     if (check_weight(weight) || n_rows < 1) return 0;
-    const Plan p = qlm_f8_host::plan_of(weight->n_out, weight->n_in, n_rows);
+    const Plan p = parts_of(weight->n_out, weight->n_in, n_rows).first;
     return p.splits > 1 ? (size_t)p.splits * n_rows * part_stride(weight->n_out) * 4 : 0;
 }
 
@@ -678,49 +733,23 @@ int qlm_f8_matmul(const qlm_f8_codes *rows, const qlm_f8 *weight, void *out, int
     // outputs that the second-level caches (32 MiB) do not hold would only push the operands out of
     // them: 8192 x 16384 x 4096 476 us through the caches, 464 past them
     a.out_past = (int64_t)a.M * a.N * size > (64 << 20);
-    const Plan p = qlm_f8_host::plan_of(weight->n_out, weight->n_in, rows->n_rows);
-    if (p.side) {
-        a.splits = p.splits;
-        a.per_split = p.per_split;
-        MatArgs o = a;
-        const int64_t ld = part_stride(a.N), run = a.M * ld;
-        if (p.splits > 1) {
-            o.out = ws;
-            o.out_stride = ld;
-            o.out_split = run;
-            o.out_wide = 1;
-            o.out_past = 0;
-            o.dtype = QLM_F32;
-        }
-        const int64_t tiles = (int64_t)((a.N + p.side - 1) / p.side) *
-                              ((a.M + (int64_t)p.side - 1) / p.side) * p.splits;
-        if (tiles > INT32_MAX / 2) return fail(QLM_ERR_CAPACITY, "too many outputs in one call");
-        if (p.side == 64)
-            launch_wide<2, 2, 2, 2, 3>(o, stream);
-        else if (p.side == 128)
-            launch_wide<4, 2, 2, 4, 2>(o, stream);
-        else
-            launch_wide<8, 4, 2, 4, 1>(o, stream);
-        hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return hip_fail(e, "k_f8_wide launch");
-        if (p.splits > 1) {
-            const int64_t grid = (a.M * (ld / 4) + 255) / 256;
-            k_f8_join<<<(unsigned)grid, 256, 0, stream>>>(a, (const float *)ws, ld, run);
-            if ((e = hipGetLastError()) != hipSuccess) return hip_fail(e, "k_f8_join launch");
-        }
-        return QLM_OK;
+    const auto parts = parts_of(weight->n_out, weight->n_in, rows->n_rows);
+    MatArgs rest = a;
+    if (parts.n_first < rows->n_rows) {        // (whole tiles of rows)
+        a.M = parts.n_first;
+        a.m_tiles = a.M / kTile;
+        rest.M -= a.M;
+        rest.m_tiles -= a.m_tiles;
+        rest.x += (int64_t)a.m_tiles * a.blocks * kTileBytes;
+        rest.xs += a.M;
+        rest.out = (char *)out + a.M * out_stride * size;
+        rest.out_wide = a.out_wide && (uintptr_t)rest.out % 16 == 0;
+        if (!fits(rest, parts.rest)) return fail(QLM_ERR_CAPACITY, "too many outputs in one call");
     }
-    const int mt = a.m_tiles == 1 ? 1 : a.m_tiles == 2 ? 2 : 4;
-    const int64_t grid = (int64_t)a.n_tiles * ((a.m_tiles + mt - 1) / mt);
-    if (!can_launch(grid, 512)) return fail(QLM_ERR_CAPACITY, "too many outputs in one call");
-    if (mt == 1)
-        k_f8_thin<1, 8, 4><<<(unsigned)grid, 512, 0, stream>>>(a);
-    else if (mt == 2)
-        k_f8_thin<2, 8, 4><<<(unsigned)grid, 512, 0, stream>>>(a);
-    else
-        k_f8_thin<4, 8, 3><<<(unsigned)grid, 512, 0, stream>>>(a);
-    hipError_t e = hipGetLastError();
-    return e == hipSuccess ? QLM_OK : hip_fail(e, "k_f8_thin launch");
+    if (!fits(a, parts.first)) return fail(QLM_ERR_CAPACITY, "too many outputs in one call");
+    hipError_t e = launch(a, parts.first, ws, stream);
+    if (e == hipSuccess && parts.n_first < rows->n_rows) e = launch(rest, parts.rest, ws, stream);
+    return e == hipSuccess ? QLM_OK : hip_fail(e, "f8 launch");
 }
 
 }  // extern "C"

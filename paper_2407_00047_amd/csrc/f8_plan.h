@@ -12,6 +12,7 @@ constexpr int kBlock = 128, kTile = 16, kCus = 256;
 // rows of a workgroup's tile (k_f8_wide).  The blocks of inputs go in `splits` runs of per_split.
 struct Plan {
     int side, splits, per_split;
+    double us;                   // the estimate
 };
 
 // The form of the least estimated time.  Measured on an MI355X (us; memory 5.1 TB/s, launches of
@@ -28,16 +29,15 @@ struct Plan {
 //    2000 x 16384 x 4096     -   /  -    / 152   / 119
 //    4096 x  4096 x 4096     -   /  -    /  72   /  61
 // and in runs, 96 x 4096 x 16384 36 as it is and 22 in 4 (tiles of 64).
-inline Plan plan_of(int n_out, int n_in, int n_rows)
+inline Plan form_of(int n_out, int n_in, int n_rows, int most_splits = 16)
 {
     const int blocks = (n_in + kBlock - 1) / kBlock;
     const int64_t n_tiles = ((int64_t)n_out + kTile - 1) / kTile;
     const int64_t m_tiles = ((int64_t)n_rows + kTile - 1) / kTile;
     const double tile = (double)kBlock * kTile * blocks;        // bytes of a tile of 16 rows
     const double groups = (double)((m_tiles + 3) / 4);
-    Plan best{0, 1, blocks};
-    double least = 5.0 + std::max(n_tiles * tile / 5.1e6,
-                                  n_tiles * tile * (m_tiles + groups) / 25e6);
+    Plan best{0, 1, blocks, 5.0 + std::max(n_tiles * tile / 5.1e6,
+                                           n_tiles * tile * (m_tiles + groups) / 25e6)};
     const struct {
         int side;
         double cost, alone;
@@ -47,20 +47,40 @@ inline Plan plan_of(int n_out, int n_in, int n_rows)
         if (tile * (f.side / kTile) >= 2147483648.0) continue;
         const double tiles = (double)((n_out + (int64_t)f.side - 1) / f.side) *
                              (double)((n_rows + (int64_t)f.side - 1) / f.side);
-        for (int s = 1; s <= 16; s *= 2) {
+        for (int s = 1; s <= most_splits; s *= 2) {
             const int per = (blocks + s - 1) / s;
             if (s > 1 && per < 4) break;
             const int runs = (blocks + per - 1) / per;
             const double turns = (double)(int64_t)((tiles * runs + kCus - 1) / kCus);
-            double t = 6.0 + per * std::max(f.alone, f.cost * turns);
+            double t = 6.0 + std::max(per * std::max(f.alone, f.cost * turns),
+                                      (n_tiles + m_tiles) * tile / 5.1e6);
             if (runs > 1) t += 4.0 + (runs + 0.5) * 4.0 * n_out * (double)n_rows / 5.1e6;
-            if (t < least) {
-                least = t;
-                best = {f.side, runs, per};
-            }
+            if (t < best.us) best = {f.side, runs, per, t};
         }
     }
     return best;
+}
+
+// The rows in two parts where that is less, the first of whole tiles of 256: a last tile of a few
+// rows takes as long as a whole one.  777 x 20001 x 5000 as a whole 113 us, as 768 rows and 9
+// 97.
+struct Parts {
+    int n_first;                 // rows of the first part
+    Plan first, rest;            // (rest: of no rows where n_first is all of them)
+};
+
+inline Parts parts_of(int n_out, int n_in, int n_rows)
+{
+    const Plan whole = form_of(n_out, n_in, n_rows);
+    const int n_first = n_rows / 256 * 256;
+    if (n_first > 0 && n_first < n_rows) {
+        const Plan first = form_of(n_out, n_in, n_first, 1);
+        const Plan rest = form_of(n_out, n_in, n_rows - n_first, 1);
+        // (a second launch follows the first without a caller's share of either)
+        if (first.us + rest.us - 3.0 < whole.us)
+            return {n_first, first, rest};
+    }
+    return {n_rows, whole, whole};
 }
 
 }  // namespace qlm_f8_host

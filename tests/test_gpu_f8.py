@@ -168,6 +168,24 @@ SIZES = [(1, 1, 1), (1, 16, 128), (1, 300, 500), (2, 129, 257), (15, 17, 127), (
          (300, 700, 2000), (513, 300, 515), (1000, 1100, 256)]
 
 
+# sizes that reach every form, its runs of inputs and its parts of rows
+FORMS = [(1779, 1510, 136), (2363, 1740, 725), (1217, 3351, 2373), (481, 1015, 7953),
+         (2216, 5381, 103), (4136, 4067, 319), (2998, 5413, 813), (196, 4159, 8591),
+         (1950, 898, 261), (1900, 574, 2101), (631, 755, 8468), (4200, 4096, 256)]
+
+
+@pytest.mark.parametrize("dtype", ["float16", "float32"])
+@pytest.mark.parametrize("m,n,k", FORMS)
+def test_forms(torch, qlm, m, n, k, dtype):
+    dt = getattr(torch, dtype)
+    got, exact, size, (x, w) = product(torch, qlm, m, n, k, dt, seed=m + n + k, spread=0.3)
+    e = (got.double() - exact).abs()
+    lim = bound(torch, exact, size, k, dt)
+    fine = exact.abs() < torch.finfo(dt).max
+    assert bool((e <= lim)[fine].all()), float((e / lim)[fine].max())
+    assert torch.equal(got.nan_to_num(0.0), qlm.f8_matmul(x, w, dtype=dt).nan_to_num(0.0))
+
+
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
 @pytest.mark.parametrize("m,n,k", SIZES)
 def test_products(torch, qlm, m, n, k, dtype):
@@ -190,12 +208,13 @@ def test_large_products(torch, qlm, m, n, k):
     assert torch.equal(got, again)                     # (bit for bit the same)
 
 
-@pytest.mark.parametrize("m", [3, 40, 70, 300])
+@pytest.mark.parametrize("m,n", [(3, 203), (40, 203), (70, 203), (300, 203), (1950, 898),
+                                 (1779, 1510), (2216, 5381), (2363, 1740)])
 @pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
-def test_strided_out(torch, qlm, m, dtype):
+def test_strided_out(torch, qlm, m, n, dtype):
     """Outputs between other columns, which stay; odd strides and starts."""
-    n, k = 203, 384
-    big = torch.full((m + 2, 451), -5.0, dtype=getattr(torch, dtype), device="cuda")
+    k = 384 if n == 203 else 261
+    big = torch.full((m + 2, n + 248), -5.0, dtype=getattr(torch, dtype), device="cuda")
     out = big[1:m + 1, 7:7 + n]
     got, exact, size, _ = product(torch, qlm, m, n, k, None, out=out, spread=0.3)
     assert got.data_ptr() == out.data_ptr()
@@ -205,10 +224,11 @@ def test_strided_out(torch, qlm, m, dtype):
     assert bool((big == -5.0).all())
 
 
-@pytest.mark.parametrize("m", [4, 40, 300])
-def test_not_a_numbers(torch, qlm, m):
+@pytest.mark.parametrize("m,n", [(4, 150), (40, 150), (300, 150), (1950, 898), (1779, 1510),
+                                 (2216, 5381)])
+def test_not_a_numbers(torch, qlm, m, n):
     """A code that is none spoils its row, one of the weights its output, and nothing else."""
-    n, k = 150, 300
+    k = 300
     _, exact, size, (x, w) = product(torch, qlm, m, n, k, torch.float32)
     codes = x.codes.view(torch.uint8)
     codes[0, 1, 2, 3, 5] = 0x7f                            # row 3
