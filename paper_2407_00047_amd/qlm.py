@@ -963,7 +963,8 @@ def kv_append_rotated(cache: DeviceKvCache, batch: KvBatch, k, v, q, rotary: Rot
         rq = _rows(q, n, heads, dim, "q")
         if out is None:
             import torch
-            out = _allocated(stream, lambda: torch.empty(q.shape, dtype=q.dtype, device=q.device))
+            make = lambda: torch.empty_like(q, memory_format=torch.contiguous_format)  # noqa: E731
+            out = make() if stream is None else _allocated(stream, make)
         elif out.shape != q.shape or out.dtype != q.dtype:
             raise ValueError("out must have q's shape and type")
         ro = _rows(out, n, heads, dim, "out")
@@ -1185,13 +1186,15 @@ class F8Rows:
         """Room for so many rows, as a call on `stream` allocates it."""
         import torch
         tiles, blocks = -(-n_rows // F8_TILE), -(-n_in // F8_BLOCK)
+        codes = lambda: torch.empty((tiles, blocks, 8, F8_TILE, 16),  # noqa: E731
+                                    dtype=torch.float8_e4m3fn, device=device)
+        scale = lambda: torch.empty((blocks, tiles * F8_TILE), dtype=torch.float32,  # noqa: E731
+                                    device=device)
         rows = cls.__new__(cls)
-        rows._hold(_allocated(stream, lambda: torch.empty((tiles, blocks, 8, F8_TILE, 16),
-                                                          dtype=torch.float8_e4m3fn,
-                                                          device=device)),
-                   _allocated(stream, lambda: torch.empty((blocks, tiles * F8_TILE),
-                                                          dtype=torch.float32, device=device)),
-                   n_rows, n_in)
+        if stream is None:
+            rows._hold(codes(), scale(), n_rows, n_in)
+        else:
+            rows._hold(_allocated(stream, codes), _allocated(stream, scale), n_rows, n_in)
         return rows
 
 
@@ -1320,14 +1323,18 @@ def draft_verify(batch: KvBatch, tokens, target, draft, uniform, lengths=None, w
         raise ValueError("tokens must be [%d rows] int32" % n)
     if uniform.dtype != torch.float32 or uniform.numel() != n or not uniform.is_contiguous():
         raise ValueError("uniform must be [%d rows] float32" % n)
-    device = batch.lengths.device
-    if lengths is None:
-        lengths = _allocated(stream, lambda: torch.empty((seqs,), dtype=torch.int32, device=device))
-    elif lengths.dtype != torch.int32 or lengths.numel() != seqs or not lengths.is_contiguous():
+    have = batch.lengths
+    if lengths is not None and (lengths.dtype != torch.int32 or lengths.numel() != seqs or
+                                not lengths.is_contiguous()):
         raise ValueError("lengths must be [n_seqs] int32")
-    out = _allocated(stream, lambda: torch.empty((seqs, batch.max_new), dtype=torch.int32,
-                                                 device=device))
-    count = _allocated(stream, lambda: torch.empty((seqs,), dtype=torch.int32, device=device))
+    one = lambda: torch.empty_like(have)  # noqa: E731
+    rows = lambda: torch.empty((seqs, batch.max_new), dtype=torch.int32,  # noqa: E731
+                               device=have.device)
+    if stream is None:
+        out, count, lengths = rows(), one(), one() if lengths is None else lengths
+    else:
+        out, count = _allocated(stream, rows), _allocated(stream, one)
+        lengths = _allocated(stream, one) if lengths is None else lengths
     if ws is None:
         ws = _allocated(stream, lambda: draft_verify_workspace(batch, vocab), False)
     if not 0 <= index == tokens.get_device() == target.get_device() == uniform.get_device() == \
@@ -1336,11 +1343,10 @@ def draft_verify(batch: KvBatch, tokens, target, draft, uniform, lengths=None, w
         _refuse_place(index, batch=batch.lengths, tokens=tokens, target=target, draft=draft,
                       uniform=uniform, lengths=lengths, ws=ws)
     # (the stride of a matrix of one row says nothing)
-    one = n <= 1
     rc = (_lib or library()).qlm_draft_verify(
         batch._ref,
-        _DRAFT.pack(vocab, kind, target.data_ptr(), near, vocab if one else stride[0],
-                    vocab if one else apart, tokens.data_ptr(), uniform.data_ptr()),
+        _DRAFT.pack(vocab, kind, target.data_ptr(), near, stride[0] if n > 1 else vocab,
+                    apart if n > 1 else vocab, tokens.data_ptr(), uniform.data_ptr()),
         out.data_ptr(), count.data_ptr(), lengths.data_ptr(), ws.data_ptr(), ws.numel(),
         _raw_stream(stream))
     if rc:
