@@ -55,11 +55,12 @@ struct PackArgs {
     uint8_t *packed;
     float *packed_scale;          // [block of outputs][block of inputs], behind the codes
     int32_t N, K, blocks;
-    int32_t wide;                 // 16 codes of a row may be read at once
+    int32_t wide, words;          // 16 codes of a row, or four, may be read at once
     int64_t chunks, scales;
 };
 
-// A thread for 16 codes.  Done once for a matrix.
+// A thread for 16 codes.  Done once for a matrix: 16384 x 4096 25 us, 5.3 TB/s; rows of 5000 codes,
+// read four at a time, 20001 of them PACK_US.
 __global__ __launch_bounds__(256) void k_f8_pack(PackArgs a)
 {
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -77,7 +78,12 @@ __global__ __launch_bounds__(256) void k_f8_pack(PackArgs a)
         } else {
             uint32_t u[4] = {0, 0, 0, 0};
             const int have = min(16, (int)(a.K - k));
-            for (int e = 0; e < have; ++e) u[e >> 2] |= (uint32_t)p[e] << (8 * (e & 3));
+            if (a.words) {                     // (their number is one of fours)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) u[e] = 4 * e < have ? ((const uint32_t *)p)[e] : 0u;
+            } else {
+                for (int e = 0; e < have; ++e) u[e >> 2] |= (uint32_t)p[e] << (8 * (e & 3));
+            }
             w = uint4{u[0], u[1], u[2], u[3]};
         }
     }
@@ -649,6 +655,7 @@ int qlm_f8_pack(const qlm_f8 *weight, const void *codes, const float *scale, qlm
     a.packed = (uint8_t *)weight->packed;
     a.packed_scale = (float *)(a.packed + 16 * a.chunks);
     a.wide = a.K % 16 == 0 && (uintptr_t)codes % 16 == 0;
+    a.words = a.K % 4 == 0 && (uintptr_t)codes % 4 == 0;
     const int64_t grid = (a.chunks + 255) / 256;
     if (!can_launch(grid, 256)) return fail(QLM_ERR_CAPACITY, "too many threads for one matrix");
     k_f8_pack<<<(unsigned)grid, 256, 0, stream>>>(a);
