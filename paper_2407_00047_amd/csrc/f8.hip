@@ -229,35 +229,48 @@ __device__ inline void store4(const MatArgs &a, int64_t m, int n, float4v v)
         if (n + i < a.N) p[i] = (uint16_t)out_bits(v[i], a.dtype);
 }
 
-// 16 outputs of MT tiles of rows to a workgroup, its W waves taking the blocks of inputs in turn,
-// U of them loaded at once.
-template <int MT, int W, int U> __global__ __launch_bounds__(64 * W) void k_f8_thin(MatArgs a)
+// NT tiles of outputs and MT of rows to a workgroup, its W waves taking the blocks of inputs in turn,
+// U of them loaded at once; their sums are added in pairs of waves.
+template <int NT, int MT, int W, int U> __global__ __launch_bounds__(64 * W) void k_f8_thin(MatArgs a)
 {
-    __shared__ float4v part[W][MT][64];
+    constexpr int TILES = NT * MT, HELD = W / 2;
+    __shared__ float4v part[HELD][TILES][64];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int nt = (int)(blockIdx.x % (uint32_t)a.n_tiles), mg = (int)(blockIdx.x / (uint32_t)a.n_tiles);
-    const int mt0 = mg * MT;
-    float4v acc[MT];
-    for (int i = 0; i < MT; ++i) acc[i] = float4v{0, 0, 0, 0};
-    const uint8_t *w = a.w + (int64_t)nt * a.blocks * kTileBytes;
-    const float *ws = a.ws + (int64_t)(nt / (kBlock / kTile)) * a.blocks;
-    const uint8_t *x[MT];
-    const float *xs[MT];
+    const uint32_t across = (uint32_t)(a.n_tiles + NT - 1) / NT;
+    // (groups of rows beside the same outputs on one of eight dies, one behind the other)
+    const uint32_t groups = (uint32_t)(a.m_tiles + MT - 1) / MT, turn = blockIdx.x / 8;
+    const uint32_t run = turn / groups * 8 + blockIdx.x % 8;
+    if (run >= across) return;
+    const int nt0 = (int)run * NT, mt0 = (int)(turn % groups) * MT;
+    float4v acc[NT][MT];
+    const uint8_t *w[NT], *x[MT];
+    const float *ws[NT], *xs[MT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int nt = min(nt0 + n, a.n_tiles - 1);
+        w[n] = a.w + (int64_t)nt * a.blocks * kTileBytes;
+        ws[n] = a.ws + (int64_t)(nt / (kBlock / kTile)) * a.blocks;
+    }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
         const int mt = min(mt0 + i, a.m_tiles - 1);
         x[i] = a.x + (int64_t)mt * a.blocks * kTileBytes;
         xs[i] = a.xs + mt * kTile + (lane & 15);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[n][i] = float4v{0, 0, 0, 0};
     }
     for (int b0 = wv; b0 < a.blocks; b0 += U * W) {
-        int8v wo[U], xo[U][MT];
-        float s[U], t[U][MT];
+        int8v wo[U][NT], xo[U][MT];
+        float s[U][NT], t[U][MT];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             // (past the last block it is read again and not used)
             const int b = min(b0 + u * W, a.blocks - 1);
-            wo[u] = operand(w + (int64_t)b * kTileBytes, lane);
-            s[u] = ws[b];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                wo[u][n] = operand(w[n] + (int64_t)b * kTileBytes, lane);
+                s[u][n] = ws[n][b];
+            }
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
                 xo[u][i] = operand(x[i] + (int64_t)b * kTileBytes, lane);
@@ -268,21 +281,38 @@ template <int MT, int W, int U> __global__ __launch_bounds__(64 * W) void k_f8_t
         for (int u = 0; u < U; ++u) {
             if (b0 + u * W >= a.blocks) break;
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const float4v c = product(wo[u], xo[u][i]);
-                const float by = s[u] * t[u][i];
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] += by * c[j];
-            }
+                for (int i = 0; i < MT; ++i) {
+                    const float4v c = product(wo[u][n], xo[u][i]);
+                    const float by = s[u][n] * t[u][i];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[n][i][j] += by * c[j];
+                }
         }
     }
-    for (int i = 0; i < MT; ++i) part[wv][i][lane] = acc[i];
+#pragma unroll
+    for (int half = HELD; half >= 1; half /= 2) {
+        if (wv >= half && wv < 2 * half)
+#pragma unroll
+            for (int k = 0; k < TILES; ++k) part[wv - half][k][lane] = acc[k / MT][k % MT];
+        __syncthreads();
+        if (half > 1 && wv < half)
+#pragma unroll
+            for (int k = 0; k < TILES; ++k) acc[k / MT][k % MT] += part[wv][k][lane];
+        if (half > 1) __syncthreads();
+    }
+    // the last pair's sums by all waves
+    static_assert(HELD >= 2, "room for the other of the last pair");
+    if (wv == 0)
+#pragma unroll
+        for (int k = 0; k < TILES; ++k) part[1][k][lane] = acc[k / MT][k % MT];
     __syncthreads();
-    for (int i = wv; i < MT; i += W) {
-        float4v v = part[0][i][lane];
-        for (int k = 1; k < W; ++k) v += part[k][i][lane];
-        const int64_t m = (int64_t)(mt0 + i) * kTile + (lane & 15);
-        if (m < a.M) store4(a, m, nt * kTile + 4 * (lane >> 4), v);
+    for (int k = wv; k < TILES; k += W) {
+        const int64_t m = (int64_t)(mt0 + k % MT) * kTile + (lane & 15);
+        if (m < a.M)
+            store4(a, m, (nt0 + k / MT) * kTile + 4 * (lane >> 4),
+                   part[1][k][lane] + part[0][k][lane]);
     }
 }
 
@@ -572,12 +602,10 @@ template <int NT, int MT, int WN, int WM, int GROUPS> void launch_wide(MatArgs a
     k_f8_wide<NT, MT, WN, WM, 5><<<(unsigned)grid, 64 * WN * WM, 0, stream>>>(a);
 }
 
-// Tiles of rows that a workgroup of k_f8_thin takes.
-int thin_rows(const MatArgs &a) { return a.m_tiles == 1 ? 1 : a.m_tiles == 2 ? 2 : 4; }
-
 int64_t thin_groups(const MatArgs &a)
 {
-    return (int64_t)a.n_tiles * ((a.m_tiles + thin_rows(a) - 1) / thin_rows(a));
+    const auto t = qlm_f8_host::thin_of(a.n_tiles, a.m_tiles, a.blocks);
+    return ((a.n_tiles + t.outs - 1ll) / t.outs + 7) / 8 * 8 * ((a.m_tiles + t.rows - 1ll) / t.rows);
 }
 
 // Whether a form's launches can be made.
@@ -592,13 +620,14 @@ bool fits(const MatArgs &a, const Plan &p)
 hipError_t launch(MatArgs a, const Plan &p, void *ws, hipStream_t stream)
 {
     if (!p.side) {
-        const unsigned grid = (unsigned)thin_groups(a);
-        if (thin_rows(a) == 1)
-            k_f8_thin<1, 8, 4><<<grid, 512, 0, stream>>>(a);
-        else if (thin_rows(a) == 2)
-            k_f8_thin<2, 8, 4><<<grid, 512, 0, stream>>>(a);
-        else
-            k_f8_thin<4, 8, 3><<<grid, 512, 0, stream>>>(a);
+        const auto t = qlm_f8_host::thin_of(a.n_tiles, a.m_tiles, a.blocks);
+        auto kern = t.outs == 4   ? k_f8_thin<4, 2, 8, 1>
+                    : t.rows == 4 ? k_f8_thin<2, 4, 8, 2>
+                    : t.rows == 3 ? k_f8_thin<2, 3, 8, 2>
+                    : t.outs == 2 ? k_f8_thin<2, 2, 8, 2>
+                    : t.rows == 2 ? k_f8_thin<1, 2, 8, 4>
+                                  : k_f8_thin<1, 1, 8, 4>;
+        kern<<<(unsigned)thin_groups(a), 512, 0, stream>>>(a);
         return hipGetLastError();
     }
     a.splits = p.splits;

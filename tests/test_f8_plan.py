@@ -19,6 +19,12 @@ extern "C" void parts(int n_out, int n_in, int rows, int *got)
                        p.rest.side, p.rest.splits, p.rest.per_split};
     for (int i = 0; i < 7; ++i) got[i] = all[i];
 }
+extern "C" void thin(int n_out, int n_in, int rows, int *got)
+{
+    const Thin t = thin_of((n_out + 15ll) / 16, (rows + 15ll) / 16, (n_in + 127) / 128);
+    got[0] = t.outs;
+    got[1] = t.rows;
+}
 """
 
 
@@ -32,11 +38,12 @@ def parts(tmp_path_factory):
                     str(d / "plan.cpp")], check=True)
     lib = ctypes.CDLL(lib)
 
-    def call(rows, n_out, n_in):
+    def call(rows, n_out, n_in, what=lib.parts):
         got = (ctypes.c_int * 7)()
-        lib.parts(n_out, n_in, rows, got)
+        what(n_out, n_in, rows, got)
         return list(got)
 
+    call.thin = lambda *sizes: tuple(call(*sizes, what=lib.thin)[:2])
     return call
 
 
@@ -54,6 +61,9 @@ def test_everything_is_taken_once(parts):
                     assert side in (0, 64, 128, 256) and splits >= 1
                     assert (splits - 1) * per < blocks <= splits * per
                     assert splits == 1 or side > 0
+                    if side == 0:
+                        assert parts.thin(rows, n_out, n_in) in \
+                            ((1, 1), (1, 2), (2, 2), (2, 3), (2, 4), (4, 2))
                     # a workgroup's offsets into its tiles
                     assert side == 0 or blocks * 2048 * (side // 16) < 1 << 31
 
@@ -66,7 +76,10 @@ def test_sizes_of_the_gpu_tests_reach_every_form(parts):
         seen.add((forms[0], forms[1] > 1, n_first < m))
         if n_first < m:
             seen.add(("rest", forms[3]))
+        elif forms[0] == 0:
+            seen.add(("thin", *parts.thin(m, n, k)))
     want = {(0, False, False), (64, False, False), (64, True, False), (128, False, False),
             (128, True, False), (256, False, False), (256, False, True), (128, False, True),
             (64, False, True), ("rest", 0), ("rest", 64)}
+    want |= {("thin", *t) for t in ((1, 1), (1, 2), (2, 2), (2, 3), (2, 4), (4, 2))}
     assert want <= seen, want - seen

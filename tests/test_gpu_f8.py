@@ -169,9 +169,11 @@ SIZES = [(1, 1, 1), (1, 16, 128), (1, 300, 500), (2, 129, 257), (15, 17, 127), (
 
 
 # sizes that reach every form, its runs of inputs and its parts of rows
-FORMS = [(1779, 1510, 136), (2363, 1740, 725), (1217, 3351, 2373), (481, 1015, 7953),
-         (2216, 5381, 103), (4136, 4067, 319), (2998, 5413, 813), (196, 4159, 8591),
-         (1950, 898, 261), (1900, 574, 2101), (631, 755, 8468), (4200, 4096, 256)]
+FORMS = [(33, 131, 146), (203, 323, 118), (580, 442, 131), (132, 3022, 147), (401, 1159, 105),
+         (300, 1647, 109), (679, 175, 962), (165, 704, 100), (802, 102, 2575), (2306, 855, 1343),
+         (714, 2709, 108), (770, 271, 3944), (466, 505, 13323), (4105, 906, 1175),
+         (1220, 6878, 5131), (1808, 6603, 903), (2216, 5381, 103), (3079, 5296, 923),
+         (291, 183, 35508), (4200, 4096, 256), (96, 4096, 5300), (2050, 2050, 130)]
 
 
 @pytest.mark.parametrize("dtype", ["float16", "float32"])
@@ -208,8 +210,8 @@ def test_large_products(torch, qlm, m, n, k):
     assert torch.equal(got, again)                     # (bit for bit the same)
 
 
-@pytest.mark.parametrize("m,n", [(3, 203), (40, 203), (70, 203), (300, 203), (1950, 898),
-                                 (1779, 1510), (2216, 5381), (2363, 1740)])
+@pytest.mark.parametrize("m,n", [(3, 203), (40, 203), (70, 203), (300, 203), (2306, 855),
+                                 (1779, 1510), (2216, 5381), (3079, 5296)])
 @pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
 def test_strided_out(torch, qlm, m, n, dtype):
     """Outputs between other columns, which stay; odd strides and starts."""
@@ -224,7 +226,7 @@ def test_strided_out(torch, qlm, m, n, dtype):
     assert bool((big == -5.0).all())
 
 
-@pytest.mark.parametrize("m,n", [(4, 150), (40, 150), (300, 150), (1950, 898), (1779, 1510),
+@pytest.mark.parametrize("m,n", [(4, 150), (40, 150), (300, 150), (2306, 855), (1779, 1510),
                                  (2216, 5381)])
 def test_not_a_numbers(torch, qlm, m, n):
     """A code that is none spoils its row, one of the weights its output, and nothing else."""
