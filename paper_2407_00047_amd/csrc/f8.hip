@@ -100,7 +100,8 @@ struct RowsArgs {
 };
 
 // A wave for a tile, eight lanes for a row of it: 16 inputs a lane, the largest magnitude over
-// the eight, and 16 codes a lane (eight rows of a chunk fill a line of memory).
+// the eight, and 16 codes a lane (eight rows of a chunk fill a line of memory).  Bound by memory:
+// 8000 rows of 16384 73 us, 5.4 TB/s; one row of 4096 3.7 us, a launch.
 template <bool BF> __global__ __launch_bounds__(256) void k_f8_rows(RowsArgs a)
 {
     const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -230,10 +231,13 @@ __device__ inline void store4(const MatArgs &a, int64_t m, int n, float4v v)
 }
 
 // NT tiles of outputs and MT of rows to a workgroup, its W waves taking the blocks of inputs in turn,
-// U of them loaded at once; their sums are added in pairs of waves.
+// U of them loaded at once.  Nothing is shared but the sums, so there is no barrier to wait at while
+// loads are under way.  1 row, 4096 x 4096: 4.7 us, 3.6 TB/s, of which 2 to 3 a launch takes; 64 rows,
+// 16384 x 4096: 15.3 us (18.5 by 1 x 4 tiles with the groups of rows behind all outputs).
 template <int NT, int MT, int W, int U> __global__ __launch_bounds__(64 * W) void k_f8_thin(MatArgs a)
 {
-    constexpr int TILES = NT * MT, HELD = W / 2;
+    // sums of few tiles are held of every wave, of more of half of them at a time
+    constexpr int TILES = NT * MT, HELD = TILES <= 2 ? W : W / 2;
     __shared__ float4v part[HELD][TILES][64];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t across = (uint32_t)(a.n_tiles + NT - 1) / NT;
@@ -291,6 +295,22 @@ template <int NT, int MT, int W, int U> __global__ __launch_bounds__(64 * W) voi
                 }
         }
     }
+    auto store = [&](int k, float4v v) {
+        const int64_t m = (int64_t)(mt0 + k % MT) * kTile + (lane & 15);
+        if (m < a.M) store4(a, m, (nt0 + k / MT) * kTile + 4 * (lane >> 4), v);
+    };
+    if constexpr (HELD == W) {
+#pragma unroll
+        for (int k = 0; k < TILES; ++k) part[wv][k][lane] = acc[k / MT][k % MT];
+        __syncthreads();
+        for (int k = wv; k < TILES; k += W) {
+            float4v v = part[0][k][lane];
+#pragma unroll
+            for (int i = 1; i < W; ++i) v += part[i][k][lane];
+            store(k, v);
+        }
+        return;
+    }
 #pragma unroll
     for (int half = HELD; half >= 1; half /= 2) {
         if (wv >= half && wv < 2 * half)
@@ -308,12 +328,7 @@ template <int NT, int MT, int W, int U> __global__ __launch_bounds__(64 * W) voi
 #pragma unroll
         for (int k = 0; k < TILES; ++k) part[1][k][lane] = acc[k / MT][k % MT];
     __syncthreads();
-    for (int k = wv; k < TILES; k += W) {
-        const int64_t m = (int64_t)(mt0 + k % MT) * kTile + (lane & 15);
-        if (m < a.M)
-            store4(a, m, (nt0 + k / MT) * kTile + 4 * (lane >> 4),
-                   part[1][k][lane] + part[0][k][lane]);
-    }
+    for (int k = wv; k < TILES; k += W) store(k, part[1][k][lane] + part[0][k][lane]);
 }
 
 // 16 bytes a lane from a buffer into shared memory, lane after lane from `to` on (uniform over the
@@ -384,7 +399,20 @@ __device__ inline void store_rows(const MatArgs &a, int split, int64_t m0, int n
         }
 }
 
-// Tiles of (16 NT WN) outputs and (16 MT WM) rows to a workgroup of WN x WM waves.
+// Tiles of (16 NT WN) outputs and (16 MT WM) rows to a workgroup of WN x WM waves, which takes one
+// after another.
+// 8192 x 16384 x 4096 by tiles of 256: 464 us, 2370 TFLOP/s (a library's product with one scale for
+// everything, which needs no additions outside the matrix instructions, 439).  The matrix instructions
+// alone would take 260 at the 2.0 GHz that the chip keeps under them; leaving out the additions, the
+// loads or the stores takes 45, 80 and 45 off.  So: as much reuse as the registers hold (128
+// sums a lane; the sums are added to outside the matrix instructions, so they cannot stand in
+// accumulation registers), for tiles of 128 x 192 and 128 x 128 with two workgroups to a unit read
+// 1.7 and 2 times as much and took 640 and 670 where this took 557; loads straight into shared memory, more
+// than a block ahead (two whole buffers, one block ahead: 556 to 517), a few at a time between
+// products (480 to 472), by buffer addresses (517 to 497: with plain addresses the compiler waits for all
+// of them at each scale); rows stored whole from shared memory (556 to 500 with the former).  The 32x32
+// instructions took 492 in place of 477, rows' operands read ahead of the barrier and wave
+// priorities changed nothing.
 template <int NT, int MT, int WN, int WM, int SLOTS>
 __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
 {

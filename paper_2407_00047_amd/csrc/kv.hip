@@ -641,7 +641,11 @@ __device__ inline void turn_queries(const AppendArgs &a, const TurnArgs &t, uint
 constexpr int kTurnHeads = 4;             // heads a thread takes of many rows
 constexpr int64_t kTurnMany = 4096;       // waves of single heads
 
-// The keys' workgroups as in k_append, then for each row those of its queries.
+// The keys' workgroups as in k_append, then for each row those of its queries.  A decode step's one
+// token for each of 64 sequences (32 heads, 8 of keys, 128 dims): 8.6 us where k_append takes 6.8, the
+// positions' and the tables' reads in its chain.  Six ragged prompts of up to 2100 tokens on three axes
+// (152 MB): 41 us, 3.7 TB/s; the keys alone 25 (k_append 20), the queries alone 26 (4.4 TB/s).
+// Angles read for each head and chunk of eight dims: 95.
 template <int FMT, int ND, bool NEIGHBOURS, int HEADS>
 __global__ __launch_bounds__(kThreads, ND <= 2 ? 4 : 2) void k_append_rotated(AppendArgs a, TurnArgs t)
 {
