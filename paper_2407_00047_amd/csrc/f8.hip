@@ -60,7 +60,7 @@ struct PackArgs {
 };
 
 // A thread for 16 codes.  Done once for a matrix: 16384 x 4096 25 us, 5.3 TB/s; rows of 5000 codes,
-// read four at a time, 20001 of them PACK_US.
+// read four at a time, 20001 of them in 42 us.
 __global__ __launch_bounds__(256) void k_f8_pack(PackArgs a)
 {
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -332,7 +332,7 @@ template <int NT, int MT, int W, int U> __global__ __launch_bounds__(64 * W) voi
 }
 
 // 16 bytes a lane from a buffer into shared memory, lane after lane from `to` on (uniform over the
-// wave); done when the loads are waited for.  Zeros past the buffer's end.
+// wave); done when the loads are waited for.
 __device__ inline void load_lds(__amdgpu_buffer_rsrc_t from, int at, int lane_at, uint8_t *to)
 {
     typedef uint32_t __attribute__((address_space(3))) *shared_ptr;
@@ -356,7 +356,7 @@ __device__ inline void store_rows(const MatArgs &a, int split, int64_t m0, int n
 {
     constexpr int ROW = 16 * NT * sizeof(T), CHUNKS = ROW / 16, MASK = (CHUNKS < 16 ? CHUNKS : 16) - 1;
     int lane = threadIdx.x & 63;
-    asm volatile("" : "+v"(lane));         // (places that depend on it are not kept from tile to tile)
+    asm volatile("" : "+v"(lane)::"memory");   // (places that depend on it are not kept from tile to tile)
     const int r = lane & 15, q = lane >> 4;
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
@@ -369,6 +369,7 @@ __device__ inline void store_rows(const MatArgs &a, int split, int64_t m0, int n
                                  out_bits(v[i][2], a.dtype) | out_bits(v[i][3], a.dtype) << 16};
         }
     }
+    asm volatile("" ::: "memory");         // (written and read as different types)
     const int rows = (int)min((int64_t)kTile, a.M - m0);
     T *out = (T *)a.out + split * a.out_split + m0 * a.out_stride + n0;
     if (a.out_wide && n0 + 16 * NT <= a.N) {
@@ -413,15 +414,15 @@ __device__ inline void store_rows(const MatArgs &a, int split, int64_t m0, int n
 // of them at each scale); rows stored whole from shared memory (556 to 500 with the former).  The 32x32
 // instructions took 492 in place of 477, rows' operands read ahead of the barrier and wave
 // priorities changed nothing.
-template <int NT, int MT, int WN, int WM, int SLOTS>
+template <int NT, int MT, int WN, int WM>
 __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
 {
     constexpr int W = WN * WM, TN = NT * WN, TM = MT * WM;
     static_assert(2 * TN % W == 0 && 2 * TM % W == 0, "a half's pieces are shared evenly");
     constexpr int kSlot = kTileBytes * (TN > TM ? TN : TM);
-    __shared__ __align__(16) uint8_t s0[kSlot], s1[kSlot], s2[kSlot], s3[kSlot],
-        s4[SLOTS > 4 ? kSlot : 16], s5[SLOTS > 5 ? kSlot : 16];
-    uint8_t *const slot[6] = {s0, s1, s2, s3, s4, s5};
+    constexpr int SLOTS = 5;
+    __shared__ __align__(16) uint8_t s0[kSlot], s1[kSlot], s2[kSlot], s3[kSlot], s4[kSlot];
+    uint8_t *const slot[SLOTS] = {s0, s1, s2, s3, s4};
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wn = wv % WN, wm = wv / WN;
     // eight dies take runs of tiles of their own, in each four rows' tiles before the next outputs'
@@ -434,6 +435,7 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
     const int tile_bytes = a.blocks * kTileBytes;
     int nt0, mt0, split, count;
     __amdgpu_buffer_rsrc_t w_from, x_from;
+    int piece[PN + PM];           // where the wave's pieces of a block start, weights' and rows'
     const float *ws, *xs;
     auto next_tile = [&] {
         const uint32_t id = blockIdx.x % 8 * per + turn;
@@ -446,14 +448,17 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
         const uint32_t high = min(4u, a.grid_m - 4 * group);
         nt0 = (int)(in / high) * TN;
         mt0 = (int)(4 * group + in % high) * TM;
-        auto from = [&](const uint8_t *p, int t0, int have, int most) {
+        // (tiles past the last one are read as the last one)
+        auto from = [&](const uint8_t *p, int t0, int have, int n, int *at) {
+            const int last = min(have - t0, 16) - 1;
+            for (int i = 0; i < n; ++i) at[i] = min(wv / 2 + i * (W / 2), last) * tile_bytes;
             const int skip = b0 * kTileBytes;
             return __builtin_amdgcn_make_buffer_rsrc((void *)(p + (int64_t)t0 * tile_bytes + skip), 0,
-                                                     min(have - t0, most) * tile_bytes - skip,
-                                                     0x00020000);
+                                                     (last + 1) * tile_bytes - skip, 0x00020000);
         };
-        w_from = from(a.w, nt0, a.n_tiles, TN);
-        x_from = from(a.x, mt0, a.m_tiles, TM);
+        static_assert(TN <= 16 && TM <= 16, "the most tiles of a workgroup");
+        w_from = from(a.w, nt0, a.n_tiles, PN, piece);
+        x_from = from(a.x, mt0, a.m_tiles, PM, piece + PN);
         ws = a.ws + (int64_t)(min(nt0 + wn * NT, a.n_tiles - 1) / (kBlock / kTile)) * a.blocks + b0;
         xs = a.xs + (int64_t)b0 * a.padded + (int64_t)mt0 * kTile;
         return true;
@@ -461,8 +466,7 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
     const int lane_at = 16 * lane + 1024 * (wv & 1);
     // half h of the loads: the weights of block h / 2, then its rows, in slot h % SLOTS
     auto fetch = [&](bool n, int i, int b, uint8_t *to) {       // piece i of a half
-        const int at = wv / 2 * tile_bytes + min(b, count - 1) * kTileBytes;
-        load_lds(n ? w_from : x_from, at + i * (W / 2) * tile_bytes, lane_at,
+        load_lds(n ? w_from : x_from, piece[n ? i : PN + i] + min(b, count - 1) * kTileBytes, lane_at,
                  to + 1024 * (i * W + wv));
     };
     float4v acc[NT][MT];
@@ -627,7 +631,7 @@ template <int NT, int MT, int WN, int WM, int GROUPS> void launch_wide(MatArgs a
     a.grid_m = (a.m_tiles + MT * WM - 1) / (MT * WM);
     const int64_t tiles = (int64_t)a.grid_n * a.grid_m * a.splits;
     const int64_t grid = std::min<int64_t>(GROUPS * kCus, (tiles + 7) / 8 * 8);
-    k_f8_wide<NT, MT, WN, WM, 5><<<(unsigned)grid, 64 * WN * WM, 0, stream>>>(a);
+    k_f8_wide<NT, MT, WN, WM><<<(unsigned)grid, 64 * WN * WM, 0, stream>>>(a);
 }
 
 int64_t thin_groups(const MatArgs &a)
