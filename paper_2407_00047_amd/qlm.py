@@ -788,6 +788,16 @@ def _raw_stream(stream):
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
+def _stream_on(index, stream):
+    """The raw stream of a call whose tensors are on GPU `index`: a launch goes to the stream's
+    GPU, so that has to be theirs."""
+    import torch
+    at = torch._C._cuda_getDevice() if stream is None else stream.device_index
+    if at != index:
+        raise ValueError("the call's tensors are on GPU %d, its stream on GPU %d" % (index, at))
+    return torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream
+
+
 class DeviceKvCache:
     """An 8-bit token cache in device memory plus the C struct (qlm_kv_cache).
 
@@ -979,7 +989,7 @@ def kv_append_rotated(cache: DeviceKvCache, batch: KvBatch, k, v, q, rotary: Rot
         _ROWS.pack(*rq) if heads else None, _ROWS.pack(*ro) if heads else None, heads,
         _ROTARY.pack(2 * rotary.pairs, rotary.interleaved, rotary.n_positions, axes,
                      *rotary._tables, at),
-        None if first_position is None else first_position.data_ptr(), _raw_stream(stream))
+        None if first_position is None else first_position.data_ptr(), _stream_on(index, stream))
     if rc:
         _check(rc)
     return out
@@ -1212,7 +1222,7 @@ def f8_pack(codes, scale, stream=None):
     nbytes = int(library().qlm_f8_packed_bytes(n, k))
     packed = _allocated(stream, lambda: torch.empty(nbytes, dtype=torch.uint8, device=codes.device))
     w = F8(packed, n, k)
-    _check(library().qlm_f8_pack(w._ref, _ptr(codes), _ptr(scale), _stream(stream)))
+    _check(library().qlm_f8_pack(w._ref, _ptr(codes), _ptr(scale), _stream_on(w.index, stream)))
     return w
 
 
@@ -1232,7 +1242,7 @@ def f8_rows(x, out=None, stream=None):
         _refuse_place(x.get_device(), x=x, out=out.codes)
     # (the stride of a matrix of one row says nothing)
     rc = (_lib or library()).qlm_f8_rows(out._struct, x.data_ptr(), x.stride(0) if n > 1 else k,
-                                         kind, _raw_stream(stream))
+                                         kind, _stream_on(out.index, stream))
     if rc:
         _check(rc)
     return out
@@ -1281,7 +1291,7 @@ def f8_matmul(x: F8Rows, weight: F8, out=None, dtype=None, ws=None, stream=None)
         _refuse_place(weight.index, weight=weight.packed, x=x.codes, out=out, ws=ws)
     rc = (_lib or library()).qlm_f8_matmul(x._struct, weight._ref, out.data_ptr(),
                                            out.stride(0) if n > 1 else weight.n_out, kind,
-                                           ws.data_ptr(), ws.numel(), _raw_stream(stream))
+                                           ws.data_ptr(), ws.numel(), _stream_on(weight.index, stream))
     if rc:
         _check(rc)
     return out
@@ -1348,7 +1358,7 @@ def draft_verify(batch: KvBatch, tokens, target, draft, uniform, lengths=None, w
         _DRAFT.pack(vocab, kind, target.data_ptr(), near, stride[0] if n > 1 else vocab,
                     apart if n > 1 else vocab, tokens.data_ptr(), uniform.data_ptr()),
         out.data_ptr(), count.data_ptr(), lengths.data_ptr(), ws.data_ptr(), ws.numel(),
-        _raw_stream(stream))
+        _stream_on(index, stream))
     if rc:
         _check(rc)
     return out, count, lengths

@@ -262,8 +262,7 @@ def test_host_tensors_are_refused(qlm, monkeypatch):
 
     h = Host(qlm)
     monkeypatch.setattr(qlm, "_lib", Library())
-    for name in ("_raw_stream", "_stream"):
-        monkeypatch.setattr(qlm, name, lambda stream: None)
+    monkeypatch.setattr(qlm, "_stream_on", lambda index, stream: None)
     for call in (h.append, h.verify, lambda: qlm.f8_pack(h.f8(4, 64), torch.zeros((1, 1))),
                  lambda: qlm.f8_rows(h.half(2, 64)), lambda: qlm.f8_matmul(h.rows, h.weight)):
         with pytest.raises(ValueError, match="must be on the GPU"):
@@ -297,8 +296,7 @@ def test_memory_of_the_calls_stream(qlm, monkeypatch):
     append = dict(k=h.half(2, 2, 32), v=h.half(2, 2, 32), q=h.half(2, 4, 32))
     codes, x = h.f8(4, 64), h.half(2, 64)
     monkeypatch.setattr(qlm, "_lib", Library())
-    for name in ("_raw_stream", "_stream"):
-        monkeypatch.setattr(qlm, name, lambda stream: None)
+    monkeypatch.setattr(qlm, "_stream_on", lambda index, stream: None)
     monkeypatch.setattr(qlm, "_refuse_place", lambda *a, **k: None)   # (no GPU here)
     monkeypatch.setattr(torch.cuda, "stream", on)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: current[-1])
@@ -316,3 +314,18 @@ def test_memory_of_the_calls_stream(qlm, monkeypatch):
             call(stream)
             assert allocated == [where] * n and len(launched) == 1
             assert recorded == (["main"] * kept if stream else [])
+
+
+def test_stream_of_another_gpu(qlm, monkeypatch):
+    """Tensors of one GPU and the current stream, or a given one, of another."""
+    import torch
+
+    class Side:
+        device_index, cuda_stream = 1, 77
+
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 50 + i, raising=False)
+    assert qlm._stream_on(0, None) == 50 and qlm._stream_on(1, Side) == 77
+    for index, stream in ((1, None), (0, Side)):
+        with pytest.raises(ValueError, match="stream on GPU"):
+            qlm._stream_on(index, stream)
