@@ -794,7 +794,8 @@ int qlm_f8_matmul(const qlm_f8_codes *rows, const qlm_f8 *weight, void *out, int
  * sum to 0 or are not finite, from w = target[r]), from w = target[r] of the last row r
  * where none is:
  *   the least word with (w[0] + .. + w[word]) > u * (sum of w), u = uniform[last row]
- * in double precision; -1 where the sum is 0 or not finite.  The token is then distributed as
+ * in double precision, never a word of no weight (also where u came out as 1); -1 where
+ * the sum is 0 or not finite.  The token is then distributed as
  * one drawn from the target, whatever the drafts.  Without `draft` the drafts were
  * chosen, not drawn: draft[r] is 1 at t and 0 elsewhere.  Bit-for-bit reproducible.
  *   tokens_out   [n_seqs][max_new]: the accepted drafts, the token drawn, -1 from there on

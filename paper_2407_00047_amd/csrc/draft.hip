@@ -268,7 +268,7 @@ template <int TYPE, bool SUMS>
 __global__ __launch_bounds__(kThreads) void k_draft_verify(DraftArgs a)
 {
     __shared__ double sums[kSegments], wave_sum[kWaves];
-    __shared__ int s_segment, s_word;
+    __shared__ int s_segment, s_last, s_word;
     const int t = threadIdx.x, lane = t & 63, wv = t >> 6, s = blockIdx.x;
     const Cut cut = cut_of(a.vocab);
     double mine = 0.0;
@@ -284,9 +284,10 @@ __global__ __launch_bounds__(kThreads) void k_draft_verify(DraftArgs a)
                 const double sum = segment_sum(w, cut, g);
                 if (lane == 0) sums[g] = sum;
             }
-        if (t == 0) s_segment = cut.segments - 1;
+        if (t == 0) s_segment = kSegments, s_last = -1;
         __syncthreads();
-        // the segment in which the running sum passes u of the whole
+        // the segment in which the running sum passes u of the whole, of those with any weight
+        // (scans of neighbours round apart: the sum may seem to pass where nothing is added)
         if (!given) mine = t < cut.segments ? sums[t] : 0.0;
         double upto = wave_scan(mine);
         if (lane == 63) wave_sum[wv] = upto;
@@ -298,14 +299,17 @@ __global__ __launch_bounds__(kThreads) void k_draft_verify(DraftArgs a)
         }
         upto += before;
         const double mark = r.u * total;
-        if (t < cut.segments && upto > mark) atomicMin(&s_segment, t);
+        const uint64_t some = __ballot(mine > 0.0), past = __ballot(mine > 0.0 && upto > mark);
+        if (lane == 0 && some) atomicMax(&s_last, 64 * wv + 63 - __builtin_clzll(some));
+        if (lane == 0 && past) atomicMin(&s_segment, 64 * wv + __builtin_ctzll(past));
         __syncthreads();
+        const int segment = min(s_segment, max(s_last, 0));
         const bool usable = total > 0.0 && total < (double)__builtin_inff();
         if (usable || !less) {
-            if (t == s_segment) sums[0] = upto - mine;   // (read by none any more)
+            if (t == segment) sums[0] = upto - mine;   // (read by none any more)
             __syncthreads();
             if (wv == 0) {
-                const int got = usable ? word_of(w, cut, s_segment, sums[0], mark) : -1;
+                const int got = usable ? word_of(w, cut, segment, sums[0], mark) : -1;
                 if (lane == 0) s_word = got;
             }
             __syncthreads();

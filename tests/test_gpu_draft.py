@@ -176,6 +176,26 @@ def test_borders(torch, qlm):
     assert got[0][:, 0].tolist() == [1, 3, 1, 6, 6, 6]
 
 
+@pytest.mark.parametrize("vocab", [3000, 131072])
+@pytest.mark.parametrize("u", [1 - 2.0 ** -24, 1.0, 1.5, float("nan")])
+def test_nothing_behind_the_last_weight(torch, qlm, vocab, u):
+    """Words of no weight after the last one of any, and between: none of them is drawn, not by a
+    uniform number that came out as 1 either."""
+    s = Step(torch, qlm, [1] * 5, vocab, seed=8)
+    s.target[:, vocab // 3:] = 0.0
+    s.target[:, : vocab // 5] = 0.0
+    s.target[1, vocab // 2] = 0.25
+    s.target[2].fill_(0.0)
+    s.target[2, 5] = 1e-30
+    s.uniform.fill_(u)
+    tokens = s.run()[0][:, 0].cpu().numpy()
+    p = s.target.cpu().numpy()
+    assert (p[np.arange(5), tokens] > 0).all()
+    assert tokens[1] == vocab // 2 and tokens[2] == 5
+    if not u < 1:
+        assert (tokens == [np.flatnonzero(row)[-1] for row in p]).all()
+
+
 def test_acceptance_border(torch, qlm):
     """u q < p exactly: equal is refused."""
     s = Step(torch, qlm, [2, 2, 2], 4)
