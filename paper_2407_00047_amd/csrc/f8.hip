@@ -349,10 +349,10 @@ template <int N> __device__ inline void wait_loads()
 
 // 16 rows of NT tiles of outputs, turned in shared memory so that a row's outputs are stored side by
 // side: 16 bytes a lane where rows and outputs are whole, else an output a lane.  `lds`: 16 rows of
-// the wave's own, a row's 16-byte pieces p at p ^ row.
+// the wave's own, a row's 16-byte pieces p at p ^ row.  v[i] is of the (i + first)-th tile.
 template <int NT, typename T>
 __device__ inline void store_rows(const MatArgs &a, int split, int64_t m0, int n0,
-                                  const float4v *v, uint8_t *lds)
+                                  const float4v *v, int first, uint8_t *lds)
 {
     constexpr int ROW = 16 * NT * sizeof(T), CHUNKS = ROW / 16, MASK = (CHUNKS < 16 ? CHUNKS : 16) - 1;
     int lane = threadIdx.x & 63;
@@ -360,7 +360,7 @@ __device__ inline void store_rows(const MatArgs &a, int split, int64_t m0, int n
     const int r = lane & 15, q = lane >> 4;
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-        const int at = (16 * i + 4 * q) * sizeof(T);
+        const int at = (16 * ((i + first) % NT) + 4 * q) * sizeof(T);
         uint8_t *to = lds + r * ROW + ((at / 16) ^ (r & MASK)) * 16 + at % 16;
         if constexpr (sizeof(T) == 4) {
             *(float4v *)to = v[i];
@@ -414,9 +414,15 @@ __device__ inline void store_rows(const MatArgs &a, int split, int64_t m0, int n
 // of them at each scale); rows stored whole from shared memory (556 to 500 with the former).  The 32x32
 // instructions took 492 in place of 477, rows' operands read ahead of the barrier and wave
 // priorities changed nothing.
-template <int NT, int MT, int WN, int WM>
+// MORE: 16 rows or fewer behind the last whole tile are taken along by the last tiles, NT / WM of the
+// outputs' tiles by each wave, whose operands it has at hand; the rows' come past shared memory,
+// which is full.  Every tile makes these products, as a branch between others would cost as much.
+// 777 x 20001 x 5000 87 us, where 768 rows and 9 in two launches took 94; 520 x 60000 x 1500 65 and 87.
+template <int NT, int MT, int WN, int WM, bool MORE>
 __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
 {
+    constexpr int E = MORE ? NT / WM : 0;      // tiles of outputs that a wave takes of the last rows
+    static_assert(!MORE || E * WM == NT, "the waves share the last rows evenly");
     constexpr int W = WN * WM, TN = NT * WN, TM = MT * WM;
     static_assert(2 * TN % W == 0 && 2 * TM % W == 0, "a half's pieces are shared evenly");
     constexpr int kSlot = kTileBytes * (TN > TM ? TN : TM);
@@ -437,6 +443,7 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
     __amdgpu_buffer_rsrc_t w_from, x_from;
     int piece[PN + PM];           // where the wave's pieces of a block start, weights' and rows'
     const float *ws, *xs;
+    int m_last;                   // the tile of rows that MORE adds
     auto next_tile = [&] {
         const uint32_t id = blockIdx.x % 8 * per + turn;
         if (turn >= per || id >= total) return false;
@@ -461,6 +468,7 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
         x_from = from(a.x, mt0, a.m_tiles, PM, piece + PN);
         ws = a.ws + (int64_t)(min(nt0 + wn * NT, a.n_tiles - 1) / (kBlock / kTile)) * a.blocks + b0;
         xs = a.xs + (int64_t)b0 * a.padded + (int64_t)mt0 * kTile;
+        m_last = min(mt0 + TM, a.m_tiles - 1);
         return true;
     };
     const int lane_at = 16 * lane + 1024 * (wv & 1);
@@ -469,8 +477,18 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
         load_lds(n ? w_from : x_from, piece[n ? i : PN + i] + min(b, count - 1) * kTileBytes, lane_at,
                  to + 1024 * (i * W + wv));
     };
-    float4v acc[NT][MT];
-    float by[MT], w_next, x_next[MT];
+    // the tiles of outputs in the wave's order: with MORE those it takes of the last rows at the end
+    const int first = MORE ? (wm + 1) * E : 0;
+    auto from_first = [&](int i) {
+        if constexpr (MORE) {
+            i = (i + first) % NT;
+            asm volatile("" : "+s"(i));        // (the places that depend on it are not all kept)
+        }
+        return i;
+    };
+    float4v acc[NT][MT], acc_last[E + 1];
+    float by[MT], w_next, x_next[MT], by_last, x_last_next;
+    int8v x_last;
     auto fetch_scales = [&](int b) {
         b = min(b, count - 1);
         w_next = ws[b];
@@ -478,19 +496,29 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
 #pragma unroll
         for (int j = 0; j < MT; ++j)
             x_next[j] = (p + min(wm * MT + j, a.m_tiles - 1 - mt0) * kTile)[lane & 15];
+        if constexpr (MORE) x_last_next = (p + (m_last - mt0) * kTile)[lane & 15];
+    };
+    auto fetch_last = [&](int b) {
+        if constexpr (MORE)
+            x_last = operand(a.x + ((int64_t)m_last * a.blocks + split * a.per_split + b) * kTileBytes,
+                             lane);
     };
     // A block's products; `more` starts the loads of later ones, a few at a time: all at once they
     // would hold the waves up until the last is on its way.
     auto step = [&](const uint8_t *wt, const uint8_t *xt, auto more) {
+        // (a tile's place is known a tile ahead of its reads: these come before the products then)
+        auto place = [&](int i) { return wt + kTileBytes * (wn * NT + from_first(i)) + 16 * lane; };
+        int8v ahead = operand(place(0), 0);
         int8v x[MT];
 #pragma unroll
         for (int j = 0; j < MT; ++j) x[j] = operand(xt + kTileBytes * (wm * MT + j), lane);
-        int8v ahead = operand(wt + kTileBytes * wn * NT, lane);
-        float4v was[MT], now[MT];
+        const uint8_t *next = place(1);
+        float4v was[MT], now[MT], was_last, now_last;
 #pragma unroll
         for (int i = 0; i <= NT; ++i) {
             const int8v w = ahead;
-            if (i + 1 < NT) ahead = operand(wt + kTileBytes * (wn * NT + i + 1), lane);
+            if (i + 1 < NT) ahead = operand(next, 0);
+            if (i + 2 < NT) next = place(i + 2);
             if (i < NT) more(i);
 #pragma unroll
             for (int j = 0; j < MT; ++j) {
@@ -499,12 +527,18 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[i - 1][j][e] += by[j] * was[j][e];
             }
+            if (i >= NT - E && i < NT) now_last = product(w, x_last);
+            if (i > NT - E)
 #pragma unroll
-            for (int j = 0; j < MT; ++j) {
+                for (int e = 0; e < 4; ++e) acc_last[i - 1 - NT + E][e] += by_last * was_last[e];
+#pragma unroll
+            for (int j = 0; j < MT + (i >= NT - E); ++j) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
                 __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
-                was[j] = now[j];
             }
+#pragma unroll
+            for (int j = 0; j < MT; ++j) was[j] = now[j];
+            was_last = now_last;
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -528,7 +562,9 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
         asm volatile("" ::: "memory");
 #pragma unroll
         for (int j = 0; j < MT; ++j) by[j] = w_next * x_next[j];
+        if constexpr (MORE) by_last = w_next * x_last_next;
         __builtin_amdgcn_sched_barrier(0);
+        fetch_last(b);                         // (used at the block's end)
         fetch_scales(b + 1);
         __builtin_amdgcn_sched_barrier(0);     // (before the loads: waited for with fewer left)
         step(slot[2 * i % SLOTS], slot[(2 * i + 1) % SLOTS], [&](int k) {
@@ -549,6 +585,8 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
         for (int i = 0; i < NT; ++i)
 #pragma unroll
             for (int j = 0; j < MT; ++j) acc[i][j] = float4v{0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc_last[e] = float4v{0, 0, 0, 0};
         int b = 0;
         for (; b + SLOTS <= count; b += SLOTS)
 #pragma unroll
@@ -561,12 +599,15 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
             for (int k = 0; k < NT; ++k)
 #pragma unroll
                 for (int j = 0; j < MT; ++j) asm volatile("" : "+v"(acc[k][j]));
+#pragma unroll
+            for (int e = 0; e < E; ++e) asm volatile("" : "+v"(acc_last[e]));
             if (b + i < count) block(b + i, i);
         }
         // the next tile's first loads are under way while this one's outputs are stored
         wait_loads<0>();
         __syncthreads();
         const int n0 = (nt0 + wn * NT) * kTile, mt = mt0 + wm * MT, part = split;
+        const bool has_last = MORE && mt0 + TM == a.m_tiles - 1;
         more = next_tile();
         if (more) begin();
         constexpr int kStage = kTile * 16 * NT * 4, kIn = kSlot / kStage;
@@ -580,10 +621,19 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
             if (mt + j >= a.m_tiles) break;
             const int64_t m0 = (int64_t)(mt + j) * kTile;
             if (a.dtype == QLM_F32)
-                store_rows<NT, float>(a, part, m0, n0, v, lds);
+                store_rows<NT, float>(a, part, m0, n0, v, first, lds);
             else
-                store_rows<NT, uint16_t>(a, part, m0, n0, v, lds);
+                store_rows<NT, uint16_t>(a, part, m0, n0, v, first, lds);
         }
+        if constexpr (MORE)
+            if (has_last) {
+                const int64_t m0 = (int64_t)(a.m_tiles - 1) * kTile;
+                const int n_last = n0 + wm * E * kTile;
+                if (a.dtype == QLM_F32)
+                    store_rows<E, float>(a, part, m0, n_last, acc_last, 0, lds);
+                else
+                    store_rows<E, uint16_t>(a, part, m0, n_last, acc_last, 0, lds);
+            }
     }
 }
 
@@ -625,13 +675,14 @@ int check_codes(const qlm_f8_codes *r)
 int64_t part_stride(int n_out) { return ((int64_t)n_out + 3) / 4 * 4; }
 
 // GROUPS: workgroups that a compute unit holds.
-template <int NT, int MT, int WN, int WM, int GROUPS> void launch_wide(MatArgs a, hipStream_t stream)
+template <int NT, int MT, int WN, int WM, int GROUPS, bool MORE = false>
+void launch_wide(MatArgs a, hipStream_t stream)
 {
     a.grid_n = (a.n_tiles + NT * WN - 1) / (NT * WN);
-    a.grid_m = (a.m_tiles + MT * WM - 1) / (MT * WM);
+    a.grid_m = MORE ? a.m_tiles / (MT * WM) : (a.m_tiles + MT * WM - 1) / (MT * WM);
     const int64_t tiles = (int64_t)a.grid_n * a.grid_m * a.splits;
     const int64_t grid = std::min<int64_t>(GROUPS * kCus, (tiles + 7) / 8 * 8);
-    k_f8_wide<NT, MT, WN, WM><<<(unsigned)grid, 64 * WN * WM, 0, stream>>>(a);
+    k_f8_wide<NT, MT, WN, WM, MORE><<<(unsigned)grid, 64 * WN * WM, 0, stream>>>(a);
 }
 
 int64_t thin_groups(const MatArgs &a)
@@ -678,6 +729,8 @@ hipError_t launch(MatArgs a, const Plan &p, void *ws, hipStream_t stream)
         launch_wide<2, 2, 2, 2, 3>(o, stream);
     else if (p.side == 128)
         launch_wide<4, 2, 2, 4, 2>(o, stream);
+    else if (p.one_more)
+        launch_wide<8, 4, 2, 4, 1, true>(o, stream);
     else
         launch_wide<8, 4, 2, 4, 1>(o, stream);
     const hipError_t e = hipGetLastError();

@@ -44,6 +44,7 @@ inline Thin thin_of(int64_t n_tiles, int64_t m_tiles, int blocks)
 struct Plan {
     int side, splits, per_split;
     double us;                   // the estimate
+    bool one_more;               // tiles of 256 take a last tile of 16 rows with them
 };
 
 // The form of the least estimated time.  Measured on an MI355X (us; memory 5.1 TB/s, launches of
@@ -53,7 +54,8 @@ struct Plan {
 //           workgroups
 //   tiles   a block of inputs takes a compute unit 0.19 for a tile of 64 x 64 (0.3 for one alone),
 //           0.48 of 128 x 128 (0.56 alone, 0.40 for one of two), 1.5 of 256 x 256, a tile of which
-//           takes 3 to begin and end; then the outputs are written
+//           takes 3 to begin and end; 1.65 and 6 of 256 with a last tile of 16 rows beside it
+//           (one_more); then the outputs are written
 // so (rows x outputs x inputs, thin / 64 / 128 / 256):
 //     128 x  4096 x 4096     8.6 /  13.3 /  16.2 /  49
 //     256 x  4096 x 4096    12.3 /  13.4 /  18   /  49
@@ -74,7 +76,7 @@ inline Plan form_of(int n_out, int n_in, int n_rows, int most_splits = 16)
     const int64_t n_tiles = ((int64_t)n_out + kTile - 1) / kTile;
     const int64_t m_tiles = ((int64_t)n_rows + kTile - 1) / kTile;
     const double tile = (double)kBlock * kTile * blocks;        // bytes of a tile of 16 rows
-    Plan best{0, 1, blocks, 1e30};
+    Plan best{0, 1, blocks, 1e30, false};
     if (n_rows <= kThinRows) {
         const Thin thin = thin_of(n_tiles, m_tiles, blocks);
         const double groups = (double)((m_tiles + thin.rows - 1) / thin.rows);
@@ -92,25 +94,29 @@ inline Plan form_of(int n_out, int n_in, int n_rows, int most_splits = 16)
     for (auto f : forms) {
         // (offsets of 32 bits into a workgroup's tiles)
         if (tile * (f.side / kTile) >= 2147483648.0) continue;
+        const bool one_more = f.side == 256 && m_tiles > 16 && m_tiles % 16 == 1;
         const double tiles = (double)((n_out + (int64_t)f.side - 1) / f.side) *
-                             (double)((n_rows + (int64_t)f.side - 1) / f.side);
+                             (double)((n_rows + (int64_t)f.side - 1) / f.side - one_more);
         for (int s = 1; s <= most_splits; s *= 2) {
             const int per = (blocks + s - 1) / s;
             if (s > 1 && per < 4) break;
             const int runs = (blocks + per - 1) / per;
             const double turns = (double)(int64_t)((tiles * runs + kCus - 1) / kCus);
-            const double cost = turns * (turns <= 1 ? f.one : turns <= 2 ? f.two : f.more);
-            double t = 6.0 + std::max(per * cost + (f.side == 256 ? 3.0 * turns : 0.0) + out, (n_tiles + m_tiles) * tile / 5.1e6);
+            const double cost =
+                turns * (one_more ? 1.65 : turns <= 1 ? f.one : turns <= 2 ? f.two : f.more);
+            const double ends = f.side < 256 ? 0.0 : one_more ? 6.0 : 3.0;
+            double t = 6.0 + std::max(per * cost + ends * turns + out,
+                                      (n_tiles + m_tiles) * tile / 5.1e6);
             if (runs > 1) t += 4.0 + (runs + 0.5) * 4.0 * n_out * (double)n_rows / 5.1e6;
-            if (t < best.us) best = {f.side, runs, per, t};
+            if (t < best.us) best = {f.side, runs, per, t, one_more};
         }
     }
     return best;
 }
 
 // The rows in two parts where that is less, the first of whole tiles of 256: a last tile of a few
-// rows takes as long as a whole one.  777 x 20001 x 5000 as a whole 113 us, as 768 rows and 9
-// 97.
+// rows takes as long as a whole one.  800 x 20000 x 5000 as a whole 110 us, as 768 rows and 32
+// 91.
 struct Parts {
     int n_first;                 // rows of the first part
     Plan first, rest;            // (rest: of no rows where n_first is all of them)

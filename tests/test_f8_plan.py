@@ -17,6 +17,8 @@ extern "C" void parts(int n_out, int n_in, int rows, int *got)
     const Parts p = parts_of(n_out, n_in, rows);
     const int all[] = {p.n_first, p.first.side, p.first.splits, p.first.per_split,
                        p.rest.side, p.rest.splits, p.rest.per_split};
+    const int more[] = {p.first.one_more, p.rest.one_more};
+    for (int i = 0; i < 2; ++i) got[7 + i] = more[i];
     for (int i = 0; i < 7; ++i) got[i] = all[i];
 }
 extern "C" void thin(int n_out, int n_in, int rows, int *got)
@@ -38,11 +40,12 @@ def parts(tmp_path_factory):
                     str(d / "plan.cpp")], check=True)
     lib = ctypes.CDLL(lib)
 
-    def call(rows, n_out, n_in, what=lib.parts):
-        got = (ctypes.c_int * 7)()
+    def call(rows, n_out, n_in, what=lib.parts, n=7):
+        got = (ctypes.c_int * 9)()
         what(n_out, n_in, rows, got)
-        return list(got)
+        return list(got)[:n]
 
+    call.more = lambda *sizes: call(*sizes, n=9)[7:]     # a last tile of rows taken along
     call.thin = lambda *sizes: tuple(call(*sizes, what=lib.thin)[:2])
     return call
 
@@ -55,6 +58,11 @@ def test_everything_is_taken_once(parts):
                 n_first, *forms = parts(rows, n_out, n_in)
                 split = n_first < rows
                 assert 0 < n_first <= rows
+                # a last tile that is taken along is one behind whole tiles of 256
+                for more, r, side in zip(parts.more(rows, n_out, n_in),
+                                         (n_first, rows - n_first if split else rows),
+                                         (forms[0], forms[3])):
+                    assert not more or (side == 256 and r > 256 and -(-r // 16) % 16 == 1)
                 # the second part starts with a tile of rows, and has no runs whose sums need room
                 assert not split or (n_first % 256 == 0 and forms[1] == 1 and forms[4] == 1)
                 for side, splits, per in (forms[:3], forms[3:])[:1 + split]:
@@ -74,12 +82,13 @@ def test_sizes_of_the_gpu_tests_reach_every_form(parts):
     for m, n, k in FORMS + SIZES:
         n_first, *forms = parts(m, n, k)
         seen.add((forms[0], forms[1] > 1, n_first < m))
+        seen.add(("more", parts.more(m, n, k)[0], forms[1] > 1))
         if n_first < m:
             seen.add(("rest", forms[3]))
         elif forms[0] == 0:
             seen.add(("thin", *parts.thin(m, n, k)))
     want = {(0, False, False), (64, False, False), (64, True, False), (128, False, False),
             (128, True, False), (256, False, False), (256, False, True), (128, False, True),
-            (64, False, True), ("rest", 0), ("rest", 64)}
+            (64, False, True), ("rest", 0), ("rest", 64), ("more", 1, False), ("more", 1, True)}
     want |= {("thin", *t) for t in ((1, 1), (1, 2), (2, 2), (2, 3), (2, 4), (4, 2))}
     assert want <= seen, want - seen

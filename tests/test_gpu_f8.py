@@ -173,7 +173,8 @@ FORMS = [(33, 131, 146), (203, 323, 118), (580, 442, 131), (132, 3022, 147), (40
          (300, 1647, 109), (679, 175, 962), (165, 704, 100), (802, 102, 2575), (2306, 855, 1343),
          (714, 2709, 108), (770, 271, 3944), (466, 505, 13323), (4105, 906, 1175),
          (1220, 6878, 5131), (1808, 6603, 903), (2216, 5381, 103), (3079, 5296, 923),
-         (291, 183, 35508), (4200, 4096, 256), (96, 4096, 5300), (2050, 2050, 130)]
+         (291, 183, 35508), (4200, 4096, 256), (96, 4096, 5300), (2050, 2050, 130),
+         (1025, 16377, 1500), (1040, 16384, 1500), (517, 8190, 9000)]
 
 
 @pytest.mark.parametrize("dtype", ["float16", "float32"])
@@ -241,6 +242,41 @@ def test_not_a_numbers(torch, qlm, m, n):
     assert torch.equal(got.isnan(), bad)
     e = (got.double() - exact).abs()
     assert bool((e <= bound(torch, exact, size, k, torch.float32))[~bad].all())
+
+
+# (few rows behind whole tiles of 256: those that take them along, one and several to a workgroup)
+@pytest.mark.parametrize("m,n,k", [(1025, 16377, 1500), (1030, 16377, 1500), (517, 8190, 9000),
+                                   (520, 60001, 1500)])
+@pytest.mark.parametrize("dtype", ["float16", "float32"])
+def test_last_rows_of_many(torch, qlm, m, n, k, dtype):
+    """The rows behind the last whole tile as in a call of their own, between other columns, with a
+    code that is none in them and in the last output; rounding of sums in another order apart."""
+    dt = getattr(torch, dtype)
+    _, _, _, (x, w) = product(torch, qlm, 17, n, k, torch.float32, spread=0.1)
+    torch.manual_seed(m)
+    rows = (torch.randn((m, k), device="cuda") * 0.01).bfloat16()
+    whole = m // 256 * 256
+    rows[m - 1, 5] = float("nan")
+    blocks = -(-k // 128)
+    w.packed[(((n - 1) // 16 * blocks + 1) * 2048 + 3 * 256 + (n - 1) % 16 * 16 + 2)] = 0x7f
+    big = torch.full((m + 1, n + 24), -5.0, dtype=dt, device="cuda")
+    out = big[:m, 8:8 + n]
+    qlm.f8_matmul(qlm.f8_rows(rows), w, out=out)
+    few = qlm.f8_matmul(qlm.f8_rows(rows[whole:]), w, dtype=torch.float32).double()
+    other = qlm.f8_matmul(qlm.f8_rows(rows[:40]), w, dtype=torch.float32).double()
+    for got, want in ((out[whole:], few), (out[:40], other)):
+        bad = want.isnan()
+        assert torch.equal(got.isnan(), bad) and bool(bad[:, n - 1].all())
+        assert bool(bad[-1].all()) == (want is few) and not bool(bad[:-1, :-1].any())
+        # sums over the blocks in another order: each of `blocks` additions rounds by 2^-24 of a
+        # sum that stays within a few times the outputs' size, then the type's half step
+        size = float(want.nan_to_num().abs().max())
+        lim = 2 * blocks * 2.0 ** -24 * 4 * size
+        half = torch.finfo(dt).eps / 2
+        e = (got.double() - want).abs()[~bad]
+        assert bool((e <= lim + half * (want.abs()[~bad] + lim) + 2.0 ** -25).all())
+    big[:m, 8:8 + n] = -5.0
+    assert bool((big == -5.0).all())
 
 
 def test_scales_of_any_size(torch, qlm):
