@@ -975,9 +975,11 @@ def kv_append_rotated(cache: DeviceKvCache, batch: KvBatch, k, v, q, rotary: Rot
             import torch
             make = lambda: torch.empty_like(q, memory_format=torch.contiguous_format)  # noqa: E731
             out = make() if stream is None else _allocated(stream, make)
+            ro = (out.data_ptr(), heads * dim, dim, rq[3])
         elif out.shape != q.shape or out.dtype != q.dtype:
             raise ValueError("out must have q's shape and type")
-        ro = _rows(out, n, heads, dim, "out")
+        else:
+            ro = _rows(out, n, heads, dim, "out")
         here = here and q.get_device() == index == out.get_device()
     elif out is not None:
         raise ValueError("out is of queries, and there are none")
@@ -1196,15 +1198,15 @@ class F8Rows:
         """Room for so many rows, as a call on `stream` allocates it."""
         import torch
         tiles, blocks = -(-n_rows // F8_TILE), -(-n_in // F8_BLOCK)
-        codes = lambda: torch.empty((tiles, blocks, 8, F8_TILE, 16),  # noqa: E731
-                                    dtype=torch.float8_e4m3fn, device=device)
-        scale = lambda: torch.empty((blocks, tiles * F8_TILE), dtype=torch.float32,  # noqa: E731
-                                    device=device)
-        rows = cls.__new__(cls)
+        kind, at, by = torch.float8_e4m3fn, (tiles, blocks, 8, F8_TILE, 16), (blocks, tiles * F8_TILE)
         if stream is None:
-            rows._hold(codes(), scale(), n_rows, n_in)
+            codes = torch.empty(at, dtype=kind, device=device)
+            scale = torch.empty(by, dtype=torch.float32, device=device)
         else:
-            rows._hold(_allocated(stream, codes), _allocated(stream, scale), n_rows, n_in)
+            codes = _allocated(stream, lambda: torch.empty(at, dtype=kind, device=device))
+            scale = _allocated(stream, lambda: torch.empty(by, dtype=torch.float32, device=device))
+        rows = cls.__new__(cls)
+        rows._hold(codes, scale, n_rows, n_in)
         return rows
 
 
@@ -1278,13 +1280,17 @@ def f8_matmul(x: F8Rows, weight: F8, out=None, dtype=None, ws=None, stream=None)
     n = x.n_rows
     if out is None:
         dtype = torch.bfloat16 if dtype is None else dtype
-        _word_type(dtype, "dtype")
-        out = _allocated(stream, lambda: torch.empty((n, weight.n_out), dtype=dtype,
-                                                     device=x.codes.device))
+        kind = _word_type(dtype, "dtype")
+        shape, dev = (n, weight.n_out), x.codes.device
+        if stream is None:
+            out = torch.empty(shape, dtype=dtype, device=dev)
+        else:
+            out = _allocated(stream, lambda: torch.empty(shape, dtype=dtype, device=dev))
     elif tuple(out.shape) != (n, weight.n_out) or (dtype is not None and out.dtype != dtype) or \
             (out.stride(1) != 1 and weight.n_out > 1):
         raise ValueError("out must be [%d, %d] with contiguous rows" % (n, weight.n_out))
-    kind = _word_type(out.dtype, "out")
+    else:
+        kind = _word_type(out.dtype, "out")
     if ws is None:
         ws = _allocated(stream, lambda: f8_workspace(weight, n), False)
     if not 0 <= weight.index == x.index == out.get_device() == ws.get_device():
