@@ -1079,8 +1079,8 @@ template <int FMT> void launch_move(const EvictArgs &a, int waves, unsigned grid
 int move_waves(int max_length, int budget)
 {
     // two waves to a block where at most a quarter of its slots can fall free (4 of
-    // 64, 8192 blocks: 31 us, four waves 36), four where more can (48 of 64, 3072
-    // blocks: 48 us, two waves 62)
+    // 64, 8192 blocks: 31 us, four waves 36), four where more can (48 of 64: 48 us,
+    // two waves 62)
     return max_length - budget <= budget / 4 ? 2 : 4;
 }
 
