@@ -243,6 +243,46 @@ __device__ inline float bits_value(uint32_t u, int dtype)
     return (float)__builtin_bit_cast(_Float16, (uint16_t)u);
 }
 
+// Eight pairs, of which the first `have` turn; whole: all of them.
+template <bool NEIGHBOURS>
+__device__ inline void turn16(float *y, const float *c, const float *s, int have, bool whole)
+{
+    if (whole) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            turn(y[NEIGHBOURS ? 2 * e : e], y[NEIGHBOURS ? 2 * e + 1 : e + 8], c[e], s[e]);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < have) turn(y[NEIGHBOURS ? 2 * e : e], y[NEIGHBOURS ? 2 * e + 1 : e + 8], c[e], s[e]);
+}
+
+// N dims' values.  (A branch for all of them: as a choice at each one it was three operations.)
+template <int N> __device__ inline void values_of(const uint32_t *w, int dtype, float *y)
+{
+    if (dtype == QLM_BF16) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] = bits_value((w[i >> 1] >> (16 * (i & 1))) & 0xffff, QLM_BF16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] = bits_value((w[i >> 1] >> (16 * (i & 1))) & 0xffff, QLM_F16);
+    }
+}
+
+template <int N> __device__ inline void bits_of(const float *y, int dtype, uint32_t *w)
+{
+    if (dtype == QLM_BF16) {
+#pragma unroll
+        for (int i = 0; i < N; i += 2)
+            w[i / 2] = row_bits(y[i], QLM_BF16) | (uint32_t)row_bits(y[i + 1], QLM_BF16) << 16;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 2)
+            w[i / 2] = row_bits(y[i], QLM_F16) | (uint32_t)row_bits(y[i + 1], QLM_F16) << 16;
+    }
+}
+
 // The greatest finite magnitude of eight dims, as bits (magnitudes order as integers).
 __device__ inline uint32_t magnitude8(uint4 x, int dtype)
 {
@@ -296,20 +336,12 @@ __device__ inline void turned16(const TurnArgs &t, int n_rows, int row, int own,
                                 int64_t at, int k, uint4 lo, uint4 hi, int dtype, float *y)
 {
     const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-#pragma unroll
-    for (int e = 0; e < 16; ++e) y[e] = bits_value((w[e >> 1] >> (16 * (e & 1))) & 0xffff, dtype);
+    values_of<16>(w, dtype, y);
     if (NEIGHBOURS || t.half % 8 == 0) {
         if (8 * k >= t.half) return;
         float c[8], s[8];
         angles<8>(t, n_rows, row, own, 8 * k, c, s);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (8 * k + e < t.half) {
-                if (NEIGHBOURS)
-                    turn(y[2 * e], y[2 * e + 1], c[e], s[e]);
-                else
-                    turn(y[e], y[e + 8], c[e], s[e]);
-            }
+        turn16<NEIGHBOURS>(y, c, s, t.half - 8 * k, t.half % 8 == 0);
         return;
     }
 #pragma unroll 1
@@ -333,8 +365,7 @@ template <int FMT> __device__ inline uint2 codes8(uint4 x, int dtype, float scal
 {
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
     float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = bits_value((w[i >> 1] >> (16 * (i & 1))) & 0xffff, dtype);
+    values_of<8>(w, dtype, v);
     return codes_of<FMT>(v, scale, exact);
 }
 
@@ -479,9 +510,15 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
         if (o >= o0 && o < o1) {
             if (!TURN) *to = codes8<FMT>(kx[p], a.k_type, newk, exk);
             const uint2 c = codes8<FMT>(vx[p], a.v_type, newv, exv);
-            uint8_t *at = few ? vc + (value_group(o) * D + d) * 16 + value_place(o)
-                              : vl + (value_group(o) * DP + d) * 16 + value_place(o);
-            for (int e = 0; e < 8; ++e) at[16 * e] = (uint8_t)((e < 4 ? c.x : c.y) >> (8 * (e & 3)));
+            // (in branches of their own: an address in either memory takes the slower stores)
+            auto spread = [&](uint8_t *at) {
+                for (int e = 0; e < 8; ++e)
+                    at[16 * e] = (uint8_t)((e < 4 ? c.x : c.y) >> (8 * (e & 3)));
+            };
+            if (few)
+                spread(vc + (value_group(o) * D + d) * 16 + value_place(o));
+            else
+                spread(vl + (value_group(o) * DP + d) * 16 + value_place(o));
         } else if (growk) {
             const uint2 w = *to;
             *to = uint2{requant4<FMT>(w.x, oldk / newk), requant4<FMT>(w.y, oldk / newk)};
@@ -600,9 +637,7 @@ __device__ inline void turn_queries(const AppendArgs &a, const TurnArgs &t, uint
         if (t.q_wide) {
             const uint32_t w[8] = {lo[r].x, lo[r].y, lo[r].z, lo[r].w,
                                    hi[r].x, hi[r].y, hi[r].z, hi[r].w};
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                x[e] = bits_value((w[e >> 1] >> (16 * (e & 1))) & 0xffff, t.q_type);
+            values_of<16>(w, t.q_type, x);
         } else {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
@@ -610,22 +645,11 @@ __device__ inline void turn_queries(const AppendArgs &a, const TurnArgs &t, uint
                 x[e] = i < (e < 8 ? n0 : n1) ? bits_value(q_bits(t, from + d + i), t.q_type) : 0.f;
             }
         }
-        if (pairs)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (8 * k + e < half) {
-                    if (NEIGHBOURS)
-                        turn(x[2 * e], x[2 * e + 1], c[e], s8[e]);
-                    else
-                        turn(x[e], x[e + 8], c[e], s8[e]);
-                }
+        if (pairs) turn16<NEIGHBOURS>(x, c, s8, half - 8 * k, half % 8 == 0);
         uint16_t *out = (uint16_t *)t.q_out + row * t.out_row + (h0 + r) * t.out_head;
         if (t.q_wide) {
             uint32_t w[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                w[e] = row_bits(x[2 * e], t.q_type) |
-                       (uint32_t)row_bits(x[2 * e + 1], t.q_type) << 16;
+            bits_of<16>(x, t.q_type, w);
             *(uint4 *)(out + d0) = uint4{w[0], w[1], w[2], w[3]};
             *(uint4 *)(out + d1) = uint4{w[4], w[5], w[6], w[7]};
             continue;
