@@ -181,31 +181,57 @@ __device__ inline int64_t table_at(const TurnArgs &t, int n_rows, int row, int o
     return (int64_t)max(0, min(p, t.n_positions - 1)) * t.half + i;
 }
 
-// cos and sin of N pairs from i on, of which those from `half` on are not read (1 and 0).  Four
-// neighbouring pairs nearly always turn by one position: their numbers stand side by side.
-template <int N>
-__device__ inline void angles(const TurnArgs &t, int n_rows, int row, int own, int i, float *c,
-                              float *s)
+// The axes of a unit's pairs, four and four.  Four neighbouring pairs nearly always turn by one position:
+// their angles then stand side by side, and the positions are under way beside the rows.
+struct Axes {
+    int axis[2];
+    bool one[2];                    // four that are read at once, by one position
+};
+
+__device__ inline Axes axes_of(const TurnArgs &t, int i)
+{
+    Axes r;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+        r.axis[g] = 0;
+        r.one[g] = t.table_wide && i + 4 * g + 4 <= t.half;
+        if (t.axis && r.one[g]) {
+            const int4 ax = *(const int4 *)(t.axis + i + 4 * g);
+            r.one[g] = ax.x == ax.y && ax.x == ax.z && ax.x == ax.w;
+            r.axis[g] = max(0, min(ax.x, t.n_axes - 1));
+        }
+    }
+    return r;
+}
+
+// The positions of a row that is given them, for each four.
+__device__ inline int2 positions_of(const TurnArgs &t, int n_rows, int64_t row, const Axes &x)
+{
+    if (!t.axis) {
+        const int p = t.position[row];
+        return {p, p};
+    }
+    return {t.position[(int64_t)x.axis[0] * n_rows + row],
+            t.position[(int64_t)x.axis[1] * n_rows + row]};
+}
+
+// cos and sin of eight pairs from i on, of which those from `half` on are not read (1 and 0).
+__device__ inline void angles(const TurnArgs &t, int n_rows, int row, int2 own, const Axes &x, int i,
+                              float *c, float *s)
 {
 #pragma unroll
-    for (int e0 = 0; e0 < N; e0 += 4) {
-        if (t.table_wide && i + e0 + 4 <= t.half) {
-            bool one = true;
-            if (t.axis) {
-                const int4 ax = *(const int4 *)(t.axis + i + e0);
-                one = ax.x == ax.y && ax.x == ax.z && ax.x == ax.w;
-            }
-            if (one) {
-                const int64_t at = table_at(t, n_rows, row, own, i + e0);
-                *(float4v *)(c + e0) = *(const float4v *)(t.cos + at);
-                *(float4v *)(s + e0) = *(const float4v *)(t.sin + at);
-                continue;
-            }
+    for (int g = 0; g < 2; ++g) {
+        const int p = g ? own.y : own.x, e0 = 4 * g;
+        if (x.one[g]) {
+            const int64_t at = (int64_t)max(0, min(p, t.n_positions - 1)) * t.half + i + e0;
+            *(float4v *)(c + e0) = *(const float4v *)(t.cos + at);
+            *(float4v *)(s + e0) = *(const float4v *)(t.sin + at);
+            continue;
         }
 #pragma unroll
         for (int e = e0; e < e0 + 4; ++e) {
             const bool in = i + e < t.half;
-            const int64_t at = table_at(t, n_rows, row, own, in ? i + e : 0);
+            const int64_t at = table_at(t, n_rows, row, p, in ? i + e : 0);
             c[e] = in ? t.cos[at] : 1.f;
             s[e] = in ? t.sin[at] : 0.f;
         }
@@ -332,15 +358,16 @@ __device__ inline void unit_dims(const TurnArgs &t, bool neighbours, int k, int 
 
 // A unit's dims, turned; lo, hi: the dims as they are, `at`: of the head's dim 0.
 template <bool NEIGHBOURS>
-__device__ inline void turned16(const TurnArgs &t, int n_rows, int row, int own, const void *data,
-                                int64_t at, int k, uint4 lo, uint4 hi, int dtype, float *y)
+__device__ inline void turned16(const TurnArgs &t, int n_rows, int row, int2 own, const Axes &axes,
+                                const void *data, int64_t at, int k, uint4 lo, uint4 hi, int dtype,
+                                float *y)
 {
     const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
     values_of<16>(w, dtype, y);
     if (NEIGHBOURS || t.half % 8 == 0) {
         if (8 * k >= t.half) return;
         float c[8], s[8];
-        angles<8>(t, n_rows, row, own, 8 * k, c, s);
+        angles(t, n_rows, row, own, axes, 8 * k, c, s);
         turn16<NEIGHBOURS>(y, c, s, t.half - 8 * k, t.half % 8 == 0);
         return;
     }
@@ -350,7 +377,7 @@ __device__ inline void turned16(const TurnArgs &t, int n_rows, int row, int own,
         if (dim >= 2 * t.half) break;
         const bool low = dim < t.half;
         const int i = low ? dim : dim - t.half;
-        const int64_t p = table_at(t, n_rows, row, own, i);
+        const int64_t p = table_at(t, n_rows, row, own.x, i);
         const uint16_t *x = (const uint16_t *)data + at;
         float p0 = bits_value(x[i], dtype), p1 = bits_value(x[i + t.half], dtype);
         turn(p0, p1, t.cos[p], t.sin[p]);
@@ -417,6 +444,9 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
     __shared__ uint4 vl4[4 * DP];
     const int t = threadIdx.x;
     const uint32_t bt = blockIdx.x / (uint32_t)a.c.H, h = blockIdx.x % (uint32_t)a.c.H;
+    const int unit_in = min(t % (CH / 2), a.c.D / 16 - 1);
+    Axes axes = {};
+    if (TURN) axes = axes_of(turned, 8 * unit_in);
     const int tb = (int)(bt % (uint32_t)a.touched), s = (int)(bt / (uint32_t)a.touched);
     int row0;
     const int n = seq_rows(a.q, s, &row0);
@@ -448,8 +478,8 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
         if (!TURN) kx[p] = row_bits8(a.k, (int64_t)h * a.k_head + r * a.k_row + dd, a.k_wide);
         vx[p] = row_bits8(a.v, (int64_t)h * a.v_head + r * a.v_row + dd, a.v_wide);
     }
-    int ud0 = 0, ud1 = 0, own[TURN ? UPASS : 1];
-    const int unit_in = min(unit, D / 16 - 1);
+    int ud0 = 0, ud1 = 0;
+    int2 own[TURN ? UPASS : 1];
     if (TURN) {
         const int64_t own0 = a.first ? a.first[s] : start;
         unit_dims(turned, TURN == 2, unit_in, &ud0, &ud1);
@@ -457,7 +487,10 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
         for (int p = 0; p < UPASS; ++p) {
             const int64_t r = r0 + min(max(uslot0 + p * UROWS, o0), o1 - 1) - o0;
             const int64_t at = (int64_t)h * a.k_head + r * a.k_row;
-            own[p] = turned.position ? turned.position[r] : position_of(own0, r - row0);
+            if (turned.position)
+                own[p] = positions_of(turned, a.q.n_rows, r, axes);
+            else
+                own[p].x = own[p].y = position_of(own0, r - row0);
             kx[2 * p] = row_bits8(a.k, at + ud0, a.k_wide);
             kx[2 * p + 1] = row_bits8(a.k, at + ud1, a.k_wide);
         }
@@ -471,7 +504,7 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
 #pragma unroll
         for (int p = 0; p < UPASS; ++p) {
             const int64_t r = r0 + min(max(uslot0 + p * UROWS, o0), o1 - 1) - o0;
-            turned16<TURN == 2>(turned, a.q.n_rows, (int)r, own[p], a.k,
+            turned16<TURN == 2>(turned, a.q.n_rows, (int)r, own[p], axes, a.k,
                                 (int64_t)h * a.k_head + r * a.k_row, unit_in, kx[2 * p],
                                 kx[2 * p + 1], a.k_type, ky[p]);
         }
@@ -612,6 +645,8 @@ __device__ inline void turn_queries(const AppendArgs &a, const TurnArgs &t, uint
         n0 = min(8, D - d0);
         n1 = max(0, min(8, D - d1));
     }
+    Axes axes = {};
+    if (pairs) axes = axes_of(t, 8 * k);
     uint4 lo[HEADS], hi[HEADS];
     if (t.q_wide)
 #pragma unroll
@@ -620,15 +655,18 @@ __device__ inline void turn_queries(const AppendArgs &a, const TurnArgs &t, uint
             lo[r] = row_bits8(t.q, from + d0, true);
             hi[r] = row_bits8(t.q, from + d1, true);
         }
-    int own = t.position ? t.position[row] : 0, place;
+    int2 own = {0, 0};
+    if (t.position) own = positions_of(t, a.q.n_rows, row, axes);
+    int place;
     const int s = row_seq(a.q, row, &place);
     if (s < 0) return;
     if (!t.position) {
         int row0;
-        own = position_of(a.first ? a.first[s] : seq_length(a.q, s) - seq_rows(a.q, s, &row0), place);
+        own.x = own.y =
+            position_of(a.first ? a.first[s] : seq_length(a.q, s) - seq_rows(a.q, s, &row0), place);
     }
     float c[8], s8[8];
-    if (pairs) angles<8>(t, a.q.n_rows, row, own, 8 * k, c, s8);
+    if (pairs) angles(t, a.q.n_rows, row, own, axes, 8 * k, c, s8);
 #pragma unroll
     for (int r = 0; r < HEADS; ++r) {
         if (h0 + r >= t.n_heads) return;
