@@ -428,8 +428,42 @@ __device__ inline int row_seq(const Seqs &q, int row, int *place)
     return *place >= 0 && *place < min(r1 - r0, q.max_new) ? s : -1;
 }
 
+// Where the 16 bytes of a group's dim stand in shared memory, and their word of 4 of slots: moved so that
+// eight dims apart and the four groups meet in no bank.
+__device__ inline int staged_unit(int u) { return u ^ ((u >> 3) & 15); }
+
+// Eight dims from d on of G neighbouring slots, whose codes are c, as bytes side by side for each dim.
+template <int G> __device__ inline void stage(uint8_t *to, int group, int dp, int d, int place, const uint2 *c)
+{
+    const int word = ((place >> 2) + group) & 3;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        auto part = [&](int i) { return half ? c[i].y : c[i].x; };
+        // bytes 0 and 1 of two slots, then 2 and 3
+        const uint32_t lo = __builtin_amdgcn_perm(part(1), part(0), 0x05010400);
+        const uint32_t hi = __builtin_amdgcn_perm(part(1), part(0), 0x07030602);
+        uint32_t w[4] = {lo, lo >> 16, hi, hi >> 16};
+        if constexpr (G == 4) {
+            const uint32_t lo2 = __builtin_amdgcn_perm(part(3), part(2), 0x05010400);
+            const uint32_t hi2 = __builtin_amdgcn_perm(part(3), part(2), 0x07030602);
+            w[0] = __builtin_amdgcn_perm(lo2, lo, 0x05040100);
+            w[1] = __builtin_amdgcn_perm(lo2, lo, 0x07060302);
+            w[2] = __builtin_amdgcn_perm(hi2, hi, 0x05040100);
+            w[3] = __builtin_amdgcn_perm(hi2, hi, 0x07060302);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint8_t *at = to + 16 * staged_unit(group * dp + d + 4 * half + e) + 4 * word;
+            if constexpr (G == 4)
+                *(uint32_t *)at = w[e];
+            else
+                *(uint16_t *)(at + (place & 3)) = (uint16_t)w[e];
+        }
+    }
+}
+
 // One workgroup for each (sequence, block that takes new slots, kv head).  A
-// thread holds eight dims of every (32 / ND)-th slot: read once, for the largest magnitude,
+// thread holds eight dims of runs of 4 (ND = 1: 2) slots: read once, for the largest magnitude,
 // then written as codes; values pass through shared memory into their order, and
 // the groups of slots that take any are read and written whole.
 // One token for each of 64 sequences (8 heads of 128): 7 us, a launch and its chain of
@@ -463,6 +497,9 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
     const bool fresh = o0 == 0;
     const int d = 8 * (t % CH), slot0 = t / CH;
     const bool in_d = d < D;
+    // a thread's slots: runs of G, whose bytes of a dim stand side by side in the values
+    constexpr int G = PASS < 4 ? PASS : 4;
+    auto slot_of = [&](int p) { return p / G * (ROWS * G) + slot0 * G + p % G; };
     uint4 kx[PASS], vx[PASS];
     // keys that are turned are held by units of 16 dims, twice as many slots at a time
     constexpr int UROWS = 2 * ROWS, UPASS = PASS / 2;
@@ -473,7 +510,7 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
     for (int p = 0; p < PASS; ++p) {
         // (a slot or dim that is not new is read as one that is: neither counts nor is
         // written)
-        const int64_t r = r0 + min(max(slot0 + p * ROWS, o0), o1 - 1) - o0;
+        const int64_t r = r0 + min(max(slot_of(p), o0), o1 - 1) - o0;
         const int dd = min(d, D - 8);
         if (!TURN) kx[p] = row_bits8(a.k, (int64_t)h * a.k_head + r * a.k_row + dd, a.k_wide);
         vx[p] = row_bits8(a.v, (int64_t)h * a.v_head + r * a.v_row + dd, a.v_wide);
@@ -536,26 +573,30 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
     // (a decode step's one token: as bytes, without reading the group they stand in)
     const bool few = o1 - o0 == 1 && !growv;
 #pragma unroll
-    for (int p = 0; p < PASS; ++p) {
-        const int o = slot0 + p * ROWS;
+    for (int p0 = 0; p0 < PASS; p0 += G) {
         if (!in_d) continue;
-        uint2 *to = (uint2 *)(kc + o * D + d);
-        if (o >= o0 && o < o1) {
-            if (!TURN) *to = codes8<FMT>(kx[p], a.k_type, newk, exk);
-            const uint2 c = codes8<FMT>(vx[p], a.v_type, newv, exv);
-            // (in branches of their own: an address in either memory takes the slower stores)
-            auto spread = [&](uint8_t *at) {
+        uint2 c[G];
+        // (slots beside the new ones are staged too, and not taken)
+        const int o = slot_of(p0);
+        const bool staged = !few && o < o1 && o + G > o0;
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            const int o = slot_of(p0 + i);
+            const bool in = o >= o0 && o < o1;
+            uint2 *to = (uint2 *)(kc + o * D + d);
+            if (in || staged) c[i] = codes8<FMT>(vx[p0 + i], a.v_type, newv, exv);
+            if (!TURN && in) *to = codes8<FMT>(kx[p0 + i], a.k_type, newk, exk);
+            if (!in && growk) {
+                const uint2 w = *to;
+                *to = uint2{requant4<FMT>(w.x, oldk / newk), requant4<FMT>(w.y, oldk / newk)};
+            }
+            if (in && few) {
+                uint8_t *at = vc + (value_group(o) * D + d) * 16 + value_place(o);
                 for (int e = 0; e < 8; ++e)
-                    at[16 * e] = (uint8_t)((e < 4 ? c.x : c.y) >> (8 * (e & 3)));
-            };
-            if (few)
-                spread(vc + (value_group(o) * D + d) * 16 + value_place(o));
-            else
-                spread(vl + (value_group(o) * DP + d) * 16 + value_place(o));
-        } else if (growk) {
-            const uint2 w = *to;
-            *to = uint2{requant4<FMT>(w.x, oldk / newk), requant4<FMT>(w.y, oldk / newk)};
+                    at[16 * e] = (uint8_t)((e < 4 ? c[i].x : c[i].y) >> (8 * (e & 3)));
+            }
         }
+        if (staged) stage<G>(vl, value_group(o), DP, d, value_place(o), c);
     }
     if (TURN)
 #pragma unroll
@@ -586,7 +627,9 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
         }
         if (!any && !growv) continue;
         uint4 *to = (uint4 *)(vc + (g * D + dim) * 16);
-        uint4 w = vl4[e];
+        uint4 w = vl4[staged_unit(e)];
+        if (g & 1) w = uint4{w.y, w.z, w.w, w.x};
+        if (g & 2) w = uint4{w.z, w.w, w.x, w.y};
         if (!all) {
             const uint4 was = *to;
             uint32_t x[4] = {was.x, was.y, was.z, was.w};
