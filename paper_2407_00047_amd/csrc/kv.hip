@@ -5,6 +5,7 @@
 #include "kv.h"
 
 #include <string>
+#include <type_traits>
 
 namespace qlm_kv {
 
@@ -470,15 +471,17 @@ template <int G> __device__ inline void stage(uint8_t *to, int group, int dp, in
 // thread holds eight dims of runs of 4 (ND = 1: 2) slots: read once, for the largest magnitude,
 // then written as codes; values pass through shared memory into their order, and
 // the groups of slots that take any are read and written whole.
-// One token for each of 64 sequences (8 heads of 128): 7 us, a launch and its chain of
+// ONE: a token a sequence at most, held by a row of threads; the others are there for a block whose
+// scale grows (in workgroups of a wave such a block took three times as long, and 512 sequences without one 13
+// us where this takes 21; with every slot's place held by a thread it was 35).
+// One token for each of 64 sequences (8 heads of 128): 6.1 us, a launch and its chain of
 // dependent reads (length, table, scale, row).  Six ragged prompts of up to 2100 tokens
-// (8 heads of 64, 20 MB): 12.5 us, 1.6 TB/s, the ends of a short launch and the pass
-// through shared memory.
-template <int FMT, int ND, int TURN>   // TURN: 1 halves, 2 neighbours make a pair
+// (8 heads of 64, 20 MB): 12.7 us, 1.6 TB/s, the ends of a short launch.
+template <int FMT, int ND, int TURN, bool ONE>   // TURN: 1 halves, 2 neighbours make a pair
 __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
 {
-    constexpr int DP = 64 * ND, CH = DP / 8, ROWS = kThreads / CH, PASS = kBlock / ROWS;
-    __shared__ float red[2 * kThreads / 64];
+    constexpr int T = kThreads, DP = 64 * ND, CH = DP / 8, ROWS = T / CH, PASS = ONE ? 1 : kBlock / ROWS;
+    __shared__ float red[2 * T / 64];
     __shared__ uint4 vl4[4 * DP];
     const int t = threadIdx.x;
     const uint32_t bt = blockIdx.x / (uint32_t)a.c.H, h = blockIdx.x % (uint32_t)a.c.H;
@@ -505,15 +508,16 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
     // few are new, those that threads side by side hold, so that no thread has many of the new ones
     // (three new tokens of 7 sequences, 4 heads of 80 dims 9.0 us and 9.8 by runs)
     constexpr int G = PASS < 4 ? PASS : 4;
-    const bool many = o1 - o0 > ROWS;
+    const bool many = !ONE && o1 - o0 > ROWS;
     auto slot_of = [&](int p) {
+        if (ONE) return o0 + slot0;            // (of its rows the first is new)
         return many ? p / G * (ROWS * G) + slot0 * G + p % G : p * ROWS + slot0;
     };
-    uint4 kx[PASS], vx[PASS];
+    uint4 kx[ONE ? 2 : PASS], vx[PASS];
     // keys that are turned are held by units of 16 dims, twice as many slots at a time
-    constexpr int UROWS = 2 * ROWS, UPASS = PASS / 2;
-    static_assert(!TURN || PASS % 2 == 0, "units of 16 dims take half the passes");
-    const int unit = t % (CH / 2), uslot0 = t / (CH / 2);
+    constexpr int UROWS = 2 * ROWS, UPASS = ONE ? 1 : PASS / 2;
+    static_assert(!TURN || ONE || PASS % 2 == 0, "units of 16 dims take half the passes");
+    const int unit = t % (CH / 2), uslot0 = (ONE ? o0 : 0) + t / (CH / 2);
     float ky[TURN ? UPASS : 1][16];
 #pragma unroll
     for (int p = 0; p < PASS; ++p) {
@@ -595,7 +599,7 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
             uint2 *to = (uint2 *)(kc + o * D + d);
             if (in || staged) c[i] = codes8<FMT>(vx[p0 + i], a.v_type, newv, exv);
             if (!TURN && in) *to = codes8<FMT>(kx[p0 + i], a.k_type, newk, exk);
-            if (!in && growk) {
+            if (!ONE && !in && growk) {
                 const uint2 w = *to;
                 *to = uint2{requant4<FMT>(w.x, oldk / newk), requant4<FMT>(w.y, oldk / newk)};
             }
@@ -609,8 +613,30 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
                         vl[staged_at(g, DP, d + e, place) + (place & 3)] = byte(e);
             }
         }
-        if (staged) stage<G>(vl, value_group(o), DP, d, value_place(o), c);
+        if constexpr (!ONE)
+            if (staged) stage<G>(vl, value_group(o), DP, d, value_place(o), c);
     }
+    // (a token alone seldom makes a block's scale grow; then all of the block is under way at once)
+    constexpr int SLOTS = ONE ? kBlock / ROWS : 1, N = 4 * DP / T;
+    if (ONE && growk && in_d) {
+        uint2 w[SLOTS];
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) w[k] = *(const uint2 *)(kc + (slot0 + k * ROWS) * D + d);
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) {
+            const int o = slot0 + k * ROWS;
+            if (o == o0) continue;
+            *(uint2 *)(kc + o * D + d) =
+                uint2{requant4<FMT>(w[k].x, oldk / newk), requant4<FMT>(w[k].y, oldk / newk)};
+        }
+    }
+    uint4 held[ONE ? N : 1];
+    if (ONE && !few)
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int e = k * T + t, dim = e % DP;
+            if (dim < D) held[k] = *(const uint4 *)(vc + (e / DP * D + dim) * 16);
+        }
     if (TURN)
 #pragma unroll
         for (int p = 0; p < UPASS; ++p) {
@@ -622,7 +648,7 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
     if (!few) __syncthreads();
     // four dims' 16 bytes at a time: which of a group's places are new
 #pragma unroll
-    for (int e0 = 0; e0 < 4 * DP; e0 += kThreads) {
+    for (int e0 = 0; e0 < 4 * DP; e0 += T) {
         if (few) break;
         const int e = e0 + t, g = e / DP, dim = e % DP;   // (g is uniform over a wave)
         if (dim >= D) continue;
@@ -644,7 +670,7 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
         if (g & 1) w = uint4{w.y, w.z, w.w, w.x};
         if (g & 2) w = uint4{w.z, w.w, w.x, w.y};
         if (!all) {
-            const uint4 was = *to;
+            const uint4 was = ONE ? held[e0 / T] : *to;
             uint32_t x[4] = {was.x, was.y, was.z, was.w};
             const uint32_t y[4] = {w.x, w.y, w.z, w.w};
             for (int q = 0; q < 4; ++q) {
@@ -655,7 +681,7 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
         }
         *to = w;
     }
-    for (int o = o0 + t; o < o1; o += kThreads) {
+    for (int o = o0 + t; o < o1; o += T) {
         if (a.c.pos)
             a.c.pos[bh * kBlock + o] =
                 a.first ? a.first[s] + (j * kBlock + o - start) : j * kBlock + o;
@@ -663,9 +689,9 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
     }
 }
 
-template <int FMT, int ND> __global__ __launch_bounds__(kThreads) void k_append(AppendArgs a)
+template <int FMT, int ND, bool ONE> __global__ __launch_bounds__(kThreads) void k_append(AppendArgs a)
 {
-    append<FMT, ND, 0>(a, TurnArgs{});
+    append<FMT, ND, 0, ONE>(a, TurnArgs{});
 }
 
 // Two bytes of a row of queries.
@@ -760,15 +786,17 @@ constexpr int kTurnHeads = 4;             // heads a thread takes of many rows
 constexpr int64_t kTurnMany = 4096;       // waves of single heads
 
 // The keys' workgroups as in k_append, then for each row those of its queries.  A decode step's one
-// token for each of 64 sequences (32 heads, 8 of keys, 128 dims): 8.6 us where k_append takes 6.8, the
+// token for each of 64 sequences (32 heads, 8 of keys, 128 dims): 7.0 us where k_append takes 6.1, the
 // positions' and the tables' reads in its chain.  Six ragged prompts of up to 2100 tokens on three axes
-// (152 MB): 41 us, 3.7 TB/s; the keys alone 25 (k_append 20), the queries alone 26 (4.4 TB/s).
+// (152 MB): 34.6 us, 4.4 TB/s; calls of the keys alone 21 (k_append 17), of the queries alone 25.  Keys'
+// and queries' workgroups in turn or the queries' first took 10 % longer, five workgroups to a unit 30 %.
 // Angles read for each head and chunk of eight dims: 95.
-template <int FMT, int ND, bool NEIGHBOURS, int HEADS>
-__global__ __launch_bounds__(kThreads, ND <= 2 ? 4 : 2) void k_append_rotated(AppendArgs a, TurnArgs t)
+template <int FMT, int ND, bool NEIGHBOURS, int HEADS, bool ONE>
+__global__ __launch_bounds__(kThreads, ONE || ND <= 2 ? 4 : 2)
+void k_append_rotated(AppendArgs a, TurnArgs t)
 {
     if (blockIdx.x < t.key_groups)
-        append<FMT, ND, NEIGHBOURS ? 2 : 1>(a, t);
+        append<FMT, ND, NEIGHBOURS ? 2 : 1, ONE>(a, t);
     else
         turn_queries<NEIGHBOURS, HEADS>(a, t, blockIdx.x - t.key_groups);
 }
@@ -1257,18 +1285,27 @@ int64_t append_groups(const AppendArgs &a, const qlm_kv_batch *batch)
     return (int64_t)batch->n_seqs * a.touched * a.c.H;
 }
 
-template <int FMT, bool NEIGHBOURS>
+template <int FMT, bool NEIGHBOURS, bool ONE>
 void launch_rotated(const AppendArgs &a, const TurnArgs &t, bool many, int64_t grid,
                     hipStream_t stream)
 {
     constexpr int H = kTurnHeads;
-    auto kern = a.c.D <= 64    ? many ? k_append_rotated<FMT, 1, NEIGHBOURS, H>
-                                      : k_append_rotated<FMT, 1, NEIGHBOURS, 1>
-                : a.c.D <= 128 ? many ? k_append_rotated<FMT, 2, NEIGHBOURS, H>
-                                      : k_append_rotated<FMT, 2, NEIGHBOURS, 1>
-                : many         ? k_append_rotated<FMT, 4, NEIGHBOURS, H>
-                               : k_append_rotated<FMT, 4, NEIGHBOURS, 1>;
+    auto kern = a.c.D <= 64    ? many ? k_append_rotated<FMT, 1, NEIGHBOURS, H, ONE>
+                                      : k_append_rotated<FMT, 1, NEIGHBOURS, 1, ONE>
+                : a.c.D <= 128 ? many ? k_append_rotated<FMT, 2, NEIGHBOURS, H, ONE>
+                                      : k_append_rotated<FMT, 2, NEIGHBOURS, 1, ONE>
+                : many         ? k_append_rotated<FMT, 4, NEIGHBOURS, H, ONE>
+                               : k_append_rotated<FMT, 4, NEIGHBOURS, 1, ONE>;
     kern<<<(unsigned)grid, kThreads, 0, stream>>>(a, t);
+}
+
+template <bool ONE> void launch_append(const AppendArgs &a, bool e4m3, int64_t grid, hipStream_t stream)
+{
+    constexpr int E = QLM_KV_E4M3, I = QLM_KV_INT8;
+    auto kern = a.c.D <= 64    ? e4m3 ? k_append<E, 1, ONE> : k_append<I, 1, ONE>
+                : a.c.D <= 128 ? e4m3 ? k_append<E, 2, ONE> : k_append<I, 2, ONE>
+                               : e4m3 ? k_append<E, 4, ONE> : k_append<I, 4, ONE>;
+    kern<<<(unsigned)grid, kThreads, 0, stream>>>(a);
 }
 
 int check_rotary(const qlm_rotary *r, int head_dim)
@@ -1303,10 +1340,10 @@ int qlm_kv_append(const qlm_kv_cache *cache, const qlm_kv_batch *batch, const ql
     const int64_t grid = append_groups(a, batch);
     if (!can_launch(grid, kThreads)) return fail(QLM_ERR_CAPACITY, "too many blocks in one append");
     const bool e4m3 = cache->format == QLM_KV_E4M3;
-    auto kern = a.c.D <= 64    ? e4m3 ? k_append<QLM_KV_E4M3, 1> : k_append<QLM_KV_INT8, 1>
-                : a.c.D <= 128 ? e4m3 ? k_append<QLM_KV_E4M3, 2> : k_append<QLM_KV_INT8, 2>
-                               : e4m3 ? k_append<QLM_KV_E4M3, 4> : k_append<QLM_KV_INT8, 4>;
-    kern<<<(unsigned)grid, kThreads, 0, stream>>>(a);
+    if (batch->max_new == 1)
+        launch_append<true>(a, e4m3, grid, stream);
+    else
+        launch_append<false>(a, e4m3, grid, stream);
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? QLM_OK : hip_fail(e, "k_append launch");
 }
@@ -1366,6 +1403,7 @@ int qlm_kv_append_rotated(const qlm_kv_cache *cache, const qlm_kv_batch *batch, 
     t.row_items = items(1);
     const bool many = (int64_t)batch->n_rows * t.row_items > kTurnMany;
     if (many) t.row_items = items(kTurnHeads);
+    const bool one = batch->max_new == 1;
     const int64_t queries = ((int64_t)batch->n_rows * t.row_items + kThreads / 64 - 1) / (kThreads / 64);
     const int64_t grid = keys + queries;
     if (!can_launch(grid, kThreads)) return fail(QLM_ERR_CAPACITY, "too many rows in one append");
@@ -1373,12 +1411,15 @@ int qlm_kv_append_rotated(const qlm_kv_cache *cache, const qlm_kv_batch *batch, 
     t.key_groups = (uint32_t)keys;
     constexpr int E = QLM_KV_E4M3, I = QLM_KV_INT8;
     const bool e4m3 = cache->format == E;
+    auto launch = [&](auto turn, auto alone) {
+        constexpr bool N = decltype(turn)::value, ONE = decltype(alone)::value;
+        e4m3 ? launch_rotated<E, N, ONE>(a, t, many, grid, stream)
+             : launch_rotated<I, N, ONE>(a, t, many, grid, stream);
+    };
     if (neighbours)
-        e4m3 ? launch_rotated<E, true>(a, t, many, grid, stream)
-             : launch_rotated<I, true>(a, t, many, grid, stream);
+        one ? launch(std::true_type{}, std::true_type{}) : launch(std::true_type{}, std::false_type{});
     else
-        e4m3 ? launch_rotated<E, false>(a, t, many, grid, stream)
-             : launch_rotated<I, false>(a, t, many, grid, stream);
+        one ? launch(std::false_type{}, std::true_type{}) : launch(std::false_type{}, std::false_type{});
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? QLM_OK : hip_fail(e, "k_append_rotated launch");
 }

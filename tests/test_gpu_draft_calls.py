@@ -260,3 +260,32 @@ def test_cache_past_four_gigabytes(torch, qlm):
         out = qlm.kv_append_rotated(cache, batch_of(torch, qlm, table, [70], [70]), k, v, q, rotary)
         got.append([out] + [x[at] for x in slots(torch, cache)])
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("kind", ["float8_e4m3fn", "int8"])
+@pytest.mark.parametrize("kv,d", [(3, 16), (2, 64), (1, 80), (2, 128), (1, 144), (1, 256)])
+def test_tokens_that_grow(torch, qlm, kv, d, kind):
+    """Tokens one by one, each larger than those before, so that blocks' scales grow, in batches of one
+    token a sequence at most and in batches that could hold two: the same cache bit for bit."""
+    torch.manual_seed(d)
+    rotary = turning(torch, qlm, 100, d // 2)
+    table = torch.arange(6, dtype=torch.int32, device="cuda").view(3, 2)
+    caches = [qlm.DeviceKvCache.empty(6, kv, d, getattr(torch, kind)) for _ in range(4)]
+    for c in caches:
+        clear(c)
+    for step in range(1, 70):
+        k, v, q = (torch.randn((3, h, d), device="cuda").bfloat16() * 1.3 ** (step % 50) for h in (kv, kv, 2))
+        lengths = torch.full((3,), step, dtype=torch.int32, device="cuda")
+        one = qlm.KvBatch(table, lengths)
+        start = torch.arange(4, dtype=torch.int32, device="cuda")
+        two = qlm.KvBatch(table, lengths, start, 3, 2)
+        qlm.kv_append(caches[0], one, k, v)
+        qlm.kv_append(caches[1], two, k, v)
+        a = qlm.kv_append_rotated(caches[2], one, k, v, q, rotary)
+        b = qlm.kv_append_rotated(caches[3], two, k, v, q, rotary)
+        assert torch.equal(a, b)
+        if step % 9 == 0 or step > 62:
+            for x, y in (caches[:2], caches[2:]):
+                assert all(torch.equal(m, n) for m, n in zip(slots(torch, x), slots(torch, y))), step
+    held = torch.arange(6, device="cuda").view(3, 2)
+    assert bool((caches[0].k_scale[held] != 0).all())
