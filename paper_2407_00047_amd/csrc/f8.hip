@@ -456,16 +456,15 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
         nt0 = (int)(in / high) * TN;
         mt0 = (int)(4 * group + in % high) * TM;
         // (tiles past the last one are read as the last one)
-        auto from = [&](const uint8_t *p, int t0, int have, int n, int *at) {
-            const int last = min(have - t0, 16) - 1;
+        auto from = [&](const uint8_t *p, int t0, int have, int own, int n, int *at) {
+            const int last = min(have - t0, own) - 1;
             for (int i = 0; i < n; ++i) at[i] = min(wv / 2 + i * (W / 2), last) * tile_bytes;
-            const int skip = b0 * kTileBytes;
-            return __builtin_amdgcn_make_buffer_rsrc((void *)(p + (int64_t)t0 * tile_bytes + skip), 0,
-                                                     (last + 1) * tile_bytes - skip, 0x00020000);
+            return __builtin_amdgcn_make_buffer_rsrc(
+                (void *)(p + (int64_t)t0 * tile_bytes + b0 * kTileBytes), 0,
+                qlm_f8_host::load_bytes(have - t0, own, a.blocks, b0), 0x00020000);
         };
-        static_assert(TN <= 16 && TM <= 16, "the most tiles of a workgroup");
-        w_from = from(a.w, nt0, a.n_tiles, PN, piece);
-        x_from = from(a.x, mt0, a.m_tiles, PM, piece + PN);
+        w_from = from(a.w, nt0, a.n_tiles, TN, PN, piece);
+        x_from = from(a.x, mt0, a.m_tiles, TM, PM, piece + PN);
         ws = a.ws + (int64_t)(min(nt0 + wn * NT, a.n_tiles - 1) / (kBlock / kTile)) * a.blocks + b0;
         xs = a.xs + (int64_t)b0 * a.padded + (int64_t)mt0 * kTile;
         m_last = min(mt0 + TM, a.m_tiles - 1);

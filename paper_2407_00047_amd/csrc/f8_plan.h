@@ -1,4 +1,4 @@
-// f8_plan.h -- which form a product in 8-bit floating point takes (host only).
+// f8_plan.h -- which form a product in 8-bit floating point takes, and what a workgroup may load then.
 #pragma once
 
 #include <algorithm>
@@ -112,6 +112,14 @@ inline Plan form_of(int n_out, int n_in, int n_rows, int most_splits = 16)
         }
     }
     return best;
+}
+
+// Bytes that a workgroup of `own` tiles of outputs (or rows) may load from its first tile's block b0 on,
+// where `left` tiles are left.  (Of its own tiles and no others: form_of holds those under 2 GiB, which 16
+// of the longest inputs pass.)
+constexpr int load_bytes(int left, int own, int blocks, int b0)
+{
+    return ((left < own ? left : own) * blocks - b0) * (kBlock * kTile);
 }
 
 // The rows in two parts where that is less, the first of whole tiles of 256: a last tile of a few

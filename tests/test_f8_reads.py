@@ -1,0 +1,62 @@
+"""What products in 8-bit floating point read of their operands, without a GPU: a workgroup's
+buffers are as long as its tiles in every form, up to the longest inputs."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+CODE = """
+#include "f8_plan.h"
+using namespace qlm_f8_host;
+extern "C" void form(int n_out, int n_in, int rows, int *got)
+{
+    const Parts p = parts_of(n_out, n_in, rows);
+    const int all[] = {p.n_first, p.first.side, p.first.splits, p.first.per_split, p.rest.side};
+    for (int i = 0; i < 5; ++i) got[i] = all[i];
+}
+extern "C" int bytes(int left, int own, int blocks, int b0) { return load_bytes(left, own, blocks, b0); }
+"""
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    d = tmp_path_factory.mktemp("reads")
+    (d / "plan.cpp").write_text(CODE)
+    lib = str(d / "plan.so")
+    subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", "-Werror", "-shared", "-fPIC", "-I",
+                    os.path.join(ROOT, "paper_2407_00047_amd", "csrc"), "-o", lib,
+                    str(d / "plan.cpp")], check=True)
+    return ctypes.CDLL(lib)
+
+
+def test_buffers_are_as_long_as_a_workgroups_tiles(plan):
+    seen = set()
+    for n_in in (1, 129, 16384, 1 << 20, (1 << 22) - 127, 1 << 23, (1 << 23) + 1, (1 << 24) - 128,
+                 (1 << 24) - 127, 1 << 24):
+        blocks = -(-n_in // 128)
+        for n_out in (16, 300, 1000, 4096, 20001):
+            for rows in (100, 256, 257, 512, 700, 1024, 4100):
+                got = (ctypes.c_int * 5)()
+                plan.form(n_out, n_in, rows, got)
+                n_first, side, splits, per, rest = got
+                forms = [(side, splits, per, n_first)]
+                if n_first < rows:
+                    forms.append((rest, 1, blocks, rows - n_first))
+                for side, splits, per, m in forms:
+                    if not side:
+                        continue
+                    own = side // 16
+                    for have in (-(-m // 16), -(-n_out // 16)):
+                        for first in {0, (have - 1) // own * own}:
+                            for split in {0, splits - 1}:
+                                b0, tiles = split * per, min(have - first, own)
+                                # (from the first tile's block b0 to the end of the last tile)
+                                want = (tiles * blocks - b0) * 2048
+                                assert want < 1 << 31
+                                assert plan.bytes(have - first, own, blocks, b0) == want, \
+                                    (rows, n_out, n_in, side, have, first, split)
+                                seen.add((side, n_in >= 1 << 23))
+    assert {(64, True), (64, False), (128, False), (256, False)} <= seen, seen
