@@ -33,6 +33,7 @@ typedef float float4v __attribute__((ext_vector_type(4)));
 typedef int int4v __attribute__((ext_vector_type(4)));
 typedef int int8v __attribute__((ext_vector_type(8)));
 
+using qlm_f8_host::fits;
 using qlm_f8_host::kBlock;
 using qlm_f8_host::kCus;
 using qlm_f8_host::kTile;
@@ -684,21 +685,6 @@ void launch_wide(MatArgs a, hipStream_t stream)
     k_f8_wide<NT, MT, WN, WM, MORE><<<(unsigned)grid, 64 * WN * WM, 0, stream>>>(a);
 }
 
-int64_t thin_groups(const MatArgs &a)
-{
-    const auto t = qlm_f8_host::thin_of(a.n_tiles, a.m_tiles, a.blocks);
-    return ((a.n_tiles + t.outs - 1ll) / t.outs + 7) / 8 * 8 * ((a.m_tiles + t.rows - 1ll) / t.rows);
-}
-
-// Whether a form's launches can be made.
-bool fits(const MatArgs &a, const Plan &p)
-{
-    if (!p.side) return can_launch(thin_groups(a), 512);
-    const int64_t tiles = (int64_t)((a.N + p.side - 1) / p.side) *
-                          ((a.M + (int64_t)p.side - 1) / p.side) * p.splits;
-    return tiles <= INT32_MAX / 2 && can_launch((a.M * (part_stride(a.N) / 4) + 255) / 256, 256);
-}
-
 hipError_t launch(MatArgs a, const Plan &p, void *ws, hipStream_t stream)
 {
     if (!p.side) {
@@ -709,7 +695,7 @@ hipError_t launch(MatArgs a, const Plan &p, void *ws, hipStream_t stream)
                     : t.outs == 2 ? k_f8_thin<2, 2, 8, 2>
                     : t.rows == 2 ? k_f8_thin<1, 2, 8, 4>
                                   : k_f8_thin<1, 1, 8, 4>;
-        kern<<<(unsigned)thin_groups(a), 512, 0, stream>>>(a);
+        kern<<<(unsigned)qlm_f8_host::thin_groups(a.n_tiles, a.m_tiles, a.blocks), 512, 0, stream>>>(a);
         return hipGetLastError();
     }
     a.splits = p.splits;
@@ -734,8 +720,8 @@ hipError_t launch(MatArgs a, const Plan &p, void *ws, hipStream_t stream)
         launch_wide<8, 4, 2, 4, 1>(o, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
-    k_f8_join<<<(unsigned)((a.M * (ld / 4) + 255) / 256), 256, 0, stream>>>(a, (const float *)ws, ld,
-                                                                          run);
+    k_f8_join<<<(unsigned)qlm_f8_host::join_groups(a.N, a.M), 256, 0, stream>>>(a, (const float *)ws, ld,
+                                                                               run);
     return hipGetLastError();
 }
 
@@ -864,9 +850,11 @@ int qlm_f8_matmul(const qlm_f8_codes *rows, const qlm_f8 *weight, void *out, int
         rest.xs += a.M;
         rest.out = (char *)out + a.M * out_stride * size;
         rest.out_wide = a.out_wide && (uintptr_t)rest.out % 16 == 0;
-        if (!fits(rest, parts.rest)) return fail(QLM_ERR_CAPACITY, "too many outputs in one call");
+        if (!fits(a.N, weight->n_in, rest.M, parts.rest))
+            return fail(QLM_ERR_CAPACITY, "too many outputs in one call");
     }
-    if (!fits(a, parts.first)) return fail(QLM_ERR_CAPACITY, "too many outputs in one call");
+    if (!fits(a.N, weight->n_in, a.M, parts.first))
+        return fail(QLM_ERR_CAPACITY, "too many outputs in one call");
     hipError_t e = launch(a, parts.first, ws, stream);
     if (e == hipSuccess && parts.n_first < rows->n_rows) e = launch(rest, parts.rest, ws, stream);
     return e == hipSuccess ? QLM_OK : hip_fail(e, "f8 launch");

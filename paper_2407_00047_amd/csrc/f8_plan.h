@@ -144,4 +144,30 @@ inline Parts parts_of(int n_out, int n_in, int n_rows)
     return {n_rows, whole, whole};
 }
 
+// Workgroups of k_f8_thin, and of the launch that joins runs' sums, four outputs a thread.
+inline int64_t thin_groups(int64_t n_tiles, int64_t m_tiles, int blocks)
+{
+    const Thin t = thin_of(n_tiles, m_tiles, blocks);
+    return ((n_tiles + t.outs - 1) / t.outs + 7) / 8 * 8 * ((m_tiles + t.rows - 1) / t.rows);
+}
+
+inline int64_t join_groups(int n_out, int n_rows)
+{
+    return (n_rows * (((int64_t)n_out + 3) / 4) + 255) / 256;
+}
+
+// Whether a form's launches can be made: fewer than 2^32 threads in each, tiles counted in 32 bits.
+inline bool fits(int n_out, int n_in, int n_rows, const Plan &p)
+{
+    auto can_launch = [](int64_t groups, int threads) { return groups < (1ll << 32) / threads; };
+    if (!p.side)
+        return can_launch(thin_groups(((int64_t)n_out + kTile - 1) / kTile,
+                                      ((int64_t)n_rows + kTile - 1) / kTile,
+                                      (n_in + kBlock - 1) / kBlock), 512);
+    const int64_t tiles = ((int64_t)n_out + p.side - 1) / p.side *
+                          (((int64_t)n_rows + p.side - 1) / p.side) * p.splits;
+    return tiles <= INT32_MAX / 2 &&
+           (p.splits == 1 || can_launch(join_groups(n_out, n_rows), 256));
+}
+
 }  // namespace qlm_f8_host

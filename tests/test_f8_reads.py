@@ -1,5 +1,6 @@
 """What products in 8-bit floating point read of their operands, without a GPU: a workgroup's
-buffers are as long as its tiles in every form, up to the longest inputs."""
+buffers are as long as its tiles in every form, up to the longest inputs; and that no product is
+refused for a launch that it does not make."""
 import ctypes
 import os
 import subprocess
@@ -16,6 +17,12 @@ extern "C" void form(int n_out, int n_in, int rows, int *got)
     const Parts p = parts_of(n_out, n_in, rows);
     const int all[] = {p.n_first, p.first.side, p.first.splits, p.first.per_split, p.rest.side};
     for (int i = 0; i < 5; ++i) got[i] = all[i];
+}
+extern "C" int fit(int n_out, int n_in, int rows)
+{
+    const Parts p = parts_of(n_out, n_in, rows);
+    return fits(n_out, n_in, p.n_first, p.first) &&
+           (p.n_first == rows || fits(n_out, n_in, rows - p.n_first, p.rest));
 }
 extern "C" int bytes(int left, int own, int blocks, int b0) { return load_bytes(left, own, blocks, b0); }
 """
@@ -60,3 +67,21 @@ def test_buffers_are_as_long_as_a_workgroups_tiles(plan):
                                     (rows, n_out, n_in, side, have, first, split)
                                 seen.add((side, n_in >= 1 << 23))
     assert {(64, True), (64, False), (128, False), (256, False)} <= seen, seen
+
+
+@pytest.mark.parametrize("rows,n_out,n_in", [(131072, 131072, 128), (131077, 131072, 100),
+                                             (65536, 262144, 4096), (1 << 20, 100000, 1000),
+                                             (1024, 1 << 24, 64), (1 << 24, 1 << 16, 128),
+                                             (640, 1 << 24, 5000), (2000000000, 128, 128)])
+def test_many_outputs_are_not_refused(plan, rows, n_out, n_in):
+    """2^34 outputs and more, of whose sums none are joined."""
+    got = (ctypes.c_int * 5)()
+    plan.form(n_out, n_in, rows, got)
+    assert got[2] == 1
+    assert plan.fit(n_out, n_in, rows)
+
+
+def test_what_cannot_be_launched_is_refused(plan):
+    """Tiles that 32 bits do not count."""
+    assert not plan.fit(1 << 24, 128, (1 << 31) - 17)
+    assert not plan.fit(1 << 24, 1 << 24, (1 << 31) - 17)

@@ -54,3 +54,18 @@ def test_the_longest_inputs(torch, qlm, rows, outs, ins):
     size[-1] = ins - 128 * (blocks - 1)
     want = (x.double() * size) @ w.double().t().contiguous()
     assert torch.equal(got.double(), want), int((got.double() != want).sum())
+
+
+def test_many_outputs(torch, qlm):
+    """More than 2^34 outputs of few inputs each: the whole numbers up to 100 that they are, in
+    bfloat16 too."""
+    rows, outs, ins = 131077, 131073, 100
+    x, w = signs(torch, rows, ins, 3), signs(torch, outs, ins, 4)
+    coded = qlm.f8_rows(x.bfloat16())
+    weight = qlm.f8_pack(codes(torch, w).view(torch.float8_e4m3fn),
+                         torch.ones((-(-outs // 128), 1), device="cuda"))
+    got = qlm.f8_matmul(coded, weight)
+    other = w.float().t().contiguous()
+    for at in range(0, rows, 8192):
+        part = got[at:at + 8192]
+        assert torch.equal(part, (x[at:at + 8192].float() @ other).bfloat16()), at
