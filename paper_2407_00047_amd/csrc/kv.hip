@@ -504,11 +504,12 @@ __device__ inline void append(const AppendArgs &a, const TurnArgs &turned)
     const bool fresh = o0 == 0;
     const int d = 8 * (t % CH), slot0 = t / CH;
     const bool in_d = d < D;
-    // a thread's slots: runs of G, whose bytes of a dim stand side by side in the values; where
-    // few are new, those that threads side by side hold, so that no thread has many of the new ones
-    // (three new tokens of 7 sequences, 4 heads of 80 dims 9.0 us and 9.8 by runs)
+    // a thread's slots: runs of G, whose bytes of a dim stand side by side in the values; where no more
+    // than three quarters of the block's are new, those that threads side by side hold, so that none has
+    // more of the new ones than another.  8 heads of 128 dims: 16 prompts of 1000 tokens by runs 24.3 us,
+    // else 25.2; 17 / 33 / 48 new of one sequence, int8, by runs 9.5 / 9.1 / 9.5, else 8.1 / 7.6 / 8.2
     constexpr int G = PASS < 4 ? PASS : 4;
-    const bool many = !ONE && o1 - o0 > ROWS;
+    const bool many = !ONE && o1 - o0 > 3 * kBlock / 4;
     auto slot_of = [&](int p) {
         if (ONE) return o0 + slot0;            // (of its rows the first is new)
         return many ? p / G * (ROWS * G) + slot0 * G + p % G : p * ROWS + slot0;
