@@ -549,9 +549,13 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
         fetch_scales(0);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int h = 0; h < AHEAD; ++h)
+        for (int h = 0; h < AHEAD; ++h) {
 #pragma unroll
             for (int i = 0; i < (h % 2 ? PM : PN); ++i) fetch(h % 2 == 0, i, h / 2, slot[h]);
+            // (half by half: the first block counts on the last half's being the last under way)
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
     auto block = [&](int b, int i) {       // i: b's place in a turn of SLOTS blocks
         // the loads that may be under way still: those of halves past this block's two
