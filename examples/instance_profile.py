@@ -94,7 +94,8 @@ class Instance:
         self.table = order.view(batch, self.width).contiguous()
         self.lengths = torch.zeros(batch, dtype=torch.int32, device="cuda")
         self.next = torch.zeros(batch, dtype=torch.int32, device="cuda")   # next position
-        self.position = 0                                # the same, known to the host
+        # the same, known to the host (behind drafted steps more: refused drafts count too)
+        self.position = 0
         self.rotary = None
         if positions:                  # keys and queries are turned by their positions
             pairs = model.dim // 2
@@ -177,7 +178,9 @@ class Instance:
 
     def drafted_step(self, tokens, n, gen):
         """One step over n drafts behind tokens [batch]: the tokens that it gives [batch, n + 1]
-        (-1 past their number) and their number [batch].  The cache keeps the accepted ones."""
+        (-1 past their number) and their number [batch].  The cache keeps the accepted ones.
+        Attention comes before the verification: the weights by which a later cut chooses hold what
+        the refused drafts' rows gave to the slots before them, too."""
         rows, near = self.draft(tokens, n, gen)
         start = torch.arange(self.batch + 1, dtype=torch.int32, device="cuda") * (n + 1)
         first = self.next.clone()

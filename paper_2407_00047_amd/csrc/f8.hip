@@ -102,7 +102,8 @@ struct RowsArgs {
 
 // A wave for a tile, eight lanes for a row of it: 16 inputs a lane, the largest magnitude over
 // the eight, and 16 codes a lane (eight rows of a chunk fill a line of memory).  Bound by memory:
-// 8000 rows of 16384 73 us, 5.4 TB/s; one row of 4096 3.7 us, a launch.
+// 8000 rows of 16384 73 us, 5.4 TB/s; one row of 4096 3.7 us, a launch.  Rows that do not all start on
+// 16 bytes are read two bytes at a time: 8000 of 16383 245 us, one of 4095 4.8.
 template <bool BF> __global__ __launch_bounds__(256) void k_f8_rows(RowsArgs a)
 {
     const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -607,7 +608,10 @@ __global__ __launch_bounds__(64 * WN * WM) void k_f8_wide(MatArgs a)
             for (int e = 0; e < E; ++e) asm volatile("" : "+v"(acc_last[e]));
             if (b + i < count) block(b + i, i);
         }
-        // the next tile's first loads are under way while this one's outputs are stored
+        // The next tile's first loads begin before this one's outputs are stored.  (The staging memory is
+        // one of two slots, which the compiler cannot tell from those being loaded: it waits for all
+        // that is under way, stores too, before a group of 16 rows is staged, and in single precision before
+        // each store.  The other tiles on the unit hide some of it: 1178 x 19884 x 896 43 us, floor 15.)
         wait_loads<0>();
         __syncthreads();
         const int n0 = (nt0 + wn * NT) * kTile, mt = mt0 + wm * MT, part = split;

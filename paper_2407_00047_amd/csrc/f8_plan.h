@@ -8,7 +8,10 @@ namespace qlm_f8_host {
 
 constexpr int kBlock = 128, kTile = 16, kCus = 256;
 constexpr int kThinRows = 640;   // the most rows that k_f8_thin takes
-constexpr int kLong = 40;        // blocks of inputs from which weights are long
+// Blocks of inputs from which weights are long: between the 32 of 96 x 16384 x 4096, of which tiles of 4 x 2 are
+// best, and the 128 of 96 x 4096 x 16384, of which they are not (sizes below).  What a cache still holds of
+// them goes by the number of outputs as well, which this leaves out.
+constexpr int kLong = 40;
 
 // Tiles of outputs and of rows to a workgroup of k_f8_thin: as many as leave every compute unit a
 // workgroup, as each tile of outputs reads the rows, and each group of rows the weights, from the

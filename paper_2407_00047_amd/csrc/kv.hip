@@ -472,8 +472,9 @@ template <int G> __device__ inline void stage(uint8_t *to, int group, int dp, in
 // then written as codes; values pass through shared memory into their order, and
 // the groups of slots that take any are read and written whole.
 // ONE: a token a sequence at most, held by a row of threads; the others are there for a block whose
-// scale grows (in workgroups of a wave such a block took three times as long, and 512 sequences without one 13
-// us where this takes 21; with every slot's place held by a thread it was 35).
+// scale grows (in workgroups of a wave such a block took three times as long).  512 sequences (8 heads of 128)
+// 14 us, 22 with every slot's place held by a thread; with 32 heads of queries turned beside them 21 and 35 (in
+// workgroups of a wave, where no scale grows, 13).
 // One token for each of 64 sequences (8 heads of 128): 6.1 us, a launch and its chain of
 // dependent reads (length, table, scale, row).  Six ragged prompts of up to 2100 tokens
 // (8 heads of 64, 20 MB): 12.7 us, 1.6 TB/s, the ends of a short launch.
@@ -791,7 +792,10 @@ constexpr int64_t kTurnMany = 4096;       // waves of single heads
 // positions' and the tables' reads in its chain.  Six ragged prompts of up to 2100 tokens on three axes
 // (152 MB): 34.6 us, 4.4 TB/s; calls of the keys alone 21 (k_append 17), of the queries alone 25.  Keys'
 // and queries' workgroups in turn or the queries' first took 10 % longer, five workgroups to a unit 30 %.
-// Angles read for each head and chunk of eight dims: 95.
+// Angles read for each head and chunk of eight dims: 95.  By halves, heads of 65 to 128 dims, more than a
+// token a sequence, spill 3 registers (int8 6) at the four waves to a SIMD that they are held to.  Keys by halves of
+// a number of pairs that eight does not divide are turned dim by dim: such prompts of heads of 80 dims, 10
+// or 20 pairs, 91 us where 40 pairs, or neighbours, take 28 to 31.
 template <int FMT, int ND, bool NEIGHBOURS, int HEADS, bool ONE>
 __global__ __launch_bounds__(kThreads, ONE || ND <= 2 ? 4 : 2)
 void k_append_rotated(AppendArgs a, TurnArgs t)

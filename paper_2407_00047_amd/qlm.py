@@ -1273,7 +1273,9 @@ def _word_type(dtype, what):
 
 def f8_matmul(x: F8Rows, weight: F8, out=None, dtype=None, ws=None, stream=None):
     """Coded rows times the matrix: [n_rows, n_out] of ``dtype`` (bfloat16 when None;
-    out's where out is given)."""
+    out's where out is given).  float32 outputs too hold sums of the 8-bit matrix
+    instructions, which keep 13 bits below the largest of eight neighbouring products:
+    1.5e-5 to 3e-5 of the outputs' norm."""
     import torch
     if x.n_in != weight.n_in:
         raise ValueError("x must be rows of %d inputs" % weight.n_in)
